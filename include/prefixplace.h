@@ -442,6 +442,171 @@ pp_status pp_replan(pp_instance *inst, const uint8_t *incumbent, int32_t n_start
                     int32_t max_rounds, int64_t epoch_requests, int64_t horizon_requests,
                     uint8_t *placement, pp_replan_result *result, pp_plan_stats *stats, void *stream);
 
+/*
+ * Serving from a target: a worker's paged K/V cache.  The paper's chunks group
+ * a serving engine's cache blocks (Section II-A); these entry points take a
+ * step of such an engine from the planned target to the attention over its
+ * blocks: pp_chunk_map lays the resident chunks out as blocks, and every step
+ * pp_block_tables makes the requests' block tables and slot map, pp_kv_write
+ * stores the new tokens' K and V rows, and pp_paged_attention attends the new
+ * tokens (chunks of a prompt or single tokens) over cached and new ones.
+ *
+ * A cache of one layer is two device buffers (K and V) of the same layout:
+ * element (block, token, head, x) is at block * block_stride + token *
+ * token_stride + head * head_stride + x, strides in elements.  Token p of a
+ * request is in block block_table[p / block_size] at p % block_size; the
+ * number of that place, block * block_size + p % block_size, is its slot.
+ */
+typedef struct pp_kv pp_kv;               /* opaque, library-owned */
+
+enum { PP_KV_BF16 = 0, PP_KV_F16 = 1 };
+
+/*
+ * pp_kv_create -- a handle of the caches of one layout; the buffers are passed
+ * to each call and stay the caller's, so one handle serves all layers.
+ *   blocks        blocks of a cache, 1 .. 2^30
+ *   block_size    tokens per block: a power of two, 8 .. 512
+ *   kv_heads      K/V heads, 1 .. 65535
+ *   head_dim      a multiple of 8, 8 .. 128
+ *   dtype         PP_KV_BF16 or PP_KV_F16, of the caches and of q, k, v, out
+ *   block_stride, token_stride, head_stride
+ *                 elements, positive multiples of 8 of at least head_dim;
+ *                 0, 0, 0: contiguous [blocks][block_size][kv_heads][head_dim]
+ *   stream        stream of the set-up; the call synchronises it
+ *   out           receives the handle (NULL on failure)
+ * The handle owns a device status word and scratch of the attention.  Its
+ * device (the current one) must be current in later calls.  pp_kv_sync reads
+ * the status.  pp_paged_attention calls on one handle use its scratch and must
+ * not overlap on the GPU; on one stream they never do.  No call after this one
+ * allocates or synchronises, so all can be captured in a CUDA graph.
+ * Errors: PP_EINVAL, PP_ENOMEM, PP_ECUDA.
+ */
+pp_status pp_kv_create(int32_t blocks, int32_t block_size, int32_t kv_heads, int32_t head_dim, int32_t dtype,
+                       int64_t block_stride, int64_t token_stride, int64_t head_stride, void *stream, pp_kv **out);
+
+/* Frees the handle and its scratch.  NULL is accepted. */
+pp_status pp_kv_destroy(pp_kv *kv);
+
+/*
+ * pp_kv_sync -- synchronise `stream`, then read and clear the handle's device
+ * status word.  Returns PP_OK, PP_EBOUNDS (a length, block, slot, chunk or
+ * token count given in device memory was out of range; what it would have
+ * reached was left out), PP_ETIMEOUT or PP_ECUDA.
+ */
+pp_status pp_kv_sync(pp_kv *kv, void *stream);
+
+/*
+ * pp_chunk_map -- host-only: lay a prefix-complete target out as cache blocks
+ * 0 .. *blocks - 1 and give, per chunk, the record that pp_block_tables reads.
+ *   parent, weight     host [n], as in pp_instance_create
+ *   resident           host [n]: nonzero = the worker holds the chunk (a row of
+ *                      pp_plan_run's placement); closed under parents
+ *   blocks_per_slot    blocks of one budget slot (tokens per slot / block_size)
+ *   map                host [n][4] out: {up, base, begin, end}
+ *   blocks             host out: blocks used
+ * A run of chunks that follow one another down the tree and in the cache is a
+ * segment.  For a resident chunk `begin` is the table index of its segment's
+ * first block, `base` that block's number, `end` the table index after the
+ * chunk's last block and `up` the chunk above the segment (-1: none): table
+ * entry j of a request through the chunk is base + j - begin for begin <= j <
+ * end, and earlier entries follow from `up`.  Other chunks have base -1, begin
+ * = end = 0 and `up` the deepest resident chunk of their path (-1: none).
+ * Errors: PP_EINVAL (not closed, weight < 1), PP_ENOTTREE, PP_EOVERFLOW (more
+ * than 2^30 blocks), PP_ENOMEM.
+ */
+pp_status pp_chunk_map(int32_t n, const int32_t *parent, const int32_t *weight, const uint8_t *resident,
+                       int32_t blocks_per_slot, int32_t *map, int32_t *blocks);
+
+/*
+ * pp_block_tables -- the block tables, slot map, positions and query offsets of
+ * one step from the requests' lengths.  Request r has length[r] tokens after
+ * the step.  With node[r] >= 0 it is admitted: its table row is built, first
+ * the blocks of the resident chunks on the path of chunk node[r], of which it
+ * takes min(what is resident, length[r] - 1 rounded down to whole blocks)
+ * tokens as cached (so the last token is always computed, into a block of the
+ * request's own), then new blocks.  With node[r] = -1 it is running: the first
+ * ceil(cached[r] / block_size) entries of its row stand and are not written.
+ * New blocks are taken from free_blocks[free_head] on, in request order.
+ *   requests      0 .. 16384
+ *   length        device [requests]
+ *   cached        device [requests]: tokens in the cache (read for running requests)
+ *   node          device [requests], or NULL: all running
+ *   n_chunks, chunk_map   device [n_chunks][4], from pp_chunk_map, aligned to
+ *                 16 bytes; not read without node
+ *   free_count, free_blocks   device [free_count]: free blocks, in the order of use
+ *   free_head     device [1]: how many of them are in use
+ *   free_head_out device [1] out: the same after this step; not free_head itself
+ *   table_width   entries per row
+ *   block_table   device [requests][table_width], in and out
+ *   max_tokens    capacity of the next two
+ *   slot_map      device [max_tokens] out: the new tokens' slots, request after
+ *                 request; -1 after the last
+ *   position      device [max_tokens] out: their positions; 0 after the last
+ *   q_start       device [requests + 1] out: a request's first new token
+ * PP_EBOUNDS in the status word: a length below 0 or above the row's room, cached above
+ * length, a node or block out of range (these are cut to the range), more new
+ * tokens than max_tokens (the rest is left out), or too few free blocks (the
+ * missing ones' table entries and slots are -1).
+ * Errors: PP_EINVAL, PP_ECUDA.
+ */
+pp_status pp_block_tables(pp_kv *kv, int32_t requests, const int32_t *length, const int32_t *cached,
+                          const int32_t *node, int32_t n_chunks, const int32_t *chunk_map, int32_t free_count,
+                          const int32_t *free_blocks, const int32_t *free_head, int32_t *free_head_out,
+                          int32_t table_width, int32_t *block_table, int32_t max_tokens, int64_t *slot_map,
+                          int32_t *position, int32_t *q_start, void *stream);
+
+/*
+ * pp_kv_write -- store the new tokens' K and V rows at their slots.
+ *   k, v          device [tokens][kv_heads][head_dim], token and head strides in
+ *                 elements (positive multiples of 8; bases aligned to 16 bytes)
+ *   slot_map      device [tokens]; a negative slot's token is left out; no slot
+ *                 may occur twice
+ *   k_cache, v_cache   device, of the handle's layout, aligned to 16 bytes
+ * A slot above the cache sets PP_EBOUNDS and is left out.
+ * Errors: PP_EINVAL, PP_ECUDA.
+ */
+pp_status pp_kv_write(pp_kv *kv, int32_t tokens, const void *k, int64_t k_token_stride, int64_t k_head_stride,
+                      const void *v, int64_t v_token_stride, int64_t v_head_stride, const int64_t *slot_map,
+                      void *k_cache, void *v_cache, void *stream);
+
+/*
+ * pp_paged_attention -- causal attention of the new tokens over the cache.
+ * Request r's queries are rows q_start[r] .. q_start[r+1] - 1 of q, the last
+ * length's tokens of the request: query i of q_len stands at p = length[r] -
+ * q_len + i and sees the keys j <= p, with window > 0 only those with j > p -
+ * window.  Query head x reads K/V head x / (q_heads / kv_heads).
+ *   out = sum_j softmax_j(scale q.k_j) v_j
+ * A query that sees nothing (p < 0) gets zeros and lse = -infinity.  Rows of
+ * the cache that a query does not see never reach its output, whatever they
+ * hold (infinities and NaN as well).
+ *   requests      0 .. 16384
+ *   tokens        rows of q and out; rows from q_start[requests] on are left alone
+ *   q, out        device [tokens][q_heads][head_dim], token and head strides in
+ *                 elements (positive multiples of 8; bases aligned to 16 bytes)
+ *   block_table   device [requests][table_width]
+ *   q_start       device [requests + 1], ascending from 0
+ *   length        device [requests]: tokens of the request, the new ones included
+ *   max_q         host: the most new tokens of any request.  It chooses the
+ *                 kernel (1: single tokens) and nothing else
+ *   window        0: none
+ *   scale         > 0
+ *   lse           device [tokens][q_heads] out, or NULL: natural log of the sum
+ *                 of exp(scale q.k)
+ * Products are of 16-bit inputs with 32-bit sums; softmax statistics and the
+ * output's sum are 32-bit; the weights are rounded to the cache's type for
+ * their product with V.  Results do not depend on the run, but the last bits
+ * may depend on which other requests are in the call.
+ * A block out of range that a query would see, or lengths and offsets out of
+ * range, set PP_EBOUNDS; what they would have reached counts as not visible.
+ * Errors: PP_EINVAL, PP_ECUDA.
+ */
+pp_status pp_paged_attention(pp_kv *kv, int32_t requests, int32_t tokens, int32_t q_heads, const void *q,
+                             int64_t q_token_stride, int64_t q_head_stride, const void *k_cache,
+                             const void *v_cache, int32_t table_width, const int32_t *block_table,
+                             const int32_t *q_start, const int32_t *length, int32_t max_q, int32_t window,
+                             float scale, void *out, int64_t out_token_stride, int64_t out_head_stride,
+                             float *lse, void *stream);
+
 /* Thread-local description of the last failure in this thread ("" if none). */
 const char *pp_last_error(void);
 

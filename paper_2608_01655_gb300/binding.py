@@ -38,6 +38,7 @@ PP_OK, PP_EINVAL, PP_ENOTTREE, PP_EOVERFLOW, PP_ENOMEM, PP_ECUDA, PP_ETIMEOUT, P
 STATUS_NAMES = ["PP_OK", "PP_EINVAL", "PP_ENOTTREE", "PP_EOVERFLOW", "PP_ENOMEM", "PP_ECUDA",
                 "PP_ETIMEOUT", "PP_EBOUNDS"]
 PP_TRANSFER_REQUESTER, PP_TRANSFER_SOURCE = 0, 1
+PP_KV_BF16, PP_KV_F16 = 0, 1
 
 
 class PPError(RuntimeError):
@@ -78,6 +79,14 @@ _SIGS = {
     "pp_default_orders": [_P, _i32, _P, _P],
     "pp_safeguards": [_P, _P, _P, _P],
     "pp_replan": [_P, _P, _i32, _P, _i32, _i64, _i64, _P, _P, _P, _P],
+    "pp_kv_create": [_i32, _i32, _i32, _i32, _i32, _i64, _i64, _i64, _P, ctypes.POINTER(_P)],
+    "pp_kv_destroy": [_P],
+    "pp_kv_sync": [_P, _P],
+    "pp_chunk_map": [_i32, _P, _P, _P, _i32, _P, ctypes.POINTER(_i32)],
+    "pp_block_tables": [_P, _i32, _P, _P, _P, _i32, _P, _i32, _P, _P, _P, _i32, _P, _i32, _P, _P, _P, _P],
+    "pp_kv_write": [_P, _i32, _P, _i64, _i64, _P, _i64, _i64, _P, _P, _P, _P],
+    "pp_paged_attention": [_P, _i32, _i32, _i32, _P, _i64, _i64, _P, _P, _i32, _P, _P, _P, _i32, _i32,
+                           ctypes.c_float, _P, _i64, _i64, _P, _P],
 }
 for _name, _args in _SIGS.items():
     _f = getattr(_lib, _name)
@@ -378,3 +387,142 @@ def pp_replan(inst: Instance, incumbent, n_starts: int, max_rounds: int, epoch_r
                           int(horizon_requests), _host(pl), ctypes.byref(res), ctypes.byref(st), _stream(stream)))
     return ReplanResult(pl[:, :inst.n].copy(), int(res.incumbent_objective), int(res.new_objective),
                         int(res.materialization_cost), int(res.break_even_requests), bool(res.adopted))
+
+
+def pp_chunk_map(parent, weight, resident, blocks_per_slot: int):
+    """Host-only layout of a target (one worker's placement row) as cache blocks.
+    Returns (map [n][4] int32, blocks used)."""
+    parent, weight, resident = _np(parent, np.int32), _np(weight, np.int32), _np(resident, np.uint8)
+    n = parent.shape[0]
+    if weight.shape != (n,) or resident.shape != (n,):
+        raise ValueError("parent, weight and resident must be [n]")
+    out = np.zeros((max(n, 1), 4), np.int32)
+    used = _i32(0)
+    _check(_lib.pp_chunk_map(n, _host(parent), _host(weight), _host(resident), int(blocks_per_slot), _host(out),
+                             ctypes.byref(used)))
+    return out[:n], int(used.value)
+
+
+def _arg(t, name, dtype, *shape):
+    """A contiguous CUDA tensor of this type and shape (None: any size)."""
+    if str(t.dtype) != "torch." + dtype or t.dim() != len(shape) or \
+            any(want is not None and have != want for have, want in zip(t.shape, shape)):
+        raise ValueError(f"{name}: expected {dtype} {list(shape)}, got {t.dtype} {list(t.shape)}")
+    return _dev(t)
+
+
+class KVCache:
+    """Owns one pp_kv: the layout of a paged K/V cache, its status word and scratch."""
+
+    _DTYPES = {"bfloat16": PP_KV_BF16, "float16": PP_KV_F16}
+
+    def __init__(self, blocks, block_size, kv_heads, head_dim, dtype="bfloat16", strides=None, stream=None):
+        """strides: (block, token, head) in elements; None: contiguous
+        [blocks][block_size][kv_heads][head_dim]."""
+        name = str(dtype).replace("torch.", "")
+        if name not in self._DTYPES:
+            raise ValueError("dtype must be bfloat16 or float16")
+        self.shape = (int(blocks), int(block_size), int(kv_heads), int(head_dim))
+        self.dtype = name
+        h = _P()
+        _check(_lib.pp_kv_create(*self.shape, self._DTYPES[name], *[int(x) for x in (strides or (0, 0, 0))],
+                                 _stream(stream), ctypes.byref(h)))
+        self._h = h
+        if strides is None:
+            strides = (self.shape[1] * self.shape[2] * self.shape[3], self.shape[2] * self.shape[3], self.shape[3])
+        self.strides = tuple(int(x) for x in strides)
+
+    @classmethod
+    def like(cls, cache, stream=None):
+        """The layout of a [blocks][block_size][kv_heads][head_dim] CUDA tensor, of any strides."""
+        if cache.dim() != 4 or cache.stride(3) != 1:
+            raise ValueError("expected [blocks][block_size][kv_heads][head_dim] with contiguous rows")
+        # an extent of 1 may carry any stride
+        strides = [s if n > 1 else cache.shape[3] for n, s in zip(cache.shape[:3], cache.stride()[:3])]
+        return cls(*cache.shape, cache.dtype, strides, stream)
+
+    @property
+    def handle(self):
+        if self._h is None:
+            raise RuntimeError("cache handle destroyed")
+        return self._h
+
+    def close(self):
+        if getattr(self, "_h", None) is not None:
+            _lib.pp_kv_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def sync(self, stream=None):
+        _check(_lib.pp_kv_sync(self.handle, _stream(stream)))
+
+    def _cache(self, t, name):
+        """Device pointer of a cache of this layout (an extent of 1 has no stride)."""
+        if not t.is_cuda or str(t.dtype) != "torch." + self.dtype or tuple(t.shape) != self.shape or \
+                t.stride(3) != 1 or any(n > 1 and a != b for n, a, b in zip(t.shape, t.stride(), self.strides)):
+            raise ValueError(f"{name}: expected a CUDA {self.dtype} tensor of shape {self.shape} and strides "
+                             f"{self.strides + (1,)}")
+        return _P(t.data_ptr())
+
+    def _rows(self, t, name, tokens, heads):
+        """Pointer, token stride and head stride of [tokens][heads][head_dim] rows."""
+        if not t.is_cuda or str(t.dtype) != "torch." + self.dtype or \
+                tuple(t.shape) != (tokens, heads, self.shape[3]) or (t.numel() and t.stride(2) != 1):
+            raise ValueError(f"{name}: expected a CUDA {self.dtype} tensor [{tokens}][{heads}][{self.shape[3]}] "
+                             "with contiguous rows")
+        # an extent of 1 may carry any stride
+        ht = t.stride(1) if heads > 1 else self.shape[3]
+        tt = t.stride(0) if tokens > 1 else max(heads * ht, 8)
+        return _P(t.data_ptr()), tt, ht
+
+
+def pp_block_tables(kv: KVCache, length, cached, block_table, slot_map, position, q_start, free_blocks, free_head,
+                    free_head_out, node=None, chunk_map=None, stream=None):
+    """A step's block tables, slot map, positions and query offsets.  length, cached, node [R] int32,
+    block_table [R][width] int32 (in and out), slot_map [T] int64, position [T] int32, q_start [R + 1] int32,
+    free_blocks [F] int32, free_head and free_head_out [1] int32, chunk_map [n][4] int32: CUDA tensors."""
+    if (node is None) != (chunk_map is None):
+        raise ValueError("node and chunk_map go together")
+    r, t = int(length.shape[0]), int(slot_map.shape[0])
+    n = 0 if node is None else int(chunk_map.shape[0])
+    _check(_lib.pp_block_tables(
+        kv.handle, r, _arg(length, "length", "int32", r), _arg(cached, "cached", "int32", r),
+        None if node is None else _arg(node, "node", "int32", r), n,
+        None if node is None else _arg(chunk_map, "chunk_map", "int32", n, 4),
+        int(free_blocks.shape[0]), _arg(free_blocks, "free_blocks", "int32", None),
+        _arg(free_head, "free_head", "int32", 1), _arg(free_head_out, "free_head_out", "int32", 1),
+        int(block_table.shape[-1]), _arg(block_table, "block_table", "int32", r, None), t,
+        _arg(slot_map, "slot_map", "int64", t), _arg(position, "position", "int32", t),
+        _arg(q_start, "q_start", "int32", r + 1), _stream(stream)))
+
+
+def pp_kv_write(kv: KVCache, k, v, slot_map, k_cache, v_cache, stream=None):
+    """Store rows k, v [T][kv_heads][head_dim] at slot_map [T] int64 (negative: left out)."""
+    t = int(slot_map.shape[0])
+    _check(_lib.pp_kv_write(kv.handle, t, *kv._rows(k, "k", t, kv.shape[2]), *kv._rows(v, "v", t, kv.shape[2]),
+                            _arg(slot_map, "slot_map", "int64", t), kv._cache(k_cache, "k_cache"),
+                            kv._cache(v_cache, "v_cache"), _stream(stream)))
+
+
+def pp_paged_attention(kv: KVCache, q, k_cache, v_cache, block_table, q_start, length, max_q: int, out,
+                       scale: float, window: int = 0, lse=None, stream=None):
+    """Causal attention of the new tokens' q [T][q_heads][head_dim] over the paged cache, into out (as q) and
+    lse [T][q_heads] float32.  block_table [R][width], q_start [R + 1], length [R]: int32 CUDA tensors."""
+    t, heads, r = int(q.shape[0]), int(q.shape[1]), int(length.shape[0])
+    _check(_lib.pp_paged_attention(
+        kv.handle, r, t, heads, *kv._rows(q, "q", t, heads), kv._cache(k_cache, "k_cache"),
+        kv._cache(v_cache, "v_cache"), int(block_table.shape[-1]), _arg(block_table, "block_table", "int32", r, None),
+        _arg(q_start, "q_start", "int32", r + 1), _arg(length, "length", "int32", r), int(max_q), int(window),
+        float(scale), *kv._rows(out, "out", t, heads),
+        None if lse is None else _arg(lse, "lse", "float32", t, heads), _stream(stream)))
