@@ -1,0 +1,313 @@
+// What the attention kernels share: the split of the work over CTAs, the
+// asynchronous copies of cache tiles, bounded waits, and the join of the
+// pieces of an item that several CTAs computed.
+//
+// An item is what one pass over keys serves (queries that share a K/V head and
+// lie together); its keys are cut into tiles.  The tiles of all items, in a
+// fixed order, are one line that is cut into equal stretches, one per CTA, so
+// that the load is even whatever the lengths are.  Every CTA works the cut
+// out by itself from q_start and length.  A stretch that covers an item only
+// in part gives a piece (output not yet divided, maximum, sum); the last CTA
+// to finish of an item's (first of a group of pieces, then of its groups) joins
+// them in a fixed order.  No CTA waits for another.
+#pragma once
+
+#include <cuda.h>
+
+#include "pp_kv.cuh"
+
+namespace pp {
+
+struct AttendDev {
+    AttendArgs c;
+    int64_t block_stride, token_stride, head_stride;
+    int32_t blocks, block_log, dim, kv_heads;
+    float scale_log2;                   // scale * log2(e)
+    int32_t *status;
+    float *piece;                       // pieces' outputs, [slot][...]
+    float *piece_stat;                  // their maxima (log2 units) and sums
+    int32_t *count;                     // [2][slots] arrivals, left at 0 by every launch
+};
+
+constexpr uint64_t kAttendLimitNs = 500ull * 1000 * 1000;   // one wait gives up after 0.5 s
+constexpr int kJoinGroup = 16;                              // pieces joined at a time
+
+// ---------------------------------------------------------------------------
+// Requests and their items
+// ---------------------------------------------------------------------------
+struct Req {
+    int32_t first, q_len, length;       // first query row, queries, tokens
+};
+
+__device__ __forceinline__ Req load_req(const AttendDev &a, int32_t r, bool report)
+{
+    const int32_t x = a.c.q_start[r], y = a.c.q_start[r + 1], n = a.c.length[r];
+    const int64_t room = (int64_t)a.c.table_width << a.block_log;
+    Req q;
+    q.first = min(max(x, 0), a.c.tokens);
+    q.q_len = min(max(y, q.first), a.c.tokens) - q.first;
+    q.length = (int32_t)min((int64_t)max(n, 0), room);
+    if (report && (q.first != x || q.first + q.q_len != y || q.length != n)) kv_bounds(a.status);
+    return q;
+}
+
+// keys that a query at `pos` sees: [lo, pos]
+__device__ __forceinline__ int32_t first_key(const AttendDev &a, int32_t pos)
+{
+    return a.c.window && pos >= a.c.window ? pos - a.c.window + 1 : 0;
+}
+
+struct Keys {
+    int32_t lo, hi;                     // first and last key of the item (hi < lo: none)
+};
+
+// An item with nothing to see still has a tile, so that its rows are written.
+template <int KT> __device__ __forceinline__ int32_t key_tiles(Keys k) { return k.hi < k.lo ? 1 : k.hi / KT - k.lo / KT + 1; }
+
+// Shape: static constants KT (keys per tile) and, for a request, inner(a, q)
+// items for each of outer(a) (heads), keys(a, q, i) of inner item i.
+struct SchedShared {
+    int64_t warp_sum[32];
+    int64_t total, begin;
+    int32_t r, outer, inner, off, count;
+};
+
+template <class S> __device__ __forceinline__ int64_t request_tiles(const AttendDev &a, const Req &q)
+{
+    int64_t s = 0;
+    for (int32_t i = 0, n = S::inner(a, q); i < n; ++i) s += key_tiles<S::KT>(S::keys(a, q, i));
+    return s * S::outer(a);
+}
+
+__device__ __forceinline__ int64_t block_scan(int64_t v, int64_t *excl, int64_t *warp_sum)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    int64_t x = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t y = __shfl_up_sync(~0u, x, o);
+        if (lane >= o) x += y;
+    }
+    __syncthreads();
+    if (lane == 31) warp_sum[warp] = x;
+    __syncthreads();
+    int64_t before = 0, total = 0;
+    for (int w = 0; w < warps; ++w) {
+        const int64_t y = warp_sum[w];
+        if (w < warp) before += y;
+        total += y;
+    }
+    *excl = before + x - v;
+    return total;
+}
+
+// The CTA's stretch: false if it has none.  All threads of the CTA call it.
+template <class S> __device__ __forceinline__ bool schedule(const AttendDev &a, SchedShared &sm)
+{
+    const int32_t R = a.c.requests, T = blockDim.x;
+    const bool report = blockIdx.x == 0;
+    if (threadIdx.x == 0) sm.count = 0;
+    int64_t total = 0, excl, mine = 0;
+    if (report && threadIdx.x == 0 && a.c.q_start[0] != 0) kv_bounds(a.status);
+    for (int32_t r = threadIdx.x; r < R; r += T) mine += request_tiles<S>(a, load_req(a, r, report));
+    total = block_scan(mine, &excl, sm.warp_sum);
+    if (total == 0) return false;
+    const int64_t ctas = min((int64_t)gridDim.x, total);
+    if (blockIdx.x >= ctas) return false;
+    const int64_t begin = total * blockIdx.x / ctas, end = total * (blockIdx.x + 1) / ctas;
+    int64_t before = 0;
+    for (int32_t base = 0; base < R; base += T) {
+        const int32_t r = base + threadIdx.x;
+        Req q = {0, 0, 0};
+        if (R > T) {
+            if (r < R) q = load_req(a, r, false);
+            mine = r < R ? request_tiles<S>(a, q) : 0;
+            const int64_t sum = block_scan(mine, &excl, sm.warp_sum);
+            excl += before;
+            before += sum;
+        } else if (r < R) {
+            q = load_req(a, r, false);
+        }
+        if (r < R && mine > 0 && excl <= begin && begin < excl + mine) {
+            const int64_t per = mine / S::outer(a);
+            int64_t rem = begin - excl;
+            sm.r = r;
+            sm.outer = (int32_t)(rem / per);
+            rem %= per;
+            int32_t i = 0;
+            for (;; ++i) {
+                const int32_t n = key_tiles<S::KT>(S::keys(a, q, i));
+                if (rem < n) break;
+                rem -= n;
+            }
+            sm.inner = i;
+            sm.off = (int32_t)rem;
+            sm.count = (int32_t)(end - begin);
+            sm.begin = begin;
+            sm.total = total;
+        }
+    }
+    __syncthreads();
+    return true;
+}
+
+// Walks the CTA's stretch item by item; every role of a CTA has its own.
+template <class S> struct Cursor {
+    int32_t r, outer, inner, off, left;
+    int64_t g;                          // tile's number on the line
+    Req q;
+    Keys k;
+    int32_t tiles, len;                 // of the item; of this CTA's part [off, off + len)
+
+    __device__ __forceinline__ Cursor(const AttendDev &a, const SchedShared &sm)
+        : r(sm.r), outer(sm.outer), inner(sm.inner), off(sm.off), left(sm.count), g(sm.begin)
+    {
+        q = load_req(a, r, false);
+        item(a);
+    }
+    __device__ __forceinline__ void item(const AttendDev &a)
+    {
+        k = S::keys(a, q, inner);
+        tiles = key_tiles<S::KT>(k);
+        len = min(tiles - off, left);
+    }
+    __device__ __forceinline__ bool next(const AttendDev &a)
+    {
+        left -= len;
+        g += len;
+        off = 0;
+        if (left <= 0) return false;
+        if (++inner >= S::inner(a, q)) {
+            inner = 0;
+            if (++outer >= S::outer(a)) {
+                outer = 0;
+                do q = load_req(a, ++r, false);
+                while (S::inner(a, q) == 0);
+            }
+        }
+        item(a);
+        return true;
+    }
+    __device__ __forceinline__ bool whole() const { return off == 0 && len == tiles; }
+};
+
+// ---------------------------------------------------------------------------
+// Barriers and copies
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count)
+{
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+        "selp.u32 %0, 1, 0, p;\n"
+        "}\n"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ uint64_t attend_ns()
+{
+    uint64_t t;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+    return t;
+}
+
+// Bounded wait.  When one runs out, `dead` (of the CTA) is set and no later
+// wait of the CTA waits: its loops run to their end over whatever is there, the
+// status says PP_ETIMEOUT, and the launch ends.
+static __device__ __noinline__ void mbar_wait_slow(uint32_t bar, uint32_t parity, volatile int32_t *dead, int32_t *status)
+{
+    const uint64_t t0 = attend_ns();
+    while (!mbar_try(bar, parity)) {
+        if (*dead) return;
+        if (attend_ns() - t0 > kAttendLimitNs) {
+            *dead = 1;
+            atomicExch(status, (int32_t)PP_ETIMEOUT);
+            return;
+        }
+    }
+}
+__device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, volatile int32_t *dead, int32_t *status)
+{
+    if (!mbar_try(bar, parity)) mbar_wait_slow(bar, parity, dead, status);
+}
+
+// box of `rows` tokens x 64 elements of one block and head to shared memory, rows
+// of 128 bytes swizzled by 128 bytes; a block number out of range gives zeros
+__device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap *map, uint32_t bar, int32_t x, int32_t token,
+                                         int32_t head, int32_t block)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(token), "r"(head), "r"(block), "r"(bar)
+        : "memory");
+}
+
+__device__ __forceinline__ void named_sync(int id, int threads)
+{
+    asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+
+__device__ __forceinline__ float exp2_approx(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+template <typename T> struct Pack;
+template <> struct Pack<__nv_bfloat16> {
+    static __device__ __forceinline__ uint32_t two(float lo, float hi)
+    {
+        uint32_t r;
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+        return r;
+    }
+};
+template <> struct Pack<__half> {
+    static __device__ __forceinline__ uint32_t two(float lo, float hi)
+    {
+        uint32_t r;
+        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+        return r;
+    }
+};
+
+// ---------------------------------------------------------------------------
+// Pieces of an item
+// ---------------------------------------------------------------------------
+// CTA whose stretch holds tile g of the line
+__device__ __forceinline__ int32_t owner(int64_t g, int64_t total, int64_t ctas)
+{
+    return (int32_t)(((g + 1) * ctas - 1) / total);
+}
+// a CTA has at most two pieces: one that goes on an item begun before it (0)
+// and one of an item that goes on after it (1)
+__device__ __forceinline__ int32_t piece_slot(int32_t cta0, int32_t p) { return p == 0 ? 2 * cta0 + 1 : 2 * (cta0 + p); }
+
+// ---------------------------------------------------------------------------
+// Host: tensor maps of a cache (pp_attend.cu)
+// ---------------------------------------------------------------------------
+pp_status cache_map(const pp_kv *kv, const void *cache, int32_t rows, CUtensorMap *map);
+AttendDev attend_dev(const pp_kv *kv, const AttendArgs &c);
+
+pp_status launch_attend_token(pp_kv *kv, const AttendArgs &c, cudaStream_t st);
+
+}  // namespace pp

@@ -387,6 +387,13 @@ extern "C" pp_status pp_kv_create(int32_t blocks, int32_t block_size, int32_t kv
         PP_CUDA(cudaDeviceGetAttribute(&kv->sm_count, cudaDevAttrMultiProcessorCount, kv->device));
         PP_CUDA(cudaMalloc(&kv->d_status, sizeof(int32_t)));
         PP_CUDA(cudaMemsetAsync(kv->d_status, 0, sizeof(int32_t), (cudaStream_t)stream));
+        // two pieces a CTA, one CTA an SM
+        const size_t slots = 2 * (size_t)kv->sm_count;
+        PP_CUDA(cudaMalloc(&kv->d_piece, slots * kPieceRows * kKvMaxDim * sizeof(float)));
+        PP_CUDA(cudaMalloc(&kv->d_piece_stat, slots * kPieceRows * 2 * sizeof(float)));
+        kv->count_bytes = 4 * slots * sizeof(int32_t);
+        PP_CUDA(cudaMalloc(&kv->d_count, kv->count_bytes));
+        PP_CUDA(cudaMemsetAsync(kv->d_count, 0, kv->count_bytes, (cudaStream_t)stream));
         PP_CUDA(cudaStreamSynchronize((cudaStream_t)stream));
         return PP_OK;
     };
@@ -407,6 +414,9 @@ extern "C" pp_status pp_kv_destroy(pp_kv *kv)
         cudaGetDevice(&cur);
         cudaSetDevice(kv->device);
         cudaFree(kv->d_status);
+        cudaFree(kv->d_piece);
+        cudaFree(kv->d_piece_stat);
+        cudaFree(kv->d_count);
         cudaSetDevice(cur);
     }
     delete kv;
@@ -421,6 +431,8 @@ extern "C" pp_status pp_kv_sync(pp_kv *kv, void *stream)
     PP_CUDA(cudaMemcpy(&v, kv->d_status, sizeof(v), cudaMemcpyDeviceToHost));
     if (v == PP_OK) return PP_OK;
     PP_CUDA(cudaMemset(kv->d_status, 0, sizeof(int32_t)));
+    // a launch that gave up may have left arrivals
+    if (v == PP_ETIMEOUT) PP_CUDA(cudaMemset(kv->d_count, 0, kv->count_bytes));
     if (v == PP_ETIMEOUT) return fail(PP_ETIMEOUT, "a bounded device wait ran out");
     if (v == PP_EBOUNDS)
         return fail(PP_EBOUNDS, "device bounds check failed (a length, block, slot, chunk or token count)");

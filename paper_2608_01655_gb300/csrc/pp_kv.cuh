@@ -18,6 +18,11 @@ struct pp_kv {
     int32_t dtype = 0;
     int64_t block_stride = 0, token_stride = 0, head_stride = 0;     // elements
     int32_t *d_status = nullptr;        // device status word
+    // scratch of the attention: pieces of items that several CTAs computed, their
+    // maxima and sums, and arrival counts (0 between launches)
+    float *d_piece = nullptr, *d_piece_stat = nullptr;
+    int32_t *d_count = nullptr;
+    size_t count_bytes = 0;
 };
 
 namespace pp {
@@ -26,6 +31,7 @@ constexpr int kKvMaxDim = 128;
 constexpr int kKvMaxBlock = 512;
 constexpr int32_t kKvMaxRequests = 16384;
 constexpr int32_t kKvMaxBlocks = 1 << 30;
+constexpr int kPieceRows = 256;                 // rows of a piece, at most
 
 // one call of pp_paged_attention, checked
 struct AttendArgs {
