@@ -596,9 +596,9 @@ pp_status pp_kv_write(pp_kv *kv, int32_t tokens, const void *k, int64_t k_token_
  * output's sum are 32-bit; the weights are rounded to the cache's type for
  * their product with V.  Results do not depend on the run, but the last bits
  * may depend on which other requests are in the call.
- * A block out of range that a query would see, or lengths and offsets out of
- * range, set PP_EBOUNDS; what they would have reached counts as not visible.
- * Errors: PP_EINVAL, PP_ECUDA.
+ * A block out of range that a query would see (its rows read as zeros), or
+ * lengths and offsets out of range (cut to the range), set PP_EBOUNDS.
+ * Errors: PP_EINVAL (also tokens * q_heads / kv_heads above 2^30), PP_ECUDA.
  */
 pp_status pp_paged_attention(pp_kv *kv, int32_t requests, int32_t tokens, int32_t q_heads, const void *q,
                              int64_t q_token_stride, int64_t q_head_stride, const void *k_cache,

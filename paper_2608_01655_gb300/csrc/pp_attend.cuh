@@ -231,8 +231,9 @@ __device__ __forceinline__ uint64_t attend_ns()
 
 // Bounded wait.  When one runs out, `dead` (of the CTA) is set and no later
 // wait of the CTA waits: its loops run to their end over whatever is there, the
-// status says PP_ETIMEOUT, and the launch ends.
-static __device__ __noinline__ void mbar_wait_slow(uint32_t bar, uint32_t parity, volatile int32_t *dead, int32_t *status)
+// status says PP_ETIMEOUT, and the launch ends.  (Inlined: a call would keep
+// registers from code that runs on a share of its own.)
+__device__ __forceinline__ void mbar_wait_slow(uint32_t bar, uint32_t parity, volatile int32_t *dead, int32_t *status)
 {
     const uint64_t t0 = attend_ns();
     while (!mbar_try(bar, parity)) {
@@ -309,5 +310,6 @@ pp_status cache_map(const pp_kv *kv, const void *cache, int32_t rows, CUtensorMa
 AttendDev attend_dev(const pp_kv *kv, const AttendArgs &c);
 
 pp_status launch_attend_token(pp_kv *kv, const AttendArgs &c, cudaStream_t st);
+pp_status launch_attend_chunk(pp_kv *kv, const AttendArgs &c, cudaStream_t st);
 
 }  // namespace pp

@@ -1,0 +1,749 @@
+// Attention of chunks of new tokens over the paged cache, on tcgen05.
+//
+// The queries of a K/V head are rows (token, head of the group), token first,
+// so 128 rows are a few neighbouring tokens whatever the group is, and only
+// tiles on the diagonal need masks.  An item is 256 rows: two stages of 128 that
+// share every K and V tile (128 keys).  Per stage and tile
+//   S = Q K^T      operands in shared memory, accumulator in tensor memory,
+//   P = exp2(scale S - m) by one warpgroup, a row a thread, written over S,
+//   O += P V       P from tensor memory, V as it lies in the cache.
+// The stages take turns: while one warpgroup works on its S, the tensor cores
+// run the other stage's products.  m follows the running maximum only when it
+// is exceeded by more than 8 in log2, so O is rescaled (in tensor memory) in the
+// first tiles and hardly ever later; weights are at most 2^8 then, which both
+// 16-bit types hold as precisely.
+//
+// Warps: 0-3 and 4-7 the stages' softmax and epilogue, 8 the products, 9 the
+// copies, 10-11 look over the V tiles that not every row may see: an infinity
+// or a NaN there would pass through a weight of 0, so it is replaced by 0 and
+// added in the epilogue to the rows that do see it.
+#include <algorithm>
+#include <climits>
+
+#include "pp_attend.cuh"
+
+namespace pp {
+
+namespace chunk {
+constexpr int KT = 128;                             // keys per tile
+constexpr int kRows = 128;                          // rows of a stage
+constexpr int kThreads = 384;
+constexpr int kVMarks = 8;                          // barriers of looked-over V tiles
+constexpr int kBad = 16;
+constexpr float kSlack = 8.f;                       // log2 by which a score may exceed m
+
+template <int HALVES> struct Layout {
+    static constexpr int half = KT * 128;                       // bytes of 64 columns of a tile
+    static constexpr int tile = half * HALVES;
+    static constexpr int slots = HALVES == 2 ? 5 : 10;          // K and V tiles in flight
+    static constexpr int width = 64 * HALVES;
+    static constexpr int bytes = 1024 + (2 + slots) * tile;
+};
+
+struct Shape {
+    static constexpr int KT = chunk::KT;
+    static __device__ __forceinline__ int32_t outer(const AttendDev &a) { return a.kv_heads; }
+    static __device__ __forceinline__ int32_t rows(const AttendDev &a, const Req &q) { return q.q_len * a.c.group; }
+    static __device__ __forceinline__ int32_t inner(const AttendDev &a, const Req &q)
+    {
+        return (rows(a, q) + 2 * kRows - 1) / (2 * kRows);
+    }
+    static __device__ __forceinline__ int32_t pos(const AttendDev &a, const Req &q, int32_t row)
+    {
+        return q.length - q.q_len + row / a.c.group;
+    }
+    static __device__ __forceinline__ Keys keys(const AttendDev &a, const Req &q, int32_t i)
+    {
+        const int32_t r0 = i * 2 * kRows, r1 = min(r0 + 2 * kRows, rows(a, q)) - 1;
+        return {first_key(a, max(pos(a, q, r0), 0)), pos(a, q, r1)};
+    }
+};
+
+// what rows [r0, r1] of a request all see
+struct Common {
+    int32_t lo, hi;
+    __device__ __forceinline__ Common(const AttendDev &a, const Req &q, int32_t r0, int32_t r1)
+        : lo(first_key(a, Shape::pos(a, q, r1))), hi(Shape::pos(a, q, r0))
+    {
+    }
+    __device__ __forceinline__ bool covers(int32_t j0) const { return j0 >= lo && j0 + KT - 1 <= hi; }
+};
+}  // namespace chunk
+
+using namespace chunk;
+
+// ---------------------------------------------------------------------------
+// tcgen05
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_commit(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+// 32 columns of this warp's 32 lanes
+__device__ __forceinline__ void tc_ld32(uint32_t *r, uint32_t addr)
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr));
+}
+__device__ __forceinline__ void tc_st32(uint32_t addr, const uint32_t *r)
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::"r"(r[0]),
+        "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
+        "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]),
+        "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(addr)
+        : "memory");
+}
+
+__device__ __forceinline__ void tc_ld8(uint32_t *r, uint32_t addr)
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(addr));
+}
+__device__ __forceinline__ void tc_st8(uint32_t addr, const uint32_t *r)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"r"(r[0]), "r"(r[1]),
+                 "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(addr)
+                 : "memory");
+}
+
+// Shared-memory operand: rows of 128 bytes swizzled by 128 bytes, groups of 8
+// rows `group` bytes apart; for an operand whose long side is contiguous
+// (V), `next` is the distance of its 64-element halves.
+__device__ __forceinline__ uint64_t smem_operand(uint32_t addr, uint32_t next, uint32_t group)
+{
+    return (uint64_t)((addr & 0x3ffff) >> 4) | (uint64_t)(next >> 4) << 16 | (uint64_t)(group >> 4) << 32 |
+           (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+// 32-bit sums of 16-bit products, 128 rows; `transposed`: B's rows run along the summed index
+template <typename T> __device__ __forceinline__ uint32_t mma_kind(int n, bool transposed)
+{
+    const uint32_t type = sizeof(KvType<T>) && std::is_same<T, __nv_bfloat16>::value ? 1 : 0;
+    return 1u << 4 | type << 7 | type << 10 | (transposed ? 1u << 16 : 0) | (uint32_t)(n / 8) << 17 | (128u / 16) << 24;
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t kind, bool add)
+{
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        "setp.ne.b32 p, %4, 0;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n"
+        "}\n" ::"r"(d),
+        "l"(a), "l"(b), "r"(kind), "r"((uint32_t)add)
+        : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t kind, bool add)
+{
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        "setp.ne.b32 p, %4, 0;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n"
+        "}\n" ::"r"(d),
+        "r"(a), "l"(b), "r"(kind), "r"((uint32_t)add)
+        : "memory");
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t pair(float lo, float hi)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float2 unpair(uint64_t x)
+{
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+
+// x * 0 + acc: stays 0 unless x has an infinity or a NaN
+template <typename T> __device__ __forceinline__ uint32_t taint(uint32_t x, uint32_t acc)
+{
+    uint32_t r;
+    if constexpr (std::is_same<T, __nv_bfloat16>::value)
+        asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(x), "r"(0u), "r"(acc));
+    else
+        asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(x), "r"(0u), "r"(acc));
+    return r;
+}
+// 16-bit value without a finite number
+template <typename T> __device__ __forceinline__ bool not_finite(uint32_t bits)
+{
+    const uint32_t e = std::is_same<T, __nv_bfloat16>::value ? 0x7f80u : 0x7c00u;
+    return (bits & e) == e;
+}
+
+// ---------------------------------------------------------------------------
+// The roles
+// ---------------------------------------------------------------------------
+struct Bars {
+    uint32_t full, empty, v_ok, q_full, s_full, p_full, o_done, o_free, fin;     // shared addresses
+};
+
+// K and V tiles of the stretch, in turn, a box a lane: lanes are (half, box).
+template <int HALVES>
+__device__ __forceinline__ void copy_role(const AttendDev &a, const SchedShared &sched, const CUtensorMap *km,
+                                          const CUtensorMap *vm, uint32_t slot0, const Bars &b, volatile int32_t *dead)
+{
+    using L = Layout<HALVES>;
+    const int lane = threadIdx.x & 31;
+    const int box_log = min(a.block_log, 7), boxes = KT >> box_log;        // 16 at most
+    const int box = lane % boxes, half = lane / boxes;
+    const bool active = half < HALVES;
+    const uint32_t dst = half * L::half + (box << box_log) * 128;
+
+    Cursor<Shape> cur(a, sched);
+    uint32_t seq = 0;
+    do {
+        const int32_t *row = a.c.block_table + (int64_t)cur.r * a.c.table_width;
+        const int32_t t0 = cur.k.lo / KT + cur.off;
+        auto entry = [&](int32_t t) {
+            const int32_t j = t * KT + (box << box_log);
+            if (!active || j > cur.k.hi || j + (1 << box_log) <= cur.k.lo) return a.blocks;
+            int32_t id = row[j >> a.block_log];
+            if (id < 0 || id >= a.blocks) {
+                kv_bounds(a.status);
+                id = a.blocks;
+            }
+            return id;
+        };
+        int32_t id = entry(t0);
+        for (int32_t i = 0; i < cur.len && !*dead; ++i) {
+            const int32_t after = i + 1 < cur.len ? entry(t0 + i + 1) : 0;
+            const int32_t token = ((t0 + i) * KT + (box << box_log)) & ((1 << a.block_log) - 1);
+#pragma unroll
+            for (int which = 0; which < 2; ++which) {
+                const uint32_t s = seq % L::slots, turn = seq / L::slots;
+                if (turn) mbar_wait(b.empty + 8 * s, (turn - 1) & 1, dead, a.status);
+                if (*dead) break;
+                if (lane == 0) mbar_expect(b.full + 8 * s, L::tile);
+                __syncwarp();
+                if (active)
+                    tma_rows(slot0 + s * L::tile + dst, which ? vm : km, b.full + 8 * s, half * 64, token, cur.outer, id);
+                ++seq;
+            }
+            id = after;
+        }
+    } while (!*dead && cur.next(a));
+    if (*dead) {
+        // copies in flight land before the CTA ends
+        int32_t none = 0;
+        for (uint32_t x = seq > L::slots ? seq - L::slots : 0; x < seq; ++x)
+            mbar_wait(b.full + 8 * (x % L::slots), (x / L::slots) & 1, &none, a.status);
+    }
+}
+
+// Tensor memory: S (and P over it) of stage s at column 128 s, O at 256 + 128 s.
+template <typename T, int HALVES>
+__device__ __forceinline__ void mma_role(const AttendDev &a, const SchedShared &sched, uint32_t q0, uint32_t slot0,
+                                         uint32_t tmem, const Bars &b, volatile int32_t *dead)
+{
+    using L = Layout<HALVES>;
+    const bool lead = (threadIdx.x & 31) == 0;
+    const uint32_t kind_s = mma_kind<T>(KT, false), kind_o = mma_kind<T>(L::width, true);
+    Cursor<Shape> sc(a, sched), pc(a, sched);          // next S, next O
+    int32_t si = 0, pi = 0;                             // their tiles within the items
+    uint32_t sk = 0, pk = 0;                            // and along the stretch
+    uint32_t q_turn[2] = {0, 0}, p_turn[2] = {0, 0}, o_turn[2] = {0, 0};
+    auto two = [&](const Cursor<Shape> &c) { return Shape::rows(a, c.q) - c.inner * 2 * kRows > kRows; };
+
+    auto issue_s = [&](int s) {
+        const uint32_t seq = 2 * sk, slot = seq % L::slots;
+        if (si == 0) {
+            mbar_wait(b.q_full + 8 * s, q_turn[s] & 1, dead, a.status);
+            q_turn[s]++;
+        }
+        mbar_wait(b.full + 8 * slot, (seq / L::slots) & 1, dead, a.status);
+        tc_after();
+        if (lead) {
+#pragma unroll
+            for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    mma_ss(tmem + 128 * s, smem_operand(q0 + s * L::tile + h * L::half + 32 * k, 16, 1024),
+                           smem_operand(slot0 + slot * L::tile + h * L::half + 32 * k, 16, 1024), kind_s, h + k > 0);
+            tc_commit(b.s_full + 8 * s);
+        }
+    };
+    auto after_s = [&]() {                              // tile done with K; on to the next
+        if (lead) tc_commit(b.empty + 8 * (2 * sk % L::slots));
+        ++sk;
+        if (++si == sc.len) {
+            si = 0;
+            return sc.next(a);
+        }
+        return true;
+    };
+    auto issue_o = [&](int s) {
+        const uint32_t seq = 2 * pk + 1, slot = seq % L::slots;
+        mbar_wait(b.p_full + 8 * s, p_turn[s] & 1, dead, a.status);
+        p_turn[s]++;
+        mbar_wait(b.v_ok + 8 * (pk % kVMarks), (pk / kVMarks) & 1, dead, a.status);
+        if (pi == 0) {
+            if (o_turn[s]) mbar_wait(b.o_free + 8 * s, (o_turn[s] - 1) & 1, dead, a.status);
+            o_turn[s]++;
+        }
+        tc_after();
+        if (lead) {
+#pragma unroll
+            for (int k = 0; k < KT / 16; ++k)
+                mma_ts(tmem + 256 + 128 * s, tmem + 128 * s + 8 * k,
+                       smem_operand(slot0 + slot * L::tile + 2048 * k, L::half, 1024), kind_o, pi > 0 || k > 0);
+            if (pi == pc.len - 1) tc_commit(b.o_done + 8 * s);
+        }
+    };
+
+    issue_s(0);
+    if (two(sc)) issue_s(1);
+    bool more = after_s();                              // an S is still to be issued
+    for (bool go = true; go;) {
+        const bool two_o = two(pc), two_s = more && two(sc), inside = pi + 1 < pc.len;
+        issue_o(0);
+        if (more && inside) issue_s(0);
+        if (two_o) issue_o(1);
+        if (lead) tc_commit(b.empty + 8 * ((2 * pk + 1) % L::slots));
+        if (more && !inside) issue_s(0);                // the next item's queries may not be there yet
+        if (two_s) issue_s(1);
+        if (more) more = after_s();
+        ++pk;
+        if (++pi == pc.len) {
+            pi = 0;
+            go = pc.next(a);
+        }
+    }
+    // every product has ended before the tensor memory is given back
+    if (lead) tc_commit(b.fin);
+    int32_t none = 0;
+    mbar_wait(b.fin, 0, &none, a.status);
+}
+
+// Looks over the V tiles that some row of the item does not see in full.
+template <typename T, int HALVES>
+__device__ __forceinline__ void look_role(const AttendDev &a, const SchedShared &sched, uint8_t *slots, const Bars &b,
+                                          volatile int32_t *bad, volatile int32_t *dead)
+{
+    using L = Layout<HALVES>;
+    const int lane = threadIdx.x & 31, w = (threadIdx.x >> 5) & 1;
+    Cursor<Shape> cur(a, sched);
+    uint32_t k = 0;
+    int32_t item = 0;
+    do {
+        const int32_t r0 = cur.inner * 2 * kRows;
+        const Common all(a, cur.q, r0, min(r0 + 2 * kRows, Shape::rows(a, cur.q)) - 1);
+        for (int32_t i = 0; i < cur.len; ++i, ++k) {
+            const uint32_t seq = 2 * k + 1, slot = seq % L::slots;
+            mbar_wait(b.full + 8 * slot, (seq / L::slots) & 1, dead, a.status);
+            const int32_t j0 = (cur.k.lo / KT + cur.off + i) * KT;
+            if (!all.covers(j0)) {
+                uint4 *v = reinterpret_cast<uint4 *>(slots + slot * L::tile) + w * (L::tile / 32);
+                uint32_t t = 0;
+#pragma unroll 8
+                for (int x = lane; x < L::tile / 32; x += 32) {
+                    const uint4 y = v[x];
+                    t = taint<T>(y.x, taint<T>(y.y, taint<T>(y.z, taint<T>(y.w, t))));
+                }
+                if (__any_sync(~0u, (t & 0x7fff7fffu) != 0)) {
+                    for (int x = lane; x < L::tile / 32; x += 32) {
+                        uint4 y = v[x];
+                        uint32_t *e = &y.x, hit = 0;
+#pragma unroll
+                        for (int n = 0; n < 4; ++n) {
+                            if (not_finite<T>(e[n])) { e[n] &= 0xffff0000u; hit = 1; }
+                            if (not_finite<T>(e[n] >> 16)) { e[n] &= 0xffffu; hit = 1; }
+                        }
+                        if (!hit) continue;
+                        v[x] = y;
+                        const int32_t j = j0 + (int32_t)((w * (L::tile / 2) + x * 16) % L::half / 128);
+                        if (j >= cur.k.lo && j <= cur.k.hi) bad[item % kBad] = item + 1;
+                    }
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(b.v_ok + 8 * (k % kVMarks));
+        }
+        ++item;
+    } while (cur.next(a));
+}
+
+// One stage: queries to shared memory, softmax of its S, its output.
+template <typename T, int HALVES>
+__device__ __forceinline__ void softmax_role(const AttendDev &a, const SchedShared &sched, uint8_t *q_smem, uint32_t tmem,
+                                             const Bars &b, volatile int32_t *bad, volatile int32_t *dead,
+                                             volatile int32_t *last)
+{
+    using L = Layout<HALVES>;
+    const int s = threadIdx.x >> 7, t = threadIdx.x & 127;
+    const uint32_t lanes = (uint32_t)(t & ~31) << 16;
+    const uint32_t t_s = tmem + lanes + 128 * s, t_o = tmem + lanes + 256 + 128 * s;
+    const int64_t total = sched.total, ctas = min((int64_t)gridDim.x, total);
+
+    // rows of stage s in an item; this thread's row
+    auto base_of = [&](const Cursor<Shape> &c) { return c.inner * 2 * kRows + s * kRows; };
+    auto load_q = [&](const Cursor<Shape> &c) {
+        const int32_t r0 = base_of(c), rows = Shape::rows(a, c.q);
+        constexpr int per = 8 * HALVES;                 // 16-byte pieces of a row
+        uint4 y[per];
+#pragma unroll
+        for (int i = 0; i < per; ++i) {
+            const int x = i * kRows + t, row = r0 + x / per, d = x % per * 8;
+            const int32_t tok = row / a.c.group, g = row % a.c.group;
+            y[i] = row < rows && d < a.dim
+                       ? __ldg(reinterpret_cast<const uint4 *>(
+                             static_cast<const T *>(a.c.q) + (int64_t)(c.q.first + tok) * a.c.q_token_stride +
+                             (int64_t)(c.outer * a.c.group + g) * a.c.q_head_stride + d))
+                       : make_uint4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < per; ++i) {
+            const int x = i * kRows + t, row = x / per, piece = x % per;
+            *reinterpret_cast<uint4 *>(q_smem + s * L::tile + (piece >> 3) * L::half + row * 128 +
+                                       (((piece ^ row) & 7) << 4)) = y[i];
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        mbar_arrive(b.q_full + 8 * s);
+    };
+
+    Cursor<Shape> cur(a, sched);
+    uint32_t s_turn = 0, o_turn = 0;
+    int32_t item = 0;
+    bool loaded = false;
+    for (bool go = true; go; ++item) {
+        const int32_t rows = Shape::rows(a, cur.q), r0 = base_of(cur), row = r0 + t;
+        if (r0 >= rows) {                               // this item has one stage only
+            go = cur.next(a);
+            continue;
+        }
+        if (!loaded) load_q(cur);
+        loaded = false;
+        const bool live = row < rows;
+        const int32_t pos = live ? Shape::pos(a, cur.q, row) : -1, lo = pos < 0 ? 0 : first_key(a, pos);
+        const Common all(a, cur.q, r0, min(r0 + kRows, rows) - 1);
+        const int32_t t0 = cur.k.lo / KT + cur.off;
+        float m = -INFINITY, l = 0.f;
+
+        for (int32_t i = 0; i < cur.len; ++i) {
+            mbar_wait(b.s_full + 8 * s, s_turn++ & 1, dead, a.status);
+            tc_after();
+            uint32_t x[KT];
+#pragma unroll
+            for (int c = 0; c < KT; c += 32) tc_ld32(x + c, t_s + c);
+            tc_wait_ld();
+            const int32_t j0 = (t0 + i) * KT;
+            if (!all.covers(j0)) {
+                const int32_t from = lo - j0, to = pos - j0;
+#pragma unroll
+                for (int c = 0; c < KT; ++c)
+                    if (c < from || c > to) x[c] = 0xff800000u;
+            }
+            float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+            for (int c = 0; c < KT; c += 8)
+#pragma unroll
+                for (int y = 0; y < 4; ++y)
+                    top[y] = max3(top[y], __uint_as_float(x[c + 2 * y]), __uint_as_float(x[c + 2 * y + 1]));
+            const float high = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.scale_log2;
+            if (i == 0) {
+                m = high;
+            } else if (__any_sync(~0u, high > m + kSlack)) {
+                // every product on O that was issued before this S has ended with it
+                const float up = high > m + kSlack ? high : m;
+                const float f = up == m ? 1.f : exp2_approx(m - up);
+                m = up;
+                l *= f;
+#pragma unroll 1
+                for (int c = 0; c < L::width; c += 8) {
+                    uint32_t o[8];
+                    tc_ld8(o, t_o + c);
+                    tc_wait_ld();
+#pragma unroll
+                    for (int y = 0; y < 8; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * f);
+                    tc_st8(t_o + c, o);
+                }
+            }
+            const float base = m == -INFINITY ? 0.f : m;
+            const uint64_t mul = pair(a.scale_log2, a.scale_log2), sub = pair(-base, -base);
+            uint64_t sum[2] = {0, 0};
+#pragma unroll
+            for (int c = 0; c < KT; c += 2) {
+                const float2 e = unpair(fma2(pair(__uint_as_float(x[c]), __uint_as_float(x[c + 1])), mul, sub));
+                const float p0 = exp2_approx(e.x), p1 = exp2_approx(e.y);
+                sum[(c >> 1) & 1] = add2(sum[(c >> 1) & 1], pair(p0, p1));
+                x[c / 2] = Pack<T>::two(p0, p1);
+            }
+            tc_st32(t_s, x);
+            tc_st32(t_s + 32, x + 32);
+            const float2 both = unpair(add2(sum[0], sum[1]));
+            l += both.x + both.y;
+            tc_wait_st();
+            tc_before();
+            mbar_arrive(b.p_full + 8 * s);
+        }
+        // the next item's queries before this one's output: its first product can start
+        Cursor<Shape> nxt = cur;
+        go = nxt.next(a);
+        if (go && base_of(nxt) < Shape::rows(a, nxt.q)) {
+            load_q(nxt);
+            loaded = true;
+        }
+
+        mbar_wait(b.o_done + 8 * s, o_turn++ & 1, dead, a.status);
+        tc_after();
+        const int32_t tok = cur.q.first + row / a.c.group, head = cur.outer * a.c.group + row % a.c.group;
+        auto put_out = [&](const float *o, int c, float inv) {
+            T *dst = static_cast<T *>(a.c.out) + (int64_t)tok * a.c.out_token_stride + (int64_t)head * a.c.out_head_stride + c;
+#pragma unroll
+            for (int y = 0; y < 32; y += 8)
+                if (live && c + y < a.dim)
+                    *reinterpret_cast<uint4 *>(dst + y) = make_uint4(
+                        Pack<T>::two(o[y] * inv, o[y + 1] * inv), Pack<T>::two(o[y + 2] * inv, o[y + 3] * inv),
+                        Pack<T>::two(o[y + 4] * inv, o[y + 5] * inv), Pack<T>::two(o[y + 6] * inv, o[y + 7] * inv));
+        };
+        auto put_lse = [&](float top, float sum) {
+            if (live && a.c.lse)
+                a.c.lse[(int64_t)tok * a.c.q_heads + head] =
+                    sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+        };
+        const bool whole = cur.whole();
+        const int64_t g0 = cur.g - cur.off;
+        const int32_t cta0 = owner(g0, total, ctas), pieces = owner(g0 + cur.tiles - 1, total, ctas) - cta0 + 1;
+        const int32_t mine = (int32_t)blockIdx.x - cta0;
+        auto stat_at = [&](int32_t p) { return a.piece_stat + (piece_slot(cta0, p) * 2 + s) * 2 * kRows + t; };
+        auto piece_at = [&](int32_t p, int c) {
+            return reinterpret_cast<float4 *>(a.piece) + ((int64_t)(piece_slot(cta0, p) * 2 + s) * (L::width / 4) + c / 4) * kRows + t;
+        };
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const bool fix = bad[item % kBad] == item + 1;
+#pragma unroll 1
+        for (int c = 0; c < L::width; c += 32) {
+            uint32_t x[32];
+            float o[32];
+            tc_ld32(x, t_o + c);
+            tc_wait_ld();
+#pragma unroll
+            for (int y = 0; y < 32; ++y) o[y] = __uint_as_float(x[y]);
+            if (fix) {
+                const Common any(a, cur.q, cur.inner * 2 * kRows, min(cur.inner * 2 * kRows + 2 * kRows, rows) - 1);
+                for (int32_t j = max(lo, t0 * KT); j <= min(pos, (t0 + cur.len) * KT - 1); ++j) {
+                    if (any.covers(j / KT * KT)) continue;
+                    const int32_t id = a.c.block_table[(int64_t)cur.r * a.c.table_width + (j >> a.block_log)];
+                    if (id < 0 || id >= a.blocks) continue;
+                    const T *v = static_cast<const T *>(a.c.v_cache) + id * a.block_stride +
+                                 (j & ((1 << a.block_log) - 1)) * a.token_stride + cur.outer * a.head_stride + c;
+#pragma unroll
+                    for (int y = 0; y < 32; ++y)
+                        if (c + y < a.dim) {
+                            const float z = KvType<T>::to_float(v[y]);
+                            if (!(fabsf(z) < INFINITY)) o[y] += z;
+                        }
+                }
+            }
+            if (whole) {
+                put_out(o, c, inv);
+            } else {
+#pragma unroll
+                for (int y = 0; y < 32; y += 4)
+                    piece_at(mine, c)[y / 4 * kRows] = make_float4(o[y], o[y + 1], o[y + 2], o[y + 3]);
+            }
+        }
+        tc_before();
+        mbar_arrive(b.o_free + 8 * s);
+        if (whole) {
+            put_lse(m, l);
+        } else {
+            stat_at(mine)[0] = m;
+            stat_at(mine)[kRows] = l;
+            auto arrive = [&](int32_t *count, int32_t of) {
+                __threadfence();
+                named_sync(1 + s, kRows);
+                if (t == 0) {
+                    last[s] = atomicAdd(count, 1) == of - 1;
+                    if (last[s]) *count = 0;
+                }
+                named_sync(1 + s, kRows);
+                __threadfence();
+                return last[s] != 0;
+            };
+            // join n pieces p0, p0 + step, ... into the output (out) or into p0
+            auto gather = [&](int32_t p0, int32_t n, int32_t step, bool out) {
+                float top = -INFINITY, sum = 0.f;
+                for (int32_t p = 0; p < n; ++p) top = fmaxf(top, __ldcg(stat_at(p0 + p * step)));
+                const float base = top == -INFINITY ? 0.f : top;
+                for (int32_t p = 0; p < n; ++p)
+                    sum = fmaf(exp2_approx(__ldcg(stat_at(p0 + p * step)) - base), __ldcg(stat_at(p0 + p * step) + kRows), sum);
+                const float scale = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll 1
+                for (int c = 0; c < L::width; c += 32) {
+                    float o[32];
+#pragma unroll
+                    for (int y = 0; y < 32; ++y) o[y] = 0.f;
+                    for (int32_t p = 0; p < n; ++p) {
+                        const float f = exp2_approx(__ldcg(stat_at(p0 + p * step)) - base);
+                        const float4 *src = piece_at(p0 + p * step, c);
+#pragma unroll
+                        for (int y = 0; y < 32; y += 4) {
+                            const float4 z = __ldcg(src + y / 4 * kRows);
+                            o[y] = fmaf(f, z.x, o[y]);
+                            o[y + 1] = fmaf(f, z.y, o[y + 1]);
+                            o[y + 2] = fmaf(f, z.z, o[y + 2]);
+                            o[y + 3] = fmaf(f, z.w, o[y + 3]);
+                        }
+                    }
+                    if (out) {
+                        put_out(o, c, scale);
+                    } else {
+#pragma unroll
+                        for (int y = 0; y < 32; y += 4)
+                            piece_at(p0, c)[y / 4 * kRows] = make_float4(o[y], o[y + 1], o[y + 2], o[y + 3]);
+                    }
+                }
+                if (out) {
+                    put_lse(top, sum);
+                } else {
+                    stat_at(p0)[0] = top;
+                    stat_at(p0)[kRows] = sum;
+                }
+            };
+            const int32_t groups = (pieces + kJoinGroup - 1) / kJoinGroup;
+            const int32_t p0 = mine / kJoinGroup * kJoinGroup, n = min(kJoinGroup, pieces - p0);
+            if (arrive(a.count + 2 * piece_slot(cta0, p0) + s, n)) {
+                gather(p0, n, 1, groups == 1);
+                if (groups > 1 && arrive(a.count + 4 * gridDim.x + 2 * piece_slot(cta0, 0) + s, groups))
+                    gather(0, groups, kJoinGroup, true);
+            }
+        }
+        cur = nxt;
+    }
+}
+
+template <typename T, int HALVES>
+__global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_constant__ AttendDev a,
+                                                              const __grid_constant__ CUtensorMap km,
+                                                              const __grid_constant__ CUtensorMap vm)
+{
+    using L = Layout<HALVES>;
+    extern __shared__ uint8_t raw[];
+    __shared__ SchedShared sched;
+    __shared__ alignas(8) uint64_t bar[2 * L::slots + kVMarks + 11];
+    __shared__ int32_t dead, last[2], bad[kBad];
+    __shared__ uint32_t tmem_at;
+    const int tid = threadIdx.x, warp = tid >> 5;
+    const uint32_t base = (smem_u32(raw) + 1023) & ~1023u;
+    uint8_t *mem = raw + (base - smem_u32(raw));
+    Bars b;
+    b.full = smem_u32(bar);
+    b.empty = b.full + 8 * L::slots;
+    b.v_ok = b.empty + 8 * L::slots;
+    b.q_full = b.v_ok + 8 * kVMarks;
+    b.s_full = b.q_full + 16;
+    b.p_full = b.s_full + 16;
+    b.o_done = b.p_full + 16;
+    b.o_free = b.o_done + 16;
+    b.fin = b.o_free + 16;
+    if (tid == 0) {
+        dead = 0;
+        for (int i = 0; i < L::slots; ++i) {
+            mbar_init(b.full + 8 * i, 1);
+            mbar_init(b.empty + 8 * i, 1);
+        }
+        for (int i = 0; i < kVMarks; ++i) mbar_init(b.v_ok + 8 * i, 2);
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(b.q_full + 8 * s, kRows);
+            mbar_init(b.s_full + 8 * s, 1);
+            mbar_init(b.p_full + 8 * s, kRows);
+            mbar_init(b.o_done + 8 * s, 1);
+            mbar_init(b.o_free + 8 * s, kRows);
+        }
+        mbar_init(b.fin, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (tid < kBad) bad[tid] = 0;
+    if (!schedule<Shape>(a, sched)) return;
+    if (warp == 8) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_at)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        tc_before();
+    }
+    __syncthreads();
+    tc_after();
+    const uint32_t tmem = tmem_at, slot0 = base + 2 * L::tile;
+
+    // 384 threads x 168 registers = 256 x 208 + 128 x 88
+    if (warp < 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+        softmax_role<T, HALVES>(a, sched, mem, tmem, b, bad, &dead, last);
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        if (warp == 8) mma_role<T, HALVES>(a, sched, base, slot0, tmem, b, &dead);
+        else if (warp == 9) copy_role<HALVES>(a, sched, &km, &vm, slot0, b, &dead);
+        else look_role<T, HALVES>(a, sched, mem + 2 * L::tile, b, bad, &dead);
+    }
+    tc_before();
+    __syncthreads();
+    if (warp == 8) {
+        tc_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+    }
+}
+
+template <typename T, int HALVES>
+static pp_status launch_t(pp_kv *kv, const AttendArgs &c, cudaStream_t st)
+{
+    const AttendDev a = attend_dev(kv, c);
+    CUtensorMap km, vm;
+    const int32_t rows = std::min(kv->block_size, KT);
+    pp_status s = cache_map(kv, c.k_cache, rows, &km);
+    if (s == PP_OK) s = cache_map(kv, c.v_cache, rows, &vm);
+    if (s != PP_OK) return s;
+    PP_CUDA(cudaFuncSetAttribute(k_attend_chunk<T, HALVES>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 Layout<HALVES>::bytes));
+    k_attend_chunk<T, HALVES><<<kv->sm_count, kThreads, Layout<HALVES>::bytes, st>>>(a, km, vm);
+    PP_CUDA(cudaGetLastError());
+    return PP_OK;
+}
+
+pp_status launch_attend_chunk(pp_kv *kv, const AttendArgs &c, cudaStream_t st)
+{
+    if ((int64_t)c.tokens * c.group > 1 << 30)
+        return fail(PP_EINVAL, "tokens * q_heads / kv_heads must be at most 2^30");
+    if (kv->dtype == PP_KV_BF16)
+        return kv->dim > 64 ? launch_t<__nv_bfloat16, 2>(kv, c, st) : launch_t<__nv_bfloat16, 1>(kv, c, st);
+    return kv->dim > 64 ? launch_t<__half, 2>(kv, c, st) : launch_t<__half, 1>(kv, c, st);
+}
+
+}  // namespace pp
