@@ -29,7 +29,7 @@ struct AttendDev {
     int32_t *count;                     // [2][slots] arrivals, left at 0 by every launch
 };
 
-constexpr uint64_t kAttendLimitNs = 500ull * 1000 * 1000;   // one wait gives up after 0.5 s
+constexpr int64_t kAttendLimitCycles = 1000ll * 1000 * 1000;  // one wait gives up after about 0.5 s
 constexpr int kJoinGroup = 16;                              // pieces joined at a time
 
 // ---------------------------------------------------------------------------
@@ -222,32 +222,25 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)
         : "memory");
     return ok != 0;
 }
-__device__ __forceinline__ uint64_t attend_ns()
-{
-    uint64_t t;
-    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-    return t;
-}
-
 // Bounded wait.  When one runs out, `dead` (of the CTA) is set and no later
 // wait of the CTA waits: its loops run to their end over whatever is there, the
 // status says PP_ETIMEOUT, and the launch ends.  (Inlined: a call would keep
 // registers from code that runs on a share of its own.)
-__device__ __forceinline__ void mbar_wait_slow(uint32_t bar, uint32_t parity, volatile int32_t *dead, int32_t *status)
+__device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, volatile int32_t *dead, int32_t *status)
 {
-    const uint64_t t0 = attend_ns();
-    while (!mbar_try(bar, parity)) {
+    int64_t t0 = 0;
+    for (uint32_t it = 0; !mbar_try(bar, parity); ++it) {
+        if ((it & 127) != 127) continue;
         if (*dead) return;
-        if (attend_ns() - t0 > kAttendLimitNs) {
+        const int64_t now = clock64();
+        if (t0 == 0) {
+            t0 = now;
+        } else if (now - t0 > kAttendLimitCycles) {
             *dead = 1;
             atomicExch(status, (int32_t)PP_ETIMEOUT);
             return;
         }
     }
-}
-__device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, volatile int32_t *dead, int32_t *status)
-{
-    if (!mbar_try(bar, parity)) mbar_wait_slow(bar, parity, dead, status);
 }
 
 // box of `rows` tokens x 64 elements of one block and head to shared memory, rows

@@ -13,8 +13,8 @@
 // first tiles and hardly ever later; weights are at most 2^8 then, which both
 // 16-bit types hold as precisely.
 //
-// Warps: 0-3 and 4-7 the stages' softmax and epilogue, 8 the products, 9 the
-// copies, 10-11 look over the V tiles that not every row may see: an infinity
+// Warps: 0-3 and 4-7 the stages' softmax and epilogue, 8 and 9 their products, 10
+// the copies, 11 looks over the V tiles that not every row may see: an infinity
 // or a NaN there would pass through a weight of 0, so it is replaced by 0 and
 // added in the epilogue to the rows that do see it.
 #include <algorithm>
@@ -191,6 +191,22 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
     return d;
 }
 
+// one lane of the warp, always the same.  The products are issued under it and
+// not under a comparison of the lane's number: the compiler knows then that a
+// single thread holds their operands (90 cycles an instruction became XX).
+__device__ __forceinline__ bool elected()
+{
+    uint32_t yes;
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        "elect.sync _|p, 0xffffffff;\n"
+        "selp.u32 %0, 1, 0, p;\n"
+        "}\n"
+        : "=r"(yes));
+    return yes != 0;
+}
+
 // x * 0 + acc: stays 0 unless x has an infinity or a NaN
 template <typename T> __device__ __forceinline__ uint32_t taint(uint32_t x, uint32_t acc)
 {
@@ -269,87 +285,79 @@ __device__ __forceinline__ void copy_role(const AttendDev &a, const SchedShared 
 }
 
 // Tensor memory: S (and P over it) of stage s at column 128 s, O at 256 + 128 s.
+// A warp issues one stage's products: issue waits for the tensor cores, so the
+// time that one warp spends on barriers and bookkeeping is the other's products'.
 template <typename T, int HALVES>
-__device__ __forceinline__ void mma_role(const AttendDev &a, const SchedShared &sched, uint32_t q0, uint32_t slot0,
+__device__ __forceinline__ void mma_role(const AttendDev &a, const SchedShared &sched, int s, uint32_t q0, uint32_t slot0,
                                          uint32_t tmem, const Bars &b, volatile int32_t *dead)
 {
     using L = Layout<HALVES>;
-    const bool lead = (threadIdx.x & 31) == 0;
     const uint32_t kind_s = mma_kind<T>(KT, false), kind_o = mma_kind<T>(L::width, true);
-    Cursor<Shape> sc(a, sched), pc(a, sched);          // next S, next O
-    int32_t si = 0, pi = 0;                             // their tiles within the items
-    uint32_t sk = 0, pk = 0;                            // and along the stretch
-    uint32_t q_turn[2] = {0, 0}, p_turn[2] = {0, 0}, o_turn[2] = {0, 0};
-    auto two = [&](const Cursor<Shape> &c) { return Shape::rows(a, c.q) - c.inner * 2 * kRows > kRows; };
-
-    auto issue_s = [&](int s) {
-        const uint32_t seq = 2 * sk, slot = seq % L::slots;
-        if (si == 0) {
-            mbar_wait(b.q_full + 8 * s, q_turn[s] & 1, dead, a.status);
-            q_turn[s]++;
+    const uint32_t t_s = tmem + 128 * s, t_o = tmem + 256 + 128 * s;
+    const uint64_t q_op = smem_operand(q0 + s * L::tile, 16, 1024);
+    Cursor<Shape> cur(a, sched);
+    uint32_t slot = 0, turn = 0, mark = 0, q_turn = 0, p_turn = 0;
+    auto step = [&]() {                                 // to the next slot of the ring
+        if (++slot == L::slots) {
+            slot = 0;
+            turn ^= 1;
         }
-        mbar_wait(b.full + 8 * slot, (seq / L::slots) & 1, dead, a.status);
+    };
+    auto issue_s = [&]() {
+        mbar_wait(b.full + 8 * slot, turn, dead, a.status);
         tc_after();
-        if (lead) {
+        const uint64_t k_op = smem_operand(slot0 + slot * L::tile, 16, 1024);
+        if (elected()) {
 #pragma unroll
             for (int h = 0; h < HALVES; ++h)
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    mma_ss(tmem + 128 * s, smem_operand(q0 + s * L::tile + h * L::half + 32 * k, 16, 1024),
-                           smem_operand(slot0 + slot * L::tile + h * L::half + 32 * k, 16, 1024), kind_s, h + k > 0);
+                for (int k = 0; k < 4; ++k) {
+                    constexpr int half = L::half >> 4;
+                    mma_ss(t_s, q_op + h * half + 2 * k, k_op + h * half + 2 * k, kind_s, h + k > 0);
+                }
             tc_commit(b.s_full + 8 * s);
+            tc_commit(b.empty + 8 * slot);
         }
     };
-    auto after_s = [&]() {                              // tile done with K; on to the next
-        if (lead) tc_commit(b.empty + 8 * (2 * sk % L::slots));
-        ++sk;
-        if (++si == sc.len) {
-            si = 0;
-            return sc.next(a);
+    do {
+        if (s * kRows >= Shape::rows(a, cur.q) - cur.inner * 2 * kRows) {        // no rows in this stage
+            for (int32_t i = 0; i < 2 * cur.len; ++i) {
+                mbar_wait(b.full + 8 * slot, turn, dead, a.status);
+                if (elected()) mbar_arrive(b.empty + 8 * slot);
+                step();
+            }
+            mark += cur.len;
+            continue;
         }
-        return true;
-    };
-    auto issue_o = [&](int s) {
-        const uint32_t seq = 2 * pk + 1, slot = seq % L::slots;
-        mbar_wait(b.p_full + 8 * s, p_turn[s] & 1, dead, a.status);
-        p_turn[s]++;
-        mbar_wait(b.v_ok + 8 * (pk % kVMarks), (pk / kVMarks) & 1, dead, a.status);
-        if (pi == 0) {
-            if (o_turn[s]) mbar_wait(b.o_free + 8 * s, (o_turn[s] - 1) & 1, dead, a.status);
-            o_turn[s]++;
-        }
-        tc_after();
-        if (lead) {
+        mbar_wait(b.q_full + 8 * s, q_turn & 1, dead, a.status);
+        issue_s();
+        // O is free when its last item's output has been read
+        if (q_turn) mbar_wait(b.o_free + 8 * s, (q_turn - 1) & 1, dead, a.status);
+        for (int32_t i = 0; i < cur.len; ++i) {
+            step();                                     // V of tile i; its K was the slot before
+            const uint32_t v_slot = slot;
+            mbar_wait(b.v_ok + 8 * (mark % kVMarks), (mark / kVMarks) & 1, dead, a.status);
+            ++mark;
+            const uint64_t v_op = smem_operand(slot0 + v_slot * L::tile, L::half, 1024);
+            mbar_wait(b.p_full + 8 * s, p_turn & 1, dead, a.status);
+            ++p_turn;
+            tc_after();
+            if (elected()) {
 #pragma unroll
-            for (int k = 0; k < KT / 16; ++k)
-                mma_ts(tmem + 256 + 128 * s, tmem + 128 * s + 8 * k,
-                       smem_operand(slot0 + slot * L::tile + 2048 * k, L::half, 1024), kind_o, pi > 0 || k > 0);
-            if (pi == pc.len - 1) tc_commit(b.o_done + 8 * s);
+                for (int k = 0; k < KT / 16; ++k)
+                    mma_ts(t_o, t_s + 8 * k, v_op + 128 * k, kind_o, i > 0 || k > 0);
+                tc_commit(b.empty + 8 * v_slot);
+                if (i == cur.len - 1) tc_commit(b.o_done + 8 * s);
+            }
+            step();
+            if (i + 1 < cur.len) issue_s();
         }
-    };
-
-    issue_s(0);
-    if (two(sc)) issue_s(1);
-    bool more = after_s();                              // an S is still to be issued
-    for (bool go = true; go;) {
-        const bool two_o = two(pc), two_s = more && two(sc), inside = pi + 1 < pc.len;
-        issue_o(0);
-        if (more && inside) issue_s(0);
-        if (two_o) issue_o(1);
-        if (lead) tc_commit(b.empty + 8 * ((2 * pk + 1) % L::slots));
-        if (more && !inside) issue_s(0);                // the next item's queries may not be there yet
-        if (two_s) issue_s(1);
-        if (more) more = after_s();
-        ++pk;
-        if (++pi == pc.len) {
-            pi = 0;
-            go = pc.next(a);
-        }
-    }
+        ++q_turn;
+    } while (cur.next(a));
     // every product has ended before the tensor memory is given back
-    if (lead) tc_commit(b.fin);
+    if (elected()) tc_commit(b.fin + 8 * s);
     int32_t none = 0;
-    mbar_wait(b.fin, 0, &none, a.status);
+    mbar_wait(b.fin + 8 * s, 0, &none, a.status);
 }
 
 // Looks over the V tiles that some row of the item does not see in full.
@@ -358,7 +366,7 @@ __device__ __forceinline__ void look_role(const AttendDev &a, const SchedShared 
                                           volatile int32_t *bad, volatile int32_t *dead)
 {
     using L = Layout<HALVES>;
-    const int lane = threadIdx.x & 31, w = (threadIdx.x >> 5) & 1;
+    const int lane = threadIdx.x & 31;
     Cursor<Shape> cur(a, sched);
     uint32_t k = 0;
     int32_t item = 0;
@@ -370,15 +378,15 @@ __device__ __forceinline__ void look_role(const AttendDev &a, const SchedShared 
             mbar_wait(b.full + 8 * slot, (seq / L::slots) & 1, dead, a.status);
             const int32_t j0 = (cur.k.lo / KT + cur.off + i) * KT;
             if (!all.covers(j0)) {
-                uint4 *v = reinterpret_cast<uint4 *>(slots + slot * L::tile) + w * (L::tile / 32);
+                uint4 *v = reinterpret_cast<uint4 *>(slots + slot * L::tile);
                 uint32_t t = 0;
 #pragma unroll 8
-                for (int x = lane; x < L::tile / 32; x += 32) {
+                for (int x = lane; x < L::tile / 16; x += 32) {
                     const uint4 y = v[x];
                     t = taint<T>(y.x, taint<T>(y.y, taint<T>(y.z, taint<T>(y.w, t))));
                 }
                 if (__any_sync(~0u, (t & 0x7fff7fffu) != 0)) {
-                    for (int x = lane; x < L::tile / 32; x += 32) {
+                    for (int x = lane; x < L::tile / 16; x += 32) {
                         uint4 y = v[x];
                         uint32_t *e = &y.x, hit = 0;
 #pragma unroll
@@ -388,7 +396,7 @@ __device__ __forceinline__ void look_role(const AttendDev &a, const SchedShared 
                         }
                         if (!hit) continue;
                         v[x] = y;
-                        const int32_t j = j0 + (int32_t)((w * (L::tile / 2) + x * 16) % L::half / 128);
+                        const int32_t j = j0 + (int32_t)(x * 16 % L::half / 128);
                         if (j >= cur.k.lo && j <= cur.k.hi) bad[item % kBad] = item + 1;
                     }
                 }
@@ -659,7 +667,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
     using L = Layout<HALVES>;
     extern __shared__ uint8_t raw[];
     __shared__ SchedShared sched;
-    __shared__ alignas(8) uint64_t bar[2 * L::slots + kVMarks + 11];
+    __shared__ alignas(8) uint64_t bar[2 * L::slots + kVMarks + 12];
     __shared__ int32_t dead, last[2], bad[kBad];
     __shared__ uint32_t tmem_at;
     const int tid = threadIdx.x, warp = tid >> 5;
@@ -679,17 +687,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
         dead = 0;
         for (int i = 0; i < L::slots; ++i) {
             mbar_init(b.full + 8 * i, 1);
-            mbar_init(b.empty + 8 * i, 1);
+            mbar_init(b.empty + 8 * i, 2);
         }
-        for (int i = 0; i < kVMarks; ++i) mbar_init(b.v_ok + 8 * i, 2);
+        for (int i = 0; i < kVMarks; ++i) mbar_init(b.v_ok + 8 * i, 1);
         for (int s = 0; s < 2; ++s) {
             mbar_init(b.q_full + 8 * s, kRows);
             mbar_init(b.s_full + 8 * s, 1);
             mbar_init(b.p_full + 8 * s, kRows);
             mbar_init(b.o_done + 8 * s, 1);
             mbar_init(b.o_free + 8 * s, kRows);
+            mbar_init(b.fin + 8 * s, 1);
         }
-        mbar_init(b.fin, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (tid < kBad) bad[tid] = 0;
@@ -709,8 +717,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
         softmax_role<T, HALVES>(a, sched, mem, tmem, b, bad, &dead, last);
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-        if (warp == 8) mma_role<T, HALVES>(a, sched, base, slot0, tmem, b, &dead);
-        else if (warp == 9) copy_role<HALVES>(a, sched, &km, &vm, slot0, b, &dead);
+        if (warp < 10) mma_role<T, HALVES>(a, sched, warp - 8, base, slot0, tmem, b, &dead);
+        else if (warp == 10) copy_role<HALVES>(a, sched, &km, &vm, slot0, b, &dead);
         else look_role<T, HALVES>(a, sched, mem + 2 * L::tile, b, bad, &dead);
     }
     tc_before();
