@@ -13,8 +13,26 @@ namespace pp {
 
 AttendDev attend_dev(const pp_kv *kv, const AttendArgs &c)
 {
-    return {c, kv->block_stride, kv->token_stride, kv->head_stride, kv->blocks, kv->block_log, kv->dim, kv->heads,
-            c.scale * 1.4426950408889634f, kv->d_status, kv->d_piece, kv->d_piece_stat, kv->d_count};
+    AttendDev a = {};
+    a.c = c;
+    a.block_stride = kv->block_stride;
+    a.token_stride = kv->token_stride;
+    a.head_stride = kv->head_stride;
+    a.blocks = kv->blocks;
+    a.block_log = kv->block_log;
+    a.dim = kv->dim;
+    a.kv_heads = kv->heads;
+    a.scale_log2 = c.scale * 1.4426950408889634f;
+    a.group_shift = 32;
+    while (1 << (a.group_shift - 32) < c.group) a.group_shift++;
+    a.group_mul = (((uint64_t)1 << a.group_shift) + c.group - 1) / c.group;
+    a.wide_out = (reinterpret_cast<uintptr_t>(c.out) & 31) == 0 && c.out_token_stride % 16 == 0 &&
+                 c.out_head_stride % 16 == 0 && kv->dim % 16 == 0;
+    a.status = kv->d_status;
+    a.piece = kv->d_piece;
+    a.piece_stat = kv->d_piece_stat;
+    a.count = kv->d_count;
+    return a;
 }
 
 // The cache as (dim, token of a block, head, block), copied in boxes of 64

@@ -23,6 +23,9 @@ struct AttendDev {
     int64_t block_stride, token_stride, head_stride;
     int32_t blocks, block_log, dim, kv_heads;
     float scale_log2;                   // scale * log2(e)
+    int32_t group_shift;                // x / group = x * group_mul >> group_shift for 0 <= x < 2^30
+    uint64_t group_mul;
+    int32_t wide_out;                   // rows of out start at 32-byte boundaries
     int32_t *status;
     float *piece;                       // pieces' outputs, [slot][...]
     float *piece_stat;                  // their maxima (log2 units) and sums
@@ -51,6 +54,13 @@ __device__ __forceinline__ Req load_req(const AttendDev &a, int32_t r, bool repo
     return q;
 }
 
+// The multiplier is 2^shift / group rounded up, shift = 32 + ceil(log2 group):
+// it is less than 2^(shift - 32) / group too large, x times that less than 1 / group.
+__device__ __forceinline__ int32_t div_group(const AttendDev &a, int32_t x)
+{
+    return (int32_t)((uint64_t)x * a.group_mul >> a.group_shift);
+}
+
 // keys that a query at `pos` sees: [lo, pos]
 __device__ __forceinline__ int32_t first_key(const AttendDev &a, int32_t pos)
 {
@@ -72,17 +82,42 @@ struct SchedShared {
     int32_t r, outer, inner, off, count;
 };
 
+__device__ __forceinline__ int64_t warp_sum64(int64_t x)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(~0u, x, o);
+    return x;
+}
+__device__ __forceinline__ Req shfl_req(const Req &q, int src)
+{
+    return {__shfl_sync(~0u, q.first, src), __shfl_sync(~0u, q.q_len, src), __shfl_sync(~0u, q.length, src)};
+}
+
+// Tiles of each lane's request, over its inner items; requests with more than a
+// few items are summed by the whole warp, one after another.
 template <class S> __device__ __forceinline__ int64_t request_tiles(const AttendDev &a, const Req &q)
 {
-    int64_t s = 0;
-    for (int32_t i = 0, n = S::inner(a, q); i < n; ++i) s += key_tiles<S::KT>(S::keys(a, q, i));
-    return s * S::outer(a);
+    const int lane = threadIdx.x & 31;
+    const int32_t n = S::inner(a, q);
+    const bool big = n > 4;
+    int64_t mine = 0;
+    if (!big)
+        for (int32_t i = 0; i < n; ++i) mine += key_tiles<S::KT>(S::keys(a, q, i));
+    for (uint32_t left = __ballot_sync(~0u, big); left; left &= left - 1) {
+        const int src = __ffs(left) - 1;
+        const Req x = shfl_req(q, src);
+        int64_t sum = 0;
+        for (int32_t i = lane, m = S::inner(a, x); i < m; i += 32) sum += key_tiles<S::KT>(S::keys(a, x, i));
+        sum = warp_sum64(sum);
+        if (lane == src) mine = sum;
+    }
+    return mine;
 }
 
 __device__ __forceinline__ int64_t block_scan(int64_t v, int64_t *excl, int64_t *warp_sum)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    int64_t x = v;
+    int64_t x = v;                                      // inclusive within the warp
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
         const int64_t y = __shfl_up_sync(~0u, x, o);
@@ -104,47 +139,64 @@ __device__ __forceinline__ int64_t block_scan(int64_t v, int64_t *excl, int64_t 
 // The CTA's stretch: false if it has none.  All threads of the CTA call it.
 template <class S> __device__ __forceinline__ bool schedule(const AttendDev &a, SchedShared &sm)
 {
-    const int32_t R = a.c.requests, T = blockDim.x;
+    const int32_t R = a.c.requests, T = blockDim.x, outer = S::outer(a);
+    const int lane = threadIdx.x & 31;
     const bool report = blockIdx.x == 0;
-    if (threadIdx.x == 0) sm.count = 0;
-    int64_t total = 0, excl, mine = 0;
     if (report && threadIdx.x == 0 && a.c.q_start[0] != 0) kv_bounds(a.status);
-    for (int32_t r = threadIdx.x; r < R; r += T) mine += request_tiles<S>(a, load_req(a, r, report));
-    total = block_scan(mine, &excl, sm.warp_sum);
+    Req q;
+    int64_t mine, sum = 0, excl, before = 0;            // tiles of one head: this lane's request, all of this lane's
+    for (int32_t base = 0; base < R; base += T) {
+        const int32_t r = base + threadIdx.x;
+        q = Req{0, 0, 0};
+        if (r < R) q = load_req(a, r, report);
+        sum += mine = request_tiles<S>(a, q);
+    }
+    const int64_t total = block_scan(sum, &excl, sm.warp_sum) * outer;
     if (total == 0) return false;
     const int64_t ctas = min((int64_t)gridDim.x, total);
     if (blockIdx.x >= ctas) return false;
     const int64_t begin = total * blockIdx.x / ctas, end = total * (blockIdx.x + 1) / ctas;
-    int64_t before = 0;
     for (int32_t base = 0; base < R; base += T) {
         const int32_t r = base + threadIdx.x;
-        Req q = {0, 0, 0};
         if (R > T) {
+            q = Req{0, 0, 0};
             if (r < R) q = load_req(a, r, false);
-            mine = r < R ? request_tiles<S>(a, q) : 0;
-            const int64_t sum = block_scan(mine, &excl, sm.warp_sum);
+            mine = request_tiles<S>(a, q);
+            const int64_t here = block_scan(mine, &excl, sm.warp_sum);
             excl += before;
-            before += sum;
-        } else if (r < R) {
-            q = load_req(a, r, false);
+            before += here;
         }
-        if (r < R && mine > 0 && excl <= begin && begin < excl + mine) {
-            const int64_t per = mine / S::outer(a);
-            int64_t rem = begin - excl;
-            sm.r = r;
-            sm.outer = (int32_t)(rem / per);
-            rem %= per;
-            int32_t i = 0;
-            for (;; ++i) {
-                const int32_t n = key_tiles<S::KT>(S::keys(a, q, i));
-                if (rem < n) break;
-                rem -= n;
+        const bool hit = mine > 0 && excl * outer <= begin && begin < (excl + mine) * outer;
+        const uint32_t who = __ballot_sync(~0u, hit);
+        if (!who) continue;
+        // this warp has the request that the stretch begins in: its lanes look for the item
+        const int src = __ffs(who) - 1;
+        const Req x = shfl_req(q, src);
+        const int64_t per = __shfl_sync(~0u, mine, src), off = begin - __shfl_sync(~0u, excl, src) * outer;
+        const int32_t head = (int32_t)(off / per), items = S::inner(a, x);
+        int64_t rem = off - head * per;
+        for (int32_t i0 = 0; i0 < items; i0 += 32) {
+            const int64_t n = i0 + lane < items ? key_tiles<S::KT>(S::keys(a, x, i0 + lane)) : 0;
+            int64_t incl = n;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int64_t y = __shfl_up_sync(~0u, incl, o);
+                if (lane >= o) incl += y;
             }
-            sm.inner = i;
-            sm.off = (int32_t)rem;
-            sm.count = (int32_t)(end - begin);
-            sm.begin = begin;
-            sm.total = total;
+            const uint32_t past = __ballot_sync(~0u, rem < incl);
+            if (past) {
+                if (lane == __ffs(past) - 1) {
+                    sm.r = r - lane + src;
+                    sm.outer = head;
+                    sm.inner = i0 + lane;
+                    sm.off = (int32_t)(rem - (incl - n));
+                    sm.count = (int32_t)(end - begin);
+                    sm.begin = begin;
+                    sm.total = total;
+                }
+                break;
+            }
+            rem -= __shfl_sync(~0u, incl, 31);
         }
     }
     __syncthreads();

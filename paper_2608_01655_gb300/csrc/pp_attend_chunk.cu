@@ -50,7 +50,7 @@ struct Shape {
     }
     static __device__ __forceinline__ int32_t pos(const AttendDev &a, const Req &q, int32_t row)
     {
-        return q.length - q.q_len + row / a.c.group;
+        return q.length - q.q_len + div_group(a, row);
     }
     static __device__ __forceinline__ Keys keys(const AttendDev &a, const Req &q, int32_t i)
     {
@@ -193,7 +193,7 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
 
 // one lane of the warp, always the same.  The products are issued under it and
 // not under a comparison of the lane's number: the compiler knows then that a
-// single thread holds their operands (90 cycles an instruction became XX).
+// single thread holds their operands (an instruction took 90 cycles otherwise, 64 now).
 __device__ __forceinline__ bool elected()
 {
     uint32_t yes;
@@ -228,7 +228,7 @@ template <typename T> __device__ __forceinline__ bool not_finite(uint32_t bits)
 // The roles
 // ---------------------------------------------------------------------------
 struct Bars {
-    uint32_t full, empty, v_ok, q_full, s_full, p_full, o_done, o_free, fin;     // shared addresses
+    uint32_t full, empty, v_ok, q_full, s_full, p_full, o_done, o_free, fin, pass;     // shared addresses
 };
 
 // K and V tiles of the stretch, in turn, a box a lane: lanes are (half, box).
@@ -287,6 +287,8 @@ __device__ __forceinline__ void copy_role(const AttendDev &a, const SchedShared 
 // Tensor memory: S (and P over it) of stage s at column 128 s, O at 256 + 128 s.
 // A warp issues one stage's products: issue waits for the tensor cores, so the
 // time that one warp spends on barriers and bookkeeping is the other's products'.
+// They pass each other the turn after every O and S: left alone the stages fall
+// into step, both at their products, then both at their softmax.
 template <typename T, int HALVES>
 __device__ __forceinline__ void mma_role(const AttendDev &a, const SchedShared &sched, int s, uint32_t q0, uint32_t slot0,
                                          uint32_t tmem, const Bars &b, volatile int32_t *dead)
@@ -296,7 +298,7 @@ __device__ __forceinline__ void mma_role(const AttendDev &a, const SchedShared &
     const uint32_t t_s = tmem + 128 * s, t_o = tmem + 256 + 128 * s;
     const uint64_t q_op = smem_operand(q0 + s * L::tile, 16, 1024);
     Cursor<Shape> cur(a, sched);
-    uint32_t slot = 0, turn = 0, mark = 0, q_turn = 0, p_turn = 0;
+    uint32_t slot = 0, turn = 0, mark = 0, q_turn = 0, p_turn = 0, pass = 0;
     auto step = [&]() {                                 // to the next slot of the ring
         if (++slot == L::slots) {
             slot = 0;
@@ -329,6 +331,7 @@ __device__ __forceinline__ void mma_role(const AttendDev &a, const SchedShared &
             mark += cur.len;
             continue;
         }
+        const bool both = Shape::rows(a, cur.q) - cur.inner * 2 * kRows > kRows;
         mbar_wait(b.q_full + 8 * s, q_turn & 1, dead, a.status);
         issue_s();
         // O is free when its last item's output has been read
@@ -341,6 +344,10 @@ __device__ __forceinline__ void mma_role(const AttendDev &a, const SchedShared &
             const uint64_t v_op = smem_operand(slot0 + v_slot * L::tile, L::half, 1024);
             mbar_wait(b.p_full + 8 * s, p_turn & 1, dead, a.status);
             ++p_turn;
+            if (both) {
+                if (s == 1 || pass) mbar_wait(b.pass + 8 * s, (pass + s + 1) & 1, dead, a.status);
+                ++pass;
+            }
             tc_after();
             if (elected()) {
 #pragma unroll
@@ -351,6 +358,7 @@ __device__ __forceinline__ void mma_role(const AttendDev &a, const SchedShared &
             }
             step();
             if (i + 1 < cur.len) issue_s();
+            if (both && elected()) mbar_arrive(b.pass + 8 * (1 - s));
         }
         ++q_turn;
     } while (cur.next(a));
@@ -430,7 +438,7 @@ __device__ __forceinline__ void softmax_role(const AttendDev &a, const SchedShar
 #pragma unroll
         for (int i = 0; i < per; ++i) {
             const int x = i * kRows + t, row = r0 + x / per, d = x % per * 8;
-            const int32_t tok = row / a.c.group, g = row % a.c.group;
+            const int32_t tok = div_group(a, row), g = row - tok * a.c.group;
             y[i] = row < rows && d < a.dim
                        ? __ldg(reinterpret_cast<const uint4 *>(
                              static_cast<const T *>(a.c.q) + (int64_t)(c.q.first + tok) * a.c.q_token_stride +
@@ -468,51 +476,60 @@ __device__ __forceinline__ void softmax_role(const AttendDev &a, const SchedShar
         for (int32_t i = 0; i < cur.len; ++i) {
             mbar_wait(b.s_full + 8 * s, s_turn++ & 1, dead, a.status);
             tc_after();
-            uint32_t x[KT];
-#pragma unroll
-            for (int c = 0; c < KT; c += 32) tc_ld32(x + c, t_s + c);
-            tc_wait_ld();
             const int32_t j0 = (t0 + i) * KT;
-            if (!all.covers(j0)) {
-                const int32_t from = lo - j0, to = pos - j0;
+            const bool edge = !all.covers(j0);
+            uint32_t x[KT];
+            uint64_t sum[2];
+            // The weights are computed from the m at hand while the maximum of these
+            // scores is still being found; if one exceeds m by too much (as in the
+            // first tile), m moves and they are computed once more.
+            for (bool sure = i == 0;;) {
 #pragma unroll
-                for (int c = 0; c < KT; ++c)
-                    if (c < from || c > to) x[c] = 0xff800000u;
-            }
-            float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                for (int c = 0; c < KT; c += 32) tc_ld32(x + c, t_s + c);
+                tc_wait_ld();
+                if (edge) {
+                    const int32_t from = lo - j0, to = pos - j0;
 #pragma unroll
-            for (int c = 0; c < KT; c += 8)
-#pragma unroll
-                for (int y = 0; y < 4; ++y)
-                    top[y] = max3(top[y], __uint_as_float(x[c + 2 * y]), __uint_as_float(x[c + 2 * y + 1]));
-            const float high = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.scale_log2;
-            if (i == 0) {
-                m = high;
-            } else if (__any_sync(~0u, high > m + kSlack)) {
-                // every product on O that was issued before this S has ended with it
-                const float up = high > m + kSlack ? high : m;
-                const float f = up == m ? 1.f : exp2_approx(m - up);
-                m = up;
-                l *= f;
-#pragma unroll 1
-                for (int c = 0; c < L::width; c += 8) {
-                    uint32_t o[8];
-                    tc_ld8(o, t_o + c);
-                    tc_wait_ld();
-#pragma unroll
-                    for (int y = 0; y < 8; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * f);
-                    tc_st8(t_o + c, o);
+                    for (int c = 0; c < KT; ++c)
+                        if (c < from || c > to) x[c] = 0xff800000u;
                 }
-            }
-            const float base = m == -INFINITY ? 0.f : m;
-            const uint64_t mul = pair(a.scale_log2, a.scale_log2), sub = pair(-base, -base);
-            uint64_t sum[2] = {0, 0};
+                float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                if (sure) {
 #pragma unroll
-            for (int c = 0; c < KT; c += 2) {
-                const float2 e = unpair(fma2(pair(__uint_as_float(x[c]), __uint_as_float(x[c + 1])), mul, sub));
-                const float p0 = exp2_approx(e.x), p1 = exp2_approx(e.y);
-                sum[(c >> 1) & 1] = add2(sum[(c >> 1) & 1], pair(p0, p1));
-                x[c / 2] = Pack<T>::two(p0, p1);
+                    for (int c = 0; c < KT; c += 2)
+                        top[(c >> 1) & 3] = max3(top[(c >> 1) & 3], __uint_as_float(x[c]), __uint_as_float(x[c + 1]));
+                    const float high = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.scale_log2;
+                    const float up = high > m + kSlack || i == 0 ? high : m;
+                    if (i > 0) {
+                        // every product on O that was issued before this S has ended with it
+                        const float f = up == m ? 1.f : exp2_approx(m - up);
+                        l *= f;
+#pragma unroll 1
+                        for (int c = 0; c < L::width; c += 8) {
+                            uint32_t o[8];
+                            tc_ld8(o, t_o + c);
+                            tc_wait_ld();
+#pragma unroll
+                            for (int y = 0; y < 8; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * f);
+                            tc_st8(t_o + c, o);
+                        }
+                    }
+                    m = up;
+                }
+                const float base = m == -INFINITY ? 0.f : m;
+                const uint64_t mul = pair(a.scale_log2, a.scale_log2), sub = pair(-base, -base);
+                sum[0] = sum[1] = 0;
+#pragma unroll
+                for (int c = 0; c < KT; c += 2) {
+                    top[(c >> 1) & 3] = max3(top[(c >> 1) & 3], __uint_as_float(x[c]), __uint_as_float(x[c + 1]));
+                    const float2 e = unpair(fma2(pair(__uint_as_float(x[c]), __uint_as_float(x[c + 1])), mul, sub));
+                    const float p0 = exp2_approx(e.x), p1 = exp2_approx(e.y);
+                    sum[(c >> 1) & 1] = add2(sum[(c >> 1) & 1], pair(p0, p1));
+                    x[c / 2] = Pack<T>::two(p0, p1);
+                }
+                const float high = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.scale_log2;
+                if (sure || !__any_sync(~0u, high > m + kSlack)) break;
+                sure = true;
             }
             tc_st32(t_s, x);
             tc_st32(t_s + 32, x + 32);
@@ -532,15 +549,27 @@ __device__ __forceinline__ void softmax_role(const AttendDev &a, const SchedShar
 
         mbar_wait(b.o_done + 8 * s, o_turn++ & 1, dead, a.status);
         tc_after();
-        const int32_t tok = cur.q.first + row / a.c.group, head = cur.outer * a.c.group + row % a.c.group;
+        const int32_t tok = cur.q.first + div_group(a, row), head = cur.outer * a.c.group + row - div_group(a, row) * a.c.group;
         auto put_out = [&](const float *o, int c, float inv) {
             T *dst = static_cast<T *>(a.c.out) + (int64_t)tok * a.c.out_token_stride + (int64_t)head * a.c.out_head_stride + c;
+            uint32_t w[16];
 #pragma unroll
-            for (int y = 0; y < 32; y += 8)
-                if (live && c + y < a.dim)
-                    *reinterpret_cast<uint4 *>(dst + y) = make_uint4(
-                        Pack<T>::two(o[y] * inv, o[y + 1] * inv), Pack<T>::two(o[y + 2] * inv, o[y + 3] * inv),
-                        Pack<T>::two(o[y + 4] * inv, o[y + 5] * inv), Pack<T>::two(o[y + 6] * inv, o[y + 7] * inv));
+            for (int y = 0; y < 16; ++y) w[y] = Pack<T>::two(o[2 * y] * inv, o[2 * y + 1] * inv);
+            if (!live) return;
+            if (a.wide_out) {                           // whole sectors
+#pragma unroll
+                for (int y = 0; y < 16; y += 8)
+                    if (c + 2 * y < a.dim)
+                        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst + 2 * y), "r"(w[y]),
+                                     "r"(w[y + 1]), "r"(w[y + 2]), "r"(w[y + 3]), "r"(w[y + 4]), "r"(w[y + 5]),
+                                     "r"(w[y + 6]), "r"(w[y + 7])
+                                     : "memory");
+            } else {
+#pragma unroll
+                for (int y = 0; y < 16; y += 4)
+                    if (c + 2 * y < a.dim)
+                        *reinterpret_cast<uint4 *>(dst + 2 * y) = make_uint4(w[y], w[y + 1], w[y + 2], w[y + 3]);
+            }
         };
         auto put_lse = [&](float top, float sum) {
             if (live && a.c.lse)
@@ -620,6 +649,7 @@ __device__ __forceinline__ void softmax_role(const AttendDev &a, const SchedShar
                     float o[32];
 #pragma unroll
                     for (int y = 0; y < 32; ++y) o[y] = 0.f;
+#pragma unroll 2
                     for (int32_t p = 0; p < n; ++p) {
                         const float f = exp2_approx(__ldcg(stat_at(p0 + p * step)) - base);
                         const float4 *src = piece_at(p0 + p * step, c);
@@ -667,7 +697,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
     using L = Layout<HALVES>;
     extern __shared__ uint8_t raw[];
     __shared__ SchedShared sched;
-    __shared__ alignas(8) uint64_t bar[2 * L::slots + kVMarks + 12];
+    __shared__ alignas(8) uint64_t bar[2 * L::slots + kVMarks + 14];
     __shared__ int32_t dead, last[2], bad[kBad];
     __shared__ uint32_t tmem_at;
     const int tid = threadIdx.x, warp = tid >> 5;
@@ -683,6 +713,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
     b.o_done = b.p_full + 16;
     b.o_free = b.o_done + 16;
     b.fin = b.o_free + 16;
+    b.pass = b.fin + 16;
     if (tid == 0) {
         dead = 0;
         for (int i = 0; i < L::slots; ++i) {
@@ -697,6 +728,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
             mbar_init(b.o_done + 8 * s, 1);
             mbar_init(b.o_free + 8 * s, kRows);
             mbar_init(b.fin + 8 * s, 1);
+            mbar_init(b.pass + 8 * s, 1);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
