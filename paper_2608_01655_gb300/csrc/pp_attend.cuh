@@ -256,10 +256,6 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar)
 {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes)
-{
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
 __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)
 {
     uint32_t ok;
@@ -295,15 +291,72 @@ __device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, volatil
     }
 }
 
-// box of `rows` tokens x 64 elements of one block and head to shared memory, rows
-// of 128 bytes swizzled by 128 bytes; a block number out of range gives zeros
-__device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap *map, uint32_t bar, int32_t x, int32_t token,
+// ---------------------------------------------------------------------------
+// Cache rows to shared memory
+// ---------------------------------------------------------------------------
+// Rows of K or V lie in halves of 64 elements, 128 bytes a row, whose 16-byte
+// pieces are swizzled by the row (piece ^ row % 8): the layout that ldmatrix
+// reads without conflicts and the tensor cores' operands take.  There are two
+// ways to get them there.  A tensor-map box costs a lane's one instruction but
+// ends with its block, and measured on this GPU machines of 128-byte rows take 52
+// cycles and 5.3 a row, from L2 as from HBM: over all SMs 3.2 TB/s with 8 rows,
+// 4.4 with 16, 6.2 with 64.  16-byte copies, a warp's 32 at a time, reach 9
+// (one warp an SM) to 21 TB/s (eight) from L2, but each costs the warp some five
+// instructions.
+__device__ __forceinline__ void copy16(uint32_t dst, const char *src, uint32_t bytes)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+// the barrier's arrival of this lane, once its copies so far have landed
+__device__ __forceinline__ void copies_arrive(uint32_t bar)
+{
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
+// A lane's share of copies of whole rows: `step` rows of 16-byte pieces at a time.
+template <int HALVES> struct RowLane {
+    static constexpr int per_row = 8 * HALVES, step = 32 / per_row;
+    uint32_t dst, bytes;                // in a group of 8 rows; 0: past the head dimension, zeros are written
+    int64_t src;
+    __device__ __forceinline__ RowLane(const AttendDev &a, uint32_t half_bytes)
+    {
+        const int lane = threadIdx.x & 31, sub = lane / per_row, piece = lane % per_row;
+        dst = (piece >> 3) * half_bytes + sub * 128 + (((piece ^ sub) & 7) << 4);
+        bytes = piece * 8 < a.dim ? 16 : 0;
+        src = 2 * sub * a.token_stride + (bytes ? piece * 16 : 0);
+    }
+    // 8 rows; `from` is the first row's head, `to` at a multiple of 1,024 bytes
+    __device__ __forceinline__ void rows8(uint32_t to, const char *from, int64_t token_bytes, bool some) const
+    {
+#pragma unroll
+        for (int x = 0; x < 8; x += step) copy16(to + x * 128 + (dst ^ (x << 4)), from + src + x * token_bytes, some ? bytes : 0);
+    }
+};
+
+// box of tokens x 64 elements of one block and head, rows swizzled as above; a
+// block number out of range gives zeros
+__device__ __forceinline__ void box_rows(uint32_t dst, const CUtensorMap *map, uint32_t bar, int32_t x, int32_t token,
                                          int32_t head, int32_t block)
 {
     asm volatile(
         "cp.async.bulk.tensor.4d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
         "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(token), "r"(head), "r"(block), "r"(bar)
         : "memory");
+}
+__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+
+// block that holds key j of the request, -1 if no row sees one of keys j .. j + n - 1
+__device__ __forceinline__ int32_t key_block(const AttendDev &a, const int32_t *row, Keys k, int32_t j, int32_t n)
+{
+    if (j > k.hi || j + n - 1 < k.lo) return -1;
+    const int32_t id = row[j >> a.block_log];
+    if (id >= 0 && id < a.blocks) return id;
+    kv_bounds(a.status);
+    return -1;
 }
 
 __device__ __forceinline__ void named_sync(int id, int threads)
@@ -348,9 +401,7 @@ __device__ __forceinline__ int32_t owner(int64_t g, int64_t total, int64_t ctas)
 // and one of an item that goes on after it (1)
 __device__ __forceinline__ int32_t piece_slot(int32_t cta0, int32_t p) { return p == 0 ? 2 * cta0 + 1 : 2 * (cta0 + p); }
 
-// ---------------------------------------------------------------------------
-// Host: tensor maps of a cache (pp_attend.cu)
-// ---------------------------------------------------------------------------
+// Host (pp_attend.cu)
 pp_status cache_map(const pp_kv *kv, const void *cache, int32_t rows, CUtensorMap *map);
 AttendDev attend_dev(const pp_kv *kv, const AttendArgs &c);
 

@@ -14,11 +14,13 @@
 // 16-bit types hold as precisely.
 //
 // Warps: 0-3 and 4-7 the stages' softmax and epilogue, 8 and 9 their products, 10
-// the copies, 11 looks over the V tiles that not every row may see: an infinity
-// or a NaN there would pass through a weight of 0, so it is replaced by 0 and
-// added in the epilogue to the rows that do see it.
+// copies K by tensor-map boxes, and 10 and 11 copy V 16 bytes a lane: either way
+// alone is slower than the products.  V tiles that not every row sees in full are looked
+// over by the softmax warps: an infinity or a NaN there would pass through a
+// weight of 0, so it is replaced by 0 and added in the epilogue to the rows that
+// do see it.
 #include <algorithm>
-#include <climits>
+#include <type_traits>
 
 #include "pp_attend.cuh"
 
@@ -28,16 +30,15 @@ namespace chunk {
 constexpr int KT = 128;                             // keys per tile
 constexpr int kRows = 128;                          // rows of a stage
 constexpr int kThreads = 384;
-constexpr int kVMarks = 8;                          // barriers of looked-over V tiles
-constexpr int kBad = 16;
+constexpr int kBad = 16;                            // marks of items, the stages are fewer apart
 constexpr float kSlack = 8.f;                       // log2 by which a score may exceed m
 
 template <int HALVES> struct Layout {
     static constexpr int half = KT * 128;                       // bytes of 64 columns of a tile
     static constexpr int tile = half * HALVES;
-    static constexpr int slots = HALVES == 2 ? 5 : 10;          // K and V tiles in flight
+    static constexpr int k_slots = HALVES == 2 ? 3 : 5, v_slots = HALVES == 2 ? 2 : 5;     // tiles in flight
     static constexpr int width = 64 * HALVES;
-    static constexpr int bytes = 1024 + (2 + slots) * tile;
+    static constexpr int bytes = 1024 + (2 + k_slots + v_slots) * tile;
 };
 
 struct Shape {
@@ -228,59 +229,80 @@ template <typename T> __device__ __forceinline__ bool not_finite(uint32_t bits)
 // The roles
 // ---------------------------------------------------------------------------
 struct Bars {
-    uint32_t full, empty, v_ok, q_full, s_full, p_full, o_done, o_free, fin, pass;     // shared addresses
+    uint32_t k_full, k_empty, v_full, v_empty, q_full, s_full, p_full, o_done, o_free, fin, pass;     // shared addresses
 };
 
-// K and V tiles of the stretch, in turn, a box a lane: lanes are (half, box).
+// Shared memory: the stages' queries, K tiles, V tiles.
+template <int HALVES> __device__ __forceinline__ uint32_t k_at(uint32_t base, uint32_t slot)
+{
+    return base + (2 + slot) * Layout<HALVES>::tile;
+}
+template <int HALVES> __device__ __forceinline__ uint32_t v_at(uint32_t base, uint32_t slot)
+{
+    return base + (2 + Layout<HALVES>::k_slots + slot) * Layout<HALVES>::tile;
+}
+__device__ __forceinline__ void to_tensor_cores() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// The tiles of the stretch: warp 0 asks for K, a box a lane (lanes are (half,
+// box)); both copy half of V's rows.
 template <int HALVES>
-__device__ __forceinline__ void copy_role(const AttendDev &a, const SchedShared &sched, const CUtensorMap *km,
-                                          const CUtensorMap *vm, uint32_t slot0, const Bars &b, volatile int32_t *dead)
+__device__ __forceinline__ void copy_role(const AttendDev &a, const SchedShared &sched, int w, const CUtensorMap *km,
+                                          uint32_t base, const Bars &b, volatile int32_t *dead)
 {
     using L = Layout<HALVES>;
     const int lane = threadIdx.x & 31;
     const int box_log = min(a.block_log, 7), boxes = KT >> box_log;        // 16 at most
     const int box = lane % boxes, half = lane / boxes;
-    const bool active = half < HALVES;
-    const uint32_t dst = half * L::half + (box << box_log) * 128;
+    const bool asks = half < HALVES;
+    const uint32_t k_dst = half * L::half + (box << box_log) * 128;
+    const RowLane<HALVES> rl(a, L::half);
+    const int64_t token_bytes = 2 * a.token_stride, block_bytes = 2 * a.block_stride;
+    const int32_t in_block = (1 << a.block_log) - 1;
 
     Cursor<Shape> cur(a, sched);
-    uint32_t seq = 0;
+    uint32_t k = 0;
     do {
         const int32_t *row = a.c.block_table + (int64_t)cur.r * a.c.table_width;
         const int32_t t0 = cur.k.lo / KT + cur.off;
-        auto entry = [&](int32_t t) {
-            const int32_t j = t * KT + (box << box_log);
-            if (!active || j > cur.k.hi || j + (1 << box_log) <= cur.k.lo) return a.blocks;
-            int32_t id = row[j >> a.block_log];
-            if (id < 0 || id >= a.blocks) {
-                kv_bounds(a.status);
-                id = a.blocks;
-            }
-            return id;
-        };
-        int32_t id = entry(t0);
-        for (int32_t i = 0; i < cur.len && !*dead; ++i) {
-            const int32_t after = i + 1 < cur.len ? entry(t0 + i + 1) : 0;
-            const int32_t token = ((t0 + i) * KT + (box << box_log)) & ((1 << a.block_log) - 1);
-#pragma unroll
-            for (int which = 0; which < 2; ++which) {
-                const uint32_t s = seq % L::slots, turn = seq / L::slots;
-                if (turn) mbar_wait(b.empty + 8 * s, (turn - 1) & 1, dead, a.status);
+        const char *v = static_cast<const char *>(a.c.v_cache) + 2 * cur.outer * a.head_stride;
+        // blocks of this lane's box of K, and, of lane g, of V's rows 64 w + 8 g on
+        auto k_block = [&](int32_t t) { return asks && w == 0 ? key_block(a, row, cur.k, t * KT + (box << box_log), 1 << box_log) : -1; };
+        auto v_block = [&](int32_t t) { return lane < 8 ? key_block(a, row, cur.k, t * KT + 64 * w + 8 * lane, 8) : -1; };
+        int32_t kb = k_block(t0), vb = v_block(t0);
+        for (int32_t i = 0; i < cur.len && !*dead; ++i, ++k) {
+            const bool more = i + 1 < cur.len;
+            const int32_t kb_next = more ? k_block(t0 + i + 1) : -1, vb_next = more ? v_block(t0 + i + 1) : -1;
+            const int32_t j0 = (t0 + i) * KT;
+            if (w == 0) {
+                const uint32_t s = k % L::k_slots;
+                if (k >= L::k_slots) mbar_wait(b.k_empty + 8 * s, (k / L::k_slots - 1) & 1, dead, a.status);
                 if (*dead) break;
-                if (lane == 0) mbar_expect(b.full + 8 * s, L::tile);
+                if (lane == 0) mbar_expect(b.k_full + 8 * s, L::tile);
                 __syncwarp();
-                if (active)
-                    tma_rows(slot0 + s * L::tile + dst, which ? vm : km, b.full + 8 * s, half * 64, token, cur.outer, id);
-                ++seq;
+                if (asks)
+                    box_rows(k_at<HALVES>(base, s) + k_dst, km, b.k_full + 8 * s, half * 64, (j0 + (box << box_log)) & in_block,
+                             cur.outer, kb < 0 ? a.blocks : kb);
             }
-            id = after;
+            const uint32_t s = k % L::v_slots;
+            if (k >= L::v_slots) mbar_wait(b.v_empty + 8 * s, (k / L::v_slots - 1) & 1, dead, a.status);
+            const uint32_t dst = v_at<HALVES>(base, s) + w * 8192;
+#pragma unroll
+            for (int g = 0; g < 8; ++g) {
+                const int32_t id = __shfl_sync(~0u, vb, g);
+                rl.rows8(dst + g * 1024, v + max(id, 0) * block_bytes + ((j0 + 64 * w + 8 * g) & in_block) * token_bytes,
+                         token_bytes, id >= 0);
+            }
+            copies_arrive(b.v_full + 8 * s);
+            kb = kb_next;
+            vb = vb_next;
         }
     } while (!*dead && cur.next(a));
-    if (*dead) {
-        // copies in flight land before the CTA ends
+    // nothing is in flight when the CTA ends
+    copies_wait();
+    if (w == 0 && *dead) {
         int32_t none = 0;
-        for (uint32_t x = seq > L::slots ? seq - L::slots : 0; x < seq; ++x)
-            mbar_wait(b.full + 8 * (x % L::slots), (x / L::slots) & 1, &none, a.status);
+        for (uint32_t x = k > L::k_slots ? k - L::k_slots : 0; x <= k; ++x)
+            mbar_wait(b.k_full + 8 * (x % L::k_slots), (x / L::k_slots) & 1, &none, a.status);
     }
 }
 
@@ -290,25 +312,25 @@ __device__ __forceinline__ void copy_role(const AttendDev &a, const SchedShared 
 // They pass each other the turn after every O and S: left alone the stages fall
 // into step, both at their products, then both at their softmax.
 template <typename T, int HALVES>
-__device__ __forceinline__ void mma_role(const AttendDev &a, const SchedShared &sched, int s, uint32_t q0, uint32_t slot0,
+__device__ __forceinline__ void mma_role(const AttendDev &a, const SchedShared &sched, int s, uint32_t base,
                                          uint32_t tmem, const Bars &b, volatile int32_t *dead)
 {
     using L = Layout<HALVES>;
     const uint32_t kind_s = mma_kind<T>(KT, false), kind_o = mma_kind<T>(L::width, true);
     const uint32_t t_s = tmem + 128 * s, t_o = tmem + 256 + 128 * s;
-    const uint64_t q_op = smem_operand(q0 + s * L::tile, 16, 1024);
+    const uint64_t q_op = smem_operand(base + s * L::tile, 16, 1024);
     Cursor<Shape> cur(a, sched);
-    uint32_t slot = 0, turn = 0, mark = 0, q_turn = 0, p_turn = 0, pass = 0;
-    auto step = [&]() {                                 // to the next slot of the ring
-        if (++slot == L::slots) {
+    uint32_t ks = 0, k_turn = 0, vs = 0, v_turn = 0, q_turn = 0, p_turn = 0, pass = 0;
+    auto step = [](uint32_t &slot, uint32_t &turn, uint32_t slots) {
+        if (++slot == slots) {
             slot = 0;
             turn ^= 1;
         }
     };
     auto issue_s = [&]() {
-        mbar_wait(b.full + 8 * slot, turn, dead, a.status);
+        mbar_wait(b.k_full + 8 * ks, k_turn, dead, a.status);
         tc_after();
-        const uint64_t k_op = smem_operand(slot0 + slot * L::tile, 16, 1024);
+        const uint64_t k_op = smem_operand(k_at<HALVES>(base, ks), 16, 1024);
         if (elected()) {
 #pragma unroll
             for (int h = 0; h < HALVES; ++h)
@@ -318,17 +340,22 @@ __device__ __forceinline__ void mma_role(const AttendDev &a, const SchedShared &
                     mma_ss(t_s, q_op + h * half + 2 * k, k_op + h * half + 2 * k, kind_s, h + k > 0);
                 }
             tc_commit(b.s_full + 8 * s);
-            tc_commit(b.empty + 8 * slot);
+            tc_commit(b.k_empty + 8 * ks);
         }
+        step(ks, k_turn, L::k_slots);
     };
     do {
         if (s * kRows >= Shape::rows(a, cur.q) - cur.inner * 2 * kRows) {        // no rows in this stage
-            for (int32_t i = 0; i < 2 * cur.len; ++i) {
-                mbar_wait(b.full + 8 * slot, turn, dead, a.status);
-                if (elected()) mbar_arrive(b.empty + 8 * slot);
-                step();
+            for (int32_t i = 0; i < cur.len; ++i) {
+                mbar_wait(b.k_full + 8 * ks, k_turn, dead, a.status);
+                mbar_wait(b.v_full + 8 * vs, v_turn, dead, a.status);
+                if (elected()) {
+                    mbar_arrive(b.k_empty + 8 * ks);
+                    mbar_arrive(b.v_empty + 8 * vs);
+                }
+                step(ks, k_turn, L::k_slots);
+                step(vs, v_turn, L::v_slots);
             }
-            mark += cur.len;
             continue;
         }
         const bool both = Shape::rows(a, cur.q) - cur.inner * 2 * kRows > kRows;
@@ -337,11 +364,9 @@ __device__ __forceinline__ void mma_role(const AttendDev &a, const SchedShared &
         // O is free when its last item's output has been read
         if (q_turn) mbar_wait(b.o_free + 8 * s, (q_turn - 1) & 1, dead, a.status);
         for (int32_t i = 0; i < cur.len; ++i) {
-            step();                                     // V of tile i; its K was the slot before
-            const uint32_t v_slot = slot;
-            mbar_wait(b.v_ok + 8 * (mark % kVMarks), (mark / kVMarks) & 1, dead, a.status);
-            ++mark;
-            const uint64_t v_op = smem_operand(slot0 + v_slot * L::tile, L::half, 1024);
+            mbar_wait(b.v_full + 8 * vs, v_turn, dead, a.status);
+            to_tensor_cores();
+            const uint64_t v_op = smem_operand(v_at<HALVES>(base, vs), L::half, 1024);
             mbar_wait(b.p_full + 8 * s, p_turn & 1, dead, a.status);
             ++p_turn;
             if (both) {
@@ -353,10 +378,10 @@ __device__ __forceinline__ void mma_role(const AttendDev &a, const SchedShared &
 #pragma unroll
                 for (int k = 0; k < KT / 16; ++k)
                     mma_ts(t_o, t_s + 8 * k, v_op + 128 * k, kind_o, i > 0 || k > 0);
-                tc_commit(b.empty + 8 * v_slot);
+                tc_commit(b.v_empty + 8 * vs);
                 if (i == cur.len - 1) tc_commit(b.o_done + 8 * s);
             }
-            step();
+            step(vs, v_turn, L::v_slots);
             if (i + 1 < cur.len) issue_s();
             if (both && elected()) mbar_arrive(b.pass + 8 * (1 - s));
         }
@@ -368,53 +393,38 @@ __device__ __forceinline__ void mma_role(const AttendDev &a, const SchedShared &
     mbar_wait(b.fin + 8 * s, 0, &none, a.status);
 }
 
-// Looks over the V tiles that some row of the item does not see in full.
+// A warpgroup replaces what is not finite in a V tile by 0.  Where that is in a
+// row from key lo to hi, `mark` says so first: the other stage's warpgroup does
+// the same beside this one and may find the zeros already.
 template <typename T, int HALVES>
-__device__ __forceinline__ void look_role(const AttendDev &a, const SchedShared &sched, uint8_t *slots, const Bars &b,
-                                          volatile int32_t *bad, volatile int32_t *dead)
+__device__ __forceinline__ void clean_tile(uint4 *v, int t, int32_t j0, int32_t lo, int32_t hi, volatile int32_t *mark,
+                                           int32_t tag)
 {
     using L = Layout<HALVES>;
-    const int lane = threadIdx.x & 31;
-    Cursor<Shape> cur(a, sched);
-    uint32_t k = 0;
-    int32_t item = 0;
-    do {
-        const int32_t r0 = cur.inner * 2 * kRows;
-        const Common all(a, cur.q, r0, min(r0 + 2 * kRows, Shape::rows(a, cur.q)) - 1);
-        for (int32_t i = 0; i < cur.len; ++i, ++k) {
-            const uint32_t seq = 2 * k + 1, slot = seq % L::slots;
-            mbar_wait(b.full + 8 * slot, (seq / L::slots) & 1, dead, a.status);
-            const int32_t j0 = (cur.k.lo / KT + cur.off + i) * KT;
-            if (!all.covers(j0)) {
-                uint4 *v = reinterpret_cast<uint4 *>(slots + slot * L::tile);
-                uint32_t t = 0;
-#pragma unroll 8
-                for (int x = lane; x < L::tile / 16; x += 32) {
-                    const uint4 y = v[x];
-                    t = taint<T>(y.x, taint<T>(y.y, taint<T>(y.z, taint<T>(y.w, t))));
-                }
-                if (__any_sync(~0u, (t & 0x7fff7fffu) != 0)) {
-                    for (int x = lane; x < L::tile / 16; x += 32) {
-                        uint4 y = v[x];
-                        uint32_t *e = &y.x, hit = 0;
+    uint32_t any = 0;
+#pragma unroll 4
+    for (int x = t; x < L::tile / 16; x += kRows) {
+        const uint4 y = v[x];
+        any = taint<T>(y.x, taint<T>(y.y, taint<T>(y.z, taint<T>(y.w, any))));
+    }
+    if ((any & 0x7fff7fffu) != 0) {
+        for (int x = t; x < L::tile / 16; x += kRows) {
+            uint4 y = v[x];
+            uint32_t e[4] = {y.x, y.y, y.z, y.w};
+            bool hit = false;
 #pragma unroll
-                        for (int n = 0; n < 4; ++n) {
-                            if (not_finite<T>(e[n])) { e[n] &= 0xffff0000u; hit = 1; }
-                            if (not_finite<T>(e[n] >> 16)) { e[n] &= 0xffffu; hit = 1; }
-                        }
-                        if (!hit) continue;
-                        v[x] = y;
-                        const int32_t j = j0 + (int32_t)(x * 16 % L::half / 128);
-                        if (j >= cur.k.lo && j <= cur.k.hi) bad[item % kBad] = item + 1;
-                    }
-                }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            for (int n = 0; n < 4; ++n) {
+                if (not_finite<T>(e[n])) { e[n] &= 0xffff0000u; hit = true; }
+                if (not_finite<T>(e[n] >> 16)) { e[n] &= 0xffffu; hit = true; }
             }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(b.v_ok + 8 * (k % kVMarks));
+            if (!hit) continue;
+            const int32_t j = j0 + (int32_t)(x * 16 % L::half / 128);
+            if (j >= lo && j <= hi) *mark = tag;
+            __threadfence_block();
+            v[x] = make_uint4(e[0], e[1], e[2], e[3]);
         }
-        ++item;
-    } while (cur.next(a));
+    }
+    to_tensor_cores();
 }
 
 // One stage: queries to shared memory, softmax of its S, its output.
@@ -451,17 +461,18 @@ __device__ __forceinline__ void softmax_role(const AttendDev &a, const SchedShar
             *reinterpret_cast<uint4 *>(q_smem + s * L::tile + (piece >> 3) * L::half + row * 128 +
                                        (((piece ^ row) & 7) << 4)) = y[i];
         }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        to_tensor_cores();
         mbar_arrive(b.q_full + 8 * s);
     };
 
     Cursor<Shape> cur(a, sched);
-    uint32_t s_turn = 0, o_turn = 0;
+    uint32_t s_turn = 0, o_turn = 0, k = 0;             // k: tile of the stretch
     int32_t item = 0;
     bool loaded = false;
     for (bool go = true; go; ++item) {
         const int32_t rows = Shape::rows(a, cur.q), r0 = base_of(cur), row = r0 + t;
         if (r0 >= rows) {                               // this item has one stage only
+            k += cur.len;
             go = cur.next(a);
             continue;
         }
@@ -470,10 +481,11 @@ __device__ __forceinline__ void softmax_role(const AttendDev &a, const SchedShar
         const bool live = row < rows;
         const int32_t pos = live ? Shape::pos(a, cur.q, row) : -1, lo = pos < 0 ? 0 : first_key(a, pos);
         const Common all(a, cur.q, r0, min(r0 + kRows, rows) - 1);
+        const Common item_sees(a, cur.q, r0 - s * kRows, min(r0 - s * kRows + 2 * kRows, rows) - 1);
         const int32_t t0 = cur.k.lo / KT + cur.off;
         float m = -INFINITY, l = 0.f;
 
-        for (int32_t i = 0; i < cur.len; ++i) {
+        for (int32_t i = 0; i < cur.len; ++i, ++k) {
             mbar_wait(b.s_full + 8 * s, s_turn++ & 1, dead, a.status);
             tc_after();
             const int32_t j0 = (t0 + i) * KT;
@@ -533,6 +545,12 @@ __device__ __forceinline__ void softmax_role(const AttendDev &a, const SchedShar
             }
             tc_st32(t_s, x);
             tc_st32(t_s + 32, x + 32);
+            if (!item_sees.covers(j0)) {
+                const uint32_t slot = k % L::v_slots;
+                mbar_wait(b.v_full + 8 * slot, (k / L::v_slots) & 1, dead, a.status);
+                clean_tile<T, HALVES>(reinterpret_cast<uint4 *>(q_smem + v_at<HALVES>(0, slot)), t, j0, cur.k.lo, cur.k.hi,
+                                      bad + item % kBad, item + 1);
+            }
             const float2 both = unpair(add2(sum[0], sum[1]));
             l += both.x + both.y;
             tc_wait_st();
@@ -595,9 +613,8 @@ __device__ __forceinline__ void softmax_role(const AttendDev &a, const SchedShar
 #pragma unroll
             for (int y = 0; y < 32; ++y) o[y] = __uint_as_float(x[y]);
             if (fix) {
-                const Common any(a, cur.q, cur.inner * 2 * kRows, min(cur.inner * 2 * kRows + 2 * kRows, rows) - 1);
                 for (int32_t j = max(lo, t0 * KT); j <= min(pos, (t0 + cur.len) * KT - 1); ++j) {
-                    if (any.covers(j / KT * KT)) continue;
+                    if (item_sees.covers(j / KT * KT)) continue;
                     const int32_t id = a.c.block_table[(int64_t)cur.r * a.c.table_width + (j >> a.block_log)];
                     if (id < 0 || id >= a.blocks) continue;
                     const T *v = static_cast<const T *>(a.c.v_cache) + id * a.block_stride +
@@ -691,23 +708,23 @@ __device__ __forceinline__ void softmax_role(const AttendDev &a, const SchedShar
 
 template <typename T, int HALVES>
 __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_constant__ AttendDev a,
-                                                              const __grid_constant__ CUtensorMap km,
-                                                              const __grid_constant__ CUtensorMap vm)
+                                                              const __grid_constant__ CUtensorMap km)
 {
     using L = Layout<HALVES>;
     extern __shared__ uint8_t raw[];
     __shared__ SchedShared sched;
-    __shared__ alignas(8) uint64_t bar[2 * L::slots + kVMarks + 14];
+    __shared__ alignas(8) uint64_t bar[2 * (L::k_slots + L::v_slots) + 14];
     __shared__ int32_t dead, last[2], bad[kBad];
     __shared__ uint32_t tmem_at;
     const int tid = threadIdx.x, warp = tid >> 5;
     const uint32_t base = (smem_u32(raw) + 1023) & ~1023u;
     uint8_t *mem = raw + (base - smem_u32(raw));
     Bars b;
-    b.full = smem_u32(bar);
-    b.empty = b.full + 8 * L::slots;
-    b.v_ok = b.empty + 8 * L::slots;
-    b.q_full = b.v_ok + 8 * kVMarks;
+    b.k_full = smem_u32(bar);
+    b.k_empty = b.k_full + 8 * L::k_slots;
+    b.v_full = b.k_empty + 8 * L::k_slots;
+    b.v_empty = b.v_full + 8 * L::v_slots;
+    b.q_full = b.v_empty + 8 * L::v_slots;
     b.s_full = b.q_full + 16;
     b.p_full = b.s_full + 16;
     b.o_done = b.p_full + 16;
@@ -716,11 +733,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
     b.pass = b.fin + 16;
     if (tid == 0) {
         dead = 0;
-        for (int i = 0; i < L::slots; ++i) {
-            mbar_init(b.full + 8 * i, 1);
-            mbar_init(b.empty + 8 * i, 2);
+        for (int i = 0; i < L::k_slots; ++i) {
+            mbar_init(b.k_full + 8 * i, 1);
+            mbar_init(b.k_empty + 8 * i, 2);
         }
-        for (int i = 0; i < kVMarks; ++i) mbar_init(b.v_ok + 8 * i, 1);
+        for (int i = 0; i < L::v_slots; ++i) {
+            mbar_init(b.v_full + 8 * i, 64);
+            mbar_init(b.v_empty + 8 * i, 2);
+        }
         for (int s = 0; s < 2; ++s) {
             mbar_init(b.q_full + 8 * s, kRows);
             mbar_init(b.s_full + 8 * s, 1);
@@ -741,7 +761,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
     }
     __syncthreads();
     tc_after();
-    const uint32_t tmem = tmem_at, slot0 = base + 2 * L::tile;
+    const uint32_t tmem = tmem_at;
 
     // 384 threads x 168 registers = 256 x 208 + 128 x 88
     if (warp < 8) {
@@ -749,9 +769,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
         softmax_role<T, HALVES>(a, sched, mem, tmem, b, bad, &dead, last);
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-        if (warp < 10) mma_role<T, HALVES>(a, sched, warp - 8, base, slot0, tmem, b, &dead);
-        else if (warp == 10) copy_role<HALVES>(a, sched, &km, &vm, slot0, b, &dead);
-        else look_role<T, HALVES>(a, sched, mem + 2 * L::tile, b, bad, &dead);
+        if (warp < 10) mma_role<T, HALVES>(a, sched, warp - 8, base, tmem, b, &dead);
+        else copy_role<HALVES>(a, sched, warp - 10, &km, base, b, &dead);
     }
     tc_before();
     __syncthreads();
@@ -765,14 +784,12 @@ template <typename T, int HALVES>
 static pp_status launch_t(pp_kv *kv, const AttendArgs &c, cudaStream_t st)
 {
     const AttendDev a = attend_dev(kv, c);
-    CUtensorMap km, vm;
-    const int32_t rows = std::min(kv->block_size, KT);
-    pp_status s = cache_map(kv, c.k_cache, rows, &km);
-    if (s == PP_OK) s = cache_map(kv, c.v_cache, rows, &vm);
+    CUtensorMap km;
+    const pp_status s = cache_map(kv, c.k_cache, std::min(kv->block_size, KT), &km);
     if (s != PP_OK) return s;
     PP_CUDA(cudaFuncSetAttribute(k_attend_chunk<T, HALVES>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                  Layout<HALVES>::bytes));
-    k_attend_chunk<T, HALVES><<<kv->sm_count, kThreads, Layout<HALVES>::bytes, st>>>(a, km, vm);
+    k_attend_chunk<T, HALVES><<<kv->sm_count, kThreads, Layout<HALVES>::bytes, st>>>(a, km);
     PP_CUDA(cudaGetLastError());
     return PP_OK;
 }

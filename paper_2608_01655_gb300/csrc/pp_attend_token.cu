@@ -5,10 +5,10 @@
 // the read of K and V (4 to 32 operations a byte); the products run on
 // m16n8k16 tensor instructions with the heads as the 16 rows (padded), which
 // keeps scores, weights and sums in registers: the score's accumulators are the
-// next product's operand as they stand.  A tile is 64 keys; four warps take 16
-// keys each, two groups of warps take turns at the tiles, and every warp has its
-// own running maximum, sum and output, joined once an item.
-#include <algorithm>
+// next product's operand as they stand.  A tile is 128 keys, 16 a warp.  Every
+// warp copies its own rows, into a ring of its own, and has its own running
+// maximum, sum and output, joined once an item: between items no warp waits for
+// another.
 #include <climits>
 
 #include "pp_attend.cuh"
@@ -16,18 +16,20 @@
 namespace pp {
 
 namespace token {
-constexpr int KT = 64;                              // keys per tile
-constexpr int kWarps = 8, kGroups = 2;
-constexpr int kThreads = 32 * (kWarps + 1);         // and one warp that copies
+constexpr int kWarps = 8, kThreads = 32 * kWarps;
+constexpr int kKeys = 16;                           // keys of a warp
+constexpr int KT = kKeys * kWarps;                  // keys per tile
 constexpr int kRows = 16;                           // query heads of an item
 
 template <int HALVES> struct Layout {
-    static constexpr int tile = KT * 128 * HALVES;              // bytes of K or of V
-    static constexpr int stages = HALVES == 2 ? 4 : 8;
+    static constexpr int half = kKeys * 128;                    // bytes of 64 columns of a warp's keys
+    static constexpr int rows = half * HALVES;                  // of its K or V
+    static constexpr int stages = HALVES == 2 ? 3 : 6;
     static constexpr int width = 64 * HALVES;
     static constexpr int pitch = width + 4;                     // floats of an output row in shared memory
-    static constexpr int join = kWarps * kRows * pitch * 4;
-    static constexpr int bytes = 1024 + stages * 2 * tile + join;
+    static constexpr int ring = kWarps * stages * 2 * rows;
+    static constexpr int join = kWarps / 2 * kRows * pitch * 4;
+    static constexpr int bytes = 128 + ring + join;
 };
 
 struct Shape {
@@ -76,110 +78,93 @@ __device__ __forceinline__ void mma16<__half>(float (&c)[4], const uint32_t (&a)
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// byte offset of element (row, 8 * chunk) of a tile: halves of 64 elements, rows of 128 bytes
-__device__ __forceinline__ uint32_t tile_at(int row, int chunk)
+// byte offset of element (row, 8 * piece) of a warp's K or V
+__device__ __forceinline__ uint32_t row_at(int row, int piece)
 {
-    return (chunk >> 3) * (KT * 128) + row * 128 + (((chunk ^ row) & 7) << 4);
+    return (piece >> 3) * (kKeys * 128) + row * 128 + (((piece ^ row) & 7) << 4);
 }
 
 // both 16-bit halves of a register kept or cleared
 __device__ __forceinline__ uint32_t keep(bool lo, bool hi) { return (lo ? 0xffffu : 0u) | (hi ? 0xffff0000u : 0u); }
 
-// Copies the stretch's tiles, one box a lane: lanes are (K or V, half, box).
-template <int HALVES>
-__device__ __forceinline__ void copy_tiles(const AttendDev &a, const SchedShared &sched, const CUtensorMap *km,
-                                           const CUtensorMap *vm, uint32_t stage0, uint32_t full, uint32_t empty,
-                                           volatile int32_t *dead)
-{
+// A warp's copies of its keys, tile after tile along the stretch.
+template <int HALVES> struct Feed {
     using L = Layout<HALVES>;
-    const int lane = threadIdx.x & 31;
-    const int box_log = min(a.block_log, 6), boxes = KT >> box_log;        // 8 at most
-    const int box = lane % boxes, which = lane / boxes;                    // (half, K or V)
-    const bool active = which < 2 * HALVES;
-    const int half = which % HALVES;
-    const bool is_v = which >= HALVES;
-    const uint32_t dst = (is_v ? L::tile : 0) + half * (KT * 128) + (box << box_log) * 128;
-    const CUtensorMap *map = is_v ? vm : km;
-
-    Cursor<Shape> cur(a, sched);
-    uint32_t seq = 0;
-    do {
-        const int32_t *row = a.c.block_table + (int64_t)cur.r * a.c.table_width;
-        const int32_t head = cur.outer / Shape::row_tiles(a);
-        const int32_t t0 = cur.k.lo / KT + cur.off;
-        auto entry = [&](int32_t t) {                   // block of this lane's box of tile t
-            const int32_t j = t * KT + (box << box_log);
-            if (!active || j > cur.k.hi || j + (1 << box_log) <= cur.k.lo) return a.blocks;
-            int32_t id = row[j >> a.block_log];
-            if (id < 0 || id >= a.blocks) {
-                kv_bounds(a.status);
-                id = a.blocks;
-            }
-            return id;
-        };
-        int32_t id = entry(t0);
-        for (int32_t i = 0; i < cur.len; ++i, ++seq) {
-            const int32_t after = i + 1 < cur.len ? entry(t0 + i + 1) : 0;
-            const uint32_t s = seq % L::stages, turn = seq / L::stages;
-            if (turn) mbar_wait(empty + 8 * s, (turn - 1) & 1, dead, a.status);
-            if (*dead) break;
-            if (lane == 0) mbar_expect(full + 8 * s, 2 * L::tile);
-            __syncwarp();
-            const int32_t j = (t0 + i) * KT + (box << box_log);
-            if (active)
-                tma_rows(stage0 + s * 2 * L::tile + dst, map, full + 8 * s, half * 64, j & ((1 << a.block_log) - 1),
-                         head, id);
-            id = after;
-        }
-    } while (!*dead && cur.next(a));
-    if (*dead) {
-        // copies in flight land before the CTA ends (the limit is the same, without a flag)
-        int32_t none = 0;
-        for (uint32_t x = seq > L::stages ? seq - L::stages : 0; x < seq; ++x)
-            mbar_wait(full + 8 * (x % L::stages), (x / L::stages) & 1, &none, a.status);
+    const AttendDev &a;
+    Cursor<Shape> cur;
+    RowLane<HALVES> rl;
+    uint32_t ring, slot = 0;
+    int32_t i = 0, b0, b1;                              // next tile of the item; blocks of its keys
+    bool more = true;
+    __device__ __forceinline__ Feed(const AttendDev &a_, const SchedShared &sched, uint32_t ring_)
+        : a(a_), cur(a_, sched), rl(a_, L::half), ring(ring_)
+    {
+        look();
     }
-}
+    __device__ __forceinline__ int32_t first() const
+    {
+        return (cur.k.lo / KT + cur.off + i) * KT + (int32_t)(threadIdx.x >> 5) * kKeys;
+    }
+    __device__ __forceinline__ void look()
+    {
+        const int32_t *row = a.c.block_table + (int64_t)cur.r * a.c.table_width;
+        b0 = key_block(a, row, cur.k, first(), 8);
+        b1 = key_block(a, row, cur.k, first() + 8, 8);
+    }
+    // asks for the next tile, into the ring's next place
+    __device__ __forceinline__ void ask()
+    {
+        if (more) {
+            const int32_t j0 = first(), in_block = (1 << a.block_log) - 1;
+            if (j0 <= cur.k.hi && j0 + kKeys - 1 >= cur.k.lo) {
+                const int64_t token_bytes = 2 * a.token_stride, head = 2 * (cur.outer / Shape::row_tiles(a)) * a.head_stride;
+                const int64_t at0 = head + max(b0, 0) * 2 * a.block_stride + (j0 & in_block) * token_bytes;
+                const int64_t at1 = head + max(b1, 0) * 2 * a.block_stride + ((j0 + 8) & in_block) * token_bytes;
+                const char *k = static_cast<const char *>(a.c.k_cache), *v = static_cast<const char *>(a.c.v_cache);
+                const uint32_t to = ring + slot * 2 * L::rows;
+                rl.rows8(to, k + at0, token_bytes, b0 >= 0);
+                rl.rows8(to + 1024, k + at1, token_bytes, b1 >= 0);
+                rl.rows8(to + L::rows, v + at0, token_bytes, b0 >= 0);
+                rl.rows8(to + L::rows + 1024, v + at1, token_bytes, b1 >= 0);
+            }
+            if (++i == cur.len) {
+                i = 0;
+                more = cur.next(a);
+            }
+            if (more) look();
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        if (++slot == L::stages) slot = 0;
+    }
+};
 
 template <typename T, int HALVES>
-__global__ void __launch_bounds__(kThreads) k_attend_token(const __grid_constant__ AttendDev a,
-                                                           const __grid_constant__ CUtensorMap km,
-                                                           const __grid_constant__ CUtensorMap vm)
+__global__ void __launch_bounds__(kThreads, 1) k_attend_token(const __grid_constant__ AttendDev a)
 {
     using L = Layout<HALVES>;
     constexpr int KS = 4 * HALVES;                      // 16-wide steps of the head dimension
     extern __shared__ uint8_t raw[];
     __shared__ SchedShared sched;
-    __shared__ alignas(8) uint64_t bars[2 * L::stages];
     __shared__ float stat[2][kWarps][kRows];
-    __shared__ int32_t dead, last;
+    __shared__ int32_t last;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const uint32_t stage0 = (smem_u32(raw) + 1023) & ~1023u;
-    float *join = reinterpret_cast<float *>(raw + (stage0 - smem_u32(raw)) + L::stages * 2 * L::tile);
-    const uint32_t full = smem_u32(bars), empty = full + 8 * L::stages;
-    if (tid == 0) {
-        dead = 0;
-        for (int s = 0; s < L::stages; ++s) {
-            mbar_init(full + 8 * s, 1);
-            mbar_init(empty + 8 * s, kWarps / kGroups);
-        }
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
-    if (!schedule<Shape>(a, sched)) return;             // its barriers order the set-up too
+    const uint32_t base = (smem_u32(raw) + 127) & ~127u;
+    float *join = reinterpret_cast<float *>(raw + (base - smem_u32(raw)) + L::ring);
+    if (!schedule<Shape>(a, sched)) return;
     const int64_t total = sched.total, ctas = min((int64_t)gridDim.x, total);
-    if (warp == kWarps) {
-        copy_tiles<HALVES>(a, sched, &km, &vm, stage0, full, empty, &dead);
-        return;
-    }
 
-    const int group = warp / (kWarps / kGroups), sub = warp % (kWarps / kGroups);
     const int r0 = lane >> 2, c0 = 2 * (lane & 3);      // this thread's rows r0, r0 + 8; its columns
     // ldmatrix rows: K (keys outside, dims inside a group of four matrices), V (the other way round)
-    const int krow = sub * 16 + (lane >> 4) * 8 + (lane & 7), kchunk = (lane >> 3) & 1;
-    const int vrow = sub * 16 + ((lane >> 3) & 1) * 8 + (lane & 7), vchunk = lane >> 4;
+    const int krow = (lane >> 4) * 8 + (lane & 7), kpiece = (lane >> 3) & 1;
+    const int vrow = ((lane >> 3) & 1) * 8 + (lane & 7), vpiece = lane >> 4;
     const int jr = tid >> 4, jd = (tid & 15) * (4 * HALVES);          // joining: row and first column
 
+    const uint32_t ring = base + warp * L::stages * 2 * L::rows;
+    Feed<HALVES> feed(a, sched, ring);
+#pragma unroll 1
+    for (int x = 0; x < L::stages; ++x) feed.ask();
     Cursor<Shape> cur(a, sched);
-    uint32_t seq = 0;
+    uint32_t slot = 0;
     do {
         const int32_t tiles_of = Shape::row_tiles(a), head = cur.outer / tiles_of;
         const int32_t row0 = cur.outer % tiles_of * kRows, rows = min(kRows, a.c.group - row0);
@@ -204,13 +189,14 @@ __global__ void __launch_bounds__(kThreads) k_attend_token(const __grid_constant
             for (int x = 0; x < 4; ++x) o[n][x] = 0.f;
 
         const int32_t t0 = cur.k.lo / KT + cur.off;
-        for (int32_t i = 0; i < cur.len; ++i, ++seq) {
-            if ((int)(seq & (kGroups - 1)) != group) continue;
-            const uint32_t s = seq % L::stages;
-            const uint32_t kt = stage0 + s * 2 * L::tile, vt = kt + L::tile;
-            const int32_t j0 = (t0 + i) * KT + sub * 16;            // this warp's first key
-            mbar_wait(full + 8 * s, (seq / L::stages) & 1, &dead, a.status);
-            if (j0 <= cur.k.hi && j0 + 15 >= cur.k.lo) {
+#pragma unroll 1
+        for (int32_t i = 0; i < cur.len; ++i) {
+            const uint32_t kt = ring + slot * 2 * L::rows, vt = kt + L::rows;
+            if (++slot == L::stages) slot = 0;
+            const int32_t j0 = (t0 + i) * KT + warp * kKeys;        // this warp's first key
+            asm volatile("cp.async.wait_group %0;" ::"n"(L::stages - 1) : "memory");
+            __syncwarp();
+            if (j0 <= cur.k.hi && j0 + kKeys - 1 >= cur.k.lo) {
                 float sc[2][4];
 #pragma unroll
                 for (int n = 0; n < 2; ++n)
@@ -219,11 +205,11 @@ __global__ void __launch_bounds__(kThreads) k_attend_token(const __grid_constant
 #pragma unroll
                 for (int k = 0; k < KS; ++k) {
                     uint32_t b[4];
-                    ldsm4(b, kt + tile_at(krow, 2 * k + kchunk));
+                    ldsm4(b, kt + row_at(krow, 2 * k + kpiece));
                     mma16<T>(sc[0], qf[k], b[0], b[1]);
                     mma16<T>(sc[1], qf[k], b[2], b[3]);
                 }
-                const bool edge = j0 < cur.k.lo || j0 + 15 > cur.k.hi;
+                const bool edge = j0 < cur.k.lo || j0 + kKeys - 1 > cur.k.hi;
                 uint32_t vk0 = ~0u, vk1 = ~0u;                      // V rows that count, as the operand holds them
                 if (edge) {
                     bool in[4];
@@ -273,7 +259,7 @@ __global__ void __launch_bounds__(kThreads) k_attend_token(const __grid_constant
 #pragma unroll
                 for (int n = 0; n < KS; ++n) {
                     uint32_t b[4];
-                    ldsm4_trans(b, vt + tile_at(vrow, 2 * n + vchunk));
+                    ldsm4_trans(b, vt + row_at(vrow, 2 * n + vpiece));
                     if (edge) {
                         b[0] &= vk0;
                         b[1] &= vk1;
@@ -285,36 +271,74 @@ __global__ void __launch_bounds__(kThreads) k_attend_token(const __grid_constant
                 }
             }
             __syncwarp();
-            if (lane == 0) mbar_arrive(empty + 8 * s);
+            feed.ask();                                             // into the place just read
         }
 
-        // join the warps: a thread has one row's 4 * HALVES columns
+        // join the warps: the upper four hand theirs to the lower four, lane by lane,
+        // then a thread has one row's 4 * HALVES columns
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
             l[x] += __shfl_xor_sync(~0u, l[x], 1);
             l[x] += __shfl_xor_sync(~0u, l[x], 2);
-            const int row = r0 + 8 * x;
             if ((lane & 3) == 0) {
-                stat[0][warp][row] = m[x];
-                stat[1][warp][row] = l[x];
-            }
-            if (row < rows) {
-                float *dst = join + (warp * kRows + row) * L::pitch + c0;
-#pragma unroll
-                for (int n = 0; n < 2 * KS; ++n)
-                    *reinterpret_cast<float2 *>(dst + 8 * n) = make_float2(o[n][2 * x], o[n][2 * x + 1]);
+                stat[0][warp][r0 + 8 * x] = m[x];
+                stat[1][warp][r0 + 8 * x] = l[x];
             }
         }
-        named_sync(1, 32 * kWarps);
+        if (warp >= kWarps / 2) {
+            float4 *dst = reinterpret_cast<float4 *>(join) + (warp - kWarps / 2) * 2 * KS * 32 + lane;
+#pragma unroll
+            for (int n = 0; n < 2 * KS; ++n) dst[32 * n] = make_float4(o[n][0], o[n][1], o[n][2], o[n][3]);
+        }
+        __syncthreads();
+        if (warp < kWarps / 2) {
+            const float4 *src = reinterpret_cast<const float4 *>(join) + warp * 2 * KS * 32 + lane;
+            float f[2], g[2];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const float other = stat[0][warp + kWarps / 2][r0 + 8 * x], up = fmaxf(m[x], other);
+                const float by = up == -INFINITY ? 0.f : up;
+                f[x] = exp2_approx(m[x] - by);
+                g[x] = exp2_approx(other - by);
+                m[x] = up;
+                l[x] = f[x] * l[x] + g[x] * stat[1][warp + kWarps / 2][r0 + 8 * x];
+            }
+#pragma unroll
+            for (int n = 0; n < 2 * KS; ++n) {
+                const float4 y = src[32 * n];
+                o[n][0] = f[0] * o[n][0] + g[0] * y.x;
+                o[n][1] = f[0] * o[n][1] + g[0] * y.y;
+                o[n][2] = f[1] * o[n][2] + g[1] * y.z;
+                o[n][3] = f[1] * o[n][3] + g[1] * y.w;
+            }
+        }
+        __syncthreads();
+        if (warp < kWarps / 2) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const int row = r0 + 8 * x;
+                if ((lane & 3) == 0) {
+                    stat[0][warp][row] = m[x];
+                    stat[1][warp][row] = l[x];
+                }
+                if (row < rows) {
+                    float *dst = join + (warp * kRows + row) * L::pitch + c0;
+#pragma unroll
+                    for (int n = 0; n < 2 * KS; ++n)
+                        *reinterpret_cast<float2 *>(dst + 8 * n) = make_float2(o[n][2 * x], o[n][2 * x + 1]);
+                }
+            }
+        }
+        __syncthreads();
         float acc[4 * HALVES], top = -INFINITY, sum = 0.f;
 #pragma unroll
         for (int d = 0; d < 4 * HALVES; ++d) acc[d] = 0.f;
         if (jr < rows) {
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) top = fmaxf(top, stat[0][w][jr]);
+            for (int w = 0; w < kWarps / 2; ++w) top = fmaxf(top, stat[0][w][jr]);
             const float base = top == -INFINITY ? 0.f : top;
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) {
+            for (int w = 0; w < kWarps / 2; ++w) {
                 const float f = exp2_approx(stat[0][w][jr] - base);
                 sum = fmaf(f, stat[1][w][jr], sum);
                 const float4 *src = reinterpret_cast<const float4 *>(join + (w * kRows + jr) * L::pitch + jd);
@@ -351,12 +375,12 @@ __global__ void __launch_bounds__(kThreads) k_attend_token(const __grid_constant
             // true in the CTA that arrives last of `of`
             auto arrive = [&](int32_t *count, int32_t of) {
                 __threadfence();
-                named_sync(1, 32 * kWarps);
+                __syncthreads();
                 if (tid == 0) {
                     last = atomicAdd(count, 1) == of - 1;
                     if (last) *count = 0;
                 }
-                named_sync(1, 32 * kWarps);
+                __syncthreads();
                 __threadfence();
                 return last != 0;
             };
@@ -417,7 +441,7 @@ __global__ void __launch_bounds__(kThreads) k_attend_token(const __grid_constant
                 a.c.lse[(int64_t)tok * a.c.q_heads + x] =
                     sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
         }
-        named_sync(1, 32 * kWarps);                     // the join's memory is free again
+        __syncthreads();                                // the join's memory is free again
     } while (cur.next(a));
 }
 
@@ -425,14 +449,9 @@ template <typename T, int HALVES>
 static pp_status launch_t(pp_kv *kv, const AttendArgs &c, cudaStream_t st)
 {
     const AttendDev a = attend_dev(kv, c);
-    CUtensorMap km, vm;
-    const int32_t rows = std::min(kv->block_size, KT);
-    pp_status s = cache_map(kv, c.k_cache, rows, &km);
-    if (s == PP_OK) s = cache_map(kv, c.v_cache, rows, &vm);
-    if (s != PP_OK) return s;
     PP_CUDA(cudaFuncSetAttribute(k_attend_token<T, HALVES>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                  Layout<HALVES>::bytes));
-    k_attend_token<T, HALVES><<<kv->sm_count, kThreads, Layout<HALVES>::bytes, st>>>(a, km, vm);
+    k_attend_token<T, HALVES><<<kv->sm_count, kThreads, Layout<HALVES>::bytes, st>>>(a);
     PP_CUDA(cudaGetLastError());
     return PP_OK;
 }
