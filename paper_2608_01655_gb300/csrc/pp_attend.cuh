@@ -296,24 +296,20 @@ __device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, volatil
 // ---------------------------------------------------------------------------
 // Rows of K or V lie in halves of 64 elements, 128 bytes a row, whose 16-byte
 // pieces are swizzled by the row (piece ^ row % 8): the layout that ldmatrix
-// reads without conflicts and the tensor cores' operands take.  There are two
-// ways to get them there.  A tensor-map box costs a lane's one instruction but
-// ends with its block, and measured on this GPU machines of 128-byte rows take 52
-// cycles and 5.3 a row, from L2 as from HBM: over all SMs 3.2 TB/s with 8 rows,
-// 4.4 with 16, 6.2 with 64.  16-byte copies, a warp's 32 at a time, reach 9
-// (one warp an SM) to 21 TB/s (eight) from L2, but each costs the warp some five
-// instructions.
+// reads without conflicts and the tensor cores' operands take.  Two ways get
+// them there.  A tensor-map box costs one lane an instruction but ends with its
+// block, and measured on this GPU machines of 128-byte rows take 52 cycles and 5.3 a
+// row, from L2 as from HBM: over all SMs 3.2 TB/s with 8 rows, 4.4 with 16, 6.2
+// with 64.  16-byte copies, a warp's 32 at a time, reach 9 TB/s (one warp an SM)
+// to 21 (eight) from L2, but each costs the warp some five instructions, and
+// operands of the tensor cores need a fence after them.  Single tokens take the
+// second way with eight warps (128 requests, blocks of 16: 256 us against 297);
+// chunks, whose warps have the softmax to do, the first (8,192 tokens after
+// 24,576: 1.97 ms against 2.31 with V by copies).
 __device__ __forceinline__ void copy16(uint32_t dst, const char *src, uint32_t bytes)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
-// the barrier's arrival of this lane, once its copies so far have landed
-__device__ __forceinline__ void copies_arrive(uint32_t bar)
-{
-    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
-
 // A lane's share of copies of whole rows: `step` rows of 16-byte pieces at a time.
 template <int HALVES> struct RowLane {
     static constexpr int per_row = 8 * HALVES, step = 32 / per_row;

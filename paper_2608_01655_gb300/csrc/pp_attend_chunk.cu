@@ -14,8 +14,7 @@
 // 16-bit types hold as precisely.
 //
 // Warps: 0-3 and 4-7 the stages' softmax and epilogue, 8 and 9 their products, 10
-// copies K by tensor-map boxes, and 10 and 11 copy V 16 bytes a lane: either way
-// alone is slower than the products.  V tiles that not every row sees in full are looked
+// and 11 the copies of K and V.  V tiles that not every row sees in full are looked
 // over by the softmax warps: an infinity or a NaN there would pass through a
 // weight of 0, so it is replaced by 0 and added in the epilogue to the rows that
 // do see it.
@@ -243,10 +242,10 @@ template <int HALVES> __device__ __forceinline__ uint32_t v_at(uint32_t base, ui
 }
 __device__ __forceinline__ void to_tensor_cores() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
-// The tiles of the stretch: warp 0 asks for K, a box a lane (lanes are (half,
-// box)); both copy half of V's rows.
+// The tiles of the stretch, of K (which = 0) or V (1), a box a lane: lanes are
+// (half, box).
 template <int HALVES>
-__device__ __forceinline__ void copy_role(const AttendDev &a, const SchedShared &sched, int w, const CUtensorMap *km,
+__device__ __forceinline__ void copy_role(const AttendDev &a, const SchedShared &sched, int which, const CUtensorMap *map,
                                           uint32_t base, const Bars &b, volatile int32_t *dead)
 {
     using L = Layout<HALVES>;
@@ -254,55 +253,45 @@ __device__ __forceinline__ void copy_role(const AttendDev &a, const SchedShared 
     const int box_log = min(a.block_log, 7), boxes = KT >> box_log;        // 16 at most
     const int box = lane % boxes, half = lane / boxes;
     const bool asks = half < HALVES;
-    const uint32_t k_dst = half * L::half + (box << box_log) * 128;
-    const RowLane<HALVES> rl(a, L::half);
-    const int64_t token_bytes = 2 * a.token_stride, block_bytes = 2 * a.block_stride;
+    const uint32_t dst = (which ? v_at<HALVES>(base, 0) : k_at<HALVES>(base, 0)) + half * L::half + (box << box_log) * 128;
+    const uint32_t full = which ? b.v_full : b.k_full, empty = which ? b.v_empty : b.k_empty;
+    const uint32_t slots = which ? L::v_slots : L::k_slots;
     const int32_t in_block = (1 << a.block_log) - 1;
 
     Cursor<Shape> cur(a, sched);
-    uint32_t k = 0;
+    uint32_t slot = 0, turn = 0, used = 0;
     do {
         const int32_t *row = a.c.block_table + (int64_t)cur.r * a.c.table_width;
         const int32_t t0 = cur.k.lo / KT + cur.off;
-        const char *v = static_cast<const char *>(a.c.v_cache) + 2 * cur.outer * a.head_stride;
-        // blocks of this lane's box of K, and, of lane g, of V's rows 64 w + 8 g on
-        auto k_block = [&](int32_t t) { return asks && w == 0 ? key_block(a, row, cur.k, t * KT + (box << box_log), 1 << box_log) : -1; };
-        auto v_block = [&](int32_t t) { return lane < 8 ? key_block(a, row, cur.k, t * KT + 64 * w + 8 * lane, 8) : -1; };
-        int32_t kb = k_block(t0), vb = v_block(t0);
-        for (int32_t i = 0; i < cur.len && !*dead; ++i, ++k) {
-            const bool more = i + 1 < cur.len;
-            const int32_t kb_next = more ? k_block(t0 + i + 1) : -1, vb_next = more ? v_block(t0 + i + 1) : -1;
-            const int32_t j0 = (t0 + i) * KT;
-            if (w == 0) {
-                const uint32_t s = k % L::k_slots;
-                if (k >= L::k_slots) mbar_wait(b.k_empty + 8 * s, (k / L::k_slots - 1) & 1, dead, a.status);
-                if (*dead) break;
-                if (lane == 0) mbar_expect(b.k_full + 8 * s, L::tile);
-                __syncwarp();
-                if (asks)
-                    box_rows(k_at<HALVES>(base, s) + k_dst, km, b.k_full + 8 * s, half * 64, (j0 + (box << box_log)) & in_block,
-                             cur.outer, kb < 0 ? a.blocks : kb);
+        auto block = [&](int32_t t) {
+            return asks ? key_block(a, row, cur.k, t * KT + (box << box_log), 1 << box_log) : -1;
+        };
+        int32_t id = block(t0);
+        for (int32_t i = 0; i < cur.len && !*dead; ++i) {
+            const int32_t after = i + 1 < cur.len ? block(t0 + i + 1) : -1;
+            if (used == slots) mbar_wait(empty + 8 * slot, turn ^ 1, dead, a.status);
+            if (*dead) break;
+            if (lane == 0) mbar_expect(full + 8 * slot, L::tile);
+            __syncwarp();
+            if (asks)
+                box_rows(dst + slot * L::tile, map, full + 8 * slot, half * 64, ((t0 + i) * KT + (box << box_log)) & in_block,
+                         cur.outer, id < 0 ? a.blocks : id);
+            id = after;
+            if (used < slots) ++used;
+            if (++slot == slots) {
+                slot = 0;
+                turn ^= 1;
             }
-            const uint32_t s = k % L::v_slots;
-            if (k >= L::v_slots) mbar_wait(b.v_empty + 8 * s, (k / L::v_slots - 1) & 1, dead, a.status);
-            const uint32_t dst = v_at<HALVES>(base, s) + w * 8192;
-#pragma unroll
-            for (int g = 0; g < 8; ++g) {
-                const int32_t id = __shfl_sync(~0u, vb, g);
-                rl.rows8(dst + g * 1024, v + max(id, 0) * block_bytes + ((j0 + 64 * w + 8 * g) & in_block) * token_bytes,
-                         token_bytes, id >= 0);
-            }
-            copies_arrive(b.v_full + 8 * s);
-            kb = kb_next;
-            vb = vb_next;
         }
     } while (!*dead && cur.next(a));
-    // nothing is in flight when the CTA ends
-    copies_wait();
-    if (w == 0 && *dead) {
+    if (*dead) {
+        // copies in flight land before the CTA ends
         int32_t none = 0;
-        for (uint32_t x = k > L::k_slots ? k - L::k_slots : 0; x <= k; ++x)
-            mbar_wait(b.k_full + 8 * (x % L::k_slots), (x / L::k_slots) & 1, &none, a.status);
+        for (uint32_t x = 0; x < used; ++x) {
+            if (slot == 0) turn ^= 1;
+            slot = slot ? slot - 1 : slots - 1;
+            mbar_wait(full + 8 * slot, turn, &none, a.status);
+        }
     }
 }
 
@@ -365,7 +354,6 @@ __device__ __forceinline__ void mma_role(const AttendDev &a, const SchedShared &
         if (q_turn) mbar_wait(b.o_free + 8 * s, (q_turn - 1) & 1, dead, a.status);
         for (int32_t i = 0; i < cur.len; ++i) {
             mbar_wait(b.v_full + 8 * vs, v_turn, dead, a.status);
-            to_tensor_cores();
             const uint64_t v_op = smem_operand(v_at<HALVES>(base, vs), L::half, 1024);
             mbar_wait(b.p_full + 8 * s, p_turn & 1, dead, a.status);
             ++p_turn;
@@ -501,9 +489,16 @@ __device__ __forceinline__ void softmax_role(const AttendDev &a, const SchedShar
                 tc_wait_ld();
                 if (edge) {
                     const int32_t from = lo - j0, to = pos - j0;
+                    if (j0 + KT - 1 > all.hi) {
 #pragma unroll
-                    for (int c = 0; c < KT; ++c)
-                        if (c < from || c > to) x[c] = 0xff800000u;
+                        for (int c = 0; c < KT; ++c)
+                            if (c > to) x[c] = 0xff800000u;
+                    }
+                    if (j0 < all.lo) {
+#pragma unroll
+                        for (int c = 0; c < KT; ++c)
+                            if (c < from) x[c] = 0xff800000u;
+                    }
                 }
                 float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
                 if (sure) {
@@ -708,7 +703,8 @@ __device__ __forceinline__ void softmax_role(const AttendDev &a, const SchedShar
 
 template <typename T, int HALVES>
 __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_constant__ AttendDev a,
-                                                              const __grid_constant__ CUtensorMap km)
+                                                              const __grid_constant__ CUtensorMap km,
+                                                              const __grid_constant__ CUtensorMap vm)
 {
     using L = Layout<HALVES>;
     extern __shared__ uint8_t raw[];
@@ -738,7 +734,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
             mbar_init(b.k_empty + 8 * i, 2);
         }
         for (int i = 0; i < L::v_slots; ++i) {
-            mbar_init(b.v_full + 8 * i, 64);
+            mbar_init(b.v_full + 8 * i, 1);
             mbar_init(b.v_empty + 8 * i, 2);
         }
         for (int s = 0; s < 2; ++s) {
@@ -770,7 +766,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
         if (warp < 10) mma_role<T, HALVES>(a, sched, warp - 8, base, tmem, b, &dead);
-        else copy_role<HALVES>(a, sched, warp - 10, &km, base, b, &dead);
+        else copy_role<HALVES>(a, sched, warp - 10, warp == 10 ? &km : &vm, base, b, &dead);
     }
     tc_before();
     __syncthreads();
@@ -784,12 +780,14 @@ template <typename T, int HALVES>
 static pp_status launch_t(pp_kv *kv, const AttendArgs &c, cudaStream_t st)
 {
     const AttendDev a = attend_dev(kv, c);
-    CUtensorMap km;
-    const pp_status s = cache_map(kv, c.k_cache, std::min(kv->block_size, KT), &km);
+    CUtensorMap km, vm;
+    const int32_t rows = std::min(kv->block_size, KT);
+    pp_status s = cache_map(kv, c.k_cache, rows, &km);
+    if (s == PP_OK) s = cache_map(kv, c.v_cache, rows, &vm);
     if (s != PP_OK) return s;
     PP_CUDA(cudaFuncSetAttribute(k_attend_chunk<T, HALVES>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                  Layout<HALVES>::bytes));
-    k_attend_chunk<T, HALVES><<<kv->sm_count, kThreads, Layout<HALVES>::bytes, st>>>(a, km);
+    k_attend_chunk<T, HALVES><<<kv->sm_count, kThreads, Layout<HALVES>::bytes, st>>>(a, km, vm);
     PP_CUDA(cudaGetLastError());
     return PP_OK;
 }
