@@ -8,10 +8,10 @@
 //   P = exp2(scale S - m) by one warpgroup, a row a thread, written over S,
 //   O += P V       P from tensor memory, V as it lies in the cache.
 // The stages take turns: while one warpgroup works on its S, the tensor cores
-// run the other stage's products.  m follows the running maximum only when it
-// is exceeded by more than 8 in log2, so O is rescaled (in tensor memory) in the
-// first tiles and hardly ever later; weights are at most 2^8 then, which both
-// 16-bit types hold as precisely.
+// run the other stage's products.  m is a maximum that was found once and moves
+// only when a tile's weights add up to more than 2^12, so O is rescaled (in tensor
+// memory) hardly ever, and no tile waits for its maximum; weights are at most
+// 2^12 then, which both 16-bit types hold as precisely as 1.
 //
 // Warps: 0-3 and 4-7 the stages' softmax and epilogue, 8 and 9 their products, 10
 // and 11 the copies of K and V.  V tiles that not every row sees in full are looked
@@ -30,7 +30,7 @@ constexpr int KT = 128;                             // keys per tile
 constexpr int kRows = 128;                          // rows of a stage
 constexpr int kThreads = 384;
 constexpr int kBad = 16;                            // marks of items, the stages are fewer apart
-constexpr float kSlack = 8.f;                       // log2 by which a score may exceed m
+constexpr float kMaxSum = 4096.f;                   // of the weights of a row and tile, before m moves
 
 template <int HALVES> struct Layout {
     static constexpr int half = KT * 128;                       // bytes of 64 columns of a tile
@@ -316,9 +316,7 @@ __device__ __forceinline__ void mma_role(const AttendDev &a, const SchedShared &
             turn ^= 1;
         }
     };
-    auto issue_s = [&]() {
-        mbar_wait(b.k_full + 8 * ks, k_turn, dead, a.status);
-        tc_after();
+    auto issue_s = [&]() {                              // K has been waited for
         const uint64_t k_op = smem_operand(k_at<HALVES>(base, ks), 16, 1024);
         if (elected()) {
 #pragma unroll
@@ -349,18 +347,22 @@ __device__ __forceinline__ void mma_role(const AttendDev &a, const SchedShared &
         }
         const bool both = Shape::rows(a, cur.q) - cur.inner * 2 * kRows > kRows;
         mbar_wait(b.q_full + 8 * s, q_turn & 1, dead, a.status);
+        mbar_wait(b.k_full + 8 * ks, k_turn, dead, a.status);
+        tc_after();
         issue_s();
         // O is free when its last item's output has been read
         if (q_turn) mbar_wait(b.o_free + 8 * s, (q_turn - 1) & 1, dead, a.status);
         for (int32_t i = 0; i < cur.len; ++i) {
+            // what is likely there already first: a wait costs 85 cycles even then
             mbar_wait(b.v_full + 8 * vs, v_turn, dead, a.status);
-            const uint64_t v_op = smem_operand(v_at<HALVES>(base, vs), L::half, 1024);
-            mbar_wait(b.p_full + 8 * s, p_turn & 1, dead, a.status);
-            ++p_turn;
+            if (i + 1 < cur.len) mbar_wait(b.k_full + 8 * ks, k_turn, dead, a.status);
             if (both) {
                 if (s == 1 || pass) mbar_wait(b.pass + 8 * s, (pass + s + 1) & 1, dead, a.status);
                 ++pass;
             }
+            const uint64_t v_op = smem_operand(v_at<HALVES>(base, vs), L::half, 1024);
+            mbar_wait(b.p_full + 8 * s, p_turn & 1, dead, a.status);
+            ++p_turn;
             tc_after();
             if (elected()) {
 #pragma unroll
@@ -425,7 +427,7 @@ __device__ __forceinline__ void softmax_role(const AttendDev &a, const SchedShar
     const int s = threadIdx.x >> 7, t = threadIdx.x & 127;
     const uint32_t lanes = (uint32_t)(t & ~31) << 16;
     const uint32_t t_s = tmem + lanes + 128 * s, t_o = tmem + lanes + 256 + 128 * s;
-    const int64_t total = sched.total, ctas = min((int64_t)gridDim.x, total);
+    const int64_t line = sched.total, ctas = min((int64_t)gridDim.x, line);
 
     // rows of stage s in an item; this thread's row
     auto base_of = [&](const Cursor<Shape> &c) { return c.inner * 2 * kRows + s * kRows; };
@@ -471,7 +473,7 @@ __device__ __forceinline__ void softmax_role(const AttendDev &a, const SchedShar
         const Common all(a, cur.q, r0, min(r0 + kRows, rows) - 1);
         const Common item_sees(a, cur.q, r0 - s * kRows, min(r0 - s * kRows + 2 * kRows, rows) - 1);
         const int32_t t0 = cur.k.lo / KT + cur.off;
-        float m = -INFINITY, l = 0.f;
+        float m = live ? -INFINITY : 0.f, l = 0.f;
 
         for (int32_t i = 0; i < cur.len; ++i, ++k) {
             mbar_wait(b.s_full + 8 * s, s_turn++ & 1, dead, a.status);
@@ -480,9 +482,11 @@ __device__ __forceinline__ void softmax_role(const AttendDev &a, const SchedShar
             const bool edge = !all.covers(j0);
             uint32_t x[KT];
             uint64_t sum[2];
-            // The weights are computed from the m at hand while the maximum of these
-            // scores is still being found; if one exceeds m by too much (as in the
-            // first tile), m moves and they are computed once more.
+            float total;
+            // The weights are computed from the m at hand, without a look at the
+            // maximum: their sum shows whether m is still good (no weight is above
+            // it).  If not, as in the first tile with a key to see, the maximum is
+            // found, m moves and they are computed once more.
             for (bool sure = i == 0;;) {
 #pragma unroll
                 for (int c = 0; c < KT; c += 32) tc_ld32(x + c, t_s + c);
@@ -500,13 +504,12 @@ __device__ __forceinline__ void softmax_role(const AttendDev &a, const SchedShar
                             if (c < from) x[c] = 0xff800000u;
                     }
                 }
-                float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
                 if (sure) {
+                    float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
                     for (int c = 0; c < KT; c += 2)
                         top[(c >> 1) & 3] = max3(top[(c >> 1) & 3], __uint_as_float(x[c]), __uint_as_float(x[c + 1]));
-                    const float high = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.scale_log2;
-                    const float up = high > m + kSlack || i == 0 ? high : m;
+                    const float up = fmaxf(m, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.scale_log2);
                     if (i > 0) {
                         // every product on O that was issued before this S has ended with it
                         const float f = up == m ? 1.f : exp2_approx(m - up);
@@ -528,14 +531,14 @@ __device__ __forceinline__ void softmax_role(const AttendDev &a, const SchedShar
                 sum[0] = sum[1] = 0;
 #pragma unroll
                 for (int c = 0; c < KT; c += 2) {
-                    top[(c >> 1) & 3] = max3(top[(c >> 1) & 3], __uint_as_float(x[c]), __uint_as_float(x[c + 1]));
                     const float2 e = unpair(fma2(pair(__uint_as_float(x[c]), __uint_as_float(x[c + 1])), mul, sub));
                     const float p0 = exp2_approx(e.x), p1 = exp2_approx(e.y);
                     sum[(c >> 1) & 1] = add2(sum[(c >> 1) & 1], pair(p0, p1));
                     x[c / 2] = Pack<T>::two(p0, p1);
                 }
-                const float high = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.scale_log2;
-                if (sure || !__any_sync(~0u, high > m + kSlack)) break;
+                const float2 both = unpair(add2(sum[0], sum[1]));
+                total = both.x + both.y;
+                if (sure || !__any_sync(~0u, !(total <= kMaxSum) || m == -INFINITY)) break;
                 sure = true;
             }
             tc_st32(t_s, x);
@@ -546,8 +549,7 @@ __device__ __forceinline__ void softmax_role(const AttendDev &a, const SchedShar
                 clean_tile<T, HALVES>(reinterpret_cast<uint4 *>(q_smem + v_at<HALVES>(0, slot)), t, j0, cur.k.lo, cur.k.hi,
                                       bad + item % kBad, item + 1);
             }
-            const float2 both = unpair(add2(sum[0], sum[1]));
-            l += both.x + both.y;
+            l += total;
             tc_wait_st();
             tc_before();
             mbar_arrive(b.p_full + 8 * s);
@@ -591,7 +593,7 @@ __device__ __forceinline__ void softmax_role(const AttendDev &a, const SchedShar
         };
         const bool whole = cur.whole();
         const int64_t g0 = cur.g - cur.off;
-        const int32_t cta0 = owner(g0, total, ctas), pieces = owner(g0 + cur.tiles - 1, total, ctas) - cta0 + 1;
+        const int32_t cta0 = owner(g0, line, ctas), pieces = owner(g0 + cur.tiles - 1, line, ctas) - cta0 + 1;
         const int32_t mine = (int32_t)blockIdx.x - cta0;
         auto stat_at = [&](int32_t p) { return a.piece_stat + (piece_slot(cta0, p) * 2 + s) * 2 * kRows + t; };
         auto piece_at = [&](int32_t p, int c) {
