@@ -76,10 +76,14 @@ template <int KT> __device__ __forceinline__ int32_t key_tiles(Keys k) { return 
 
 // Shape: static constants KT (keys per tile) and, for a request, inner(a, q)
 // items for each of outer(a) (heads), keys(a, q, i) of inner item i.
+struct Place {
+    int32_t r, outer, inner, off;       // an item and a tile of it
+};
 struct SchedShared {
     int64_t warp_sum[32];
     int64_t total, begin;
-    int32_t r, outer, inner, off, count;
+    int32_t count, extra;
+    Place first, end;                   // where the stretch begins; the tile after it
 };
 
 __device__ __forceinline__ int64_t warp_sum64(int64_t x)
@@ -139,20 +143,25 @@ __device__ __forceinline__ int64_t block_scan(int64_t v, int64_t *excl, int64_t 
 // The CTA's stretch: false if it has none.  All threads of the CTA call it.
 template <class S> __device__ __forceinline__ bool schedule(const AttendDev &a, SchedShared &sm)
 {
+    static_assert(S::extra < 4, "every stretch has a tile");
     const int32_t R = a.c.requests, T = blockDim.x, outer = S::outer(a);
     const int lane = threadIdx.x & 31;
     const bool report = blockIdx.x == 0;
     if (report && threadIdx.x == 0 && a.c.q_start[0] != 0) kv_bounds(a.status);
     Req q;
-    int64_t mine, sum = 0, excl, before = 0;            // tiles of one head: this lane's request, all of this lane's
+    int64_t mine, tiles = 0, items = 0, excl, before = 0;      // of one head: this lane's request, all of this lane's
     for (int32_t base = 0; base < R; base += T) {
         const int32_t r = base + threadIdx.x;
         q = Req{0, 0, 0};
         if (r < R) q = load_req(a, r, report);
-        sum += mine = request_tiles<S>(a, q);
+        tiles += mine = request_tiles<S>(a, q);
+        items += S::inner(a, q);
     }
-    const int64_t total = block_scan(sum, &excl, sm.warp_sum) * outer;
-    if (total == 0) return false;
+    tiles = block_scan(tiles, &excl, sm.warp_sum) * outer;
+    if (tiles == 0) return false;
+    // with few tiles a CTA, every tile to a CTA of its own counts more than an even load
+    const int32_t extra = tiles >= 4 * (int64_t)gridDim.x ? S::extra : 0;
+    const int64_t total = tiles + (extra ? block_scan(items, &excl, sm.warp_sum) * outer * extra : 0);
     const int64_t ctas = min((int64_t)gridDim.x, total);
     if (blockIdx.x >= ctas) return false;
     const int64_t begin = total * blockIdx.x / ctas, end = total * (blockIdx.x + 1) / ctas;
@@ -162,82 +171,123 @@ template <class S> __device__ __forceinline__ bool schedule(const AttendDev &a, 
             q = Req{0, 0, 0};
             if (r < R) q = load_req(a, r, false);
             mine = request_tiles<S>(a, q);
-            const int64_t here = block_scan(mine, &excl, sm.warp_sum);
-            excl += before;
-            before += here;
         }
-        const bool hit = mine > 0 && excl * outer <= begin && begin < (excl + mine) * outer;
-        const uint32_t who = __ballot_sync(~0u, hit);
-        if (!who) continue;
-        // this warp has the request that the stretch begins in: its lanes look for the item
-        const int src = __ffs(who) - 1;
-        const Req x = shfl_req(q, src);
-        const int64_t per = __shfl_sync(~0u, mine, src), off = begin - __shfl_sync(~0u, excl, src) * outer;
-        const int32_t head = (int32_t)(off / per), items = S::inner(a, x);
-        int64_t rem = off - head * per;
-        for (int32_t i0 = 0; i0 < items; i0 += 32) {
-            const int64_t n = i0 + lane < items ? key_tiles<S::KT>(S::keys(a, x, i0 + lane)) : 0;
-            int64_t incl = n;
+        mine += (int64_t)S::inner(a, q) * extra;
+        const int64_t here = block_scan(mine, &excl, sm.warp_sum);
+        excl += before;
+        before += here;
+        // the warp that has the request of the stretch's first tile, or of the one after it, looks for the item
+#pragma unroll 1
+        for (int which = 0; which < 2; ++which) {
+            const int64_t tile = which ? end : begin;
+            const uint32_t who =
+                __ballot_sync(~0u, mine > 0 && excl * outer <= tile && tile < (excl + mine) * outer);
+            if (!who) continue;
+            const int src = __ffs(who) - 1;
+            const Req x = shfl_req(q, src);
+            const int64_t per = __shfl_sync(~0u, mine, src), off = tile - __shfl_sync(~0u, excl, src) * outer;
+            const int32_t head = (int32_t)(off / per), count = S::inner(a, x);
+            int64_t rem = off - head * per;
+            for (int32_t i0 = 0; i0 < count; i0 += 32) {
+                const int64_t n = i0 + lane < count ? key_tiles<S::KT>(S::keys(a, x, i0 + lane)) + extra : 0;
+                int64_t incl = n;
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int64_t y = __shfl_up_sync(~0u, incl, o);
-                if (lane >= o) incl += y;
-            }
-            const uint32_t past = __ballot_sync(~0u, rem < incl);
-            if (past) {
-                if (lane == __ffs(past) - 1) {
-                    sm.r = r - lane + src;
-                    sm.outer = head;
-                    sm.inner = i0 + lane;
-                    sm.off = (int32_t)(rem - (incl - n));
-                    sm.count = (int32_t)(end - begin);
-                    sm.begin = begin;
-                    sm.total = total;
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int64_t y = __shfl_up_sync(~0u, incl, o);
+                    if (lane >= o) incl += y;
                 }
-                break;
+                const uint32_t past = __ballot_sync(~0u, rem < incl);
+                if (past) {
+                    if (lane == __ffs(past) - 1)
+                        (which ? sm.end : sm.first) = Place{r - lane + src, head, i0 + lane, (int32_t)(rem - (incl - n))};
+                    break;
+                }
+                rem -= __shfl_sync(~0u, incl, 31);
             }
-            rem -= __shfl_sync(~0u, incl, 31);
         }
+    }
+    if (threadIdx.x == 0) {
+        if (end == total) sm.end = Place{0, 0, 0, 0};   // nothing goes on after the last tile
+        sm.count = (int32_t)(end - begin);
+        sm.extra = extra;
+        sm.begin = begin;
+        sm.total = total;
     }
     __syncthreads();
     return true;
 }
 
-// Walks the CTA's stretch item by item; every role of a CTA has its own.
+// Walks the CTA's stretch item by item; every role of a CTA has its own.  The
+// parts of items that other CTAs have the rest of come first, so that the joins
+// of their pieces run beside the whole items' tiles.
 template <class S> struct Cursor {
-    int32_t r, outer, inner, off, left;
-    int64_t g;                          // tile's number on the line
+    int32_t r, outer, inner, off;       // the item and the first tile of it
+    int32_t tiles, len;                 // of the item; of this CTA's part [off, off + len), 0: nothing in the stretch
+    int64_t g;                          // that tile's number on the line
     Req q;
     Keys k;
-    int32_t tiles, len;                 // of the item; of this CTA's part [off, off + len)
+    int32_t left, tail;                 // of the line: whole items to come, the part that ends the stretch
+    Place after;                        // the next whole item
+    int64_t after_g;
+    const SchedShared *sched;
 
-    __device__ __forceinline__ Cursor(const AttendDev &a, const SchedShared &sm)
-        : r(sm.r), outer(sm.outer), inner(sm.inner), off(sm.off), left(sm.count), g(sm.begin)
+    __device__ __forceinline__ Cursor(const AttendDev &a, const SchedShared &sm) : after(sm.first), after_g(sm.begin), sched(&sm)
     {
-        q = load_req(a, r, false);
-        item(a);
+        // the end's part, unless that is in the first item
+        tail = sm.end.off > 0 && sm.end.off < sm.count ? sm.end.off : 0;
+        left = sm.count - tail;
+        go(a, sm.first, sm.begin);
+        len = max(0, min(tiles - off, sm.count));
+        if (whole() && tail) {
+            to_tail(a);
+        } else {
+            taken(a, min(tiles + sm.extra - off, left));
+            if (len == 0) next(a);      // all of the first item was before the stretch
+        }
     }
-    __device__ __forceinline__ void item(const AttendDev &a)
+    __device__ __forceinline__ void go(const AttendDev &a, const Place &p, int64_t at)
     {
+        r = p.r;
+        outer = p.outer;
+        inner = p.inner;
+        off = p.off;
+        g = at;
+        q = load_req(a, r, false);
         k = S::keys(a, q, inner);
         tiles = key_tiles<S::KT>(k);
-        len = min(tiles - off, left);
+    }
+    __device__ __forceinline__ void to_tail(const AttendDev &a)
+    {
+        go(a, Place{sched->end.r, sched->end.outer, sched->end.inner, 0}, sched->begin + sched->count - tail);
+        len = min(tail, tiles);
+        tail = 0;
+    }
+    // `after` moves past the current item, to a request that may have none
+    __device__ __forceinline__ void taken(const AttendDev &a, int32_t of_line)
+    {
+        after_g += of_line;
+        left -= of_line;
+        after = Place{r, outer, inner + 1, 0};
+        if (after.inner >= S::inner(a, q)) {
+            after.inner = 0;
+            if (++after.outer >= S::outer(a)) {
+                after.outer = 0;
+                ++after.r;
+            }
+        }
     }
     __device__ __forceinline__ bool next(const AttendDev &a)
     {
-        left -= len;
-        g += len;
-        off = 0;
-        if (left <= 0) return false;
-        if (++inner >= S::inner(a, q)) {
-            inner = 0;
-            if (++outer >= S::outer(a)) {
-                outer = 0;
-                do q = load_req(a, ++r, false);
-                while (S::inner(a, q) == 0);
-            }
+        if (tail) {
+            to_tail(a);
+            return true;
         }
-        item(a);
+        if (left <= 0) return false;
+        if (after.inner == 0 && after.outer == 0)       // a new request: the next one with items
+            while (S::inner(a, load_req(a, after.r, false)) == 0) ++after.r;
+        go(a, after, after_g);
+        len = tiles;
+        taken(a, tiles + sched->extra);
         return true;
     }
     __device__ __forceinline__ bool whole() const { return off == 0 && len == tiles; }
@@ -310,6 +360,8 @@ __device__ __forceinline__ void copy16(uint32_t dst, const char *src, uint32_t b
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
 // A lane's share of copies of whole rows: `step` rows of 16-byte pieces at a time.
 template <int HALVES> struct RowLane {
     static constexpr int per_row = 8 * HALVES, step = 32 / per_row;

@@ -13,8 +13,8 @@
 // memory) hardly ever, and no tile waits for its maximum; weights are at most
 // 2^12 then, which both 16-bit types hold as precisely as 1.
 //
-// Warps: 0-3 and 4-7 the stages' softmax and epilogue, 8 and 9 their products, 10
-// and 11 the copies of K and V.  V tiles that not every row sees in full are looked
+// Warps: 0-3 and 4-7 the stages' softmax, 8-11 the outputs of both, 12 and 13 the
+// stages' products, 14 and 15 the copies of K and V.  V tiles that not every row sees in full are looked
 // over by the softmax warps: an infinity or a NaN there would pass through a
 // weight of 0, so it is replaced by 0 and added in the epilogue to the rows that
 // do see it.
@@ -28,7 +28,7 @@ namespace pp {
 namespace chunk {
 constexpr int KT = 128;                             // keys per tile
 constexpr int kRows = 128;                          // rows of a stage
-constexpr int kThreads = 384;
+constexpr int kThreads = 512;
 constexpr int kBad = 16;                            // marks of items, the stages are fewer apart
 constexpr float kMaxSum = 4096.f;                   // of the weights of a row and tile, before m moves
 
@@ -37,11 +37,12 @@ template <int HALVES> struct Layout {
     static constexpr int tile = half * HALVES;
     static constexpr int k_slots = HALVES == 2 ? 3 : 5, v_slots = HALVES == 2 ? 2 : 5;     // tiles in flight
     static constexpr int width = 64 * HALVES;
-    static constexpr int bytes = 1024 + (2 + k_slots + v_slots) * tile;
+    static constexpr int tiles = (2 + k_slots + v_slots) * tile;
 };
 
 struct Shape {
     static constexpr int KT = chunk::KT;
+    static constexpr int32_t extra = 2;
     static __device__ __forceinline__ int32_t outer(const AttendDev &a) { return a.kv_heads; }
     static __device__ __forceinline__ int32_t rows(const AttendDev &a, const Req &q) { return q.q_len * a.c.group; }
     static __device__ __forceinline__ int32_t inner(const AttendDev &a, const Req &q)
@@ -228,7 +229,7 @@ template <typename T> __device__ __forceinline__ bool not_finite(uint32_t bits)
 // The roles
 // ---------------------------------------------------------------------------
 struct Bars {
-    uint32_t k_full, k_empty, v_full, v_empty, q_full, s_full, p_full, o_done, o_free, fin, pass;     // shared addresses
+    uint32_t k_full, k_empty, v_full, v_empty, q_full, s_full, p_full, o_done, o_free, fin, pass, stat_full, stat_free;     // shared addresses
 };
 
 // Shared memory: the stages' queries, K tiles, V tiles.
@@ -361,8 +362,7 @@ __device__ __forceinline__ void mma_role(const AttendDev &a, const SchedShared &
                 ++pass;
             }
             const uint64_t v_op = smem_operand(v_at<HALVES>(base, vs), L::half, 1024);
-            mbar_wait(b.p_full + 8 * s, p_turn & 1, dead, a.status);
-            ++p_turn;
+            mbar_wait(b.p_full + 8 * s, p_turn++ & 1, dead, a.status);
             tc_after();
             if (elected()) {
 #pragma unroll
@@ -392,14 +392,15 @@ __device__ __forceinline__ void clean_tile(uint4 *v, int t, int32_t j0, int32_t 
 {
     using L = Layout<HALVES>;
     uint32_t any = 0;
-#pragma unroll 4
+#pragma unroll 8
     for (int x = t; x < L::tile / 16; x += kRows) {
         const uint4 y = v[x];
         any = taint<T>(y.x, taint<T>(y.y, taint<T>(y.z, taint<T>(y.w, any))));
     }
     if ((any & 0x7fff7fffu) != 0) {
+#pragma unroll 1
         for (int x = t; x < L::tile / 16; x += kRows) {
-            uint4 y = v[x];
+            const uint4 y = v[x];
             uint32_t e[4] = {y.x, y.y, y.z, y.w};
             bool hit = false;
 #pragma unroll
@@ -417,99 +418,122 @@ __device__ __forceinline__ void clean_tile(uint4 *v, int t, int32_t j0, int32_t 
     to_tensor_cores();
 }
 
-// One stage: queries to shared memory, softmax of its S, its output.
+// The stages' rows of an item.
+__device__ __forceinline__ int32_t stage_row(const Cursor<Shape> &c, int s) { return c.inner * 2 * kRows + s * kRows; }
+
+// What the roles share beside the tiles; a stage's softmax hands its rows' m and l
+// to the output.
+template <int HALVES> struct Shared {
+    SchedShared sched;
+    float m[2][kRows], l[2][kRows];
+    uint64_t bar[2 * (Layout<HALVES>::k_slots + Layout<HALVES>::v_slots) + 18];
+    int32_t dead, last, bad[kBad];
+    uint32_t tmem;
+};
+
+// One stage: queries to shared memory, softmax of its S.
 template <typename T, int HALVES>
-__device__ __forceinline__ void softmax_role(const AttendDev &a, const SchedShared &sched, uint8_t *q_smem, uint32_t tmem,
-                                             const Bars &b, volatile int32_t *bad, volatile int32_t *dead,
-                                             volatile int32_t *last)
+__device__ __forceinline__ void softmax_role(const AttendDev &a, const SchedShared &sched, int s, uint8_t *mem, uint32_t base,
+                                             uint32_t tmem, const Bars &b, volatile float *m_out, volatile float *l_out,
+                                             volatile int32_t *bad, volatile int32_t *dead)
 {
     using L = Layout<HALVES>;
-    const int s = threadIdx.x >> 7, t = threadIdx.x & 127;
-    const uint32_t lanes = (uint32_t)(t & ~31) << 16;
-    const uint32_t t_s = tmem + lanes + 128 * s, t_o = tmem + lanes + 256 + 128 * s;
-    const int64_t line = sched.total, ctas = min((int64_t)gridDim.x, line);
+    const int t = threadIdx.x & 127;
+    const uint32_t t_s = tmem + ((uint32_t)(t & ~31) << 16) + 128 * s, t_o = t_s + 256;
 
-    // rows of stage s in an item; this thread's row
-    auto base_of = [&](const Cursor<Shape> &c) { return c.inner * 2 * kRows + s * kRows; };
-    auto load_q = [&](const Cursor<Shape> &c) {
-        const int32_t r0 = base_of(c), rows = Shape::rows(a, c.q);
-        constexpr int per = 8 * HALVES;                 // 16-byte pieces of a row
-        uint4 y[per];
-#pragma unroll
-        for (int i = 0; i < per; ++i) {
-            const int x = i * kRows + t, row = r0 + x / per, d = x % per * 8;
-            const int32_t tok = div_group(a, row), g = row - tok * a.c.group;
-            y[i] = row < rows && d < a.dim
-                       ? __ldg(reinterpret_cast<const uint4 *>(
-                             static_cast<const T *>(a.c.q) + (int64_t)(c.q.first + tok) * a.c.q_token_stride +
-                             (int64_t)(c.outer * a.c.group + g) * a.c.q_head_stride + d))
-                       : make_uint4(0, 0, 0, 0);
+    // asks for the stage's queries, a fixed 16-byte piece of every 16th or 8th row a thread
+    auto ask_q = [&](const Cursor<Shape> &c) {
+        constexpr int per = 8 * HALVES, step = kRows / per;
+        const int piece = t % per, first = t / per;
+        const int32_t rows = Shape::rows(a, c.q), r0 = stage_row(c, s);
+        const bool in = piece * 8 < a.dim;
+        const char *q = reinterpret_cast<const char *>(static_cast<const T *>(a.c.q) + (int64_t)c.q.first * a.c.q_token_stride +
+                                                       (int64_t)c.outer * a.c.group * a.c.q_head_stride + (in ? piece * 8 : 0));
+        const uint32_t dst = base + s * L::tile + (piece >> 3) * L::half + first * 128;
+#pragma unroll 4
+        for (int i = 0; i < kRows / step; ++i) {
+            const int32_t row = min(r0 + first + i * step, rows - 1), tok = div_group(a, row), g = row - tok * a.c.group;
+            copy16(dst + i * step * 128 + (((piece ^ (first + i * step)) & 7) << 4),
+                   q + 2 * (tok * a.c.q_token_stride + g * a.c.q_head_stride), in && r0 + first + i * step < rows ? 16 : 0);
         }
-#pragma unroll
-        for (int i = 0; i < per; ++i) {
-            const int x = i * kRows + t, row = x / per, piece = x % per;
-            *reinterpret_cast<uint4 *>(q_smem + s * L::tile + (piece >> 3) * L::half + row * 128 +
-                                       (((piece ^ row) & 7) << 4)) = y[i];
-        }
+    };
+    auto have_q = [&]() {
+        copies_wait();
         to_tensor_cores();
         mbar_arrive(b.q_full + 8 * s);
     };
 
     Cursor<Shape> cur(a, sched);
-    uint32_t s_turn = 0, o_turn = 0, k = 0;             // k: tile of the stretch
+    uint32_t s_turn = 0, k = 0, given = 0;              // k: tile of the stretch
     int32_t item = 0;
-    bool loaded = false;
+    bool asked = false;
     for (bool go = true; go; ++item) {
-        const int32_t rows = Shape::rows(a, cur.q), r0 = base_of(cur), row = r0 + t;
+        const int32_t rows = Shape::rows(a, cur.q), r0 = stage_row(cur, s), row = r0 + t;
         if (r0 >= rows) {                               // this item has one stage only
             k += cur.len;
             go = cur.next(a);
             continue;
         }
-        if (!loaded) load_q(cur);
-        loaded = false;
+        if (!asked) {
+            ask_q(cur);
+            have_q();
+        }
+        asked = false;
         const bool live = row < rows;
         const int32_t pos = live ? Shape::pos(a, cur.q, row) : -1, lo = pos < 0 ? 0 : first_key(a, pos);
         const Common all(a, cur.q, r0, min(r0 + kRows, rows) - 1);
         const Common item_sees(a, cur.q, r0 - s * kRows, min(r0 - s * kRows + 2 * kRows, rows) - 1);
-        const int32_t t0 = cur.k.lo / KT + cur.off;
+        const int32_t t0 = cur.k.lo / KT + cur.off, len = cur.len;
+        const Keys keys = cur.k;
         float m = live ? -INFINITY : 0.f, l = 0.f;
 
-        for (int32_t i = 0; i < cur.len; ++i, ++k) {
+        for (int32_t i = 0; i < len; ++i, ++k) {
             mbar_wait(b.s_full + 8 * s, s_turn++ & 1, dead, a.status);
             tc_after();
+            if (i == len - 1) {
+                // the last S is there, so the queries' place is free: the next item's are asked for
+                go = cur.next(a);
+                asked = go && stage_row(cur, s) < Shape::rows(a, cur.q);
+                if (asked) ask_q(cur);
+            }
             const int32_t j0 = (t0 + i) * KT;
-            const bool edge = !all.covers(j0);
-            uint32_t x[KT];
-            uint64_t sum[2];
+            const bool late = j0 + KT - 1 > all.hi, early = j0 < all.lo;
+            const int32_t from = lo - j0, to = pos - j0;
+            // 64 columns of S; keys that the row does not see are -infinity
+            auto load = [&](uint32_t (&x)[64], int h) {
+                tc_ld32(x, t_s + 64 * h);
+                tc_ld32(x + 32, t_s + 64 * h + 32);
+                tc_wait_ld();
+                if (late) {
+#pragma unroll
+                    for (int c = 0; c < 64; ++c)
+                        if (c > to - 64 * h) x[c] = 0xff800000u;
+                }
+                if (early) {
+#pragma unroll
+                    for (int c = 0; c < 64; ++c)
+                        if (c < from - 64 * h) x[c] = 0xff800000u;
+                }
+            };
+            uint32_t p[64];
             float total;
             // The weights are computed from the m at hand, without a look at the
             // maximum: their sum shows whether m is still good (no weight is above
             // it).  If not, as in the first tile with a key to see, the maximum is
             // found, m moves and they are computed once more.
             for (bool sure = i == 0;;) {
-#pragma unroll
-                for (int c = 0; c < KT; c += 32) tc_ld32(x + c, t_s + c);
-                tc_wait_ld();
-                if (edge) {
-                    const int32_t from = lo - j0, to = pos - j0;
-                    if (j0 + KT - 1 > all.hi) {
-#pragma unroll
-                        for (int c = 0; c < KT; ++c)
-                            if (c > to) x[c] = 0xff800000u;
-                    }
-                    if (j0 < all.lo) {
-#pragma unroll
-                        for (int c = 0; c < KT; ++c)
-                            if (c < from) x[c] = 0xff800000u;
-                    }
-                }
                 if (sure) {
-                    float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    float up = m;
+#pragma unroll 1
+                    for (int h = 0; h < 2; ++h) {
+                        uint32_t x[64];
+                        load(x, h);
+                        float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                    for (int c = 0; c < KT; c += 2)
-                        top[(c >> 1) & 3] = max3(top[(c >> 1) & 3], __uint_as_float(x[c]), __uint_as_float(x[c + 1]));
-                    const float up = fmaxf(m, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.scale_log2);
+                        for (int c = 0; c < 64; c += 2)
+                            top[(c >> 1) & 3] = max3(top[(c >> 1) & 3], __uint_as_float(x[c]), __uint_as_float(x[c + 1]));
+                        up = fmaxf(up, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.scale_log2);
+                    }
                     if (i > 0) {
                         // every product on O that was issued before this S has ended with it
                         const float f = up == m ? 1.f : exp2_approx(m - up);
@@ -526,27 +550,32 @@ __device__ __forceinline__ void softmax_role(const AttendDev &a, const SchedShar
                     }
                     m = up;
                 }
-                const float base = m == -INFINITY ? 0.f : m;
-                const uint64_t mul = pair(a.scale_log2, a.scale_log2), sub = pair(-base, -base);
-                sum[0] = sum[1] = 0;
+                const float at = m == -INFINITY ? 0.f : m;
+                const uint64_t mul = pair(a.scale_log2, a.scale_log2), sub = pair(-at, -at);
+                uint64_t sum[2] = {0, 0};
 #pragma unroll
-                for (int c = 0; c < KT; c += 2) {
-                    const float2 e = unpair(fma2(pair(__uint_as_float(x[c]), __uint_as_float(x[c + 1])), mul, sub));
-                    const float p0 = exp2_approx(e.x), p1 = exp2_approx(e.y);
-                    sum[(c >> 1) & 1] = add2(sum[(c >> 1) & 1], pair(p0, p1));
-                    x[c / 2] = Pack<T>::two(p0, p1);
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t x[64];
+                    load(x, h);
+#pragma unroll
+                    for (int c = 0; c < 64; c += 2) {
+                        const float2 e = unpair(fma2(pair(__uint_as_float(x[c]), __uint_as_float(x[c + 1])), mul, sub));
+                        const float p0 = exp2_approx(e.x), p1 = exp2_approx(e.y);
+                        sum[(c >> 1) & 1] = add2(sum[(c >> 1) & 1], pair(p0, p1));
+                        p[32 * h + c / 2] = Pack<T>::two(p0, p1);
+                    }
                 }
                 const float2 both = unpair(add2(sum[0], sum[1]));
                 total = both.x + both.y;
                 if (sure || !__any_sync(~0u, !(total <= kMaxSum) || m == -INFINITY)) break;
                 sure = true;
             }
-            tc_st32(t_s, x);
-            tc_st32(t_s + 32, x + 32);
+            tc_st32(t_s, p);
+            tc_st32(t_s + 32, p + 32);
             if (!item_sees.covers(j0)) {
                 const uint32_t slot = k % L::v_slots;
                 mbar_wait(b.v_full + 8 * slot, (k / L::v_slots) & 1, dead, a.status);
-                clean_tile<T, HALVES>(reinterpret_cast<uint4 *>(q_smem + v_at<HALVES>(0, slot)), t, j0, cur.k.lo, cur.k.hi,
+                clean_tile<T, HALVES>(reinterpret_cast<uint4 *>(mem + v_at<HALVES>(0, slot)), t, j0, keys.lo, keys.hi,
                                       bad + item % kBad, item + 1);
             }
             l += total;
@@ -554,121 +583,157 @@ __device__ __forceinline__ void softmax_role(const AttendDev &a, const SchedShar
             tc_before();
             mbar_arrive(b.p_full + 8 * s);
         }
-        // the next item's queries before this one's output: its first product can start
-        Cursor<Shape> nxt = cur;
-        go = nxt.next(a);
-        if (go && base_of(nxt) < Shape::rows(a, nxt.q)) {
-            load_q(nxt);
-            loaded = true;
-        }
+        if (asked) have_q();
+        if (given) mbar_wait(b.stat_free + 8 * s, (given - 1) & 1, dead, a.status);
+        ++given;
+        m_out[t] = m;
+        l_out[t] = l;
+        mbar_arrive(b.stat_full + 8 * s);
+    }
+}
 
-        mbar_wait(b.o_done + 8 * s, o_turn++ & 1, dead, a.status);
-        tc_after();
-        const int32_t tok = cur.q.first + div_group(a, row), head = cur.outer * a.c.group + row - div_group(a, row) * a.c.group;
-        auto put_out = [&](const float *o, int c, float inv) {
-            T *dst = static_cast<T *>(a.c.out) + (int64_t)tok * a.c.out_token_stride + (int64_t)head * a.c.out_head_stride + c;
-            uint32_t w[16];
-#pragma unroll
-            for (int y = 0; y < 16; ++y) w[y] = Pack<T>::two(o[2 * y] * inv, o[2 * y + 1] * inv);
-            if (!live) return;
-            if (a.wide_out) {                           // whole sectors
-#pragma unroll
-                for (int y = 0; y < 16; y += 8)
-                    if (c + 2 * y < a.dim)
-                        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst + 2 * y), "r"(w[y]),
-                                     "r"(w[y + 1]), "r"(w[y + 2]), "r"(w[y + 3]), "r"(w[y + 4]), "r"(w[y + 5]),
-                                     "r"(w[y + 6]), "r"(w[y + 7])
-                                     : "memory");
-            } else {
-#pragma unroll
-                for (int y = 0; y < 16; y += 4)
-                    if (c + 2 * y < a.dim)
-                        *reinterpret_cast<uint4 *>(dst + 2 * y) = make_uint4(w[y], w[y + 1], w[y + 2], w[y + 3]);
-            }
-        };
-        auto put_lse = [&](float top, float sum) {
-            if (live && a.c.lse)
-                a.c.lse[(int64_t)tok * a.c.q_heads + head] =
-                    sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
-        };
+// Outputs, and the join of items in pieces, of both stages in turn, while the
+// other warps are at the next item.
+template <typename T, int HALVES>
+__device__ __forceinline__ void output_role(const AttendDev &a, const SchedShared &sched, uint32_t tmem, const Bars &b,
+                                            const volatile float *m_in, const volatile float *l_in,
+                                            volatile int32_t *bad, volatile int32_t *dead, volatile int32_t *last)
+{
+    using L = Layout<HALVES>;
+    const int t = threadIdx.x & 127;
+    const int64_t line = sched.total, ctas = min((int64_t)gridDim.x, line);
+    Cursor<Shape> cur(a, sched);
+    uint32_t turn[2] = {0, 0};
+    int32_t item = 0;
+    do {
+        const int32_t rows = Shape::rows(a, cur.q), t0 = cur.k.lo / KT + cur.off;
         const bool whole = cur.whole();
         const int64_t g0 = cur.g - cur.off;
-        const int32_t cta0 = owner(g0, line, ctas), pieces = owner(g0 + cur.tiles - 1, line, ctas) - cta0 + 1;
+        const int32_t cta0 = owner(g0, line, ctas), pieces = whole ? 1 : owner(g0 + cur.tiles - 1, line, ctas) - cta0 + 1;
         const int32_t mine = (int32_t)blockIdx.x - cta0;
-        auto stat_at = [&](int32_t p) { return a.piece_stat + (piece_slot(cta0, p) * 2 + s) * 2 * kRows + t; };
-        auto piece_at = [&](int32_t p, int c) {
-            return reinterpret_cast<float4 *>(a.piece) + ((int64_t)(piece_slot(cta0, p) * 2 + s) * (L::width / 4) + c / 4) * kRows + t;
-        };
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        const bool fix = bad[item % kBad] == item + 1;
 #pragma unroll 1
-        for (int c = 0; c < L::width; c += 32) {
-            uint32_t x[32];
-            float o[32];
-            tc_ld32(x, t_o + c);
-            tc_wait_ld();
+        for (int s = 0; s < 2; ++s) {
+            const int32_t row = stage_row(cur, s) + t;
+            if (row - t >= rows) break;
+            const bool live = row < rows;
+            const int32_t pos = live ? Shape::pos(a, cur.q, row) : -1, lo = pos < 0 ? 0 : first_key(a, pos);
+            const int32_t in = div_group(a, row);
+            const int32_t tok = cur.q.first + in, head = cur.outer * a.c.group + row - in * a.c.group;
+            T *const out = static_cast<T *>(a.c.out) + (int64_t)tok * a.c.out_token_stride + (int64_t)head * a.c.out_head_stride;
+            const uint32_t t_o = tmem + ((uint32_t)(t & ~31) << 16) + 256 + 128 * s;
+
+            const uint32_t now = s ? turn[1]++ & 1 : turn[0]++ & 1;
+            mbar_wait(b.stat_full + 8 * s, now, dead, a.status);
+            const float m = m_in[kRows * s + t], l = l_in[kRows * s + t];
+            mbar_arrive(b.stat_free + 8 * s);
+            mbar_wait(b.o_done + 8 * s, now, dead, a.status);
+            tc_after();
+
+            // 16 columns of a row
+            auto put_out = [&](const float (&o)[16], int c, float inv) {
+                uint32_t w[8];
 #pragma unroll
-            for (int y = 0; y < 32; ++y) o[y] = __uint_as_float(x[y]);
-            if (fix) {
-                for (int32_t j = max(lo, t0 * KT); j <= min(pos, (t0 + cur.len) * KT - 1); ++j) {
-                    if (item_sees.covers(j / KT * KT)) continue;
-                    const int32_t id = a.c.block_table[(int64_t)cur.r * a.c.table_width + (j >> a.block_log)];
-                    if (id < 0 || id >= a.blocks) continue;
-                    const T *v = static_cast<const T *>(a.c.v_cache) + id * a.block_stride +
-                                 (j & ((1 << a.block_log) - 1)) * a.token_stride + cur.outer * a.head_stride + c;
+                for (int y = 0; y < 8; ++y) w[y] = Pack<T>::two(o[2 * y] * inv, o[2 * y + 1] * inv);
+                if (!live) return;
+                T *dst = out + c;
+                if (a.wide_out) {                       // whole sectors
+                    if (c < a.dim)
+                        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst), "r"(w[0]),
+                                     "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                                     : "memory");
+                } else {
 #pragma unroll
-                    for (int y = 0; y < 32; ++y)
-                        if (c + y < a.dim) {
-                            const float z = KvType<T>::to_float(v[y]);
-                            if (!(fabsf(z) < INFINITY)) o[y] += z;
+                    for (int y = 0; y < 8; y += 4)
+                        if (c + 2 * y < a.dim)
+                            *reinterpret_cast<uint4 *>(dst + 2 * y) = make_uint4(w[y], w[y + 1], w[y + 2], w[y + 3]);
+                }
+            };
+            auto put_lse = [&](float top, float sum) {
+                if (live && a.c.lse)
+                    a.c.lse[(int64_t)tok * a.c.q_heads + head] =
+                        sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+            };
+            auto stat_at = [&](int32_t p) { return a.piece_stat + (piece_slot(cta0, p) * 2 + s) * 2 * kRows + t; };
+            auto piece_at = [&](int32_t p, int c) {
+                return reinterpret_cast<float4 *>(a.piece) +
+                       ((int64_t)(piece_slot(cta0, p) * 2 + s) * (L::width / 4) + c / 4) * kRows + t;
+            };
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            const bool fix = bad[item % kBad] == item + 1;
+#pragma unroll 1
+            for (int c = 0; c < L::width; c += 32) {
+                uint32_t x[32];
+                tc_ld32(x, t_o + c);
+                tc_wait_ld();
+#pragma unroll
+                for (int n = 0; n < 32; n += 16) {
+                    float o[16];
+#pragma unroll
+                    for (int y = 0; y < 16; ++y) o[y] = __uint_as_float(x[n + y]);
+                    if (fix) {
+                        const int32_t r0 = stage_row(cur, 0);
+                        const Common item_sees(a, cur.q, r0, min(r0 + 2 * kRows, rows) - 1);
+                        for (int32_t j = max(lo, t0 * KT); j <= min(pos, (t0 + cur.len) * KT - 1); ++j) {
+                            if (item_sees.covers(j / KT * KT)) continue;
+                            const int32_t id = a.c.block_table[(int64_t)cur.r * a.c.table_width + (j >> a.block_log)];
+                            if (id < 0 || id >= a.blocks) continue;
+                            const T *v = static_cast<const T *>(a.c.v_cache) + id * a.block_stride +
+                                         (j & ((1 << a.block_log) - 1)) * a.token_stride + cur.outer * a.head_stride + c + n;
+#pragma unroll
+                            for (int y = 0; y < 16; ++y)
+                                if (c + n + y < a.dim) {
+                                    const float z = KvType<T>::to_float(v[y]);
+                                    if (!(fabsf(z) < INFINITY)) o[y] += z;
+                                }
                         }
+                    }
+                    if (whole) {
+                        put_out(o, c + n, inv);
+                    } else {
+#pragma unroll
+                        for (int y = 0; y < 16; y += 4)
+                            piece_at(mine, c + n)[y / 4 * kRows] = make_float4(o[y], o[y + 1], o[y + 2], o[y + 3]);
+                    }
                 }
             }
+            tc_before();
+            mbar_arrive(b.o_free + 8 * s);
             if (whole) {
-                put_out(o, c, inv);
-            } else {
-#pragma unroll
-                for (int y = 0; y < 32; y += 4)
-                    piece_at(mine, c)[y / 4 * kRows] = make_float4(o[y], o[y + 1], o[y + 2], o[y + 3]);
+                put_lse(m, l);
+                continue;
             }
-        }
-        tc_before();
-        mbar_arrive(b.o_free + 8 * s);
-        if (whole) {
-            put_lse(m, l);
-        } else {
             stat_at(mine)[0] = m;
             stat_at(mine)[kRows] = l;
             auto arrive = [&](int32_t *count, int32_t of) {
                 __threadfence();
-                named_sync(1 + s, kRows);
+                named_sync(1, kRows);
                 if (t == 0) {
-                    last[s] = atomicAdd(count, 1) == of - 1;
-                    if (last[s]) *count = 0;
+                    *last = atomicAdd(count, 1) == of - 1;
+                    if (*last) *count = 0;
                 }
-                named_sync(1 + s, kRows);
+                named_sync(1, kRows);
                 __threadfence();
-                return last[s] != 0;
+                return *last != 0;
             };
-            // join n pieces p0, p0 + step, ... into the output (out) or into p0
-            auto gather = [&](int32_t p0, int32_t n, int32_t step, bool out) {
+            // join n pieces p0, p0 + step, ... into the output (final) or into p0
+            auto gather = [&](int32_t p0, int32_t n, int32_t step, bool final) {
                 float top = -INFINITY, sum = 0.f;
                 for (int32_t p = 0; p < n; ++p) top = fmaxf(top, __ldcg(stat_at(p0 + p * step)));
-                const float base = top == -INFINITY ? 0.f : top;
+                const float at = top == -INFINITY ? 0.f : top;
                 for (int32_t p = 0; p < n; ++p)
-                    sum = fmaf(exp2_approx(__ldcg(stat_at(p0 + p * step)) - base), __ldcg(stat_at(p0 + p * step) + kRows), sum);
+                    sum = fmaf(exp2_approx(__ldcg(stat_at(p0 + p * step)) - at), __ldcg(stat_at(p0 + p * step) + kRows), sum);
                 const float scale = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll 1
-                for (int c = 0; c < L::width; c += 32) {
-                    float o[32];
+                for (int c = 0; c < L::width; c += 16) {
+                    float o[16];
 #pragma unroll
-                    for (int y = 0; y < 32; ++y) o[y] = 0.f;
+                    for (int y = 0; y < 16; ++y) o[y] = 0.f;
 #pragma unroll 2
                     for (int32_t p = 0; p < n; ++p) {
-                        const float f = exp2_approx(__ldcg(stat_at(p0 + p * step)) - base);
+                        const float f = exp2_approx(__ldcg(stat_at(p0 + p * step)) - at);
                         const float4 *src = piece_at(p0 + p * step, c);
 #pragma unroll
-                        for (int y = 0; y < 32; y += 4) {
+                        for (int y = 0; y < 16; y += 4) {
                             const float4 z = __ldcg(src + y / 4 * kRows);
                             o[y] = fmaf(f, z.x, o[y]);
                             o[y + 1] = fmaf(f, z.y, o[y + 1]);
@@ -676,15 +741,15 @@ __device__ __forceinline__ void softmax_role(const AttendDev &a, const SchedShar
                             o[y + 3] = fmaf(f, z.w, o[y + 3]);
                         }
                     }
-                    if (out) {
+                    if (final) {
                         put_out(o, c, scale);
                     } else {
 #pragma unroll
-                        for (int y = 0; y < 32; y += 4)
+                        for (int y = 0; y < 16; y += 4)
                             piece_at(p0, c)[y / 4 * kRows] = make_float4(o[y], o[y + 1], o[y + 2], o[y + 3]);
                     }
                 }
-                if (out) {
+                if (final) {
                     put_lse(top, sum);
                 } else {
                     stat_at(p0)[0] = top;
@@ -699,8 +764,8 @@ __device__ __forceinline__ void softmax_role(const AttendDev &a, const SchedShar
                     gather(0, groups, kJoinGroup, true);
             }
         }
-        cur = nxt;
-    }
+        ++item;
+    } while (cur.next(a));
 }
 
 template <typename T, int HALVES>
@@ -709,16 +774,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
                                                               const __grid_constant__ CUtensorMap vm)
 {
     using L = Layout<HALVES>;
-    extern __shared__ uint8_t raw[];
-    __shared__ SchedShared sched;
-    __shared__ alignas(8) uint64_t bar[2 * (L::k_slots + L::v_slots) + 14];
-    __shared__ int32_t dead, last[2], bad[kBad];
-    __shared__ uint32_t tmem_at;
+    extern __shared__ __align__(1024) uint8_t raw[];
+    Shared<HALVES> &sh = *reinterpret_cast<Shared<HALVES> *>(raw + L::tiles);
     const int tid = threadIdx.x, warp = tid >> 5;
-    const uint32_t base = (smem_u32(raw) + 1023) & ~1023u;
-    uint8_t *mem = raw + (base - smem_u32(raw));
+    const uint32_t base = smem_u32(raw);
+    if (base & 1023) {                                  // the swizzle counts from multiples of 1,024 bytes
+        if (tid == 0) atomicExch(a.status, (int32_t)PP_ECUDA);
+        return;
+    }
     Bars b;
-    b.k_full = smem_u32(bar);
+    b.k_full = smem_u32(sh.bar);
     b.k_empty = b.k_full + 8 * L::k_slots;
     b.v_full = b.k_empty + 8 * L::k_slots;
     b.v_empty = b.v_full + 8 * L::v_slots;
@@ -729,8 +794,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
     b.o_free = b.o_done + 16;
     b.fin = b.o_free + 16;
     b.pass = b.fin + 16;
+    b.stat_full = b.pass + 16;
+    b.stat_free = b.stat_full + 16;
     if (tid == 0) {
-        dead = 0;
+        sh.dead = 0;
         for (int i = 0; i < L::k_slots; ++i) {
             mbar_init(b.k_full + 8 * i, 1);
             mbar_init(b.k_empty + 8 * i, 2);
@@ -747,32 +814,37 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
             mbar_init(b.o_free + 8 * s, kRows);
             mbar_init(b.fin + 8 * s, 1);
             mbar_init(b.pass + 8 * s, 1);
+            mbar_init(b.stat_full + 8 * s, kRows);
+            mbar_init(b.stat_free + 8 * s, kRows);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (tid < kBad) bad[tid] = 0;
-    if (!schedule<Shape>(a, sched)) return;
-    if (warp == 8) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_at)) : "memory");
+    if (tid < kBad) sh.bad[tid] = 0;
+    if (!schedule<Shape>(a, sh.sched)) return;
+    if (warp == 12) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&sh.tmem)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
         tc_before();
     }
     __syncthreads();
     tc_after();
-    const uint32_t tmem = tmem_at;
+    const uint32_t tmem = sh.tmem;
 
-    // 384 threads x 168 registers = 256 x 208 + 128 x 88
+    // 512 threads x 128 registers = 256 x 136 + 128 x 144 + 128 x 96
     if (warp < 8) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
-        softmax_role<T, HALVES>(a, sched, mem, tmem, b, bad, &dead, last);
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 136;");
+        softmax_role<T, HALVES>(a, sh.sched, warp >> 2, raw, base, tmem, b, sh.m[warp >> 2], sh.l[warp >> 2], sh.bad, &sh.dead);
+    } else if (warp < 12) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 144;");
+        output_role<T, HALVES>(a, sh.sched, tmem, b, sh.m[0], sh.l[0], sh.bad, &sh.dead, &sh.last);
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-        if (warp < 10) mma_role<T, HALVES>(a, sched, warp - 8, base, tmem, b, &dead);
-        else copy_role<HALVES>(a, sched, warp - 10, warp == 10 ? &km : &vm, base, b, &dead);
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+        if (warp < 14) mma_role<T, HALVES>(a, sh.sched, warp - 12, base, tmem, b, &sh.dead);
+        else copy_role<HALVES>(a, sh.sched, warp - 14, warp == 14 ? &km : &vm, base, b, &sh.dead);
     }
     tc_before();
     __syncthreads();
-    if (warp == 8) {
+    if (warp == 12) {
         tc_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
     }
@@ -787,9 +859,10 @@ static pp_status launch_t(pp_kv *kv, const AttendArgs &c, cudaStream_t st)
     pp_status s = cache_map(kv, c.k_cache, rows, &km);
     if (s == PP_OK) s = cache_map(kv, c.v_cache, rows, &vm);
     if (s != PP_OK) return s;
-    PP_CUDA(cudaFuncSetAttribute(k_attend_chunk<T, HALVES>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 Layout<HALVES>::bytes));
-    k_attend_chunk<T, HALVES><<<kv->sm_count, kThreads, Layout<HALVES>::bytes, st>>>(a, km, vm);
+    constexpr int bytes = Layout<HALVES>::tiles + sizeof(Shared<HALVES>);
+    static_assert(bytes <= 232448, "shared memory of a CTA");
+    PP_CUDA(cudaFuncSetAttribute(k_attend_chunk<T, HALVES>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+    k_attend_chunk<T, HALVES><<<kv->sm_count, kThreads, bytes, st>>>(a, km, vm);
     PP_CUDA(cudaGetLastError());
     return PP_OK;
 }

@@ -34,6 +34,7 @@ template <int HALVES> struct Layout {
 
 struct Shape {
     static constexpr int KT = token::KT;
+    static constexpr int32_t extra = 1;
     static __device__ __forceinline__ int32_t row_tiles(const AttendDev &a) { return (a.c.group + kRows - 1) / kRows; }
     static __device__ __forceinline__ int32_t outer(const AttendDev &a) { return a.kv_heads * row_tiles(a); }
     static __device__ __forceinline__ int32_t inner(const AttendDev &, const Req &q) { return q.q_len; }
