@@ -19,6 +19,7 @@
 // weight of 0, so it is replaced by 0 and added in the epilogue to the rows that
 // do see it.
 #include <algorithm>
+#include <new>
 #include <type_traits>
 
 #include "pp_attend.cuh"
@@ -427,15 +428,17 @@ template <int HALVES> struct Shared {
     SchedShared sched;
     float m[2][kRows], l[2][kRows];
     uint64_t bar[2 * (Layout<HALVES>::k_slots + Layout<HALVES>::v_slots) + 18];
-    int32_t dead, last, bad[kBad];
+    int32_t dead, last, more[2], bad[kBad];
     uint32_t tmem;
+    alignas(8) uint8_t walk[2][sizeof(Cursor<Shape>)];  // the softmax's, kept out of its registers
 };
 
 // One stage: queries to shared memory, softmax of its S.
 template <typename T, int HALVES>
 __device__ __forceinline__ void softmax_role(const AttendDev &a, const SchedShared &sched, int s, uint8_t *mem, uint32_t base,
                                              uint32_t tmem, const Bars &b, volatile float *m_out, volatile float *l_out,
-                                             volatile int32_t *bad, volatile int32_t *dead)
+                                             volatile int32_t *bad, volatile int32_t *dead, Cursor<Shape> *walk,
+                                             volatile int32_t *more)
 {
     using L = Layout<HALVES>;
     const int t = threadIdx.x & 127;
@@ -463,7 +466,16 @@ __device__ __forceinline__ void softmax_role(const AttendDev &a, const SchedShar
         mbar_arrive(b.q_full + 8 * s);
     };
 
-    Cursor<Shape> cur(a, sched);
+    // one thread walks, all read
+    Cursor<Shape> &cur = *walk;
+    if (t == 0) new (walk) Cursor<Shape>(a, sched);
+    named_sync(2 + s, kRows);
+    auto walk_on = [&]() {
+        named_sync(2 + s, kRows);
+        if (t == 0) *more = cur.next(a);
+        named_sync(2 + s, kRows);
+        return *more != 0;
+    };
     uint32_t s_turn = 0, k = 0, given = 0;              // k: tile of the stretch
     int32_t item = 0;
     bool asked = false;
@@ -471,7 +483,7 @@ __device__ __forceinline__ void softmax_role(const AttendDev &a, const SchedShar
         const int32_t rows = Shape::rows(a, cur.q), r0 = stage_row(cur, s), row = r0 + t;
         if (r0 >= rows) {                               // this item has one stage only
             k += cur.len;
-            go = cur.next(a);
+            go = walk_on();
             continue;
         }
         if (!asked) {
@@ -492,7 +504,7 @@ __device__ __forceinline__ void softmax_role(const AttendDev &a, const SchedShar
             tc_after();
             if (i == len - 1) {
                 // the last S is there, so the queries' place is free: the next item's are asked for
-                go = cur.next(a);
+                go = walk_on();
                 asked = go && stage_row(cur, s) < Shape::rows(a, cur.q);
                 if (asked) ask_q(cur);
             }
@@ -592,6 +604,103 @@ __device__ __forceinline__ void softmax_role(const AttendDev &a, const SchedShar
     }
 }
 
+// A row of the output: where it goes.
+template <typename T> struct OutRow {
+    const AttendDev &a;
+    T *out;
+    float *lse;
+    bool live;
+    __device__ __forceinline__ OutRow(const AttendDev &a_, const Cursor<Shape> &c, int32_t row)
+        : a(a_), live(row < Shape::rows(a_, c.q))
+    {
+        const int32_t in = div_group(a, row), tok = c.q.first + in, head = c.outer * a.c.group + row - in * a.c.group;
+        out = static_cast<T *>(a.c.out) + (int64_t)tok * a.c.out_token_stride + (int64_t)head * a.c.out_head_stride;
+        lse = a.c.lse ? a.c.lse + (int64_t)tok * a.c.q_heads + head : nullptr;
+    }
+    // 16 columns
+    __device__ __forceinline__ void put(const float *o, int c, float inv) const
+    {
+        uint32_t w[8];
+#pragma unroll
+        for (int y = 0; y < 8; ++y) w[y] = Pack<T>::two(o[2 * y] * inv, o[2 * y + 1] * inv);
+        if (!live) return;
+        if (a.wide_out) {                               // whole sectors
+            if (c < a.dim)
+                asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out + c), "r"(w[0]), "r"(w[1]),
+                             "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                             : "memory");
+        } else {
+#pragma unroll
+            for (int y = 0; y < 8; y += 4)
+                if (c + 2 * y < a.dim)
+                    *reinterpret_cast<uint4 *>(out + c + 2 * y) = make_uint4(w[y], w[y + 1], w[y + 2], w[y + 3]);
+        }
+    }
+    __device__ __forceinline__ void put_lse(float top, float sum) const
+    {
+        if (live && lse) *lse = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+    }
+};
+
+// The pieces of an item, from the CTA that has its first tile on.
+template <int HALVES> struct Pieces {
+    static constexpr int width = Layout<HALVES>::width;
+    const AttendDev &a;
+    int32_t cta0;
+    __device__ __forceinline__ float *stat(int32_t p, int s, int t) const
+    {
+        return a.piece_stat + (piece_slot(cta0, p) * 2 + s) * 2 * kRows + t;
+    }
+    __device__ __forceinline__ float4 *at(int32_t p, int s, int c, int t) const
+    {
+        return reinterpret_cast<float4 *>(a.piece) + ((int64_t)(piece_slot(cta0, p) * 2 + s) * (width / 4) + c / 4) * kRows + t;
+    }
+    // joins a stage's n pieces p0, p0 + step, ... into the output (final) or into p0
+    template <typename T>
+    __device__ __forceinline__ void join(int s, int t, int32_t p0, int32_t n, int32_t step, const OutRow<T> *final) const
+    {
+        float top = -INFINITY, sum = 0.f;
+        for (int32_t p = 0; p < n; ++p) top = fmaxf(top, __ldcg(stat(p0 + p * step, s, t)));
+        const float base = top == -INFINITY ? 0.f : top;
+        for (int32_t p = 0; p < n; ++p)
+            sum = fmaf(exp2_approx(__ldcg(stat(p0 + p * step, s, t)) - base), __ldcg(stat(p0 + p * step, s, t) + kRows), sum);
+        const float scale = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll 1
+        for (int c = 0; c < width; c += 32) {
+            float o[32];
+#pragma unroll
+            for (int y = 0; y < 32; ++y) o[y] = 0.f;
+#pragma unroll 2
+            for (int32_t p = 0; p < n; ++p) {
+                const float f = exp2_approx(__ldcg(stat(p0 + p * step, s, t)) - base);
+                const float4 *src = at(p0 + p * step, s, c, t);
+#pragma unroll
+                for (int y = 0; y < 32; y += 4) {
+                    const float4 z = __ldcg(src + y / 4 * kRows);
+                    o[y] = fmaf(f, z.x, o[y]);
+                    o[y + 1] = fmaf(f, z.y, o[y + 1]);
+                    o[y + 2] = fmaf(f, z.z, o[y + 2]);
+                    o[y + 3] = fmaf(f, z.w, o[y + 3]);
+                }
+            }
+            if (final) {
+                final->put(o, c, scale);
+                final->put(o + 16, c + 16, scale);
+            } else {
+#pragma unroll
+                for (int y = 0; y < 32; y += 4)
+                    at(p0, s, c, t)[y / 4 * kRows] = make_float4(o[y], o[y + 1], o[y + 2], o[y + 3]);
+            }
+        }
+        if (final) {
+            final->put_lse(top, sum);
+        } else {
+            *stat(p0, s, t) = top;
+            stat(p0, s, t)[kRows] = sum;
+        }
+    }
+};
+
 // Outputs, and the join of items in pieces, of both stages in turn, while the
 // other warps are at the next item.
 template <typename T, int HALVES>
@@ -607,103 +716,72 @@ __device__ __forceinline__ void output_role(const AttendDev &a, const SchedShare
     int32_t item = 0;
     do {
         const int32_t rows = Shape::rows(a, cur.q), t0 = cur.k.lo / KT + cur.off;
+        const int stages = rows - stage_row(cur, 0) > kRows ? 2 : 1;
         const bool whole = cur.whole();
         const int64_t g0 = cur.g - cur.off;
-        const int32_t cta0 = owner(g0, line, ctas), pieces = whole ? 1 : owner(g0 + cur.tiles - 1, line, ctas) - cta0 + 1;
-        const int32_t mine = (int32_t)blockIdx.x - cta0;
+        const Pieces<HALVES> ps = {a, owner(g0, line, ctas)};
+        const int32_t mine = (int32_t)blockIdx.x - ps.cta0;
 #pragma unroll 1
-        for (int s = 0; s < 2; ++s) {
+        for (int s = 0; s < stages; ++s) {
             const int32_t row = stage_row(cur, s) + t;
-            if (row - t >= rows) break;
-            const bool live = row < rows;
-            const int32_t pos = live ? Shape::pos(a, cur.q, row) : -1, lo = pos < 0 ? 0 : first_key(a, pos);
-            const int32_t in = div_group(a, row);
-            const int32_t tok = cur.q.first + in, head = cur.outer * a.c.group + row - in * a.c.group;
-            T *const out = static_cast<T *>(a.c.out) + (int64_t)tok * a.c.out_token_stride + (int64_t)head * a.c.out_head_stride;
+            const OutRow<T> out(a, cur, row);
             const uint32_t t_o = tmem + ((uint32_t)(t & ~31) << 16) + 256 + 128 * s;
-
             const uint32_t now = s ? turn[1]++ & 1 : turn[0]++ & 1;
             mbar_wait(b.stat_full + 8 * s, now, dead, a.status);
             const float m = m_in[kRows * s + t], l = l_in[kRows * s + t];
             mbar_arrive(b.stat_free + 8 * s);
             mbar_wait(b.o_done + 8 * s, now, dead, a.status);
             tc_after();
-
-            // 16 columns of a row
-            auto put_out = [&](const float (&o)[16], int c, float inv) {
-                uint32_t w[8];
-#pragma unroll
-                for (int y = 0; y < 8; ++y) w[y] = Pack<T>::two(o[2 * y] * inv, o[2 * y + 1] * inv);
-                if (!live) return;
-                T *dst = out + c;
-                if (a.wide_out) {                       // whole sectors
-                    if (c < a.dim)
-                        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst), "r"(w[0]),
-                                     "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
-                                     : "memory");
-                } else {
-#pragma unroll
-                    for (int y = 0; y < 8; y += 4)
-                        if (c + 2 * y < a.dim)
-                            *reinterpret_cast<uint4 *>(dst + 2 * y) = make_uint4(w[y], w[y + 1], w[y + 2], w[y + 3]);
-                }
-            };
-            auto put_lse = [&](float top, float sum) {
-                if (live && a.c.lse)
-                    a.c.lse[(int64_t)tok * a.c.q_heads + head] =
-                        sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
-            };
-            auto stat_at = [&](int32_t p) { return a.piece_stat + (piece_slot(cta0, p) * 2 + s) * 2 * kRows + t; };
-            auto piece_at = [&](int32_t p, int c) {
-                return reinterpret_cast<float4 *>(a.piece) +
-                       ((int64_t)(piece_slot(cta0, p) * 2 + s) * (L::width / 4) + c / 4) * kRows + t;
-            };
             const float inv = l == 0.f ? 0.f : 1.f / l;
             const bool fix = bad[item % kBad] == item + 1;
 #pragma unroll 1
             for (int c = 0; c < L::width; c += 32) {
                 uint32_t x[32];
+                float o[32];
                 tc_ld32(x, t_o + c);
                 tc_wait_ld();
 #pragma unroll
-                for (int n = 0; n < 32; n += 16) {
-                    float o[16];
+                for (int y = 0; y < 32; ++y) o[y] = __uint_as_float(x[y]);
+                if (fix) {
+                    const int32_t pos = out.live ? Shape::pos(a, cur.q, row) : -1, r0 = stage_row(cur, 0);
+                    const Common item_sees(a, cur.q, r0, min(r0 + 2 * kRows, rows) - 1);
+#pragma unroll 1
+                    for (int32_t j = max(pos < 0 ? 0 : first_key(a, pos), t0 * KT); j <= min(pos, (t0 + cur.len) * KT - 1); ++j) {
+                        if (item_sees.covers(j / KT * KT)) continue;
+                        const int32_t id = a.c.block_table[(int64_t)cur.r * a.c.table_width + (j >> a.block_log)];
+                        if (id < 0 || id >= a.blocks) continue;
+                        const T *v = static_cast<const T *>(a.c.v_cache) + id * a.block_stride +
+                                     (j & ((1 << a.block_log) - 1)) * a.token_stride + cur.outer * a.head_stride + c;
 #pragma unroll
-                    for (int y = 0; y < 16; ++y) o[y] = __uint_as_float(x[n + y]);
-                    if (fix) {
-                        const int32_t r0 = stage_row(cur, 0);
-                        const Common item_sees(a, cur.q, r0, min(r0 + 2 * kRows, rows) - 1);
-                        for (int32_t j = max(lo, t0 * KT); j <= min(pos, (t0 + cur.len) * KT - 1); ++j) {
-                            if (item_sees.covers(j / KT * KT)) continue;
-                            const int32_t id = a.c.block_table[(int64_t)cur.r * a.c.table_width + (j >> a.block_log)];
-                            if (id < 0 || id >= a.blocks) continue;
-                            const T *v = static_cast<const T *>(a.c.v_cache) + id * a.block_stride +
-                                         (j & ((1 << a.block_log) - 1)) * a.token_stride + cur.outer * a.head_stride + c + n;
-#pragma unroll
-                            for (int y = 0; y < 16; ++y)
-                                if (c + n + y < a.dim) {
-                                    const float z = KvType<T>::to_float(v[y]);
-                                    if (!(fabsf(z) < INFINITY)) o[y] += z;
-                                }
-                        }
+                        for (int y = 0; y < 32; ++y)
+                            if (c + y < a.dim) {
+                                const float z = KvType<T>::to_float(v[y]);
+                                if (!(fabsf(z) < INFINITY)) o[y] += z;
+                            }
                     }
-                    if (whole) {
-                        put_out(o, c + n, inv);
-                    } else {
+                }
+                if (whole) {
+                    out.put(o, c, inv);
+                    out.put(o + 16, c + 16, inv);
+                } else {
 #pragma unroll
-                        for (int y = 0; y < 16; y += 4)
-                            piece_at(mine, c + n)[y / 4 * kRows] = make_float4(o[y], o[y + 1], o[y + 2], o[y + 3]);
-                    }
+                    for (int y = 0; y < 32; y += 4)
+                        ps.at(mine, s, c, t)[y / 4 * kRows] = make_float4(o[y], o[y + 1], o[y + 2], o[y + 3]);
                 }
             }
             tc_before();
             mbar_arrive(b.o_free + 8 * s);
             if (whole) {
-                put_lse(m, l);
-                continue;
+                out.put_lse(m, l);
+            } else {
+                *ps.stat(mine, s, t) = m;
+                ps.stat(mine, s, t)[kRows] = l;
             }
-            stat_at(mine)[0] = m;
-            stat_at(mine)[kRows] = l;
+        }
+        if (!whole) {
+            const int32_t pieces = owner(g0 + cur.tiles - 1, line, ctas) - ps.cta0 + 1;
+            const int32_t groups = (pieces + kJoinGroup - 1) / kJoinGroup;
+            // true in the CTA that arrives last of `of`
             auto arrive = [&](int32_t *count, int32_t of) {
                 __threadfence();
                 named_sync(1, kRows);
@@ -715,53 +793,21 @@ __device__ __forceinline__ void output_role(const AttendDev &a, const SchedShare
                 __threadfence();
                 return *last != 0;
             };
-            // join n pieces p0, p0 + step, ... into the output (final) or into p0
-            auto gather = [&](int32_t p0, int32_t n, int32_t step, bool final) {
-                float top = -INFINITY, sum = 0.f;
-                for (int32_t p = 0; p < n; ++p) top = fmaxf(top, __ldcg(stat_at(p0 + p * step)));
-                const float at = top == -INFINITY ? 0.f : top;
-                for (int32_t p = 0; p < n; ++p)
-                    sum = fmaf(exp2_approx(__ldcg(stat_at(p0 + p * step)) - at), __ldcg(stat_at(p0 + p * step) + kRows), sum);
-                const float scale = sum == 0.f ? 0.f : 1.f / sum;
+            // first a group's pieces, then the groups
+            int32_t p0 = mine / kJoinGroup * kJoinGroup, n = min(kJoinGroup, pieces - p0), step = 1;
+            int32_t *count = a.count + piece_slot(ps.cta0, p0);
+            while (arrive(count, n)) {
+                const bool final = step > 1 || groups == 1;
 #pragma unroll 1
-                for (int c = 0; c < L::width; c += 16) {
-                    float o[16];
-#pragma unroll
-                    for (int y = 0; y < 16; ++y) o[y] = 0.f;
-#pragma unroll 2
-                    for (int32_t p = 0; p < n; ++p) {
-                        const float f = exp2_approx(__ldcg(stat_at(p0 + p * step)) - at);
-                        const float4 *src = piece_at(p0 + p * step, c);
-#pragma unroll
-                        for (int y = 0; y < 16; y += 4) {
-                            const float4 z = __ldcg(src + y / 4 * kRows);
-                            o[y] = fmaf(f, z.x, o[y]);
-                            o[y + 1] = fmaf(f, z.y, o[y + 1]);
-                            o[y + 2] = fmaf(f, z.z, o[y + 2]);
-                            o[y + 3] = fmaf(f, z.w, o[y + 3]);
-                        }
-                    }
-                    if (final) {
-                        put_out(o, c, scale);
-                    } else {
-#pragma unroll
-                        for (int y = 0; y < 16; y += 4)
-                            piece_at(p0, c)[y / 4 * kRows] = make_float4(o[y], o[y + 1], o[y + 2], o[y + 3]);
-                    }
+                for (int s = 0; s < stages; ++s) {
+                    const OutRow<T> out(a, cur, stage_row(cur, s) + t);
+                    ps.join(s, t, p0, n, step, final ? &out : nullptr);
                 }
-                if (final) {
-                    put_lse(top, sum);
-                } else {
-                    stat_at(p0)[0] = top;
-                    stat_at(p0)[kRows] = sum;
-                }
-            };
-            const int32_t groups = (pieces + kJoinGroup - 1) / kJoinGroup;
-            const int32_t p0 = mine / kJoinGroup * kJoinGroup, n = min(kJoinGroup, pieces - p0);
-            if (arrive(a.count + 2 * piece_slot(cta0, p0) + s, n)) {
-                gather(p0, n, 1, groups == 1);
-                if (groups > 1 && arrive(a.count + 4 * gridDim.x + 2 * piece_slot(cta0, 0) + s, groups))
-                    gather(0, groups, kJoinGroup, true);
+                if (final) break;
+                p0 = 0;
+                n = groups;
+                step = kJoinGroup;
+                count = a.count + 2 * gridDim.x + piece_slot(ps.cta0, 0);
             }
         }
         ++item;
@@ -830,15 +876,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
     tc_after();
     const uint32_t tmem = sh.tmem;
 
-    // 512 threads x 128 registers = 256 x 136 + 128 x 144 + 128 x 96
+    // 512 threads x 128 registers = 128 x (2 for softmax + for output + for the others)
+    constexpr int kSoftmax = HALVES == 2 ? 144 : 128, kOutput = HALVES == 2 ? 144 : 160, kOthers = 512 - 2 * kSoftmax - kOutput;
     if (warp < 8) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 136;");
-        softmax_role<T, HALVES>(a, sh.sched, warp >> 2, raw, base, tmem, b, sh.m[warp >> 2], sh.l[warp >> 2], sh.bad, &sh.dead);
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmax));
+        softmax_role<T, HALVES>(a, sh.sched, warp >> 2, raw, base, tmem, b, sh.m[warp >> 2], sh.l[warp >> 2], sh.bad, &sh.dead,
+                                reinterpret_cast<Cursor<Shape> *>(sh.walk[warp >> 2]), &sh.more[warp >> 2]);
     } else if (warp < 12) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 144;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kOutput));
         output_role<T, HALVES>(a, sh.sched, tmem, b, sh.m[0], sh.l[0], sh.bad, &sh.dead, &sh.last);
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOthers));
         if (warp < 14) mma_role<T, HALVES>(a, sh.sched, warp - 12, base, tmem, b, &sh.dead);
         else copy_role<HALVES>(a, sh.sched, warp - 14, warp == 14 ? &km : &vm, base, b, &sh.dead);
     }
