@@ -403,12 +403,12 @@ def pp_chunk_map(parent, weight, resident, blocks_per_slot: int):
     return out[:n], int(used.value)
 
 
-def _arg(t, name, dtype, *shape):
-    """A contiguous CUDA tensor of this type and shape (None: any size)."""
-    if str(t.dtype) != "torch." + dtype or t.dim() != len(shape) or \
-            any(want is not None and have != want for have, want in zip(t.shape, shape)):
-        raise ValueError(f"{name}: expected {dtype} {list(shape)}, got {t.dtype} {list(t.shape)}")
-    return _dev(t)
+def _arg(t, name, dtype, shape):
+    """Device pointer of a contiguous CUDA tensor of this type and shape."""
+    if t.dtype is dtype and t.shape == shape and t.is_cuda and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{name}: expected a contiguous CUDA tensor {list(shape)} of {dtype}, got {list(t.shape)} of "
+                     f"{t.dtype} on {t.device}, strides {list(t.stride())}")
 
 
 class KVCache:
@@ -422,8 +422,13 @@ class KVCache:
         name = str(dtype).replace("torch.", "")
         if name not in self._DTYPES:
             raise ValueError("dtype must be bfloat16 or float16")
+        import torch
         self.shape = (int(blocks), int(block_size), int(kv_heads), int(head_dim))
-        self.dtype = name
+        self.dtype = getattr(torch, name)
+        self._i32, self._i64, self._f32 = torch.int32, torch.int64, torch.float32
+        self._device = torch.cuda.current_device()
+        # the current stream's handle at a fiftieth of the cost of current_stream()
+        self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         h = _P()
         _check(_lib.pp_kv_create(*self.shape, self._DTYPES[name], *[int(x) for x in (strides or (0, 0, 0))],
                                  _stream(stream), ctypes.byref(h)))
@@ -467,24 +472,31 @@ class KVCache:
     def sync(self, stream=None):
         _check(_lib.pp_kv_sync(self.handle, _stream(stream)))
 
+    def _on(self, stream):
+        if stream is None and self._raw_stream is not None:
+            return self._raw_stream(self._device)
+        return _stream(stream)
+
     def _cache(self, t, name):
         """Device pointer of a cache of this layout (an extent of 1 has no stride)."""
-        if not t.is_cuda or str(t.dtype) != "torch." + self.dtype or tuple(t.shape) != self.shape or \
-                t.stride(3) != 1 or any(n > 1 and a != b for n, a, b in zip(t.shape, t.stride(), self.strides)):
-            raise ValueError(f"{name}: expected a CUDA {self.dtype} tensor of shape {self.shape} and strides "
-                             f"{self.strides + (1,)}")
-        return _P(t.data_ptr())
+        if t.dtype is self.dtype and t.shape == self.shape and t.is_cuda:
+            st = t.stride()
+            if st[3] == 1 and (st[:3] == self.strides or
+                               all(n == 1 or a == b for n, a, b in zip(self.shape, st, self.strides))):
+                return t.data_ptr()
+        raise ValueError(f"{name}: expected a CUDA {self.dtype} tensor of shape {self.shape} and strides "
+                         f"{self.strides + (1,)}")
 
     def _rows(self, t, name, tokens, heads):
         """Pointer, token stride and head stride of [tokens][heads][head_dim] rows."""
-        if not t.is_cuda or str(t.dtype) != "torch." + self.dtype or \
-                tuple(t.shape) != (tokens, heads, self.shape[3]) or (t.numel() and t.stride(2) != 1):
-            raise ValueError(f"{name}: expected a CUDA {self.dtype} tensor [{tokens}][{heads}][{self.shape[3]}] "
-                             "with contiguous rows")
-        # an extent of 1 may carry any stride
-        ht = t.stride(1) if heads > 1 else self.shape[3]
-        tt = t.stride(0) if tokens > 1 else max(heads * ht, 8)
-        return _P(t.data_ptr()), tt, ht
+        if t.dtype is self.dtype and t.shape == (tokens, heads, self.shape[3]) and t.is_cuda:
+            st = t.stride()
+            if st[2] == 1 or not tokens:
+                # an extent of 1 may carry any stride
+                ht = st[1] if heads > 1 else self.shape[3]
+                return t.data_ptr(), st[0] if tokens > 1 else heads * ht, ht
+        raise ValueError(f"{name}: expected a CUDA {self.dtype} tensor [{tokens}][{heads}][{self.shape[3]}] "
+                         "with contiguous rows")
 
 
 def pp_block_tables(kv: KVCache, length, cached, block_table, slot_map, position, q_start, free_blocks, free_head,
@@ -494,35 +506,34 @@ def pp_block_tables(kv: KVCache, length, cached, block_table, slot_map, position
     free_blocks [F] int32, free_head and free_head_out [1] int32, chunk_map [n][4] int32: CUDA tensors."""
     if (node is None) != (chunk_map is None):
         raise ValueError("node and chunk_map go together")
-    r, t = int(length.shape[0]), int(slot_map.shape[0])
-    n = 0 if node is None else int(chunk_map.shape[0])
+    r, t, width, i32 = length.shape[0], slot_map.shape[0], block_table.shape[-1], kv._i32
+    n = 0 if node is None else chunk_map.shape[0]
     _check(_lib.pp_block_tables(
-        kv.handle, r, _arg(length, "length", "int32", r), _arg(cached, "cached", "int32", r),
-        None if node is None else _arg(node, "node", "int32", r), n,
-        None if node is None else _arg(chunk_map, "chunk_map", "int32", n, 4),
-        int(free_blocks.shape[0]), _arg(free_blocks, "free_blocks", "int32", None),
-        _arg(free_head, "free_head", "int32", 1), _arg(free_head_out, "free_head_out", "int32", 1),
-        int(block_table.shape[-1]), _arg(block_table, "block_table", "int32", r, None), t,
-        _arg(slot_map, "slot_map", "int64", t), _arg(position, "position", "int32", t),
-        _arg(q_start, "q_start", "int32", r + 1), _stream(stream)))
+        kv.handle, r, _arg(length, "length", i32, (r,)), _arg(cached, "cached", i32, (r,)),
+        None if node is None else _arg(node, "node", i32, (r,)), n,
+        None if node is None else _arg(chunk_map, "chunk_map", i32, (n, 4)),
+        free_blocks.shape[0], _arg(free_blocks, "free_blocks", i32, free_blocks.shape[:1]),
+        _arg(free_head, "free_head", i32, (1,)), _arg(free_head_out, "free_head_out", i32, (1,)),
+        width, _arg(block_table, "block_table", i32, (r, width)), t, _arg(slot_map, "slot_map", kv._i64, (t,)),
+        _arg(position, "position", i32, (t,)), _arg(q_start, "q_start", i32, (r + 1,)), kv._on(stream)))
 
 
 def pp_kv_write(kv: KVCache, k, v, slot_map, k_cache, v_cache, stream=None):
     """Store rows k, v [T][kv_heads][head_dim] at slot_map [T] int64 (negative: left out)."""
-    t = int(slot_map.shape[0])
-    _check(_lib.pp_kv_write(kv.handle, t, *kv._rows(k, "k", t, kv.shape[2]), *kv._rows(v, "v", t, kv.shape[2]),
-                            _arg(slot_map, "slot_map", "int64", t), kv._cache(k_cache, "k_cache"),
-                            kv._cache(v_cache, "v_cache"), _stream(stream)))
+    t, h = slot_map.shape[0], kv.shape[2]
+    _check(_lib.pp_kv_write(kv.handle, t, *kv._rows(k, "k", t, h), *kv._rows(v, "v", t, h),
+                            _arg(slot_map, "slot_map", kv._i64, (t,)), kv._cache(k_cache, "k_cache"),
+                            kv._cache(v_cache, "v_cache"), kv._on(stream)))
 
 
 def pp_paged_attention(kv: KVCache, q, k_cache, v_cache, block_table, q_start, length, max_q: int, out,
                        scale: float, window: int = 0, lse=None, stream=None):
     """Causal attention of the new tokens' q [T][q_heads][head_dim] over the paged cache, into out (as q) and
     lse [T][q_heads] float32.  block_table [R][width], q_start [R + 1], length [R]: int32 CUDA tensors."""
-    t, heads, r = int(q.shape[0]), int(q.shape[1]), int(length.shape[0])
+    t, heads, r, width, i32 = q.shape[0], q.shape[1], length.shape[0], block_table.shape[-1], kv._i32
     _check(_lib.pp_paged_attention(
         kv.handle, r, t, heads, *kv._rows(q, "q", t, heads), kv._cache(k_cache, "k_cache"),
-        kv._cache(v_cache, "v_cache"), int(block_table.shape[-1]), _arg(block_table, "block_table", "int32", r, None),
-        _arg(q_start, "q_start", "int32", r + 1), _arg(length, "length", "int32", r), int(max_q), int(window),
-        float(scale), *kv._rows(out, "out", t, heads),
-        None if lse is None else _arg(lse, "lse", "float32", t, heads), _stream(stream)))
+        kv._cache(v_cache, "v_cache"), width, _arg(block_table, "block_table", i32, (r, width)),
+        _arg(q_start, "q_start", i32, (r + 1,)), _arg(length, "length", i32, (r,)), max_q, window, scale,
+        *kv._rows(out, "out", t, heads), None if lse is None else _arg(lse, "lse", kv._f32, (t, heads)),
+        kv._on(stream)))

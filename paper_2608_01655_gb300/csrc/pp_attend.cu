@@ -63,6 +63,12 @@ pp_status cache_map(const pp_kv *kv, const void *cache, int32_t rows, CUtensorMa
     return PP_OK;
 }
 
+pp_status prepare_attend()
+{
+    const pp_status s = prepare_attend_token();
+    return s == PP_OK ? prepare_attend_chunk() : s;
+}
+
 pp_status launch_attend(pp_kv *kv, const AttendArgs &c, cudaStream_t st)
 {
     return c.max_q == 1 ? launch_attend_token(kv, c, st) : launch_attend_chunk(kv, c, st);

@@ -453,6 +453,8 @@ __device__ __forceinline__ int32_t piece_slot(int32_t cta0, int32_t p) { return 
 pp_status cache_map(const pp_kv *kv, const void *cache, int32_t rows, CUtensorMap *map);
 AttendDev attend_dev(const pp_kv *kv, const AttendArgs &c);
 
+pp_status prepare_attend_token();
+pp_status prepare_attend_chunk();
 pp_status launch_attend_token(pp_kv *kv, const AttendArgs &c, cudaStream_t st);
 pp_status launch_attend_chunk(pp_kv *kv, const AttendArgs &c, cudaStream_t st);
 

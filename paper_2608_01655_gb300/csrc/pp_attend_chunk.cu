@@ -898,6 +898,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
     }
 }
 
+template <int HALVES> constexpr int shared_bytes()
+{
+    constexpr int bytes = Layout<HALVES>::tiles + sizeof(Shared<HALVES>);
+    static_assert(bytes <= 232448, "shared memory of a CTA");
+    return bytes;
+}
+
+template <typename T, int HALVES> static cudaError_t prepare_t()
+{
+    return cudaFuncSetAttribute(k_attend_chunk<T, HALVES>, cudaFuncAttributeMaxDynamicSharedMemorySize, shared_bytes<HALVES>());
+}
+
 template <typename T, int HALVES>
 static pp_status launch_t(pp_kv *kv, const AttendArgs &c, cudaStream_t st)
 {
@@ -907,11 +919,17 @@ static pp_status launch_t(pp_kv *kv, const AttendArgs &c, cudaStream_t st)
     pp_status s = cache_map(kv, c.k_cache, rows, &km);
     if (s == PP_OK) s = cache_map(kv, c.v_cache, rows, &vm);
     if (s != PP_OK) return s;
-    constexpr int bytes = Layout<HALVES>::tiles + sizeof(Shared<HALVES>);
-    static_assert(bytes <= 232448, "shared memory of a CTA");
-    PP_CUDA(cudaFuncSetAttribute(k_attend_chunk<T, HALVES>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
-    k_attend_chunk<T, HALVES><<<kv->sm_count, kThreads, bytes, st>>>(a, km, vm);
+    k_attend_chunk<T, HALVES><<<kv->sm_count, kThreads, shared_bytes<HALVES>(), st>>>(a, km, vm);
     PP_CUDA(cudaGetLastError());
+    return PP_OK;
+}
+
+pp_status prepare_attend_chunk()
+{
+    PP_CUDA((prepare_t<__nv_bfloat16, 1>()));
+    PP_CUDA((prepare_t<__nv_bfloat16, 2>()));
+    PP_CUDA((prepare_t<__half, 1>()));
+    PP_CUDA((prepare_t<__half, 2>()));
     return PP_OK;
 }
 

@@ -446,14 +446,26 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_token(const __grid_const
     } while (cur.next(a));
 }
 
+template <typename T, int HALVES> static cudaError_t prepare_t()
+{
+    return cudaFuncSetAttribute(k_attend_token<T, HALVES>, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<HALVES>::bytes);
+}
+
 template <typename T, int HALVES>
 static pp_status launch_t(pp_kv *kv, const AttendArgs &c, cudaStream_t st)
 {
     const AttendDev a = attend_dev(kv, c);
-    PP_CUDA(cudaFuncSetAttribute(k_attend_token<T, HALVES>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 Layout<HALVES>::bytes));
     k_attend_token<T, HALVES><<<kv->sm_count, kThreads, Layout<HALVES>::bytes, st>>>(a);
     PP_CUDA(cudaGetLastError());
+    return PP_OK;
+}
+
+pp_status prepare_attend_token()
+{
+    PP_CUDA((prepare_t<__nv_bfloat16, 1>()));
+    PP_CUDA((prepare_t<__nv_bfloat16, 2>()));
+    PP_CUDA((prepare_t<__half, 1>()));
+    PP_CUDA((prepare_t<__half, 2>()));
     return PP_OK;
 }
 

@@ -330,6 +330,7 @@ static pp_status check_device(const pp_kv *kv)
 }
 
 pp_status launch_attend(pp_kv *kv, const AttendArgs &a, cudaStream_t st);
+pp_status prepare_attend();            // kernel attributes on the current device
 
 }  // namespace pp
 
@@ -387,6 +388,10 @@ extern "C" pp_status pp_kv_create(int32_t blocks, int32_t block_size, int32_t kv
         PP_CUDA(cudaDeviceGetAttribute(&kv->sm_count, cudaDevAttrMultiProcessorCount, kv->device));
         PP_CUDA(cudaMalloc(&kv->d_status, sizeof(int32_t)));
         PP_CUDA(cudaMemsetAsync(kv->d_status, 0, sizeof(int32_t), (cudaStream_t)stream));
+        PP_CUDA(cudaFuncSetAttribute(k_block_tables, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                     (int)(sizeof(int32_t) * (3 * (size_t)kKvMaxRequests + 2))));
+        pp_status s = prepare_attend();
+        if (s != PP_OK) return s;
         // two pieces a CTA, one CTA an SM
         const size_t slots = 2 * (size_t)kv->sm_count;
         PP_CUDA(cudaMalloc(&kv->d_piece, slots * kPieceRows * kKvMaxDim * sizeof(float)));
@@ -466,8 +471,6 @@ extern "C" pp_status pp_block_tables(pp_kv *kv, int32_t requests, const int32_t 
     const int64_t want = std::max<int64_t>((max_tokens + 2047) / 2048, (requests + 63) / 64);
     const int grid = (int)std::min<int64_t>(std::max<int64_t>(want, 1), kv->sm_count);
     const size_t smem = sizeof(int32_t) * (3 * (size_t)requests + 2);
-    PP_CUDA(cudaFuncSetAttribute(k_block_tables, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 (int)(sizeof(int32_t) * (3 * (size_t)kKvMaxRequests + 2))));
     k_block_tables<<<grid, kTabThreads, smem, (cudaStream_t)stream>>>(a);
     PP_CUDA(cudaGetLastError());
     return PP_OK;
