@@ -118,7 +118,9 @@ template <class S> __device__ __forceinline__ int64_t request_tiles(const Attend
     return mine;
 }
 
-__device__ __forceinline__ int64_t block_scan(int64_t v, int64_t *excl, int64_t *warp_sum)
+// Sum over the warp (few: every warp has the same values) or the CTA, and the sum
+// before this thread.
+__device__ __forceinline__ int64_t scan64(int64_t v, int64_t *excl, int64_t *warp_total, bool few)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     int64_t x = v;                                      // inclusive within the warp
@@ -127,12 +129,16 @@ __device__ __forceinline__ int64_t block_scan(int64_t v, int64_t *excl, int64_t 
         const int64_t y = __shfl_up_sync(~0u, x, o);
         if (lane >= o) x += y;
     }
+    if (few) {
+        *excl = x - v;
+        return __shfl_sync(~0u, x, 31);
+    }
     __syncthreads();
-    if (lane == 31) warp_sum[warp] = x;
+    if (lane == 31) warp_total[warp] = x;
     __syncthreads();
     int64_t before = 0, total = 0;
     for (int w = 0; w < warps; ++w) {
-        const int64_t y = warp_sum[w];
+        const int64_t y = warp_total[w];
         if (w < warp) before += y;
         total += y;
     }
@@ -140,42 +146,53 @@ __device__ __forceinline__ int64_t block_scan(int64_t v, int64_t *excl, int64_t 
     return total;
 }
 
+// x / y for 0 <= x, 0 < y: most are small, and a 64-bit division takes three times as long
+__device__ __forceinline__ int64_t quotient(int64_t x, int64_t y)
+{
+    return ((x | y) >> 32) == 0 ? (int64_t)((uint32_t)x / (uint32_t)y) : x / y;
+}
+
 // The CTA's stretch: false if it has none.  All threads of the CTA call it.
 template <class S> __device__ __forceinline__ bool schedule(const AttendDev &a, SchedShared &sm)
 {
     static_assert(S::extra < 4, "every stretch has a tile");
-    const int32_t R = a.c.requests, T = blockDim.x, outer = S::outer(a);
-    const int lane = threadIdx.x & 31;
+    // up to 32 requests every warp works all of it out, which takes one barrier in all
+    const bool few = a.c.requests <= 32;
+    const int lane = threadIdx.x & 31, me = few ? lane : threadIdx.x;
+    const int32_t R = a.c.requests, T = few ? 32 : blockDim.x, outer = S::outer(a);
     const bool report = blockIdx.x == 0;
     if (report && threadIdx.x == 0 && a.c.q_start[0] != 0) kv_bounds(a.status);
     Req q;
-    int64_t mine, tiles = 0, items = 0, excl, before = 0;      // of one head: this lane's request, all of this lane's
+    int64_t mine, tiles = 0, items = 0, excl, excl_items = 0, before = 0;   // of one head: this lane's request, all of its requests
     for (int32_t base = 0; base < R; base += T) {
-        const int32_t r = base + threadIdx.x;
+        const int32_t r = base + me;
         q = Req{0, 0, 0};
         if (r < R) q = load_req(a, r, report);
         tiles += mine = request_tiles<S>(a, q);
         items += S::inner(a, q);
     }
-    tiles = block_scan(tiles, &excl, sm.warp_sum) * outer;
+    tiles = scan64(tiles, &excl, sm.warp_sum, few) * outer;
     if (tiles == 0) return false;
     // with few tiles a CTA, every tile to a CTA of its own counts more than an even load
     const int32_t extra = tiles >= 4 * (int64_t)gridDim.x ? S::extra : 0;
-    const int64_t total = tiles + (extra ? block_scan(items, &excl, sm.warp_sum) * outer * extra : 0);
+    const int64_t total = tiles + (extra ? scan64(items, &excl_items, sm.warp_sum, few) * outer * extra : 0);
+    excl += excl_items * extra;
     const int64_t ctas = min((int64_t)gridDim.x, total);
     if (blockIdx.x >= ctas) return false;
-    const int64_t begin = total * blockIdx.x / ctas, end = total * (blockIdx.x + 1) / ctas;
+    const int64_t begin = quotient(total * blockIdx.x, ctas), end = quotient(total * (blockIdx.x + 1), ctas);
     for (int32_t base = 0; base < R; base += T) {
-        const int32_t r = base + threadIdx.x;
+        const int32_t r = base + me;
         if (R > T) {
             q = Req{0, 0, 0};
             if (r < R) q = load_req(a, r, false);
             mine = request_tiles<S>(a, q);
         }
         mine += (int64_t)S::inner(a, q) * extra;
-        const int64_t here = block_scan(mine, &excl, sm.warp_sum);
-        excl += before;
-        before += here;
+        if (R > T) {
+            const int64_t here = scan64(mine, &excl, sm.warp_sum, few);
+            excl += before;
+            before += here;
+        }
         // the warp that has the request of the stretch's first tile, or of the one after it, looks for the item
 #pragma unroll 1
         for (int which = 0; which < 2; ++which) {
@@ -186,8 +203,12 @@ template <class S> __device__ __forceinline__ bool schedule(const AttendDev &a, 
             const int src = __ffs(who) - 1;
             const Req x = shfl_req(q, src);
             const int64_t per = __shfl_sync(~0u, mine, src), off = tile - __shfl_sync(~0u, excl, src) * outer;
-            const int32_t head = (int32_t)(off / per), count = S::inner(a, x);
+            const int32_t head = (int32_t)quotient(off, per), count = S::inner(a, x);
             int64_t rem = off - head * per;
+            if (count == 1) {
+                if (lane == 0) (which ? sm.end : sm.first) = Place{r - lane + src, head, 0, (int32_t)rem};
+                continue;
+            }
             for (int32_t i0 = 0; i0 < count; i0 += 32) {
                 const int64_t n = i0 + lane < count ? key_tiles<S::KT>(S::keys(a, x, i0 + lane)) + extra : 0;
                 int64_t incl = n;
@@ -397,7 +418,7 @@ __device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes)
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 
-// block that holds key j of the request, -1 if no row sees one of keys j .. j + n - 1
+// block that holds key j of the request, -1 if the item sees none of keys j .. j + n - 1
 __device__ __forceinline__ int32_t key_block(const AttendDev &a, const int32_t *row, Keys k, int32_t j, int32_t n)
 {
     if (j > k.hi || j + n - 1 < k.lo) return -1;
@@ -443,7 +464,7 @@ template <> struct Pack<__half> {
 // CTA whose stretch holds tile g of the line
 __device__ __forceinline__ int32_t owner(int64_t g, int64_t total, int64_t ctas)
 {
-    return (int32_t)(((g + 1) * ctas - 1) / total);
+    return (int32_t)quotient((g + 1) * ctas - 1, total);
 }
 // a CTA has at most two pieces: one that goes on an item begun before it (0)
 // and one of an item that goes on after it (1)

@@ -37,6 +37,9 @@ struct Shape {
     static constexpr int32_t extra = 1;
     static __device__ __forceinline__ int32_t row_tiles(const AttendDev &a) { return (a.c.group + kRows - 1) / kRows; }
     static __device__ __forceinline__ int32_t outer(const AttendDev &a) { return a.kv_heads * row_tiles(a); }
+    // K/V head of outer item x, and which 16 of its query heads
+    static __device__ __forceinline__ int32_t head(const AttendDev &a, int32_t x) { return a.c.group <= kRows ? x : x / row_tiles(a); }
+    static __device__ __forceinline__ int32_t row0(const AttendDev &a, int32_t x) { return a.c.group <= kRows ? 0 : x % row_tiles(a) * kRows; }
     static __device__ __forceinline__ int32_t inner(const AttendDev &, const Req &q) { return q.q_len; }
     static __device__ __forceinline__ Keys keys(const AttendDev &a, const Req &q, int32_t i)
     {
@@ -88,37 +91,41 @@ __device__ __forceinline__ uint32_t row_at(int row, int piece)
 // both 16-bit halves of a register kept or cleared
 __device__ __forceinline__ uint32_t keep(bool lo, bool hi) { return (lo ? 0xffffu : 0u) | (hi ? 0xffff0000u : 0u); }
 
-// A warp's copies of its keys, tile after tile along the stretch.
+// A warp's copies of its keys, tile after tile along the stretch.  Lane l keeps
+// the block of the warp's keys in the l-th of the next 32 tiles (two blocks of 8
+// tokens: the second's in `upper`), so that a tile waits for no table entry.
 template <int HALVES> struct Feed {
     using L = Layout<HALVES>;
     const AttendDev &a;
     Cursor<Shape> cur;
     RowLane<HALVES> rl;
     uint32_t ring, slot = 0;
-    int32_t i = 0, b0, b1;                              // next tile of the item; blocks of its keys
-    bool more = true;
+    int32_t i = 0, lower, upper;
+    bool more;
     __device__ __forceinline__ Feed(const AttendDev &a_, const SchedShared &sched, uint32_t ring_)
-        : a(a_), cur(a_, sched), rl(a_, L::half), ring(ring_)
+        : a(a_), cur(a_, sched), rl(a_, L::half), ring(ring_), more(true)
     {
         look();
     }
-    __device__ __forceinline__ int32_t first() const
+    __device__ __forceinline__ int32_t first(int32_t tile) const
     {
-        return (cur.k.lo / KT + cur.off + i) * KT + (int32_t)(threadIdx.x >> 5) * kKeys;
+        return (cur.k.lo / KT + cur.off + tile) * KT + (int32_t)(threadIdx.x >> 5) * kKeys;
     }
     __device__ __forceinline__ void look()
     {
         const int32_t *row = a.c.block_table + (int64_t)cur.r * a.c.table_width;
-        b0 = key_block(a, row, cur.k, first(), 8);
-        b1 = key_block(a, row, cur.k, first() + 8, 8);
+        const int32_t tile = i + (threadIdx.x & 31), j = first(tile);
+        lower = tile < cur.len ? key_block(a, row, cur.k, j, 8) : -1;
+        upper = tile >= cur.len ? -1 : a.block_log > 3 && lower >= 0 && j + 8 <= cur.k.hi ? lower : key_block(a, row, cur.k, j + 8, 8);
     }
     // asks for the next tile, into the ring's next place
     __device__ __forceinline__ void ask()
     {
         if (more) {
-            const int32_t j0 = first(), in_block = (1 << a.block_log) - 1;
+            const int32_t j0 = first(i), in_block = (1 << a.block_log) - 1;
+            const int32_t b0 = __shfl_sync(~0u, lower, i & 31), b1 = __shfl_sync(~0u, upper, i & 31);
             if (j0 <= cur.k.hi && j0 + kKeys - 1 >= cur.k.lo) {
-                const int64_t token_bytes = 2 * a.token_stride, head = 2 * (cur.outer / Shape::row_tiles(a)) * a.head_stride;
+                const int64_t token_bytes = 2 * a.token_stride, head = 2 * Shape::head(a, cur.outer) * a.head_stride;
                 const int64_t at0 = head + max(b0, 0) * 2 * a.block_stride + (j0 & in_block) * token_bytes;
                 const int64_t at1 = head + max(b1, 0) * 2 * a.block_stride + ((j0 + 8) & in_block) * token_bytes;
                 const char *k = static_cast<const char *>(a.c.k_cache), *v = static_cast<const char *>(a.c.v_cache);
@@ -131,8 +138,10 @@ template <int HALVES> struct Feed {
             if (++i == cur.len) {
                 i = 0;
                 more = cur.next(a);
+                if (more) look();
+            } else if ((i & 31) == 0) {
+                look();
             }
-            if (more) look();
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
         if (++slot == L::stages) slot = 0;
@@ -167,8 +176,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_token(const __grid_const
     Cursor<Shape> cur(a, sched);
     uint32_t slot = 0;
     do {
-        const int32_t tiles_of = Shape::row_tiles(a), head = cur.outer / tiles_of;
-        const int32_t row0 = cur.outer % tiles_of * kRows, rows = min(kRows, a.c.group - row0);
+        const int32_t head = Shape::head(a, cur.outer), row0 = Shape::row0(a, cur.outer), rows = min(kRows, a.c.group - row0);
         const int32_t tok = cur.q.first + cur.inner;
         const T *qp = static_cast<const T *>(a.c.q) + (int64_t)tok * a.c.q_token_stride +
                       (int64_t)(head * a.c.group + row0) * a.c.q_head_stride;

@@ -95,6 +95,7 @@ struct TablesArgs {
     int32_t *free_head_out, *table, *position, *q_start;
     int64_t *slot;
     int32_t *status;
+    int32_t wide;                       // slot and position start at 16-byte boundaries
 };
 
 constexpr int kTabThreads = 1024;
@@ -148,10 +149,17 @@ __device__ __forceinline__ int32_t tab_find(const int32_t *pre, int32_t n, int32
     return lo;
 }
 
-// Every CTA scans all requests' counts (12 bytes a request, from L2 after the
-// first) and keeps the prefix sums in shared memory, so one launch without any
-// exchange between CTAs does it; then table rows, new blocks and tokens are
-// shared out evenly.  Latency bounds it up to some hundred thousand tokens.
+// Every CTA scans all requests' counts (12 bytes a request and two chunk records
+// of an admitted one, from L2 after the first) and keeps the prefix sums in shared
+// memory, so one launch without any exchange between CTAs does it.  Then a
+// quarter of the warps walks the admitted requests' paths, a chain of dependent
+// loads a segment, and fills in the new blocks, while the others write the tokens'
+// slots and positions, four a thread.  Latency bounds it up to some hundred
+// thousand new tokens, then the 12 bytes a token.
+constexpr int kTabWalkers = kTabThreads / 4;
+constexpr int kTabRun = 4;                          // tokens of a thread
+constexpr int kTabPass = kTabRun * (kTabThreads - kTabWalkers);    // tokens that a CTA writes at once
+
 __global__ void __launch_bounds__(kTabThreads) k_block_tables(TablesArgs a)
 {
     extern __shared__ int32_t sm[];
@@ -160,45 +168,46 @@ __global__ void __launch_bounds__(kTabThreads) k_block_tables(TablesArgs a)
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int32_t bs = 1 << a.block_log;
 
-    int64_t tot_t = 0, tot_b = 0;
-    for (int32_t base = 0; base < a.requests; base += kTabThreads) {
-        const int32_t r = base + tid;
-        int64_t t = 0, b = 0;
-        int32_t c = 0;
-        if (r < a.requests) {
-            const TabRow w = tab_row(a, r, blockIdx.x == 0);
-            c = w.cached;
-            t = w.length - w.cached;
-            b = ((w.length + (int64_t)bs - 1) >> a.block_log) - ((w.cached + (int64_t)bs - 1) >> a.block_log);
-        }
-        int64_t st = t, sb = b;
+    // each thread takes neighbouring requests: new tokens and new blocks, summed up
+    const int32_t per = (a.requests + kTabThreads - 1) / kTabThreads;
+    const int32_t first = min(tid * per, a.requests), past = min(first + per, a.requests);
+    int64_t my_t = 0, my_b = 0;
+#pragma unroll 2
+    for (int32_t r = first; r < past; ++r) {
+        const TabRow w = tab_row(a, r, blockIdx.x == 0);
+        const int32_t t = w.length - w.cached;
+        const int32_t b = (int32_t)(((w.length + (int64_t)bs - 1) >> a.block_log) - ((w.cached + (int64_t)bs - 1) >> a.block_log));
+        tok[r] = t;
+        nbk[r] = b;
+        held[r] = w.cached;
+        my_t += t;
+        my_b += b;
+    }
+    int64_t st = my_t, sb = my_b;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int64_t x = __shfl_up_sync(~0u, st, o), y = __shfl_up_sync(~0u, sb, o);
-            if (lane >= o) { st += x; sb += y; }
-        }
-        if (lane == 31) { wsum[0][warp] = st; wsum[1][warp] = sb; }
-        __syncthreads();
-        if (warp == 0) {
-            int64_t x = wsum[0][lane], y = wsum[1][lane];
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t x = __shfl_up_sync(~0u, st, o), y = __shfl_up_sync(~0u, sb, o);
+        if (lane >= o) { st += x; sb += y; }
+    }
+    if (lane == 31) { wsum[0][warp] = st; wsum[1][warp] = sb; }
+    __syncthreads();
+    int64_t tot_t = wsum[0][lane], tot_b = wsum[1][lane];
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int64_t u = __shfl_up_sync(~0u, x, o), v = __shfl_up_sync(~0u, y, o);
-                if (lane >= o) { x += u; y += v; }
-            }
-            wsum[0][lane] = x;
-            wsum[1][lane] = y;
-        }
-        __syncthreads();
-        const int64_t bt = tot_t + (warp ? wsum[0][warp - 1] : 0), bb = tot_b + (warp ? wsum[1][warp - 1] : 0);
-        if (r < a.requests) {
-            tok[r] = (int32_t)min(bt + st - t, (int64_t)INT_MAX);
-            nbk[r] = (int32_t)min(bb + sb - b, (int64_t)INT_MAX);
-            held[r] = c;
-        }
-        tot_t += wsum[0][31];
-        tot_b += wsum[1][31];
-        __syncthreads();
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t u = __shfl_up_sync(~0u, tot_t, o), v = __shfl_up_sync(~0u, tot_b, o);
+        if (lane >= o) { tot_t += u; tot_b += v; }
+    }
+    const int64_t before_t = __shfl_sync(~0u, tot_t, warp ? warp - 1 : 0), before_b = __shfl_sync(~0u, tot_b, warp ? warp - 1 : 0);
+    tot_t = __shfl_sync(~0u, tot_t, 31);
+    tot_b = __shfl_sync(~0u, tot_b, 31);
+    st += (warp ? before_t : 0) - my_t;
+    sb += (warp ? before_b : 0) - my_b;
+    for (int32_t r = first; r < past; ++r) {
+        const int32_t t = tok[r], b = nbk[r];
+        tok[r] = (int32_t)min(st, (int64_t)INT_MAX);
+        nbk[r] = (int32_t)min(sb, (int64_t)INT_MAX);
+        st += t;
+        sb += b;
     }
     const int32_t tokens = (int32_t)min(tot_t, (int64_t)a.max_tokens);
     const int32_t fresh_blocks = (int32_t)min(tot_b, (int64_t)INT_MAX);
@@ -216,66 +225,99 @@ __global__ void __launch_bounds__(kTabThreads) k_block_tables(TablesArgs a)
     }
     __syncthreads();
 
-    const int32_t gtid = blockIdx.x * kTabThreads + tid, gthreads = gridDim.x * kTabThreads;
-    for (int32_t r = gtid; r <= a.requests; r += gthreads) a.q_start[r] = tok[r];
+    // blocks held by a request before the step
+    auto have_of = [&](int32_t r) { return (int32_t)(((int64_t)held[r] + bs - 1) >> a.block_log); };
 
-    // admitted requests' shared blocks: a warp a request walks the segments of its path upwards
-    if (a.node) {
-        for (int32_t r = gtid >> 5; r < a.requests; r += gthreads >> 5) {
-            if (a.node[r] < 0) continue;
-            int32_t cur = tab_row(a, r, false).up, top = held[r] >> a.block_log, last = INT_MAX;
-            int32_t *row = a.table + (int64_t)r * a.table_width;
-            while (cur >= 0 && top > 0) {
-                const int4 seg = a.map[cur];
-                // a map of pp_chunk_map only goes down, to a segment that begins at 0
-                bool bad = seg.x >= a.n_chunks || seg.y < 0 || seg.z < 0 || seg.z >= seg.w || seg.z >= last;
-                if (!bad) {
-                    for (int32_t j = seg.z + lane; j < min(seg.w, top); j += 32) {
-                        const int64_t id = (int64_t)seg.y + (j - seg.z);
-                        if (id >= a.blocks) bad = true;
-                        row[j] = id < a.blocks ? (int32_t)id : -1;
+    if (tid < kTabWalkers) {
+        const int32_t gtid = blockIdx.x * kTabWalkers + tid, gthreads = gridDim.x * kTabWalkers;
+        for (int32_t r = gtid; r <= a.requests; r += gthreads) a.q_start[r] = tok[r];
+        // admitted requests' shared blocks: a warp a request walks the segments of its path upwards
+        if (a.node) {
+            for (int32_t r = warp * gridDim.x + blockIdx.x; r < a.requests; r += gridDim.x * (kTabWalkers / 32)) {
+                if (a.node[r] < 0) continue;
+                int32_t cur = tab_row(a, r, false).up, top = held[r] >> a.block_log, last = INT_MAX;
+                int32_t *row = a.table + (int64_t)r * a.table_width;
+                while (cur >= 0 && top > 0) {
+                    const int4 seg = a.map[cur];
+                    // a map of pp_chunk_map only goes down, to a segment that begins at 0
+                    bool bad = seg.x >= a.n_chunks || seg.y < 0 || seg.z < 0 || seg.z >= seg.w || seg.z >= last;
+                    if (!bad) {
+                        for (int32_t j = seg.z + lane; j < min(seg.w, top); j += 32) {
+                            const int64_t id = (int64_t)seg.y + (j - seg.z);
+                            if (id >= a.blocks) bad = true;
+                            row[j] = id < a.blocks ? (int32_t)id : -1;
+                        }
                     }
+                    if (__any_sync(~0u, bad)) {
+                        if (lane == 0) kv_bounds(a.status);
+                        break;
+                    }
+                    top = min(top, seg.z);
+                    last = seg.z;
+                    cur = seg.x;
                 }
-                if (__any_sync(~0u, bad)) {
-                    if (lane == 0) kv_bounds(a.status);
-                    break;
-                }
-                top = min(top, seg.z);
-                last = seg.z;
-                cur = seg.x;
             }
         }
+        // new blocks
+        for (int64_t x = gtid; x < fresh_blocks; x += gthreads) {
+            const int32_t i = (int32_t)x, r = tab_find(nbk, a.requests, i);
+            int32_t id = i < spare ? a.free_blocks[head + i] : -1;
+            if (id >= a.blocks || (id < 0 && i < spare)) { kv_bounds(a.status); id = -1; }
+            a.table[(int64_t)r * a.table_width + have_of(r) + (i - nbk[r])] = id;
+        }
+        return;
     }
-    // new blocks
-    for (int64_t x = gtid; x < fresh_blocks; x += gthreads) {
-        const int32_t i = (int32_t)x, r = tab_find(nbk, a.requests, i);
-        const int32_t j = (int32_t)(((int64_t)held[r] + bs - 1) >> a.block_log) + (i - nbk[r]);
-        int32_t id = i < spare ? a.free_blocks[head + i] : -1;
-        if (id >= a.blocks || (id < 0 && i < spare)) { kv_bounds(a.status); id = -1; }
-        a.table[(int64_t)r * a.table_width + j] = id;
-    }
+
     // tokens; a running request's last partly filled block is the only old entry read
-    for (int64_t x = gtid; x < a.max_tokens; x += gthreads) {
-        const int32_t i = (int32_t)x;
-        int64_t slot = -1;
-        int32_t pos = 0;
-        if (i < tokens) {
-            const int32_t r = tab_find(tok, a.requests, i);
-            pos = held[r] + (i - tok[r]);
-            const int32_t j = pos >> a.block_log;
-            const int32_t have = (int32_t)(((int64_t)held[r] + bs - 1) >> a.block_log);
-            int32_t id;
-            if (j < have) {
-                id = a.table[(int64_t)r * a.table_width + j];
-                if (id < 0 || id >= a.blocks) kv_bounds(a.status);
-            } else {
-                const int64_t k = (int64_t)nbk[r] + (j - have);
-                id = k < spare ? a.free_blocks[head + k] : -1;
+    constexpr int kRun = kTabRun;
+    const int64_t runs = ((int64_t)a.max_tokens + kRun - 1) / kRun;
+    const int64_t step = (int64_t)gridDim.x * (kTabThreads - kTabWalkers);
+    for (int64_t x = (int64_t)blockIdx.x * (kTabThreads - kTabWalkers) + tid - kTabWalkers; x < runs; x += step) {
+        const int32_t i0 = (int32_t)(kRun * x), n = min(kRun, a.max_tokens - i0);
+        int64_t slot[kRun];
+        int32_t pos[kRun];
+        int32_t r = i0 < tokens ? tab_find(tok, a.requests, i0) : 0, block = -1, id = -1;
+#pragma unroll
+        for (int y = 0; y < kRun; ++y) {
+            const int32_t i = i0 + y;
+            slot[y] = -1;
+            pos[y] = 0;
+            if (i >= tokens || y >= n) continue;
+            if (i >= tok[r + 1]) {                      // the next request with new tokens
+                do ++r;
+                while (i >= tok[r + 1]);
+                block = -1;
             }
-            if (id >= 0 && id < a.blocks) slot = ((int64_t)id << a.block_log) + (pos & (bs - 1));
+            pos[y] = held[r] + (i - tok[r]);
+            const int32_t j = pos[y] >> a.block_log;
+            if (j != block) {
+                block = j;
+                const int32_t have = have_of(r);
+                if (j < have) {
+                    id = a.table[(int64_t)r * a.table_width + j];
+                    if (id < 0 || id >= a.blocks) kv_bounds(a.status);
+                } else {
+                    const int64_t k = (int64_t)nbk[r] + (j - have);
+                    id = k < spare ? a.free_blocks[head + k] : -1;
+                }
+            }
+            if (id >= 0 && id < a.blocks) slot[y] = ((int64_t)id << a.block_log) + (pos[y] & (bs - 1));
         }
-        a.slot[i] = slot;
-        a.position[i] = pos;
+        if (n == kRun && a.wide) {
+#pragma unroll
+            for (int y = 0; y < kRun; y += 2)
+                *reinterpret_cast<longlong2 *>(a.slot + i0 + y) = make_longlong2(slot[y], slot[y + 1]);
+#pragma unroll
+            for (int y = 0; y < kRun; y += 4)
+                *reinterpret_cast<int4 *>(a.position + i0 + y) = make_int4(pos[y], pos[y + 1], pos[y + 2], pos[y + 3]);
+        } else {
+#pragma unroll
+            for (int y = 0; y < kRun; ++y)
+                if (y < n) {
+                    a.slot[i0 + y] = slot[y];
+                    a.position[i0 + y] = pos[y];
+                }
+        }
     }
 }
 
@@ -466,9 +508,11 @@ extern "C" pp_status pp_block_tables(pp_kv *kv, int32_t requests, const int32_t 
     if (s != PP_OK) return s;
     TablesArgs a = {requests, n_chunks, free_count, table_width, max_tokens, kv->blocks, kv->block_log,
                     length, cached, node, reinterpret_cast<const int4 *>(chunk_map), free_blocks, free_head,
-                    free_head_out, block_table, position, q_start, slot_map, kv->d_status};
-    // a CTA for every 2,048 tokens or 64 table rows, as many as there are SMs at most
-    const int64_t want = std::max<int64_t>((max_tokens + 2047) / 2048, (requests + 63) / 64);
+                    free_head_out, block_table, position, q_start, slot_map, kv->d_status,
+                    aligned16(slot_map) && aligned16(position)};
+    // a CTA for every kTabPass tokens (one pass of its warps) or 8 table rows (a warp's walk each), as many as
+    // there are SMs at most
+    const int64_t want = std::max<int64_t>(((int64_t)max_tokens + kTabPass - 1) / kTabPass, (requests + 7) / 8);
     const int grid = (int)std::min<int64_t>(std::max<int64_t>(want, 1), kv->sm_count);
     const size_t smem = sizeof(int32_t) * (3 * (size_t)requests + 2);
     k_block_tables<<<grid, kTabThreads, smem, (cudaStream_t)stream>>>(a);
