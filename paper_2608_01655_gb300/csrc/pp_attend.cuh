@@ -74,8 +74,9 @@ struct Keys {
 // An item with nothing to see still has a tile, so that its rows are written.
 template <int KT> __device__ __forceinline__ int32_t key_tiles(Keys k) { return k.hi < k.lo ? 1 : k.hi / KT - k.lo / KT + 1; }
 
-// Shape: static constants KT (keys per tile) and, for a request, inner(a, q)
-// items for each of outer(a) (heads), keys(a, q, i) of inner item i.
+// Shape: static constants KT (keys per tile), extra (below) and many (requests
+// may have many items) and, for a request, inner(a, q) items for each of outer(a)
+// (heads), keys(a, q, i) of inner item i.
 struct Place {
     int32_t r, outer, inner, off;       // an item and a tile of it
 };
@@ -86,11 +87,11 @@ struct SchedShared {
     Place first, end;                   // where the stretch begins; the tile after it
 };
 
+// for sums below 2^57
 __device__ __forceinline__ int64_t warp_sum64(int64_t x)
 {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(~0u, x, o);
-    return x;
+    const uint32_t low = (uint32_t)(x & 0x3ffffff), high = (uint32_t)(x >> 26);
+    return (int64_t)__reduce_add_sync(~0u, low) + ((int64_t)__reduce_add_sync(~0u, high) << 26);
 }
 __device__ __forceinline__ Req shfl_req(const Req &q, int src)
 {
@@ -164,12 +165,28 @@ template <class S> __device__ __forceinline__ bool schedule(const AttendDev &a, 
     if (report && threadIdx.x == 0 && a.c.q_start[0] != 0) kv_bounds(a.status);
     Req q;
     int64_t mine, tiles = 0, items = 0, excl, excl_items = 0, before = 0;   // of one head: this lane's request, all of its requests
-    for (int32_t base = 0; base < R; base += T) {
-        const int32_t r = base + me;
+    if (S::many && few) {
+        // requests of many items: a warp sums up one after another, lanes taking items
+        for (int32_t r = threadIdx.x >> 5; r < R; r += blockDim.x >> 5) {
+            q = load_req(a, r, report);
+            int64_t sum = 0;
+            for (int32_t i = lane, n = S::inner(a, q); i < n; i += 32) sum += key_tiles<S::KT>(S::keys(a, q, i));
+            sum = warp_sum64(sum);
+            if (lane == 0) sm.warp_sum[r] = sum;
+        }
+        __syncthreads();
         q = Req{0, 0, 0};
-        if (r < R) q = load_req(a, r, report);
-        tiles += mine = request_tiles<S>(a, q);
-        items += S::inner(a, q);
+        if (lane < R) q = load_req(a, lane, false);
+        tiles = mine = lane < R ? sm.warp_sum[lane] : 0;
+        items = S::inner(a, q);
+    } else {
+        for (int32_t base = 0; base < R; base += T) {
+            const int32_t r = base + me;
+            q = Req{0, 0, 0};
+            if (r < R) q = load_req(a, r, report);
+            tiles += mine = request_tiles<S>(a, q);
+            items += S::inner(a, q);
+        }
     }
     tiles = scan64(tiles, &excl, sm.warp_sum, few) * outer;
     if (tiles == 0) return false;

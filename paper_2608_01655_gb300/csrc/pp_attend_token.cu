@@ -35,6 +35,7 @@ template <int HALVES> struct Layout {
 struct Shape {
     static constexpr int KT = token::KT;
     static constexpr int32_t extra = 1;
+    static constexpr bool many = false;
     static __device__ __forceinline__ int32_t row_tiles(const AttendDev &a) { return (a.c.group + kRows - 1) / kRows; }
     static __device__ __forceinline__ int32_t outer(const AttendDev &a) { return a.kv_heads * row_tiles(a); }
     // K/V head of outer item x, and which 16 of its query heads
