@@ -504,3 +504,98 @@ def test_refusals(pp):
         kv.sync()
     with pytest.raises(RuntimeError):
         pp.pp_paged_attention(kv, **ok)
+
+
+@pytest.mark.parametrize("fresh", [[1, 1, 1], [70, 1, 140]])
+@pytest.mark.parametrize("dim,lead", [(128, 8), (64, 16), (72, 8)])
+def test_output_in_a_wider_buffer(pp, fresh, dim, lead):
+    """Output rows inside rows of another buffer, at 16-byte boundaries that are and are not 32-byte ones."""
+    torch.manual_seed(6)
+    length = [f + 90 for f in fresh]
+    blocks = sum(-(-n // 16) for n in length)
+    kc, vc = (torch.randn((blocks, 16, 2, dim), device="cuda").to(torch.bfloat16) for _ in range(2))
+    table, at = np.zeros((3, 20)), 0
+    for r, n in enumerate(length):
+        table[r, :-(-n // 16)] = np.arange(at, at - (-n // 16))
+        at -= -n // 16
+    table = _i32(table)
+    q = torch.randn((sum(fresh), 6, dim), device="cuda").to(torch.bfloat16)
+    buf = torch.full((sum(fresh), 6 * dim + 2 * lead), 3.0, dtype=torch.bfloat16, device="cuda")
+    out = buf[:, lead:-lead].unflatten(1, (6, dim))
+    q_start = np.concatenate([[0], np.cumsum(fresh)])
+    with pp.KVCache.like(kc) as kv:
+        pp.pp_paged_attention(kv, q, kc, vc, table, _i32(q_start), _i32(length), max(fresh), out, dim ** -0.5)
+        kv.sync()
+    want, _, tol, _ = ref.attention(q, kc, vc, table, q_start, length, dim ** -0.5, 0)
+    assert not ((out.double() - want).abs() > tol).any()
+    assert (buf[:, :lead] == 3).all() and (buf[:, -lead:] == 3).all()
+
+
+def test_many_requests_of_chunks(pp):
+    """More requests than the kernel has threads, most of them small."""
+    rng = np.random.default_rng(9)
+    _attention_case(pp, [int(x) for x in rng.integers(0, 6, size=1100)], [int(x) for x in rng.integers(0, 60, size=1100)],
+                    4, 2, 64, seed=9)
+
+
+@pytest.mark.parametrize("fresh", [[1, 1, 1, 1], [90, 200, 3, 1]])
+def test_a_query_out_of_range_stays_alone(pp, fresh):
+    """NaN and infinite queries change their own rows only; the same call twice gives the same bits."""
+    torch.manual_seed(7)
+    length = [f + 300 for f in fresh]
+    need = [-(-n // 16) for n in length]
+    kc, vc = (torch.randn((sum(need), 16, 2, 64), device="cuda").to(torch.float16) for _ in range(2))
+    table, at = np.zeros((4, 40)), 0
+    for r, n in enumerate(need):
+        table[r, :n] = np.arange(at, at + n)
+        at += n
+    q = torch.randn((sum(fresh), 8, 64), device="cuda").to(torch.float16)
+    args = (_i32(table), _i32(np.concatenate([[0], np.cumsum(fresh)])), _i32(length), max(fresh))
+    clean, again, out = (torch.empty_like(q) for _ in range(3))
+    with pp.KVCache.like(kc) as kv:
+        pp.pp_paged_attention(kv, q, kc, vc, *args, clean, 0.125)
+        pp.pp_paged_attention(kv, q, kc, vc, *args, again, 0.125)
+        bad = q.clone()
+        bad[1, 3, 5] = float("nan")
+        bad[2, 7] = float("inf")
+        pp.pp_paged_attention(kv, bad, kc, vc, *args, out, 0.125)
+        kv.sync()
+    assert torch.equal(clean.view(torch.int16), again.view(torch.int16))
+    hit = torch.zeros(out.shape[:2], dtype=torch.bool, device="cuda")
+    hit[1, 3] = hit[2, 7] = True
+    assert torch.equal(out[~hit], clean[~hit]) and out[hit].isnan().all()
+
+
+def test_chunks_in_a_graph(pp):
+    torch.manual_seed(8)
+    kc, vc = (torch.randn((64, 16, 2, 128), device="cuda").to(torch.bfloat16) for _ in range(2))
+    table = _i32(np.arange(64).reshape(2, 32))
+    q_start, lens = _i32([0, 60, 200]), _i32([500, 300])
+    q = torch.randn((200, 8, 128), device="cuda").to(torch.bfloat16)
+    out = torch.empty_like(q)
+    with pp.KVCache.like(kc) as kv:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            pp.pp_paged_attention(kv, q, kc, vc, table, q_start, lens, 140, out, 0.09)
+        q_start.copy_(_i32([0, 100, 180]))
+        lens.copy_(_i32([100, 512]))
+        out.fill_(2)
+        graph.replay()
+        kv.sync()
+    want, _, tol, _ = ref.attention(q[:180], kc, vc, table, [0, 100, 180], [100, 512], 0.09, 0)
+    assert not ((out[:180].double() - want).abs() > tol).any() and (out[180:] == 2).all()
+
+
+def test_block_tables_in_unaligned_buffers(pp):
+    """Slot map and positions that start between 16-byte boundaries."""
+    slots = torch.zeros(101, dtype=torch.int64, device="cuda")[1:]
+    pos = torch.zeros(103, dtype=torch.int32, device="cuda")[3:]
+    table = _i32(np.full((2, 8), -1))
+    with pp.KVCache(20, 16, 1, 8) as kv:
+        q, out = _i32([0] * 3), _i32([0])
+        pp.pp_block_tables(kv, _i32([50, 37]), _i32([0, 0]), table, slots, pos, q, _i32(np.arange(20)[::-1].copy()),
+                           _i32([2]), out)
+        kv.sync()
+    want = ref.block_tables([50, 37], [0, 0], None, None, np.full((2, 8), -1), np.arange(20)[::-1], 2, 16, 100)
+    for got, exp in zip((table, slots, pos, q, out[0]), want):
+        assert np.array_equal(got.cpu().numpy(), exp)
