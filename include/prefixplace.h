@@ -474,8 +474,8 @@ enum { PP_KV_BF16 = 0, PP_KV_F16 = 1 };
  *                 0, 0, 0: contiguous [blocks][block_size][kv_heads][head_dim]
  *   stream        stream of the set-up; the call synchronises it
  *   out           receives the handle (NULL on failure)
- * The handle owns a device status word and scratch of the attention.  Its
- * device (the current one) must be current in later calls.  pp_kv_sync reads
+ * The handle owns a device status word and 40 MB of scratch of the attention
+ * (on 152 SMs).  Its device (the current one) must be current in later calls.  pp_kv_sync reads
  * the status.  pp_paged_attention calls on one handle use its scratch and must
  * not overlap on the GPU; on one stream they never do.  No call after this one
  * allocates or synchronises, so all can be captured in a CUDA graph.

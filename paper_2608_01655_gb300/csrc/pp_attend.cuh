@@ -9,7 +9,10 @@
 // out by itself from q_start and length.  A stretch that covers an item only
 // in part gives a piece (output not yet divided, maximum, sum); the last CTA
 // to finish of an item's (first of a group of pieces, then of its groups) joins
-// them in a fixed order.  No CTA waits for another.
+// them in a fixed order.  No CTA waits for another.  Equal stretches cost two
+// joins a CTA at most, 10 to 20 thousand cycles that mostly run beside other
+// tiles; whole items only would leave SMs idle (8 requests of 60 to 700 new tokens
+// after up to 8,192: 144 items of up to 70 tiles on 152 SMs, 39 tiles a stretch).
 #pragma once
 
 #include <cuda.h>
@@ -32,7 +35,7 @@ struct AttendDev {
     int32_t *count;                     // [2][slots] arrivals, left at 0 by every launch
 };
 
-constexpr int64_t kAttendLimitCycles = 1000ll * 1000 * 1000;  // one wait gives up after about 0.5 s
+constexpr int64_t kAttendLimitCycles = 4000ll * 1000 * 1000;  // one wait gives up after about 2 s
 constexpr int kJoinGroup = 16;                              // pieces joined at a time
 
 // ---------------------------------------------------------------------------
@@ -391,8 +394,8 @@ __device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, volatil
 // with 64.  16-byte copies, a warp's 32 at a time, reach 9 TB/s (one warp an SM)
 // to 21 (eight) from L2, but each costs the warp some five instructions, and
 // operands of the tensor cores need a fence after them.  Single tokens take the
-// second way with eight warps (128 requests, blocks of 16: 256 us against 297);
-// chunks, whose warps have the softmax to do, the first (8,192 tokens after
+// second way with eight warps (128 requests, 1.52 GB in blocks of 16: 256 us against
+// 297); chunks, whose warps have the softmax to do, the first (8,192 tokens after
 // 24,576: 1.97 ms against 2.31 with V by copies).
 __device__ __forceinline__ void copy16(uint32_t dst, const char *src, uint32_t bytes)
 {

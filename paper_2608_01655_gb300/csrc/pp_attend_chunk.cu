@@ -14,10 +14,20 @@
 // 2^12 then, which both 16-bit types hold as precisely as 1.
 //
 // Warps: 0-3 and 4-7 the stages' softmax, 8-11 the outputs of both, 12 and 13 the
-// stages' products, 14 and 15 the copies of K and V.  V tiles that not every row sees in full are looked
-// over by the softmax warps: an infinity or a NaN there would pass through a
-// weight of 0, so it is replaced by 0 and added in the epilogue to the rows that
-// do see it.
+// stages' products, 14 and 15 the copies of K and V.  V tiles that not every row
+// sees in full are looked over by the softmax warps: an infinity or a NaN there
+// would pass through a weight of 0, so it is replaced by 0 and added in the
+// epilogue to the rows that do see it.
+//
+// What bounds it: at width 128 a tile of both stages is 2,048 cycles of products
+// (57% tensor cycles in a 2,048-token chunk after 4,096), 1,100 to 1,300 cycles of
+// softmax a stage (128 exponentials a thread at 5 cycles, two warps a scheduler)
+// and 1,000 cycles of hand-over; at width 64 the products are half and the
+// exponentials bound it.  256 rows an item is what tensor memory holds (two S and
+// two O of 128 columns).
+// Measured: 8,192 new tokens after 24,576 (28 heads on 4, width 128) 1.90 ms, 1,770
+// TFLOP/s or 95% of the measured library product; 8,192 tokens of 16 heads from
+// nothing 225 us, 1,200 TFLOP/s; the same at width 64 175 us, 780 TFLOP/s.
 #include <algorithm>
 #include <new>
 #include <type_traits>

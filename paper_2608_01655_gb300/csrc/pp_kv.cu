@@ -155,7 +155,10 @@ __device__ __forceinline__ int32_t tab_find(const int32_t *pre, int32_t n, int32
 // quarter of the warps walks the admitted requests' paths, a chain of dependent
 // loads a segment, and fills in the new blocks, while the others write the tokens'
 // slots and positions, four a thread.  Latency bounds it up to some hundred
-// thousand new tokens, then the 12 bytes a token.
+// thousand new tokens, then the 12 bytes a token.  Measured: 16 requests of a
+// token each 5 us, 192 admitted with 58,000 new tokens 7 us, 2,048 requests with 2.3
+// million 16 us (1.7 TB/s; 4 us at the copy rate: the scan is 4 us, each of five
+// passes over the tokens a search in the prefix sums and a table look-up).
 constexpr int kTabWalkers = kTabThreads / 4;
 constexpr int kTabRun = 4;                          // tokens of a thread
 constexpr int kTabPass = kTabRun * (kTabThreads - kTabWalkers);    // tokens that a CTA writes at once
@@ -322,7 +325,9 @@ __global__ void __launch_bounds__(kTabThreads) k_block_tables(TablesArgs a)
 }
 
 // ---------------------------------------------------------------------------
-// Write of new rows: 16 bytes of K and of V a thread and step.
+// Write of new rows: 16 bytes of K and of V a thread and step, a CTA some whole
+// tokens.  Bound by memory: 30,011 tokens of 4 heads of 128 (123 MB) 18.4 us,
+// 6.7 TB/s; 64 tokens 4 us, a launch.
 // ---------------------------------------------------------------------------
 struct WriteArgs {
     int32_t tokens, per_token, per_head, tokens_per_cta;     // vectors per token and per head
