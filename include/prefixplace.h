@@ -557,6 +557,7 @@ pp_status pp_block_tables(pp_kv *kv, int32_t requests, const int32_t *length, co
 
 /*
  * pp_kv_write -- store the new tokens' K and V rows at their slots.
+ *   tokens        0 .. 2^30
  *   k, v          device [tokens][kv_heads][head_dim], token and head strides in
  *                 elements (positive multiples of 8; bases aligned to 16 bytes)
  *   slot_map      device [tokens]; a negative slot's token is left out; no slot
@@ -587,7 +588,7 @@ pp_status pp_kv_write(pp_kv *kv, int32_t tokens, const void *k, int64_t k_token_
  *   q_start       device [requests + 1], ascending from 0
  *   length        device [requests]: tokens of the request, the new ones included
  *   max_q         host: the most new tokens of any request.  It chooses the
- *                 kernel (1: single tokens) and nothing else
+ *                 kernel (few rows or many) and nothing else
  *   window        0: none
  *   scale         > 0
  *   lse           device [tokens][q_heads] out, or NULL: natural log of the sum
@@ -598,7 +599,8 @@ pp_status pp_kv_write(pp_kv *kv, int32_t tokens, const void *k, int64_t k_token_
  * may depend on which other requests are in the call.
  * A block out of range that a query would see (its rows read as zeros), or
  * lengths and offsets out of range (cut to the range), set PP_EBOUNDS.
- * Errors: PP_EINVAL (also tokens * q_heads / kv_heads above 2^30), PP_ECUDA.
+ * Errors: PP_EINVAL (also q_heads above 2^20, tokens * q_heads / kv_heads above
+ * 2^30), PP_ECUDA.
  */
 pp_status pp_paged_attention(pp_kv *kv, int32_t requests, int32_t tokens, int32_t q_heads, const void *q,
                              int64_t q_token_stride, int64_t q_head_stride, const void *k_cache,

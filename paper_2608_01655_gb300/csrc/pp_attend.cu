@@ -69,9 +69,11 @@ pp_status prepare_attend()
     return s == PP_OK ? prepare_attend_chunk() : s;
 }
 
+constexpr int64_t kFewRows = 32;
+
 pp_status launch_attend(pp_kv *kv, const AttendArgs &c, cudaStream_t st)
 {
-    return c.max_q == 1 ? launch_attend_token(kv, c, st) : launch_attend_chunk(kv, c, st);
+    return (int64_t)c.max_q * c.group <= kFewRows ? launch_attend_token(kv, c, st) : launch_attend_chunk(kv, c, st);
 }
 
 }  // namespace pp

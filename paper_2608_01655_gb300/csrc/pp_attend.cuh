@@ -36,7 +36,6 @@ struct AttendDev {
 };
 
 constexpr int64_t kAttendLimitCycles = 4000ll * 1000 * 1000;  // one wait gives up after about 2 s
-constexpr int kJoinGroup = 16;                              // pieces joined at a time
 
 // ---------------------------------------------------------------------------
 // Requests and their items

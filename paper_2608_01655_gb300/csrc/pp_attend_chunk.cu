@@ -691,8 +691,9 @@ template <int HALVES> struct Pieces {
     }
     // joins a stage's n pieces p0, p0 + step, ... into the output (final) or into p0
     template <typename T>
-    __device__ __forceinline__ void join(int s, int t, int32_t p0, int32_t n, int32_t step, const OutRow<T> *final) const
+    __device__ __forceinline__ void join(int s, int t, int32_t p0, int32_t n, int32_t step, const OutRow<T> &out, bool final) const
     {
+        if (!out.live) return;
         float top = -INFINITY, sum = 0.f;
         for (int32_t p = 0; p < n; ++p) top = fmaxf(top, __ldcg(stat(p0 + p * step, s, t)));
         const float base = top == -INFINITY ? 0.f : top;
@@ -718,8 +719,8 @@ template <int HALVES> struct Pieces {
                 }
             }
             if (final) {
-                final->put(o, c, scale);
-                final->put(o + 16, c + 16, scale);
+                out.put(o, c, scale);
+                out.put(o + 16, c + 16, scale);
             } else {
 #pragma unroll
                 for (int y = 0; y < 32; y += 4)
@@ -727,7 +728,7 @@ template <int HALVES> struct Pieces {
             }
         }
         if (final) {
-            final->put_lse(top, sum);
+            out.put_lse(top, sum);
         } else {
             *stat(p0, s, t) = top;
             stat(p0, s, t)[kRows] = sum;
@@ -796,7 +797,7 @@ __device__ __forceinline__ void output_role(const AttendDev &a, const SchedShare
                 if (whole) {
                     out.put(o, c, inv);
                     out.put(o + 16, c + 16, inv);
-                } else {
+                } else if (out.live) {
 #pragma unroll
                     for (int y = 0; y < 32; y += 4)
                         ps.at(mine, s, c, t)[y / 4 * kRows] = make_float4(o[y], o[y + 1], o[y + 2], o[y + 3]);
@@ -813,7 +814,12 @@ __device__ __forceinline__ void output_role(const AttendDev &a, const SchedShare
         }
         if (!whole) {
             const int32_t pieces = owner(g0 + cur.tiles - 1, line, ctas) - ps.cta0 + 1;
-            const int32_t groups = (pieces + kJoinGroup - 1) / kJoinGroup;
+            // A piece is up to 128 KB and a join's rate is one SM's, so many pieces are joined in groups of
+            // their square root, a group by a CTA: 8 in a row instead of 16 of 16 pieces.
+            int32_t size = pieces;
+            if (pieces > 4)
+                for (size = 2; size * size < pieces;) ++size;
+            const int32_t groups = (pieces + size - 1) / size;
             // true in the CTA that arrives last of `of`
             auto arrive = [&](int32_t *count, int32_t of) {
                 __threadfence();
@@ -827,19 +833,19 @@ __device__ __forceinline__ void output_role(const AttendDev &a, const SchedShare
                 return *last != 0;
             };
             // first a group's pieces, then the groups
-            int32_t p0 = mine / kJoinGroup * kJoinGroup, n = min(kJoinGroup, pieces - p0), step = 1;
+            int32_t p0 = mine / size * size, n = min(size, pieces - p0), step = 1;
             int32_t *count = a.count + piece_slot(ps.cta0, p0);
             while (arrive(count, n)) {
                 const bool final = step > 1 || groups == 1;
 #pragma unroll 1
                 for (int s = 0; s < stages; ++s) {
                     const OutRow<T> out(a, cur, stage_row(cur, s) + t);
-                    ps.join(s, t, p0, n, step, final ? &out : nullptr);
+                    ps.join(s, t, p0, n, step, out, final);
                 }
                 if (final) break;
                 p0 = 0;
                 n = groups;
-                step = kJoinGroup;
+                step = size;
                 count = a.count + 2 * gridDim.x + piece_slot(ps.cta0, 0);
             }
         }
@@ -968,8 +974,6 @@ pp_status prepare_attend_chunk()
 
 pp_status launch_attend_chunk(pp_kv *kv, const AttendArgs &c, cudaStream_t st)
 {
-    if ((int64_t)c.tokens * c.group > 1 << 30)
-        return fail(PP_EINVAL, "tokens * q_heads / kv_heads must be at most 2^30");
     if (kv->dtype == PP_KV_BF16)
         return kv->dim > 64 ? launch_t<__nv_bfloat16, 2>(kv, c, st) : launch_t<__nv_bfloat16, 1>(kv, c, st);
     return kv->dim > 64 ? launch_t<__half, 2>(kv, c, st) : launch_t<__half, 1>(kv, c, st);

@@ -16,6 +16,8 @@
 // of the line and the first rows' latency, 5 the joins of 38 pieces an item.
 // DRAM 69% of its cycles and 18% of the tensor instructions' in the former.
 #include <climits>
+#include <cstring>
+#include <type_traits>
 
 #include "pp_attend.cuh"
 
@@ -25,7 +27,8 @@ namespace token {
 constexpr int kWarps = 8, kThreads = 32 * kWarps;
 constexpr int kKeys = 16;                           // keys of a warp
 constexpr int KT = kKeys * kWarps;                  // keys per tile
-constexpr int kRows = 16;                           // query heads of an item
+constexpr int kRows = 16;                           // rows of an item
+constexpr int kJoinGroup = 16;                      // pieces (8 KB) joined at a time, then their groups
 
 template <int HALVES> struct Layout {
     static constexpr int half = kKeys * 128;                    // bytes of 64 columns of a warp's keys
@@ -38,20 +41,22 @@ template <int HALVES> struct Layout {
     static constexpr int bytes = 128 + ring + join;
 };
 
+// Rows are (token, head of the group), token first; an item is 16 of them.
 struct Shape {
     static constexpr int KT = token::KT;
     static constexpr int32_t extra = 1;
     static constexpr bool many = false;
-    static __device__ __forceinline__ int32_t row_tiles(const AttendDev &a) { return (a.c.group + kRows - 1) / kRows; }
-    static __device__ __forceinline__ int32_t outer(const AttendDev &a) { return a.kv_heads * row_tiles(a); }
-    // K/V head of outer item x, and which 16 of its query heads
-    static __device__ __forceinline__ int32_t head(const AttendDev &a, int32_t x) { return a.c.group <= kRows ? x : x / row_tiles(a); }
-    static __device__ __forceinline__ int32_t row0(const AttendDev &a, int32_t x) { return a.c.group <= kRows ? 0 : x % row_tiles(a) * kRows; }
-    static __device__ __forceinline__ int32_t inner(const AttendDev &, const Req &q) { return q.q_len; }
+    static __device__ __forceinline__ int32_t outer(const AttendDev &a) { return a.kv_heads; }
+    static __device__ __forceinline__ int32_t rows(const AttendDev &a, const Req &q) { return q.q_len * a.c.group; }
+    static __device__ __forceinline__ int32_t inner(const AttendDev &a, const Req &q) { return (rows(a, q) + kRows - 1) / kRows; }
+    static __device__ __forceinline__ int32_t pos(const AttendDev &a, const Req &q, int32_t row)
+    {
+        return q.length - q.q_len + div_group(a, row);
+    }
     static __device__ __forceinline__ Keys keys(const AttendDev &a, const Req &q, int32_t i)
     {
-        const int32_t pos = q.length - q.q_len + i;
-        return {pos < 0 ? 0 : first_key(a, pos), pos};
+        const int32_t r0 = i * kRows, r1 = min(r0 + kRows, rows(a, q)) - 1;
+        return {first_key(a, max(pos(a, q, r0), 0)), pos(a, q, r1)};
     }
 };
 }  // namespace token
@@ -95,6 +100,28 @@ __device__ __forceinline__ uint32_t row_at(int row, int piece)
     return (piece >> 3) * (kKeys * 128) + row * 128 + (((piece ^ row) & 7) << 4);
 }
 
+// 16-bit halves that are infinite or NaN become 0
+template <typename T> __device__ __forceinline__ uint32_t finite_only(uint32_t x)
+{
+    constexpr uint32_t e = std::is_same<T, __nv_bfloat16>::value ? 0x7f80u : 0x7c00u;
+    if ((x & e) == e) x &= 0xffff0000u;
+    if ((x & e << 16) == e << 16) x &= 0xffffu;
+    return x;
+}
+template <typename T> __device__ __forceinline__ float half_value(uint32_t bits)
+{
+    const uint16_t h = (uint16_t)bits;
+    T v;
+    memcpy(&v, &h, 2);
+    return KvType<T>::to_float(v);
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t addr)
+{
+    uint32_t x;
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(addr));
+    return x;
+}
+
 // both 16-bit halves of a register kept or cleared
 __device__ __forceinline__ uint32_t keep(bool lo, bool hi) { return (lo ? 0xffffu : 0u) | (hi ? 0xffff0000u : 0u); }
 
@@ -132,7 +159,7 @@ template <int HALVES> struct Feed {
             const int32_t j0 = first(i), in_block = (1 << a.block_log) - 1;
             const int32_t b0 = __shfl_sync(~0u, lower, i & 31), b1 = __shfl_sync(~0u, upper, i & 31);
             if (j0 <= cur.k.hi && j0 + kKeys - 1 >= cur.k.lo) {
-                const int64_t token_bytes = 2 * a.token_stride, head = 2 * Shape::head(a, cur.outer) * a.head_stride;
+                const int64_t token_bytes = 2 * a.token_stride, head = 2 * cur.outer * a.head_stride;
                 const int64_t at0 = head + max(b0, 0) * 2 * a.block_stride + (j0 & in_block) * token_bytes;
                 const int64_t at1 = head + max(b1, 0) * 2 * a.block_stride + ((j0 + 8) & in_block) * token_bytes;
                 const char *k = static_cast<const char *>(a.c.k_cache), *v = static_cast<const char *>(a.c.v_cache);
@@ -183,21 +210,29 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_token(const __grid_const
     Cursor<Shape> cur(a, sched);
     uint32_t slot = 0;
     do {
-        const int32_t head = Shape::head(a, cur.outer), row0 = Shape::row0(a, cur.outer), rows = min(kRows, a.c.group - row0);
-        const int32_t tok = cur.q.first + cur.inner;
-        const T *qp = static_cast<const T *>(a.c.q) + (int64_t)tok * a.c.q_token_stride +
-                      (int64_t)(head * a.c.group + row0) * a.c.q_head_stride;
+        const int32_t row0 = cur.inner * kRows, rows = min(kRows, Shape::rows(a, cur.q) - row0);
+        auto q_row = [&](int32_t row, int64_t token_stride, int64_t head_stride) {      // place of the item's row
+            const int32_t tok = div_group(a, row0 + row);
+            return (int64_t)(cur.q.first + tok) * token_stride +
+                   (int64_t)(cur.outer * a.c.group + row0 + row - tok * a.c.group) * head_stride;
+        };
         uint32_t qf[KS][4];
 #pragma unroll
-        for (int k = 0; k < KS; ++k) {
+        for (int x = 0; x < 2; ++x) {
+            const bool in = r0 + 8 * x < rows;
+            const T *qp = static_cast<const T *>(a.c.q) + (in ? q_row(r0 + 8 * x, a.c.q_token_stride, a.c.q_head_stride) : 0);
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const int row = r0 + 8 * (x & 1), d = 16 * k + c0 + 8 * (x >> 1);
-                qf[k][x] = row < rows && d < a.dim
-                               ? __ldg(reinterpret_cast<const uint32_t *>(qp + row * a.c.q_head_stride + d))
-                               : 0u;
+            for (int k = 0; k < KS; ++k) {
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const int d = 16 * k + c0 + 8 * y;
+                    qf[k][x + 2 * y] = in && d < a.dim ? __ldg(reinterpret_cast<const uint32_t *>(qp + d)) : 0u;
+                }
             }
         }
+        // keys that all rows see; the rows of one token see the same
+        const int32_t pos0 = Shape::pos(a, cur.q, row0), pos1 = cur.k.hi;
+        const int32_t all_lo = first_key(a, pos1), all_hi = pos0;
         float o[2 * KS][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 #pragma unroll
         for (int n = 0; n < 2 * KS; ++n)
@@ -225,15 +260,20 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_token(const __grid_const
                     mma16<T>(sc[0], qf[k], b[0], b[1]);
                     mma16<T>(sc[1], qf[k], b[2], b[3]);
                 }
-                const bool edge = j0 < cur.k.lo || j0 + kKeys - 1 > cur.k.hi;
-                uint32_t vk0 = ~0u, vk1 = ~0u;                      // V rows that count, as the operand holds them
+                const bool edge = j0 < all_lo || j0 + kKeys - 1 > all_hi;
+                uint32_t vk0 = ~0u, vk1 = ~0u;                      // V rows that some row sees, as the operand holds them
                 if (edge) {
                     bool in[4];
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        const int32_t j = j0 + c0 + (x & 1) + 8 * (x >> 1);
-                        in[x] = j >= cur.k.lo && j <= cur.k.hi;
-                        if (!in[x]) sc[x >> 1][x & 1] = sc[x >> 1][2 + (x & 1)] = -INFINITY;
+                    for (int y = 0; y < 2; ++y) {
+                        const int32_t pos = r0 + 8 * y < rows ? Shape::pos(a, cur.q, row0 + r0 + 8 * y) : -1;
+                        const int32_t lo = pos < 0 ? 0 : first_key(a, pos);
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            const int32_t j = j0 + c0 + (x & 1) + 8 * (x >> 1);
+                            in[x] = j >= cur.k.lo && j <= cur.k.hi;
+                            if (j < lo || j > pos) sc[x >> 1][2 * y + (x & 1)] = -INFINITY;
+                        }
                     }
                     vk0 = keep(in[0], in[1]);
                     vk1 = keep(in[2], in[3]);
@@ -259,7 +299,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_token(const __grid_const
                         }
                     }
                 }
-                uint32_t pf[4];
+                uint32_t pf[4], strange = 0;
 #pragma unroll
                 for (int x = 0; x < 2; ++x) base[x] = m[x] == -INFINITY ? 0.f : m[x];
 #pragma unroll
@@ -281,9 +321,35 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_token(const __grid_const
                         b[1] &= vk1;
                         b[2] &= vk0;
                         b[3] &= vk1;
+                        if (pos0 != pos1) {
+                            // some rows see keys that others do not: what is not finite is added by row below
+#pragma unroll
+                            for (int x = 0; x < 4; ++x) {
+                                const uint32_t c = finite_only<T>(b[x]);
+                                strange |= c ^ b[x];
+                                b[x] = c;
+                            }
+                        }
                     }
                     mma16<T>(o[2 * n], pf, b[0], b[1]);
                     mma16<T>(o[2 * n + 1], pf, b[2], b[3]);
+                }
+                if (edge && __any_sync(~0u, strange != 0)) {
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const int32_t pos = r0 + 8 * y < rows ? Shape::pos(a, cur.q, row0 + r0 + 8 * y) : -1;
+                        const int32_t lo = pos < 0 ? 0 : first_key(a, pos);
+#pragma unroll 1
+                        for (int32_t j = max(j0, lo); j <= min(j0 + kKeys - 1, pos); ++j) {
+#pragma unroll
+                            for (int n = 0; n < 2 * KS; ++n) {
+                                const uint32_t two = lds32(vt + row_at(j - j0, n) + 2 * c0);
+                                const uint32_t odd = two ^ finite_only<T>(two);     // only what is not finite is left
+                                if (odd & 0xffffu) o[n][2 * y] += half_value<T>(two);
+                                if (odd >> 16) o[n][2 * y + 1] += half_value<T>(two >> 16);
+                            }
+                        }
+                    }
                 }
             }
             __syncwarp();
@@ -441,8 +507,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_token(const __grid_const
         }
         if (write && jr < rows) {
             const float inv = sum == 0.f ? 0.f : 1.f / sum;
-            const int32_t x = head * a.c.group + row0 + jr;
-            T *dst = static_cast<T *>(a.c.out) + (int64_t)tok * a.c.out_token_stride + x * a.c.out_head_stride + jd;
+            T *dst = static_cast<T *>(a.c.out) + q_row(jr, a.c.out_token_stride, a.c.out_head_stride) + jd;
             if constexpr (HALVES == 2) {
                 if (jd < a.dim)
                     *reinterpret_cast<uint4 *>(dst) =
@@ -454,7 +519,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_token(const __grid_const
                         make_uint2(Pack<T>::two(acc[0] * inv, acc[1] * inv), Pack<T>::two(acc[2] * inv, acc[3] * inv));
             }
             if (a.c.lse && jd == 0)
-                a.c.lse[(int64_t)tok * a.c.q_heads + x] =
+                a.c.lse[q_row(jr, a.c.q_heads, 1)] =
                     sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
         }
         __syncthreads();                                // the join's memory is free again

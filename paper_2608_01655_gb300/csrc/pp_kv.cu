@@ -530,7 +530,7 @@ extern "C" pp_status pp_kv_write(pp_kv *kv, int32_t tokens, const void *k, int64
                                  const int64_t *slot_map, void *k_cache, void *v_cache, void *stream)
 {
     if (!kv) return fail(PP_EINVAL, "null cache handle");
-    if (tokens < 0) return fail(PP_EINVAL, "tokens must be >= 0");
+    if (tokens < 0 || tokens > 1 << 30) return fail(PP_EINVAL, "tokens must be between 0 and 2^30");
     if (tokens == 0) return PP_OK;
     if (!k || !v || !slot_map || !k_cache || !v_cache) return fail(PP_EINVAL, "null pointer");
     if (!aligned16(k) || !aligned16(v) || !aligned16(k_cache) || !aligned16(v_cache))
@@ -577,9 +577,12 @@ extern "C" pp_status pp_paged_attention(pp_kv *kv, int32_t requests, int32_t tok
     if (requests < 0 || requests > kKvMaxRequests) return fail(PP_EINVAL, "requests must be between 0 and 16384");
     if (tokens < 0 || max_q < 0 || window < 0 || table_width < 1)
         return fail(PP_EINVAL, "tokens, max_q and window must be >= 0, table_width >= 1");
-    if (q_heads < 1 || q_heads % kv->heads) return fail(PP_EINVAL, "q_heads must be a positive multiple of kv_heads");
+    if (q_heads < 1 || q_heads % kv->heads || q_heads > 1 << 20)
+        return fail(PP_EINVAL, "q_heads must be a positive multiple of kv_heads, at most 2^20");
+    if ((int64_t)tokens * (q_heads / kv->heads) > 1 << 30)
+        return fail(PP_EINVAL, "tokens * q_heads / kv_heads must be at most 2^30");
     if (!(scale > 0) || scale > 1e30f) return fail(PP_EINVAL, "scale must be positive and finite");
-    if (requests == 0 || tokens == 0 || max_q == 0) return PP_OK;
+    if (requests == 0 || tokens == 0) return PP_OK;
     if (!q || !k_cache || !v_cache || !block_table || !q_start || !length || !out)
         return fail(PP_EINVAL, "null pointer");
     if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out))
