@@ -69,6 +69,15 @@ pp_status prepare_attend()
     return s == PP_OK ? prepare_attend_chunk() : s;
 }
 
+// Rows (new tokens x heads of a group) of the longest request up to which a call
+// goes to the kernel of single tokens.  That one reads K and V once for every 16
+// rows and has short items to begin and to join; the chunk kernel pays for 256 rows
+// whatever there are.  Kernel of single tokens against chunks', in us, 2 K/V heads
+// of 128, 32 requests after 5,000 tokens / 4 after 2,000 / 1 after 50,000:
+//   16 rows  52 : 61 / 22 : 34 / 34 : 52
+//   32       66 : 61 / 22 : 34 / 37 : 50
+//   64      108 : 62 / 28 : 34 / 44 : 52
+// so at 64 it loses more in batches than it gains for single requests.
 constexpr int64_t kFewRows = 32;
 
 pp_status launch_attend(pp_kv *kv, const AttendArgs &c, cudaStream_t st)

@@ -7,11 +7,11 @@
 // fixed order, are one line that is cut into equal stretches, one per CTA, so
 // that the load is even whatever the lengths are.  Every CTA works the cut
 // out by itself from q_start and length.  A stretch that covers an item only
-// in part gives a piece (output not yet divided, maximum, sum); the last CTA
-// to finish of an item's (first of a group of pieces, then of its groups) joins
-// them in a fixed order.  No CTA waits for another.  Equal stretches cost two
-// joins a CTA at most, 10 to 20 thousand cycles that mostly run beside other
-// tiles; whole items only would leave SMs idle (8 requests of 60 to 700 new tokens
+// in part gives a piece (output not yet divided, maximum, sum).  The last CTA
+// to leave a piece of an item sees to their join, in a fixed order and, of chunks,
+// with the help of those that are at their end; no CTA has to wait for another.
+// Equal stretches cost two joins a CTA at most, 10 to 20 thousand cycles that
+// mostly run beside other tiles; whole items only would leave SMs idle (8 requests of 60 to 700 new tokens
 // after up to 8,192: 144 items of up to 70 tiles on 152 SMs, 39 tiles a stretch).
 #pragma once
 
@@ -32,7 +32,7 @@ struct AttendDev {
     int32_t *status;
     float *piece;                       // pieces' outputs, [slot][...]
     float *piece_stat;                  // their maxima (log2 units) and sums
-    int32_t *count;                     // [2][slots] arrivals, left at 0 by every launch
+    int32_t *count;                     // [2][slots] state of the joins, left at 0 by every launch
 };
 
 constexpr int64_t kAttendLimitCycles = 4000ll * 1000 * 1000;  // one wait gives up after about 2 s

@@ -689,16 +689,14 @@ template <int HALVES> struct Pieces {
     {
         return reinterpret_cast<float4 *>(a.piece) + ((int64_t)(piece_slot(cta0, p) * 2 + s) * (width / 4) + c / 4) * kRows + t;
     }
-    // joins a stage's n pieces p0, p0 + step, ... into the output (final) or into p0
-    template <typename T>
-    __device__ __forceinline__ void join(int s, int t, int32_t p0, int32_t n, int32_t step, const OutRow<T> &out, bool final) const
+    // joins a stage's n pieces
+    template <typename T> __device__ __forceinline__ void join(int s, int t, int32_t n, const OutRow<T> &out) const
     {
         if (!out.live) return;
-        float top = -INFINITY, sum = 0.f;
-        for (int32_t p = 0; p < n; ++p) top = fmaxf(top, __ldcg(stat(p0 + p * step, s, t)));
-        const float base = top == -INFINITY ? 0.f : top;
+        const float top = highest(s, t, n), base = top == -INFINITY ? 0.f : top;
+        float sum = 0.f;
         for (int32_t p = 0; p < n; ++p)
-            sum = fmaf(exp2_approx(__ldcg(stat(p0 + p * step, s, t)) - base), __ldcg(stat(p0 + p * step, s, t) + kRows), sum);
+            sum = fmaf(exp2_approx(__ldcg(stat(p, s, t)) - base), __ldcg(stat(p, s, t) + kRows), sum);
         const float scale = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll 1
         for (int c = 0; c < width; c += 32) {
@@ -706,32 +704,141 @@ template <int HALVES> struct Pieces {
 #pragma unroll
             for (int y = 0; y < 32; ++y) o[y] = 0.f;
 #pragma unroll 2
-            for (int32_t p = 0; p < n; ++p) {
-                const float f = exp2_approx(__ldcg(stat(p0 + p * step, s, t)) - base);
-                const float4 *src = at(p0 + p * step, s, c, t);
-#pragma unroll
-                for (int y = 0; y < 32; y += 4) {
-                    const float4 z = __ldcg(src + y / 4 * kRows);
-                    o[y] = fmaf(f, z.x, o[y]);
-                    o[y + 1] = fmaf(f, z.y, o[y + 1]);
-                    o[y + 2] = fmaf(f, z.z, o[y + 2]);
-                    o[y + 3] = fmaf(f, z.w, o[y + 3]);
-                }
-            }
-            if (final) {
-                out.put(o, c, scale);
-                out.put(o + 16, c + 16, scale);
-            } else {
-#pragma unroll
-                for (int y = 0; y < 32; y += 4)
-                    at(p0, s, c, t)[y / 4 * kRows] = make_float4(o[y], o[y + 1], o[y + 2], o[y + 3]);
-            }
+            for (int32_t p = 0; p < n; ++p) add<32>(o, exp2_approx(__ldcg(stat(p, s, t)) - base), at(p, s, c, t));
+            out.put(o, c, scale);
+            out.put(o + 16, c + 16, scale);
         }
-        if (final) {
-            out.put_lse(top, sum);
+        out.put_lse(top, sum);
+    }
+    // 16 columns of it
+    template <typename T>
+    __device__ __forceinline__ void join_share(int s, int t, int32_t n, const OutRow<T> &out, int c, float top) const
+    {
+        if (!out.live) return;
+        const float base = top == -INFINITY ? 0.f : top;
+        float sum = 0.f, o[16];
+#pragma unroll
+        for (int y = 0; y < 16; ++y) o[y] = 0.f;
+#pragma unroll 4
+        for (int32_t p = 0; p < n; ++p) {
+            const float f = exp2_approx(__ldcg(stat(p, s, t)) - base);
+            sum = fmaf(f, __ldcg(stat(p, s, t) + kRows), sum);
+            add<16>(o, f, at(p, s, c, t));
+        }
+        out.put(o, c, sum == 0.f ? 0.f : 1.f / sum);
+        if (c == 0) out.put_lse(top, sum);
+    }
+    __device__ __forceinline__ float highest(int s, int t, int32_t n) const
+    {
+        float top = -INFINITY;
+#pragma unroll 8
+        for (int32_t p = 0; p < n; ++p) top = fmaxf(top, __ldcg(stat(p, s, t)));
+        return top;
+    }
+
+private:
+    template <int N> static __device__ __forceinline__ void add(float *o, float f, const float4 *src)
+    {
+#pragma unroll
+        for (int y = 0; y < N; y += 4) {
+            const float4 z = __ldcg(src + y / 4 * kRows);
+            o[y] = fmaf(f, z.x, o[y]);
+            o[y + 1] = fmaf(f, z.y, o[y + 1]);
+            o[y + 2] = fmaf(f, z.z, o[y + 2]);
+            o[y + 3] = fmaf(f, z.w, o[y + 3]);
+        }
+    }
+};
+
+// The join of an item, in its counters: the first counts the CTAs that have left
+// their piece (low half) and, of many pieces, those that are through with the join
+// (high half), the second the shares taken. Up to kAlone pieces are joined by the
+// CTA that is last to leave one, beside its next tiles. More would take it long (a
+// piece is up to 128 KB, and a join's rate is one SM's), so the join is cut into
+// shares of 16 columns of a stage, which the last CTA and those that are at their
+// end take one by one; those wait for it a little while, and nothing depends on it
+// that they do.  100 new tokens after 50,000 (16 heads on 2, 19 pieces an item): 61
+// us, 83 where one CTA joins; 30 after 8,000, 4 requests: 42 against 64.  Shares
+// from 3 pieces on cost more than they give (8 x 60-700 tokens after 512-8,192: 101
+// against 95 us), from 9 on less (500 tokens after 20,000: 91 against 87).
+template <typename T, int HALVES> struct Joiner {
+    static constexpr int32_t kAlone = 4;
+    static constexpr int64_t kPatience = 40000;         // cycles
+    const AttendDev &a;
+    const Cursor<Shape> &cur;
+    const Pieces<HALVES> ps;
+    const int32_t pieces;
+    volatile int32_t *word;                             // shared memory
+    __device__ __forceinline__ Joiner(const AttendDev &a_, const Cursor<Shape> &c, int64_t line, int64_t ctas, volatile int32_t *w)
+        : a(a_), cur(c), ps{a_, owner(c.g - c.off, line, ctas)},
+          pieces(owner(c.g - c.off + c.tiles - 1, line, ctas) - ps.cta0 + 1), word(w)
+    {
+    }
+    __device__ __forceinline__ int32_t mine() const { return (int32_t)blockIdx.x - ps.cta0; }
+    __device__ __forceinline__ int stages() const { return Shape::rows(a, cur.q) - stage_row(cur, 0) > kRows ? 2 : 1; }
+    __device__ __forceinline__ int32_t *count() const { return a.count + piece_slot(ps.cta0, 0); }
+    __device__ __forceinline__ int32_t *taken() const { return count() + 2 * gridDim.x; }
+    // what thread 0 says
+    template <class F> __device__ __forceinline__ int32_t agree(F say) const
+    {
+        named_sync(1, kRows);
+        if ((threadIdx.x & 127) == 0) *word = say();
+        named_sync(1, kRows);
+        return *word;
+    }
+    // after this CTA's piece; true: help() is to follow
+    __device__ __forceinline__ bool arrive() const
+    {
+        __threadfence();
+        const bool last = agree([&] { return (atomicAdd(count(), 1) & 0xffff) == pieces - 1; }) != 0;
+        if (!last) return pieces > kAlone;
+        __threadfence();
+        if (pieces > kAlone) {
+            take();
         } else {
-            *stat(p0, s, t) = top;
-            stat(p0, s, t)[kRows] = sum;
+            const int t = threadIdx.x & 127;
+            if (t == 0) *count() = 0;
+#pragma unroll 1
+            for (int s = 0; s < stages(); ++s) ps.template join<T>(s, t, pieces, OutRow<T>(a, cur, stage_row(cur, s) + t));
+        }
+        return false;
+    }
+    // at the CTA's end, if it was not the last
+    __device__ __forceinline__ void help() const
+    {
+        const bool all = agree([&] {
+            const int64_t start = clock64();
+            int32_t n;
+            do {
+                asm volatile("ld.acquire.gpu.global.b32 %0, [%1];" : "=r"(n) : "l"(count()) : "memory");
+            } while ((n & 0xffff) != pieces && clock64() - start < kPatience);
+            return (n & 0xffff) == pieces;
+        }) != 0;
+        __threadfence();
+        take(all);
+    }
+
+private:
+    // shares while there are any; the last CTA to be through leaves the counters at 0
+    __device__ __forceinline__ void take(bool any = true) const
+    {
+        constexpr int32_t per_stage = Layout<HALVES>::width / 16;
+        const int t = threadIdx.x & 127;
+        const int32_t shares = stages() * per_stage;
+        int at = -1;
+        float top = 0.f;
+#pragma unroll 1
+        while (any) {
+            const int32_t x = agree([&] { return atomicAdd(taken(), 1); });
+            if (x >= shares) break;
+            const int s = x / per_stage;
+            if (s != at) top = ps.highest(s, t, pieces);
+            at = s;
+            ps.template join_share<T>(s, t, pieces, OutRow<T>(a, cur, stage_row(cur, s) + t), x % per_stage * 16, top);
+        }
+        if (t == 0 && atomicAdd(count(), 1 << 16) >> 16 == pieces - 1) {
+            *taken() = 0;
+            *count() = 0;
         }
     }
 };
@@ -749,6 +856,7 @@ __device__ __forceinline__ void output_role(const AttendDev &a, const SchedShare
     Cursor<Shape> cur(a, sched);
     uint32_t turn[2] = {0, 0};
     int32_t item = 0;
+    uint32_t waits = 0;                                 // this CTA's pieces (bits) whose join it is to help with
     do {
         const int32_t rows = Shape::rows(a, cur.q), t0 = cur.k.lo / KT + cur.off;
         const int stages = rows - stage_row(cur, 0) > kRows ? 2 : 1;
@@ -812,45 +920,16 @@ __device__ __forceinline__ void output_role(const AttendDev &a, const SchedShare
                 ps.stat(mine, s, t)[kRows] = l;
             }
         }
-        if (!whole) {
-            const int32_t pieces = owner(g0 + cur.tiles - 1, line, ctas) - ps.cta0 + 1;
-            // A piece is up to 128 KB and a join's rate is one SM's, so many pieces are joined in groups of
-            // their square root, a group by a CTA: 8 in a row instead of 16 of 16 pieces.
-            int32_t size = pieces;
-            if (pieces > 4)
-                for (size = 2; size * size < pieces;) ++size;
-            const int32_t groups = (pieces + size - 1) / size;
-            // true in the CTA that arrives last of `of`
-            auto arrive = [&](int32_t *count, int32_t of) {
-                __threadfence();
-                named_sync(1, kRows);
-                if (t == 0) {
-                    *last = atomicAdd(count, 1) == of - 1;
-                    if (*last) *count = 0;
-                }
-                named_sync(1, kRows);
-                __threadfence();
-                return *last != 0;
-            };
-            // first a group's pieces, then the groups
-            int32_t p0 = mine / size * size, n = min(size, pieces - p0), step = 1;
-            int32_t *count = a.count + piece_slot(ps.cta0, p0);
-            while (arrive(count, n)) {
-                const bool final = step > 1 || groups == 1;
-#pragma unroll 1
-                for (int s = 0; s < stages; ++s) {
-                    const OutRow<T> out(a, cur, stage_row(cur, s) + t);
-                    ps.join(s, t, p0, n, step, out, final);
-                }
-                if (final) break;
-                p0 = 0;
-                n = groups;
-                step = size;
-                count = a.count + 2 * gridDim.x + piece_slot(ps.cta0, 0);
-            }
-        }
+        if (!whole && Joiner<T, HALVES>(a, cur, line, ctas, last).arrive()) waits |= 1u << item;
         ++item;
     } while (cur.next(a));
+    // a CTA's pieces are of its first two items at most
+    if (!waits) return;
+    Cursor<Shape> again(a, sched);
+    do {
+        if (waits & 1) Joiner<T, HALVES>(a, again, line, ctas, last).help();
+        waits >>= 1;
+    } while (waits && again.next(a));
 }
 
 template <typename T, int HALVES>

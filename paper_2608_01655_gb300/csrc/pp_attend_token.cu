@@ -1,15 +1,17 @@
-// Attention of single new tokens over the paged cache.
+// Attention of single new tokens, or of a few, over the paged cache.
 //
-// An item is one new token and up to 16 query heads of one K/V head: they see
-// the same keys, so each K and V row is read once for them.  What bounds it is
-// the read of K and V (4 to 32 operations a byte); the products run on
-// m16n8k16 tensor instructions with the heads as the 16 rows (padded), which
+// An item is 16 rows (new token, query head) of one K/V head, token first: they
+// see the same keys, or all but a few, so each K and V row is read once for them.
+// What bounds it is the read of K and V (4 to 32 operations a byte); the products
+// run on m16n8k16 tensor instructions with those 16 rows (padded), which
 // keeps scores, weights and sums in registers: the score's accumulators are the
 // next product's operand as they stand (a 128-row product would have 120 rows of
 // padding and pass its weights through tensor memory).  A tile is 128 keys, 16 a
 // warp.  Every warp copies its own rows, into a ring of its own (three tiles of
 // 64 KB an SM are on their way), and has its own running maximum, sum and output,
-// joined once an item: between items no warp waits for another.
+// joined once an item: between items no warp waits for another.  Keys that not
+// every row sees are masked row by row; an infinite or NaN V row among them is
+// replaced by zeros and added to the rows that see it.
 // Measured: 128 requests of 200 to 16,000 tokens (28 heads on 4, width 128, blocks
 // of 16, 1.52 GB) 256 us, 5.9 TB/s or 88% of the measured copy rate; two contexts of
 // 131,000 and 200,000 tokens 84 us, 4.1 TB/s: 10 us of it are the launch, the cut

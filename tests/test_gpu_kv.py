@@ -599,3 +599,81 @@ def test_block_tables_in_unaligned_buffers(pp):
     want = ref.block_tables([50, 37], [0, 0], None, None, np.full((2, 8), -1), np.arange(20)[::-1], 2, 16, 100)
     for got, exp in zip((table, slots, pos, q, out[0]), want):
         assert np.array_equal(got.cpu().numpy(), exp)
+
+
+# few rows (new tokens x heads of a group) take the kernel of single tokens up to 32, the next one that of chunks
+FEW = [([2, 1, 2], 4, 4), ([4, 3, 1, 0, 4], 8, 1), ([8, 5, 1], 8, 2), ([2, 2], 16, 1), ([3, 1], 14, 2), ([6, 2], 5, 1),
+       ([32, 7, 0, 31], 2, 2), ([33, 1], 2, 2), ([5, 2], 14, 2), ([1, 1], 33, 1)]
+
+
+@pytest.mark.parametrize("fresh,heads,kv_heads", FEW)
+@pytest.mark.parametrize("dim,dtype,block,order", [(128, torch.bfloat16, 16, "token"), (64, torch.float16, 8, "head"),
+                                                   (80, torch.float16, 64, "token")])
+def test_few_rows(pp, fresh, heads, kv_heads, dim, dtype, block, order):
+    cached = [0, 901, 127, 128, 3000][:len(fresh)]
+    _attention_case(pp, fresh, cached, heads, kv_heads, dim, dtype, block=block, order=order)
+
+
+@pytest.mark.parametrize("window", [1, 2, 3, 17, 128, 129, 700])
+@pytest.mark.parametrize("fresh,heads,kv_heads", [([4, 1, 3], 8, 2), ([4, 2], 8, 1), ([32, 20], 1, 1)])
+def test_few_rows_window(pp, fresh, heads, kv_heads, window):
+    _attention_case(pp, fresh, [1000, 255, 0][:len(fresh)], heads, kv_heads, 128, window=window)
+
+
+def test_few_rows_that_see_nothing(pp):
+    """The first queries stand before the first key, the last request has no token at all."""
+    out = _attention_case(pp, [4, 8, 3], [-2, -7, -3], 8, 2, 64)
+    assert int((out[:2] != 0).sum()) == 0 and int((out[4:11] != 0).sum()) == 0
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("fresh,row", [([2], 202), ([4], 203), ([4], 190), ([8], 204), ([10], 100)])
+@pytest.mark.parametrize("window", [0, 12])
+def test_few_rows_values_out_of_range(pp, bad, fresh, row, window):
+    test_values_out_of_range_stay_with_those_who_see_them(pp, bad, fresh, row, window)
+
+
+@pytest.mark.parametrize("fresh,row", [([2], 202), ([10], 207), ([7], 120)])
+def test_few_rows_nan_key(pp, fresh, row):
+    test_a_nan_key_stays_with_those_who_see_it(pp, fresh, row)
+
+
+@pytest.mark.parametrize("fresh,cached,heads,kv_heads,dim", [
+    ([100], [20_000], 8, 1, 128), ([100], [20_000], 8, 2, 64), ([65, 65, 65], [9000, 11_000, 300], 4, 1, 128),
+    ([300, 1, 33], [7000, 20_000, 5], 8, 2, 128), ([33], [30_000], 1, 1, 72)])
+def test_many_pieces(pp, fresh, cached, heads, kv_heads, dim):
+    """Items that many CTAs compute, joined in shares."""
+    _attention_case(pp, fresh, cached, heads, kv_heads, dim)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_many_pieces_again_and_again(pp, dim):
+    """Calls of one handle by turns: the same bits each time, whoever joins, and nothing left behind."""
+    torch.manual_seed(9)
+    kc, vc = (torch.randn((1300, 16, 2, dim), device="cuda").to(torch.bfloat16) for _ in range(2))
+    calls = []
+    for fresh, length in ([[40], [20_000]], [[30, 50], [5000, 9000]], [[4], [20_000]], [[90, 3, 200], [300, 6000, 8000]]):
+        n = sum(fresh)
+        table = torch.arange(1300, dtype=torch.int32, device="cuda").repeat(len(fresh), 1)
+        q = torch.randn((n, 8, dim), device="cuda").to(torch.bfloat16)
+        calls.append((q, table, _i32(np.concatenate([[0], np.cumsum(fresh)])), _i32(length), max(fresh)))
+    first = {}
+    with pp.KVCache.like(kc) as kv:
+        for turn in range(25):
+            for i, (q, *args) in enumerate(calls):
+                out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
+                pp.pp_paged_attention(kv, q, kc, vc, *args, out, 0.1, lse=lse)
+                want = first.setdefault(i, (out, lse))
+                assert torch.equal(out.view(torch.int16), want[0].view(torch.int16)) and torch.equal(lse, want[1])
+        kv.sync()
+    for i, (q, table, q_start, length, _) in enumerate(calls):
+        want, _, tol, _ = ref.attention(q, kc, vc, table, q_start.tolist(), length.tolist(), 0.1, 0)
+        assert not ((first[i][0].double() - want).abs() > tol).any()
+
+
+def test_refuses_too_many_heads(pp):
+    kc, vc = (torch.zeros((1, 16, 1, 8), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    q = torch.zeros((1, (1 << 20) + 1, 8), dtype=torch.bfloat16, device="cuda")
+    with pp.KVCache.like(kc) as kv:
+        with pytest.raises(pp.PPError, match="at most 2\\^20"):
+            pp.pp_paged_attention(kv, q, kc, vc, _i32([[0]]), _i32([0, 1]), _i32([1]), 1, torch.empty_like(q), 0.1)
