@@ -301,7 +301,44 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_token(const __grid_const
                         }
                     }
                 }
-                uint32_t pf[4], strange = 0;
+                if (edge && pos0 != pos1) {
+                    // some rows see keys that others do not: what is not finite is added to those who do, then cleared
+                    bool strange = false;
+                    uint4 *const v = reinterpret_cast<uint4 *>(raw + (vt - smem_u32(raw))) + lane;
+#pragma unroll
+                    for (int x = 0; x < L::rows / 512; ++x) {
+                        const int32_t j = j0 + ((4 * x + (lane >> 3)) & (kKeys - 1));   // 128 bytes a key, in each half
+                        const uint4 y = v[32 * x];
+                        const bool odd = finite_only<T>(y.x) != y.x || finite_only<T>(y.y) != y.y || finite_only<T>(y.z) != y.z ||
+                                         finite_only<T>(y.w) != y.w;
+                        strange |= odd && j >= cur.k.lo && j <= cur.k.hi;
+                    }
+                    if (__any_sync(~0u, strange)) {
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) {
+                            const int32_t pos = r0 + 8 * y < rows ? Shape::pos(a, cur.q, row0 + r0 + 8 * y) : -1;
+                            const int32_t lo = pos < 0 ? 0 : first_key(a, pos);
+#pragma unroll 1
+                            for (int32_t j = max(j0, lo); j <= min(j0 + kKeys - 1, pos); ++j) {
+#pragma unroll
+                                for (int n = 0; n < 2 * KS; ++n) {
+                                    const uint32_t two = lds32(vt + row_at(j - j0, n) + 2 * c0);
+                                    const uint32_t odd = two ^ finite_only<T>(two);     // only what is not finite is left
+                                    if (odd & 0xffffu) o[n][2 * y] += half_value<T>(two);
+                                    if (odd >> 16) o[n][2 * y + 1] += half_value<T>(two >> 16);
+                                }
+                            }
+                        }
+                        __syncwarp();
+#pragma unroll 1
+                        for (int x = 0; x < L::rows / 512; ++x) {
+                            const uint4 y = v[32 * x];
+                            v[32 * x] = make_uint4(finite_only<T>(y.x), finite_only<T>(y.y), finite_only<T>(y.z), finite_only<T>(y.w));
+                        }
+                        __syncwarp();
+                    }
+                }
+                uint32_t pf[4];
 #pragma unroll
                 for (int x = 0; x < 2; ++x) base[x] = m[x] == -INFINITY ? 0.f : m[x];
 #pragma unroll
@@ -323,35 +360,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_token(const __grid_const
                         b[1] &= vk1;
                         b[2] &= vk0;
                         b[3] &= vk1;
-                        if (pos0 != pos1) {
-                            // some rows see keys that others do not: what is not finite is added by row below
-#pragma unroll
-                            for (int x = 0; x < 4; ++x) {
-                                const uint32_t c = finite_only<T>(b[x]);
-                                strange |= c ^ b[x];
-                                b[x] = c;
-                            }
-                        }
                     }
                     mma16<T>(o[2 * n], pf, b[0], b[1]);
                     mma16<T>(o[2 * n + 1], pf, b[2], b[3]);
-                }
-                if (edge && __any_sync(~0u, strange != 0)) {
-#pragma unroll
-                    for (int y = 0; y < 2; ++y) {
-                        const int32_t pos = r0 + 8 * y < rows ? Shape::pos(a, cur.q, row0 + r0 + 8 * y) : -1;
-                        const int32_t lo = pos < 0 ? 0 : first_key(a, pos);
-#pragma unroll 1
-                        for (int32_t j = max(j0, lo); j <= min(j0 + kKeys - 1, pos); ++j) {
-#pragma unroll
-                            for (int n = 0; n < 2 * KS; ++n) {
-                                const uint32_t two = lds32(vt + row_at(j - j0, n) + 2 * c0);
-                                const uint32_t odd = two ^ finite_only<T>(two);     // only what is not finite is left
-                                if (odd & 0xffffu) o[n][2 * y] += half_value<T>(two);
-                                if (odd >> 16) o[n][2 * y + 1] += half_value<T>(two >> 16);
-                            }
-                        }
-                    }
                 }
             }
             __syncwarp();
