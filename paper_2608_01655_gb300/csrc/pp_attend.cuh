@@ -158,7 +158,6 @@ __device__ __forceinline__ int64_t quotient(int64_t x, int64_t y)
 // The CTA's stretch: false if it has none.  All threads of the CTA call it.
 template <class S> __device__ __forceinline__ bool schedule(const AttendDev &a, SchedShared &sm)
 {
-    static_assert(S::extra < 4, "every stretch has a tile");
     // up to 32 requests every warp works all of it out, which takes one barrier in all
     const bool few = a.c.requests <= 32;
     const int lane = threadIdx.x & 31, me = few ? lane : threadIdx.x;
@@ -192,8 +191,8 @@ template <class S> __device__ __forceinline__ bool schedule(const AttendDev &a, 
     }
     tiles = scan64(tiles, &excl, sm.warp_sum, few) * outer;
     if (tiles == 0) return false;
-    // with few tiles a CTA, every tile to a CTA of its own counts more than an even load
-    const int32_t extra = tiles >= 4 * (int64_t)gridDim.x ? S::extra : 0;
+    // with few tiles a CTA, every tile to a CTA of its own counts more than an even load; every stretch has a tile
+    const int32_t extra = tiles >= (S::extra < 4 ? 4 : S::extra + 1) * (int64_t)gridDim.x ? S::extra : 0;
     const int64_t total = tiles + (extra ? scan64(items, &excl_items, sm.warp_sum, few) * outer * extra : 0);
     excl += excl_items * extra;
     const int64_t ctas = min((int64_t)gridDim.x, total);

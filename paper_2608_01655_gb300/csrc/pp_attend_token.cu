@@ -46,7 +46,9 @@ template <int HALVES> struct Layout {
 // Rows are (token, head of the group), token first; an item is 16 of them.
 struct Shape {
     static constexpr int KT = token::KT;
-    static constexpr int32_t extra = 1;
+    // what an item weighs beside its tiles (first rows, join): 1, 2, 3, 5 tiles take 60 requests x 4 tokens after 50 to
+    // 9,000 56, 53, 48, 46 us, 300 single tokens after 50 to 3,000 85, 81, 79, 79, 256 after 100 to 8,000 -, 461, 462, 472
+    static constexpr int32_t extra = 3;
     static constexpr bool many = false;
     static __device__ __forceinline__ int32_t outer(const AttendDev &a) { return a.kv_heads; }
     static __device__ __forceinline__ int32_t rows(const AttendDev &a, const Req &q) { return q.q_len * a.c.group; }
