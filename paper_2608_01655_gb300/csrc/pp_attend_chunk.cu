@@ -40,6 +40,7 @@ namespace chunk {
 constexpr int KT = 128;                             // keys per tile
 constexpr int kRows = 128;                          // rows of a stage
 constexpr int kThreads = 512;
+constexpr int kAlone = 4;                           // pieces of an item that one CTA joins
 constexpr int kBad = 16;                            // marks of items, the stages are fewer apart
 constexpr float kMaxSum = 4096.f;                   // of the weights of a row and tile, before m moves
 
@@ -692,28 +693,39 @@ template <int HALVES> struct Pieces {
     {
         return reinterpret_cast<float4 *>(a.piece) + ((int64_t)(piece_slot(cta0, p) * 2 + s) * (width / 4) + c / 4) * kRows + t;
     }
-    // joins a stage's n pieces
+    // joins a stage's n <= kAlone pieces; the statistics' loads are on their way together
     template <typename T> __device__ __forceinline__ void join(int s, int t, int32_t n, const OutRow<T> &out) const
     {
         if (!out.live) return;
-        const float top = highest(s, t, n), base = top == -INFINITY ? 0.f : top;
-        float sum = 0.f;
-        for (int32_t p = 0; p < n; ++p)
-            sum = fmaf(exp2_approx(__ldcg(stat(p, s, t)) - base), __ldcg(stat(p, s, t) + kRows), sum);
+        float f[kAlone], part[kAlone], top = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (int p = 0; p < kAlone; ++p) {
+            f[p] = __ldcg(stat(min(p, n - 1), s, t));
+            part[p] = __ldcg(stat(min(p, n - 1), s, t) + kRows);
+        }
+#pragma unroll
+        for (int p = 0; p < kAlone; ++p) top = fmaxf(top, f[p]);
+        const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+        for (int p = 0; p < kAlone; ++p) {
+            f[p] = exp2_approx(f[p] - base);
+            if (p < n) sum = fmaf(f[p], part[p], sum);
+        }
         const float scale = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll 1
         for (int c = 0; c < width; c += 32) {
             float o[32];
 #pragma unroll
             for (int y = 0; y < 32; ++y) o[y] = 0.f;
-#pragma unroll 2
-            for (int32_t p = 0; p < n; ++p) add<32>(o, exp2_approx(__ldcg(stat(p, s, t)) - base), at(p, s, c, t));
+#pragma unroll
+            for (int p = 0; p < kAlone; ++p)
+                if (p < n) add<32>(o, f[p], at(p, s, c, t));
             out.put(o, c, scale);
             out.put(o + 16, c + 16, scale);
         }
         out.put_lse(top, sum);
     }
-    // 16 columns of it
+    // 16 columns of a stage's n pieces
     template <typename T>
     __device__ __forceinline__ void join_share(int s, int t, int32_t n, const OutRow<T> &out, int c, float top) const
     {
@@ -765,7 +777,6 @@ private:
 // from 3 pieces on cost more than they give (8 x 60-700 tokens after 512-8,192: 101
 // against 95 us), from 9 on less (500 tokens after 20,000: 91 against 87).
 template <typename T, int HALVES> struct Joiner {
-    static constexpr int32_t kAlone = 4;
     static constexpr int64_t kPatience = 40000;         // cycles
     const AttendDev &a;
     const Cursor<Shape> &cur;
