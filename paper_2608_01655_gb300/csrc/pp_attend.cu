@@ -74,9 +74,9 @@ pp_status prepare_attend()
 // rows and has short items to begin and to join; the chunk kernel pays for 256 rows
 // whatever there are.  Kernel of single tokens against chunks', in us, 2 K/V heads
 // of 128, 32 requests after 5,000 tokens / 4 after 2,000 / 1 after 50,000:
-//   16 rows  52 : 61 / 22 : 34 / 34 : 52
-//   32       66 : 61 / 22 : 34 / 37 : 50
-//   64      108 : 62 / 28 : 34 / 44 : 52
+//   16 rows  51 : 61 / 22 : 34 / 34 : 50
+//   32       64 : 61 / 22 : 34 / 36 : 47
+//   64      105 : 61 / 28 : 34 / 42 : 50
 // so at 64 it loses more in batches than it gains for single requests.
 constexpr int64_t kFewRows = 32;
 

@@ -27,7 +27,7 @@
 // two O of 128 columns).
 // Measured: 8,192 new tokens after 24,576 (28 heads on 4, width 128) 1.90 ms, 1,770
 // TFLOP/s or 95% of the measured library product; 8,192 tokens of 16 heads from
-// nothing 225 us, 1,200 TFLOP/s; the same at width 64 175 us, 780 TFLOP/s.
+// nothing 220 us, 1,250 TFLOP/s; the same at width 64 175 us, 780 TFLOP/s.
 #include <algorithm>
 #include <new>
 #include <type_traits>
