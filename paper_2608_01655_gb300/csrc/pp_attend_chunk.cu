@@ -734,7 +734,7 @@ template <int HALVES> struct Pieces {
         float sum = 0.f, o[16];
 #pragma unroll
         for (int y = 0; y < 16; ++y) o[y] = 0.f;
-#pragma unroll 4
+#pragma unroll 2
         for (int32_t p = 0; p < n; ++p) {
             const float f = exp2_approx(__ldcg(stat(p, s, t)) - base);
             sum = fmaf(f, __ldcg(stat(p, s, t) + kRows), sum);
@@ -746,7 +746,7 @@ template <int HALVES> struct Pieces {
     __device__ __forceinline__ float highest(int s, int t, int32_t n) const
     {
         float top = -INFINITY;
-#pragma unroll 8
+#pragma unroll 4
         for (int32_t p = 0; p < n; ++p) top = fmaxf(top, __ldcg(stat(p, s, t)));
         return top;
     }
