@@ -677,3 +677,33 @@ def test_refuses_too_many_heads(pp):
     with pp.KVCache.like(kc) as kv:
         with pytest.raises(pp.PPError, match="at most 2\\^20"):
             pp.pp_paged_attention(kv, q, kc, vc, _i32([[0]]), _i32([0, 1]), _i32([1]), 1, torch.empty_like(q), 0.1)
+
+
+def test_two_handles_on_two_streams(pp):
+    """Calls whose joins many CTAs share, at the same time: each has its own scratch, and neither waits for the other."""
+    torch.manual_seed(10)
+    kc, vc = (torch.randn((700, 16, 2, 128), device="cuda").to(torch.bfloat16) for _ in range(2))
+    table = torch.arange(700, dtype=torch.int32, device="cuda")[None]
+    calls = []
+    for fresh, length in ((50, 11_000), (300, 10_000), (2, 11_200)):
+        q = torch.randn((fresh, 8, 128), device="cuda").to(torch.bfloat16)
+        calls.append((q, table, _i32([0, fresh]), _i32([length]), fresh))
+    outs = [[], []]
+    torch.cuda.synchronize()
+    with pp.KVCache.like(kc) as one, pp.KVCache.like(kc) as two:
+        streams = torch.cuda.Stream(), torch.cuda.Stream()
+        for turn in range(10):
+            for kv, stream, out in zip((one, two), streams, outs):
+                with torch.cuda.stream(stream):
+                    for q, *args in calls:
+                        out.append(torch.empty_like(q))
+                        pp.pp_paged_attention(kv, q, kc, vc, table, *args[1:], out[-1], 0.1)
+        torch.cuda.synchronize()
+        one.sync()
+        two.sync()
+    for i, (q, _, q_start, length, _) in enumerate(calls):
+        want, _, tol, _ = ref.attention(q, kc, vc, table, q_start.tolist(), length.tolist(), 0.1, 0)
+        assert not ((outs[0][i].double() - want).abs() > tol).any()
+        for out in outs:
+            for turn in range(10):
+                assert torch.equal(out[3 * turn + i].view(torch.int16), outs[0][i].view(torch.int16))
