@@ -567,11 +567,13 @@ __device__ __forceinline__ void softmax_role(const AttendDev &a, const SchedShar
                 }
             };
             uint32_t p[64];
-            float total;
             // The weights are computed from the m at hand, without a look at the
             // maximum: their sum shows whether m is still good (no weight is above
             // it).  If not, as in the first tile with a key to see, the maximum is
-            // found, m moves and they are computed once more.
+            // found, m moves and they are computed once more.  A warp does that
+            // together, but a row whose m is good keeps it: its bits do not depend
+            // on the rows beside it, which may see keys that it does not.
+            float total = INFINITY;
             for (bool sure = i == 0;;) {
                 if (sure) {
                     float up = m;
@@ -585,6 +587,7 @@ __device__ __forceinline__ void softmax_role(const AttendDev &a, const SchedShar
                             top[(c >> 1) & 3] = max3(top[(c >> 1) & 3], __uint_as_float(x[c]), __uint_as_float(x[c + 1]));
                         up = fmaxf(up, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.scale_log2);
                     }
+                    if (total <= kMaxSum && m != -INFINITY) up = m;
                     if (i > 0) {
                         // every product on O that was issued before this S has ended with it
                         const float f = up == m ? 1.f : exp2_approx(m - up);
