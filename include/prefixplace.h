@@ -577,7 +577,8 @@ pp_status pp_kv_write(pp_kv *kv, int32_t tokens, const void *k, int64_t k_token_
  * q_len + i and sees the keys j <= p, with window > 0 only those with j > p -
  * window.  Query head x reads K/V head x / (q_heads / kv_heads).
  *   out = sum_j softmax_j(scale q.k_j) v_j
- * A query that sees nothing (p < 0) gets zeros and lse = -infinity.  Rows of
+ * A query that sees nothing (p < 0) gets zeros and lse = -infinity, one whose
+ * visible keys all score -infinity NaN (0 / 0) and lse = -infinity.  Rows of
  * the cache that a query does not see never reach its output, whatever they
  * hold (infinities and NaN as well).
  *   requests      0 .. 16384

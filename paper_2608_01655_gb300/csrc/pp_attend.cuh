@@ -458,6 +458,13 @@ __device__ __forceinline__ float exp2_approx(float x)
     return y;
 }
 
+// What a row's output is multiplied with.  No weight is above 0 where the row sees no
+// key (zeros), or only scores of -infinity: 0 / 0 then, as the formula has it.
+__device__ __forceinline__ float inverse_sum(float sum, bool sees)
+{
+    return sum == 0.f ? (sees ? NAN : 0.f) : 1.f / sum;
+}
+
 template <typename T> struct Pack;
 template <> struct Pack<__nv_bfloat16> {
     static __device__ __forceinline__ uint32_t two(float lo, float hi)

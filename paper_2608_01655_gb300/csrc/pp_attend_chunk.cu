@@ -650,14 +650,16 @@ template <typename T> struct OutRow {
     const AttendDev &a;
     T *out;
     float *lse;
-    bool live;
+    bool live, sees;                                    // a row of the request; one with a key to see
     __device__ __forceinline__ OutRow(const AttendDev &a_, const Cursor<Shape> &c, int32_t row)
         : a(a_), live(row < Shape::rows(a_, c.q))
     {
         const int32_t in = div_group(a, row), tok = c.q.first + in, head = c.outer * a.c.group + row - in * a.c.group;
         out = static_cast<T *>(a.c.out) + (int64_t)tok * a.c.out_token_stride + (int64_t)head * a.c.out_head_stride;
         lse = a.c.lse ? a.c.lse + (int64_t)tok * a.c.q_heads + head : nullptr;
+        sees = c.q.length - c.q.q_len + in >= 0;
     }
+    __device__ __forceinline__ float inverse(float sum) const { return inverse_sum(sum, sees); }
     // 16 columns
     __device__ __forceinline__ void put(const float *o, int c, float inv) const
     {
@@ -714,7 +716,7 @@ template <int HALVES> struct Pieces {
             f[p] = exp2_approx(f[p] - base);
             if (p < n) sum = fmaf(f[p], part[p], sum);
         }
-        const float scale = sum == 0.f ? 0.f : 1.f / sum;
+        const float scale = out.inverse(sum);
 #pragma unroll 1
         for (int c = 0; c < width; c += 32) {
             float o[32];
@@ -743,7 +745,7 @@ template <int HALVES> struct Pieces {
             sum = fmaf(f, __ldcg(stat(p, s, t) + kRows), sum);
             add<16>(o, f, at(p, s, c, t));
         }
-        out.put(o, c, sum == 0.f ? 0.f : 1.f / sum);
+        out.put(o, c, out.inverse(sum));
         if (c == 0) out.put_lse(top, sum);
     }
     __device__ __forceinline__ float highest(int s, int t, int32_t n) const
@@ -892,7 +894,7 @@ __device__ __forceinline__ void output_role(const AttendDev &a, const SchedShare
             mbar_arrive(b.stat_free + 8 * s);
             mbar_wait(b.o_done + 8 * s, now, dead, a.status);
             tc_after();
-            const float inv = l == 0.f ? 0.f : 1.f / l;
+            const float inv = out.inverse(l);
             const bool fix = bad[item % kBad] == item + 1;
 #pragma unroll 1
             for (int c = 0; c < L::width; c += 32) {

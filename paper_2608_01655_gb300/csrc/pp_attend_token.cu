@@ -522,7 +522,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_token(const __grid_const
             }
         }
         if (write && jr < rows) {
-            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+            const float inv = inverse_sum(sum, Shape::pos(a, cur.q, row0 + jr) >= 0);
             T *dst = static_cast<T *>(a.c.out) + q_row(jr, a.c.out_token_stride, a.c.out_head_stride) + jd;
             if constexpr (HALVES == 2) {
                 if (jd < a.dim)
