@@ -470,7 +470,8 @@ enum { PP_KV_BF16 = 0, PP_KV_F16 = 1 };
  *   head_dim      a multiple of 8, 8 .. 128
  *   dtype         PP_KV_BF16 or PP_KV_F16, of the caches and of q, k, v, out
  *   block_stride, token_stride, head_stride
- *                 elements, positive multiples of 8 of at least head_dim;
+ *                 elements, positive multiples of 8 of at least head_dim, of a
+ *                 layout in which no two rows overlap;
  *                 0, 0, 0: contiguous [blocks][block_size][kv_heads][head_dim]
  *   stream        stream of the set-up; the call synchronises it
  *   out           receives the handle (NULL on failure)

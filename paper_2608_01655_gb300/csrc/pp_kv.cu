@@ -2,6 +2,8 @@
 // step's block tables and slot map, and the write of new K and V rows.
 #include <algorithm>
 #include <climits>
+#include <cstdlib>
+#include <initializer_list>
 #include <new>
 #include <vector>
 
@@ -368,6 +370,40 @@ __global__ void __launch_bounds__(kWriteThreads) k_kv_write(WriteArgs a)
 static bool stride_ok(int64_t s) { return s > 0 && s % 8 == 0 && s < (int64_t)1 << 38; }
 static bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
+// Whether rows of `dim` elements at sums of d * stride (0 <= d < extent) share an
+// element.  Where each stride passes all that lies within the smaller ones, as in every
+// order of dimensions with any padding, they do not.  Other layouts are searched: for
+// each difference along two dimensions the nearest ones of the third, the longest.
+struct Extent {
+    int64_t stride, count;
+};
+static bool rows_overlap(int64_t dim, std::initializer_list<Extent> all)
+{
+    Extent e[3] = {{0, 1}, {0, 1}, {0, 1}};
+    int n = 0;
+    for (const Extent &x : all)
+        if (x.count > 1) e[n++] = x;
+    std::sort(e, e + n, [](const Extent &x, const Extent &y) { return x.stride < y.stride; });
+    __int128 span = dim;
+    bool nested = true;
+    for (int i = 0; i < n; ++i) {
+        nested = nested && e[i].stride >= span;
+        span += (__int128)(e[i].count - 1) * e[i].stride;
+    }
+    if (nested) return false;
+    std::sort(e, e + n, [](const Extent &x, const Extent &y) { return x.count > y.count; });
+    for (int64_t x = 0; x < e[1].count; ++x)
+        for (int64_t y = x ? 1 - e[2].count : 0; y < e[2].count; ++y) {
+            const int64_t at = x * e[1].stride + y * e[2].stride;
+            const int64_t down = (at >= 0 ? at : at - e[0].stride + 1) / e[0].stride;
+            for (int64_t z = down; z <= down + 1; ++z) {
+                if (x == 0 && y == 0 && z == 0) continue;
+                if (std::abs(z) < e[0].count && std::abs(at - z * e[0].stride) < dim) return true;
+            }
+        }
+    return false;
+}
+
 static pp_status check_device(const pp_kv *kv)
 {
     int dev = 0;
@@ -419,6 +455,8 @@ extern "C" pp_status pp_kv_create(int32_t blocks, int32_t block_size, int32_t kv
         return fail(PP_EINVAL, "strides must be positive multiples of 8 elements below 2^38");
     if (token_stride < head_dim || head_stride < head_dim || block_stride < head_dim)
         return fail(PP_EINVAL, "strides must be at least head_dim: rows would overlap");
+    if (rows_overlap(head_dim, {{block_stride, blocks}, {token_stride, block_size}, {head_stride, kv_heads}}))
+        return fail(PP_EINVAL, "rows of the cache would overlap with these strides");
     pp_kv *kv = new (std::nothrow) pp_kv();
     if (!kv) return fail(PP_ENOMEM, "host allocation failed");
     kv->blocks = blocks;
