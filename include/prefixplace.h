@@ -585,7 +585,8 @@ pp_status pp_kv_write(pp_kv *kv, int32_t tokens, const void *k, int64_t k_token_
  *   requests      0 .. 16384
  *   tokens        rows of q and out; rows from q_start[requests] on are left alone
  *   q, out        device [tokens][q_heads][head_dim], token and head strides in
- *                 elements (positive multiples of 8; bases aligned to 16 bytes)
+ *                 elements (positive multiples of 8; bases aligned to 16 bytes);
+ *                 no two rows of out may overlap
  *   block_table   device [requests][table_width]
  *   q_start       device [requests + 1], ascending from 0
  *   length        device [requests]: tokens of the request, the new ones included

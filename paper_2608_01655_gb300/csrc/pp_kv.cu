@@ -628,6 +628,8 @@ extern "C" pp_status pp_paged_attention(pp_kv *kv, int32_t requests, int32_t tok
     if (!stride_ok(q_token_stride) || !stride_ok(q_head_stride) || !stride_ok(out_token_stride) ||
         !stride_ok(out_head_stride))
         return fail(PP_EINVAL, "strides must be positive multiples of 8 elements below 2^38");
+    if (rows_overlap(kv->dim, {{out_token_stride, tokens}, {out_head_stride, q_heads}}))
+        return fail(PP_EINVAL, "rows of out would overlap with these strides");
     pp_status s = check_device(kv);
     if (s != PP_OK) return s;
     const AttendArgs a = {requests, tokens, q_heads, q_heads / kv->heads, q, q_token_stride, q_head_stride, k_cache,
