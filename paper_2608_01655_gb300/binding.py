@@ -403,14 +403,6 @@ def pp_chunk_map(parent, weight, resident, blocks_per_slot: int):
     return out[:n], int(used.value)
 
 
-def _arg(t, name, dtype, shape):
-    """Device pointer of a contiguous CUDA tensor of this type and shape."""
-    if t.dtype is dtype and t.shape == shape and t.is_cuda and t.is_contiguous():
-        return t.data_ptr()
-    raise ValueError(f"{name}: expected a contiguous CUDA tensor {list(shape)} of {dtype}, got {list(t.shape)} of "
-                     f"{t.dtype} on {t.device}, strides {list(t.stride())}")
-
-
 class KVCache:
     """Owns one pp_kv: the layout of a paged K/V cache, its status word and scratch."""
 
@@ -477,26 +469,33 @@ class KVCache:
             return self._raw_stream(self._device)
         return _stream(stream)
 
+    def _arg(self, t, name, dtype, shape):
+        """Device pointer of a contiguous tensor of this type and shape on the handle's device."""
+        if t.dtype is dtype and t.shape == shape and t.get_device() == self._device and t.is_contiguous():
+            return t.data_ptr()
+        raise ValueError(f"{name}: expected a contiguous tensor {list(shape)} of {dtype} on cuda:{self._device}, got "
+                         f"{list(t.shape)} of {t.dtype} on {t.device}, strides {list(t.stride())}")
+
     def _cache(self, t, name):
         """Device pointer of a cache of this layout (an extent of 1 has no stride)."""
-        if t.dtype is self.dtype and t.shape == self.shape and t.is_cuda:
+        if t.dtype is self.dtype and t.shape == self.shape and t.get_device() == self._device:
             st = t.stride()
             if st[3] == 1 and (st[:3] == self.strides or
                                all(n == 1 or a == b for n, a, b in zip(self.shape, st, self.strides))):
                 return t.data_ptr()
-        raise ValueError(f"{name}: expected a CUDA {self.dtype} tensor of shape {self.shape} and strides "
-                         f"{self.strides + (1,)}")
+        raise ValueError(f"{name}: expected a {self.dtype} tensor on cuda:{self._device} of shape {self.shape} and "
+                         f"strides {self.strides + (1,)}")
 
     def _rows(self, t, name, tokens, heads):
         """Pointer, token stride and head stride of [tokens][heads][head_dim] rows."""
-        if t.dtype is self.dtype and t.shape == (tokens, heads, self.shape[3]) and t.is_cuda:
+        if t.dtype is self.dtype and t.shape == (tokens, heads, self.shape[3]) and t.get_device() == self._device:
             st = t.stride()
             if st[2] == 1 or not tokens:
                 # an extent of 1 may carry any stride
                 ht = st[1] if heads > 1 else self.shape[3]
                 return t.data_ptr(), st[0] if tokens > 1 else heads * ht, ht
-        raise ValueError(f"{name}: expected a CUDA {self.dtype} tensor [{tokens}][{heads}][{self.shape[3]}] "
-                         "with contiguous rows")
+        raise ValueError(f"{name}: expected a {self.dtype} tensor [{tokens}][{heads}][{self.shape[3]}] on "
+                         f"cuda:{self._device} with contiguous rows")
 
 
 def pp_block_tables(kv: KVCache, length, cached, block_table, slot_map, position, q_start, free_blocks, free_head,
@@ -509,20 +508,20 @@ def pp_block_tables(kv: KVCache, length, cached, block_table, slot_map, position
     r, t, width, i32 = length.shape[0], slot_map.shape[0], block_table.shape[-1], kv._i32
     n = 0 if node is None else chunk_map.shape[0]
     _check(_lib.pp_block_tables(
-        kv.handle, r, _arg(length, "length", i32, (r,)), _arg(cached, "cached", i32, (r,)),
-        None if node is None else _arg(node, "node", i32, (r,)), n,
-        None if node is None else _arg(chunk_map, "chunk_map", i32, (n, 4)),
-        free_blocks.shape[0], _arg(free_blocks, "free_blocks", i32, free_blocks.shape[:1]),
-        _arg(free_head, "free_head", i32, (1,)), _arg(free_head_out, "free_head_out", i32, (1,)),
-        width, _arg(block_table, "block_table", i32, (r, width)), t, _arg(slot_map, "slot_map", kv._i64, (t,)),
-        _arg(position, "position", i32, (t,)), _arg(q_start, "q_start", i32, (r + 1,)), kv._on(stream)))
+        kv.handle, r, kv._arg(length, "length", i32, (r,)), kv._arg(cached, "cached", i32, (r,)),
+        None if node is None else kv._arg(node, "node", i32, (r,)), n,
+        None if node is None else kv._arg(chunk_map, "chunk_map", i32, (n, 4)),
+        free_blocks.shape[0], kv._arg(free_blocks, "free_blocks", i32, free_blocks.shape[:1]),
+        kv._arg(free_head, "free_head", i32, (1,)), kv._arg(free_head_out, "free_head_out", i32, (1,)),
+        width, kv._arg(block_table, "block_table", i32, (r, width)), t, kv._arg(slot_map, "slot_map", kv._i64, (t,)),
+        kv._arg(position, "position", i32, (t,)), kv._arg(q_start, "q_start", i32, (r + 1,)), kv._on(stream)))
 
 
 def pp_kv_write(kv: KVCache, k, v, slot_map, k_cache, v_cache, stream=None):
     """Store rows k, v [T][kv_heads][head_dim] at slot_map [T] int64 (negative: left out)."""
     t, h = slot_map.shape[0], kv.shape[2]
     _check(_lib.pp_kv_write(kv.handle, t, *kv._rows(k, "k", t, h), *kv._rows(v, "v", t, h),
-                            _arg(slot_map, "slot_map", kv._i64, (t,)), kv._cache(k_cache, "k_cache"),
+                            kv._arg(slot_map, "slot_map", kv._i64, (t,)), kv._cache(k_cache, "k_cache"),
                             kv._cache(v_cache, "v_cache"), kv._on(stream)))
 
 
@@ -533,7 +532,7 @@ def pp_paged_attention(kv: KVCache, q, k_cache, v_cache, block_table, q_start, l
     t, heads, r, width, i32 = q.shape[0], q.shape[1], length.shape[0], block_table.shape[-1], kv._i32
     _check(_lib.pp_paged_attention(
         kv.handle, r, t, heads, *kv._rows(q, "q", t, heads), kv._cache(k_cache, "k_cache"),
-        kv._cache(v_cache, "v_cache"), width, _arg(block_table, "block_table", i32, (r, width)),
-        _arg(q_start, "q_start", i32, (r + 1,)), _arg(length, "length", i32, (r,)), max_q, window, scale,
-        *kv._rows(out, "out", t, heads), None if lse is None else _arg(lse, "lse", kv._f32, (t, heads)),
+        kv._cache(v_cache, "v_cache"), width, kv._arg(block_table, "block_table", i32, (r, width)),
+        kv._arg(q_start, "q_start", i32, (r + 1,)), kv._arg(length, "length", i32, (r,)), max_q, window, scale,
+        *kv._rows(out, "out", t, heads), None if lse is None else kv._arg(lse, "lse", kv._f32, (t, heads)),
         kv._on(stream)))
