@@ -404,7 +404,15 @@ def pp_chunk_map(parent, weight, resident, blocks_per_slot: int):
 
 
 class KVCache:
-    """Owns one pp_kv: the layout of a paged K/V cache, its status word and scratch."""
+    """Owns one pp_kv: the layout of a paged K/V cache, its status word and scratch.
+
+    Attention calls use the handle's scratch and must not overlap on the GPU.  Here a call on another stream
+    than the last one's waits for that one on the GPU, so calls from several streams are safe, one after
+    another; a handle a stream lets them overlap.  Calls captured in CUDA graphs are not followed: replays
+    that may run beside other calls take a handle of their own.  sync() on the last call's stream comes before
+    that stream is destroyed (torch's own streams never are)."""
+
+    _last = None                        # stream of the last attention call that may still run
 
     _DTYPES = {"bfloat16": PP_KV_BF16, "float16": PP_KV_F16}
 
@@ -462,12 +470,35 @@ class KVCache:
         self.close()
 
     def sync(self, stream=None):
-        _check(_lib.pp_kv_sync(self.handle, _stream(stream)))
+        stream = _stream(stream)
+        _check(_lib.pp_kv_sync(self.handle, stream))
+        if self._last == (stream.value or 0):
+            self._last = None
 
     def _on(self, stream):
         if stream is None and self._raw_stream is not None:
             return self._raw_stream(self._device)
         return _stream(stream)
+
+    def _on_after_last(self, stream):
+        """The stream of an attention call, made to wait for the last one's."""
+        stream = self._on(stream)
+        raw = stream if type(stream) is int else stream.value or 0
+        if raw != self._last and (self._last is None or self._wait(raw, self._last)):
+            self._last = raw
+        return stream
+
+    def _wait(self, new, old):
+        """Work to come on stream `new` waits for `old`'s.  False if one of them is being captured."""
+        import torch
+        streams = [torch.cuda.ExternalStream(s, self._device) if s else torch.cuda.default_stream(self._device)
+                   for s in (new, old)]
+        for s in streams:
+            with torch.cuda.stream(s):
+                if torch.cuda.is_current_stream_capturing():
+                    return False
+        streams[0].wait_stream(streams[1])
+        return True
 
     def _arg(self, t, name, dtype, shape):
         """Device pointer of a contiguous tensor of this type and shape on the handle's device."""
@@ -535,4 +566,4 @@ def pp_paged_attention(kv: KVCache, q, k_cache, v_cache, block_table, q_start, l
         kv._cache(v_cache, "v_cache"), width, kv._arg(block_table, "block_table", i32, (r, width)),
         kv._arg(q_start, "q_start", i32, (r + 1,)), kv._arg(length, "length", i32, (r,)), max_q, window, scale,
         *kv._rows(out, "out", t, heads), None if lse is None else kv._arg(lse, "lse", kv._f32, (t, heads)),
-        kv._on(stream)))
+        kv._on_after_last(stream)))

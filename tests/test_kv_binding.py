@@ -79,3 +79,50 @@ def test_tensors_of_another_device_are_refused(pp, call):
             with pytest.raises(ValueError, match=f"{name}: expected.*cuda:0"):
                 fn(pp.kv, **args)
     assert len(pp.calls) == 1
+
+
+class _Stream:
+    def __init__(self, raw):
+        self.cuda_stream = raw
+
+
+def test_attention_on_another_stream_waits_for_the_last_one(pp, monkeypatch):
+    """The scratch is one per handle: whoever comes from another stream is ordered after the last call."""
+    waits = []
+    monkeypatch.setattr(pp.module.KVCache, "_wait", lambda self, new, old: waits.append((new, old)) or True, raising=False)
+    monkeypatch.setattr(pp.module._lib, "pp_kv_sync", lambda handle, stream: 0, raising=False)
+    args = _arguments()
+    call = lambda stream: pp.module.pp_paged_attention(pp.kv, **args["pp_paged_attention"], stream=stream)
+    call(None)
+    call(None)
+    assert waits == []
+    call(_Stream(5))
+    assert waits == [(5, 0)]
+    call(_Stream(5))
+    call(7)
+    call(None)
+    assert waits == [(5, 0), (7, 5), (0, 7)]
+    assert [a[-1].value or 0 if hasattr(a[-1], "value") else a[-1] for _, a in pp.calls] == [0, 0, 5, 5, 7, 0]
+    # tables and writes use no scratch
+    pp.module.pp_kv_write(pp.kv, **args["pp_kv_write"], stream=_Stream(9))
+    pp.module.pp_block_tables(pp.kv, **args["pp_block_tables"], stream=_Stream(9))
+    assert len(waits) == 3
+    # a sync of another stream says nothing of the last call, one of its own that it has ended
+    pp.kv.sync(_Stream(9))
+    call(_Stream(5))
+    assert waits[3:] == [(5, 0)]
+    pp.kv.sync(_Stream(5))
+    call(_Stream(7))
+    assert len(waits) == 4
+
+
+def test_captured_calls_are_not_followed(pp, monkeypatch):
+    """_wait refuses while a stream is captured; the call to wait for stays the last one outside."""
+    answers = iter([False, False, True])
+    waits = []
+    monkeypatch.setattr(pp.module.KVCache, "_wait", lambda self, new, old: waits.append((new, old)) or next(answers),
+                        raising=False)
+    call = lambda stream: pp.module.pp_paged_attention(pp.kv, **_arguments()["pp_paged_attention"], stream=stream)
+    for raw in (3, 8, 8, 4):
+        call(_Stream(raw))
+    assert waits == [(8, 3), (8, 3), (4, 3)]
