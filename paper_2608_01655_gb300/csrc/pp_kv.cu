@@ -481,9 +481,9 @@ extern "C" pp_status pp_kv_create(int32_t blocks, int32_t block_size, int32_t kv
         const size_t slots = 2 * (size_t)kv->sm_count;
         PP_CUDA(cudaMalloc(&kv->d_piece, slots * kPieceRows * kKvMaxDim * sizeof(float)));
         PP_CUDA(cudaMalloc(&kv->d_piece_stat, slots * kPieceRows * 2 * sizeof(float)));
-        kv->count_bytes = 4 * slots * sizeof(int32_t);
-        PP_CUDA(cudaMalloc(&kv->d_count, kv->count_bytes));
-        PP_CUDA(cudaMemsetAsync(kv->d_count, 0, kv->count_bytes, (cudaStream_t)stream));
+        const size_t count_bytes = 4 * slots * sizeof(int32_t);
+        PP_CUDA(cudaMalloc(&kv->d_count, count_bytes));
+        PP_CUDA(cudaMemsetAsync(kv->d_count, 0, count_bytes, (cudaStream_t)stream));
         PP_CUDA(cudaStreamSynchronize((cudaStream_t)stream));
         return PP_OK;
     };
@@ -516,13 +516,16 @@ extern "C" pp_status pp_kv_destroy(pp_kv *kv)
 extern "C" pp_status pp_kv_sync(pp_kv *kv, void *stream)
 {
     if (!kv) return fail(PP_EINVAL, "null cache handle");
-    PP_CUDA(cudaStreamSynchronize((cudaStream_t)stream));
+    // on `stream` itself: the legacy stream would wait for other work, and clear the word after later
+    // calls on streams that do not wait for it.  A launch that gave up has no arrivals left to clear:
+    // its CTAs still leave their pieces, and the joins put their counters back to 0.
+    const cudaStream_t st = (cudaStream_t)stream;
     int32_t v = 0;
-    PP_CUDA(cudaMemcpy(&v, kv->d_status, sizeof(v), cudaMemcpyDeviceToHost));
+    PP_CUDA(cudaMemcpyAsync(&v, kv->d_status, sizeof(v), cudaMemcpyDeviceToHost, st));
+    PP_CUDA(cudaStreamSynchronize(st));
     if (v == PP_OK) return PP_OK;
-    PP_CUDA(cudaMemset(kv->d_status, 0, sizeof(int32_t)));
-    // a launch that gave up may have left arrivals
-    if (v == PP_ETIMEOUT) PP_CUDA(cudaMemset(kv->d_count, 0, kv->count_bytes));
+    PP_CUDA(cudaMemsetAsync(kv->d_status, 0, sizeof(int32_t), st));
+    PP_CUDA(cudaStreamSynchronize(st));
     if (v == PP_ETIMEOUT) return fail(PP_ETIMEOUT, "a bounded device wait ran out");
     if (v == PP_EBOUNDS)
         return fail(PP_EBOUNDS, "device bounds check failed (a length, block, slot, chunk or token count)");

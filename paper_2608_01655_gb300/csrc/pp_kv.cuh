@@ -22,7 +22,6 @@ struct pp_kv {
     // maxima and sums, and arrival counts (0 between launches)
     float *d_piece = nullptr, *d_piece_stat = nullptr;
     int32_t *d_count = nullptr;
-    size_t count_bytes = 0;
 };
 
 namespace pp {

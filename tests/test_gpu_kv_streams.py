@@ -77,3 +77,23 @@ def test_an_eager_call_beside_a_capture(pp):
         kv.sync(side)
     for out in (captured, beside, after):
         assert torch.equal(out.view(torch.int16), first.view(torch.int16))
+
+
+def test_sync_is_of_its_own_stream(pp):
+    """Reading the status on a stream neither waits for work elsewhere nor leaves its clearing to it."""
+    kc = torch.zeros((4, 16, 1, 8), dtype=torch.bfloat16, device="cuda")
+    rows, wrong = torch.ones((1, 1, 8), dtype=torch.bfloat16, device="cuda"), torch.tensor([64], device="cuda")
+    side, busy = torch.cuda.Stream(), torch.cuda.Event()
+    with pp.KVCache.like(kc) as kv:
+        pp.pp_kv_write(kv, rows, rows, wrong - 60, kc, kc.clone())
+        torch.cuda.synchronize()
+        torch.cuda._sleep(1_000_000_000)                    # half a second of the default stream
+        busy.record()
+        kv.sync(side)
+        for _ in range(20):
+            pp.pp_kv_write(kv, rows, rows, wrong, kc, kc, stream=side)
+            with pytest.raises(pp.PPError, match="PP_EBOUNDS"):
+                kv.sync(side)
+        kv.sync(side)
+        assert not busy.query()
+        torch.cuda.synchronize()
