@@ -329,13 +329,17 @@ pp_status pp_plan_run(pp_instance *inst, int32_t n_starts, const int32_t *orders
                       pp_plan_stats *stats, void *stream);
 
 /*
- * pp_test_inject -- testing hook for the failure path of the DP kernel's
- * bounded waits; it makes no GPU fault.  kind 1: from the next launch on, the
+ * pp_test_inject -- testing hook for the failure path of the kernels' bounded
+ * waits; it makes no GPU fault.  kind 1: from the next launch on, the
  * chain warp with index `value` (-1 = none, the default) stops publishing
  * its ring counter, so the warp to its right waits until its time limit
  * (0.5 s) runs out, every warp of the launch leaves its loop, and
  * pp_instance_sync() reports PP_ETIMEOUT with the context still usable.
- * Applies to the current device.  Errors: PP_EINVAL, PP_ECUDA.
+ * Applies to the current device.  kind 2: with `value` >= 0 (-1 = off, the
+ * default) the pp_paged_attention calls that follow in this process, where
+ * they take the kernel of chunks, wait for 16 bytes a K tile that never come,
+ * 2 ms at most; they end all the same and pp_kv_sync() reports PP_ETIMEOUT.
+ * Errors: PP_EINVAL, PP_ECUDA.
  */
 pp_status pp_test_inject(int32_t kind, int32_t value);
 

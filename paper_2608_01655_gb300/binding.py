@@ -303,7 +303,8 @@ def pp_plan_run(inst: Instance, n_starts: int, orders=None, max_rounds: int = 0,
 
 def pp_test_inject(kind: int, value: int):
     """Testing hook: kind 1 makes chain warp `value` of later DP launches stop
-    publishing its ring counter (-1 restores normal operation)."""
+    publishing its ring counter; kind 2 makes later attention calls of chunks wait
+    for copies that never come (value >= 0).  -1 restores normal operation."""
     _check(_lib.pp_test_inject(int(kind), int(value)))
 
 

@@ -7,9 +7,15 @@
 //   lse = m + log sum_j exp(s_j - m);  without a visible key o = 0, lse = -inf.
 #include <cudaTypedefs.h>
 
+#include <atomic>
+
 #include "pp_attend.cuh"
 
 namespace pp {
+
+static std::atomic<bool> g_lose_copies{false};
+
+void attend_lose_copies(bool on) { g_lose_copies.store(on); }
 
 AttendDev attend_dev(const pp_kv *kv, const AttendArgs &c)
 {
@@ -32,6 +38,9 @@ AttendDev attend_dev(const pp_kv *kv, const AttendArgs &c)
     a.piece = kv->d_piece;
     a.piece_stat = kv->d_piece_stat;
     a.count = kv->d_count;
+    const bool lose = g_lose_copies.load(std::memory_order_relaxed);
+    a.wait_limit = lose ? kAttendTestCycles : kAttendLimitCycles;
+    a.lost = lose ? 16 : 0;
     return a;
 }
 

@@ -33,9 +33,12 @@ struct AttendDev {
     float *piece;                       // pieces' outputs, [slot][...]
     float *piece_stat;                  // their maxima (log2 units) and sums
     int32_t *count;                     // [2][slots] state of the joins, left at 0 by every launch
+    int64_t wait_limit;                 // cycles after which one wait gives up
+    uint32_t lost;                      // bytes of a K tile that are waited for and never come (tests)
 };
 
-constexpr int64_t kAttendLimitCycles = 4000ll * 1000 * 1000;  // one wait gives up after about 2 s
+constexpr int64_t kAttendLimitCycles = 4000ll * 1000 * 1000;  // about 2 s
+constexpr int64_t kAttendTestCycles = 4ll * 1000 * 1000;      // about 2 ms, while pp_test_inject has copies lost
 
 // ---------------------------------------------------------------------------
 // Requests and their items
@@ -363,7 +366,7 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)
 // wait of the CTA waits: its loops run to their end over whatever is there, the
 // status says PP_ETIMEOUT, and the launch ends.  (Inlined: a call would keep
 // registers from code that runs on a share of its own.)
-__device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, volatile int32_t *dead, int32_t *status)
+__device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, volatile int32_t *dead, const AttendDev &a)
 {
     int64_t t0 = 0;
     for (uint32_t it = 0; !mbar_try(bar, parity); ++it) {
@@ -372,9 +375,9 @@ __device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, volatil
         const int64_t now = clock64();
         if (t0 == 0) {
             t0 = now;
-        } else if (now - t0 > kAttendLimitCycles) {
+        } else if (now - t0 > a.wait_limit) {
             *dead = 1;
-            atomicExch(status, (int32_t)PP_ETIMEOUT);
+            atomicExch(a.status, (int32_t)PP_ETIMEOUT);
             return;
         }
     }

@@ -302,7 +302,9 @@ __device__ __forceinline__ void copy_role(const AttendDev &a, const SchedShared 
     const int32_t in_block = (1 << a.block_log) - 1;
 
     Cursor<Shape> cur(a, sched);
+    const uint32_t lost = which ? 0 : a.lost;
     uint32_t slot = 0, turn = 0, used = 0;
+    bool stop = false;
     do {
         const int32_t *row = a.c.block_table + (int64_t)cur.r * a.c.table_width;
         const int32_t t0 = cur.k.lo / KT + cur.off;
@@ -310,11 +312,12 @@ __device__ __forceinline__ void copy_role(const AttendDev &a, const SchedShared 
             return asks ? key_block(a, row, cur.k, t * KT + (box << box_log), 1 << box_log) : -1;
         };
         int32_t id = block(t0);
-        for (int32_t i = 0; i < cur.len && !*dead; ++i) {
+        for (int32_t i = 0; i < cur.len; ++i) {
             const int32_t after = i + 1 < cur.len ? block(t0 + i + 1) : -1;
-            if (used == slots) mbar_wait(empty + 8 * slot, turn ^ 1, dead, a.status);
-            if (*dead) break;
-            if (lane == 0) mbar_expect(full + 8 * slot, L::tile);
+            if (used == slots) mbar_wait(empty + 8 * slot, turn ^ 1, dead, a);
+            stop = __any_sync(~0u, *dead);              // all lanes go on, or none
+            if (stop) break;
+            if (lane == 0) mbar_expect(full + 8 * slot, L::tile + lost);
             __syncwarp();
             if (asks)
                 box_rows(dst + slot * L::tile, map, full + 8 * slot, half * 64, ((t0 + i) * KT + (box << box_log)) & in_block,
@@ -326,15 +329,13 @@ __device__ __forceinline__ void copy_role(const AttendDev &a, const SchedShared 
                 turn ^= 1;
             }
         }
-    } while (!*dead && cur.next(a));
-    if (*dead) {
-        // copies in flight land before the CTA ends
-        int32_t none = 0;
-        for (uint32_t x = 0; x < used; ++x) {
-            if (slot == 0) turn ^= 1;
-            slot = slot ? slot - 1 : slots - 1;
-            mbar_wait(full + 8 * slot, turn, &none, a.status);
-        }
+    } while (!stop && cur.next(a));
+    // copies in flight land before the CTA ends, which may not wait for them any more
+    int32_t none = 0;
+    for (uint32_t x = 0; x < used; ++x) {
+        if (slot == 0) turn ^= 1;
+        slot = slot ? slot - 1 : slots - 1;
+        mbar_wait(full + 8 * slot, turn, &none, a);
     }
 }
 
@@ -377,8 +378,8 @@ __device__ __forceinline__ void mma_role(const AttendDev &a, const SchedShared &
     do {
         if (s * kRows >= Shape::rows(a, cur.q) - cur.inner * 2 * kRows) {        // no rows in this stage
             for (int32_t i = 0; i < cur.len; ++i) {
-                mbar_wait(b.k_full + 8 * ks, k_turn, dead, a.status);
-                mbar_wait(b.v_full + 8 * vs, v_turn, dead, a.status);
+                mbar_wait(b.k_full + 8 * ks, k_turn, dead, a);
+                mbar_wait(b.v_full + 8 * vs, v_turn, dead, a);
                 if (elected()) {
                     mbar_arrive(b.k_empty + 8 * ks);
                     mbar_arrive(b.v_empty + 8 * vs);
@@ -389,22 +390,22 @@ __device__ __forceinline__ void mma_role(const AttendDev &a, const SchedShared &
             continue;
         }
         const bool both = Shape::rows(a, cur.q) - cur.inner * 2 * kRows > kRows;
-        mbar_wait(b.q_full + 8 * s, q_turn & 1, dead, a.status);
-        mbar_wait(b.k_full + 8 * ks, k_turn, dead, a.status);
+        mbar_wait(b.q_full + 8 * s, q_turn & 1, dead, a);
+        mbar_wait(b.k_full + 8 * ks, k_turn, dead, a);
         tc_after();
         issue_s();
         // O is free when its last item's output has been read
-        if (q_turn) mbar_wait(b.o_free + 8 * s, (q_turn - 1) & 1, dead, a.status);
+        if (q_turn) mbar_wait(b.o_free + 8 * s, (q_turn - 1) & 1, dead, a);
         for (int32_t i = 0; i < cur.len; ++i) {
             // what is likely there already first: a wait costs 85 cycles even then
-            mbar_wait(b.v_full + 8 * vs, v_turn, dead, a.status);
-            if (i + 1 < cur.len) mbar_wait(b.k_full + 8 * ks, k_turn, dead, a.status);
+            mbar_wait(b.v_full + 8 * vs, v_turn, dead, a);
+            if (i + 1 < cur.len) mbar_wait(b.k_full + 8 * ks, k_turn, dead, a);
             if (both) {
-                if (s == 1 || pass) mbar_wait(b.pass + 8 * s, (pass + s + 1) & 1, dead, a.status);
+                if (s == 1 || pass) mbar_wait(b.pass + 8 * s, (pass + s + 1) & 1, dead, a);
                 ++pass;
             }
             const uint64_t v_op = smem_operand(v_at<HALVES>(base, vs), L::half, 1024);
-            mbar_wait(b.p_full + 8 * s, p_turn++ & 1, dead, a.status);
+            mbar_wait(b.p_full + 8 * s, p_turn++ & 1, dead, a);
             tc_after();
             if (elected()) {
 #pragma unroll
@@ -422,7 +423,7 @@ __device__ __forceinline__ void mma_role(const AttendDev &a, const SchedShared &
     // every product has ended before the tensor memory is given back
     if (elected()) tc_commit(b.fin + 8 * s);
     int32_t none = 0;
-    mbar_wait(b.fin + 8 * s, 0, &none, a.status);
+    mbar_wait(b.fin + 8 * s, 0, &none, a);
 }
 
 // A warpgroup replaces what is not finite in a V tile by 0.  Where that is in a
@@ -541,7 +542,7 @@ __device__ __forceinline__ void softmax_role(const AttendDev &a, const SchedShar
         float m = live ? -INFINITY : 0.f, l = 0.f;
 
         for (int32_t i = 0; i < len; ++i, ++k) {
-            mbar_wait(b.s_full + 8 * s, s_turn++ & 1, dead, a.status);
+            mbar_wait(b.s_full + 8 * s, s_turn++ & 1, dead, a);
             tc_after();
             if (i == len - 1) {
                 // the last S is there, so the queries' place is free: the next item's are asked for
@@ -627,7 +628,7 @@ __device__ __forceinline__ void softmax_role(const AttendDev &a, const SchedShar
             tc_st32(t_s + 32, p + 32);
             if (!item_sees.covers(j0)) {
                 const uint32_t slot = k % L::v_slots;
-                mbar_wait(b.v_full + 8 * slot, (k / L::v_slots) & 1, dead, a.status);
+                mbar_wait(b.v_full + 8 * slot, (k / L::v_slots) & 1, dead, a);
                 clean_tile<T, HALVES>(reinterpret_cast<uint4 *>(mem + v_at<HALVES>(0, slot)), t, j0, keys.lo, keys.hi,
                                       bad + item % kBad, item + 1);
             }
@@ -637,7 +638,7 @@ __device__ __forceinline__ void softmax_role(const AttendDev &a, const SchedShar
             mbar_arrive(b.p_full + 8 * s);
         }
         if (asked) have_q();
-        if (given) mbar_wait(b.stat_free + 8 * s, (given - 1) & 1, dead, a.status);
+        if (given) mbar_wait(b.stat_free + 8 * s, (given - 1) & 1, dead, a);
         ++given;
         m_out[t] = m;
         l_out[t] = l;
@@ -889,10 +890,10 @@ __device__ __forceinline__ void output_role(const AttendDev &a, const SchedShare
             const OutRow<T> out(a, cur, row);
             const uint32_t t_o = tmem + ((uint32_t)(t & ~31) << 16) + 256 + 128 * s;
             const uint32_t now = s ? turn[1]++ & 1 : turn[0]++ & 1;
-            mbar_wait(b.stat_full + 8 * s, now, dead, a.status);
+            mbar_wait(b.stat_full + 8 * s, now, dead, a);
             const float m = m_in[kRows * s + t], l = l_in[kRows * s + t];
             mbar_arrive(b.stat_free + 8 * s);
-            mbar_wait(b.o_done + 8 * s, now, dead, a.status);
+            mbar_wait(b.o_done + 8 * s, now, dead, a);
             tc_after();
             const float inv = out.inverse(l);
             const bool fix = bad[item % kBad] == item + 1;

@@ -1145,6 +1145,10 @@ extern "C" pp_status pp_tree_dp(pp_instance *inst, int32_t batch, const int64_t 
 
 extern "C" pp_status pp_test_inject(int32_t kind, int32_t value)
 {
+    if (kind == 2) {
+        attend_lose_copies(value >= 0);
+        return PP_OK;
+    }
     if (kind != 1) return fail(PP_EINVAL, "unknown injection kind");
     PP_CUDA(cudaMemcpyToSymbol(g_drop_publish_warp, &value, sizeof(value)));
     int dev = 0;

@@ -280,6 +280,8 @@ size_t reduce_item_bytes(const pp_instance *inst);
 // whether launches of this instance try the reduction first (not without
 // pruning, and not while pp_test_inject makes a warp of the sweep silent)
 bool reduce_on(const pp_instance *inst);
+// pp_test_inject: attention calls from here on wait for copies that never come (pp_attend.cu)
+void attend_lose_copies(bool on);
 pp_status launch_reduce(pp_instance *inst, int batch, const int64_t *profit, bool by_node,
                         const int32_t *item_budget, const int32_t *item_active, int64_t *best, const DpWork &work,
                         cudaStream_t st, int32_t max_budget, unsigned long long *rows_kept);
