@@ -459,6 +459,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_token(const __grid_const
             const int32_t mine = (int32_t)blockIdx.x - cta0;
             const int32_t groups = (pieces + kJoinGroup - 1) / kJoinGroup;
             auto put = [&](int32_t slot) {
+                __syncwarp();                           // a row's 16 lanes have read what one of them writes over
                 if (jr < rows) {
                     float4 *dst = reinterpret_cast<float4 *>(a.piece + ((int64_t)slot * kRows + jr) * L::width + jd);
 #pragma unroll
