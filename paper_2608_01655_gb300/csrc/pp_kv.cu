@@ -3,6 +3,7 @@
 #include <algorithm>
 #include <climits>
 #include <cstdlib>
+#include <exception>
 #include <initializer_list>
 #include <new>
 #include <vector>
@@ -21,15 +22,16 @@ namespace pp {
 static pp_status chunk_map(int32_t n, const int32_t *parent, const int32_t *weight, const uint8_t *resident,
                            int32_t blocks_per_slot, int32_t *map, int32_t *blocks)
 {
-    // order: every parent before its children
-    std::vector<int32_t> kids(n, 0), order;
-    std::vector<int64_t> first(n + 1, 0);
     for (int32_t v = 0; v < n; ++v) {
         if (parent[v] < -1 || parent[v] >= n || parent[v] == v)
             return fail(PP_ENOTTREE, "parent id out of range or self-parent at node " + std::to_string(v));
         if (weight[v] < 1) return fail(PP_EINVAL, "chunk weight must be >= 1");
-        if (parent[v] >= 0) kids[parent[v]]++;
     }
+    // order: every parent before its children
+    std::vector<int32_t> kids(n, 0), order;
+    std::vector<int64_t> first((size_t)n + 1, 0);
+    for (int32_t v = 0; v < n; ++v)
+        if (parent[v] >= 0) kids[parent[v]]++;
     for (int32_t v = 0; v < n; ++v) first[v + 1] = first[v] + kids[v];
     std::vector<int32_t> child(n);
     std::vector<int64_t> at(first.begin(), first.end() - 1);
@@ -428,7 +430,7 @@ extern "C" pp_status pp_chunk_map(int32_t n, const int32_t *parent, const int32_
         return fail(PP_EINVAL, "blocks_per_slot must be between 1 and 2^30");
     try {
         return chunk_map(n, parent, weight, resident, blocks_per_slot, map, blocks);
-    } catch (const std::bad_alloc &) {
+    } catch (const std::exception &) {
         return fail(PP_ENOMEM, "host allocation failed");
     }
 }
