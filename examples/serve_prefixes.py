@@ -11,6 +11,7 @@ token to each.  The model is one attention layer with random weights over
 embeddings of token and position; what the cached rows give is compared with
 attention over whole prompts computed anew.
 """
+import math
 import os
 import sys
 
@@ -138,7 +139,10 @@ def check(layer, sequence, length, starts, out, some):
         score = (q[:, n - (b - a):] @ k.transpose(1, 2)) * DIM ** -0.5
         score.masked_fill_(position > position[n - (b - a):, None], float("-inf"))
         want = (score.softmax(-1) @ v).transpose(0, 1)
-        worst = max(worst, float((out[a:b].double() - want).abs().max() / want.abs().max()))
+        error = float((out[a:b].double() - want).abs().max() / want.abs().max())
+        if not math.isfinite(error):                        # max() below would pass over a NaN
+            raise ArithmeticError(f"attention gave infinities or NaN for request {r}")
+        worst = max(worst, error)
     return worst
 
 
