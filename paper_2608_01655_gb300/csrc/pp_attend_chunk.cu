@@ -177,7 +177,7 @@ __device__ __forceinline__ uint64_t smem_operand(uint32_t addr, uint32_t next, u
 // 32-bit sums of 16-bit products, 128 rows; `transposed`: B's rows run along the summed index
 template <typename T> __device__ __forceinline__ uint32_t mma_kind(int n, bool transposed)
 {
-    const uint32_t type = sizeof(KvType<T>) && std::is_same<T, __nv_bfloat16>::value ? 1 : 0;
+    const uint32_t type = std::is_same<T, __nv_bfloat16>::value ? 1 : 0;
     return 1u << 4 | type << 7 | type << 10 | (transposed ? 1u << 16 : 0) | (uint32_t)(n / 8) << 17 | (128u / 16) << 24;
 }
 __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t kind, bool add)

@@ -18,7 +18,6 @@
 // of the line and the first rows' latency, 5 the joins of 38 pieces an item; 32
 // requests of 4 tokens after 5,000 (16 rows on each of 2 heads, 164 MB) 51 us.
 // DRAM 75% of its cycles and 17% of the tensor instructions' in the former's half.
-#include <climits>
 #include <cstring>
 #include <type_traits>
 

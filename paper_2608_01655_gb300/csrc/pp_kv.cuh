@@ -57,11 +57,9 @@ __device__ __forceinline__ void kv_bounds(int32_t *status)
 template <typename T> struct KvType;
 template <> struct KvType<__nv_bfloat16> {
     static __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
-    static __device__ __forceinline__ __nv_bfloat16 from_float(float x) { return __float2bfloat16_rn(x); }
 };
 template <> struct KvType<__half> {
     static __device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
-    static __device__ __forceinline__ __half from_float(float x) { return __float2half_rn(x); }
 };
 
 }  // namespace pp
