@@ -82,10 +82,11 @@ pp_status prepare_attend()
 // goes to the kernel of single tokens.  That one reads K and V once for every 16
 // rows and has short items to begin and to join; the chunk kernel pays for 256 rows
 // whatever there are.  Kernel of single tokens against chunks', in us, 2 K/V heads
-// of 128, 32 requests after 5,000 tokens / 4 after 2,000 / 1 after 50,000:
-//   16 rows  51 : 61 / 22 : 34 / 34 : 50
-//   32       64 : 61 / 22 : 34 / 36 : 47
-//   64      105 : 61 / 28 : 34 / 42 : 50
+// of 128, 32 requests after 5,000 tokens / 4 after 2,000 / 1 after 50,000 (single
+// passes after a flush of L2):
+//   16 rows  50 : 61 / 22 : 33 / 34 : 56
+//   32       64 : 61 / 21 : 31 / 36 : 56
+//   64      104 : 61 / 28 : 32 / 42 : 54
 // so at 64 it loses more in batches than it gains for single requests.
 constexpr int64_t kFewRows = 32;
 

@@ -25,9 +25,11 @@
 // and 1,000 cycles of hand-over; at width 64 the products are half and the
 // exponentials bound it.  256 rows an item is what tensor memory holds (two S and
 // two O of 128 columns).
-// Measured: 8,192 new tokens after 24,576 (28 heads on 4, width 128) 1.90 ms, 1,770
-// TFLOP/s or 95% of the measured library product; 8,192 tokens of 16 heads from
-// nothing 220 us, 1,250 TFLOP/s; the same at width 64 175 us, 780 TFLOP/s.
+// Measured, single passes after a pause: 8,192 new tokens after 24,576 (28 heads on 4,
+// width 128) 1.90 ms, 1,770 TFLOP/s or 95% of the measured library product (in a row,
+// under the power limit, 2.07 ms and 1,630, of a library product's 1,722 there); 8,192
+// tokens of 16 heads from nothing 217 us, 1,270 TFLOP/s; the same at width 64 166 us,
+// 830 TFLOP/s.
 #include <algorithm>
 #include <new>
 #include <type_traits>

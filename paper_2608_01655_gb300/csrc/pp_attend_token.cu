@@ -2,8 +2,9 @@
 //
 // An item is 16 rows (new token, query head) of one K/V head, token first: they
 // see the same keys, or all but a few, so each K and V row is read once for them.
-// What bounds it is the read of K and V (4 to 32 operations a byte); the products
-// run on m16n8k16 tensor instructions with those 16 rows (padded), which
+// What bounds it is the read of K and V: an operation a byte for each row that
+// shares it, 1 (a single token of a head of its own) to 16, and 32 where a second
+// item's read comes from L2.  The products run on m16n8k16 tensor instructions with those 16 rows (padded), which
 // keeps scores, weights and sums in registers: the score's accumulators are the
 // next product's operand as they stand (a 128-row product would have 120 rows of
 // padding and pass its weights through tensor memory).  A tile is 128 keys, 16 a
@@ -12,11 +13,12 @@
 // joined once an item: between items no warp waits for another.  Keys that not
 // every row sees are masked row by row; an infinite or NaN V row among them is
 // replaced by zeros and added to the rows that see it.
-// Measured: 128 requests of 200 to 16,000 tokens (28 heads on 4, width 128, blocks
-// of 16, 1.52 GB) 253 us, 6.0 TB/s or 89% of the measured copy rate; two contexts of
-// 131,000 and 200,000 tokens 85 us, 4.0 TB/s: 10 us of it are the launch, the cut
+// Measured, single passes after a flush of L2: 128 requests of 200 to 16,000 tokens
+// (28 heads on 4, width 128, blocks of 16, 1.52 GB) 253 us, 6.0 TB/s or 89% of the
+// measured copy rate (among other passes 237, 6.4); two contexts of 131,000 and
+// 200,000 tokens 85 us, 4.1 TB/s (67, 5.2): 10 us of it are the launch, the cut
 // of the line and the first rows' latency, 5 the joins of 38 pieces an item; 32
-// requests of 4 tokens after 5,000 (16 rows on each of 2 heads, 164 MB) 51 us.
+// requests of 4 tokens after 5,000 (16 rows on each of 2 heads, 164 MB) 50 us.
 // DRAM 75% of its cycles and 17% of the tensor instructions' in the former's half.
 #include <cstring>
 #include <type_traits>
