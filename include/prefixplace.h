@@ -463,7 +463,8 @@ pp_status pp_replan(pp_instance *inst, const uint8_t *incumbent, int32_t n_start
  */
 typedef struct pp_kv pp_kv;               /* opaque, library-owned */
 
-enum { PP_KV_BF16 = 0, PP_KV_F16 = 1 };
+/* The last two: caches of 8-bit numbers (below), rows of the 16-bit type. */
+enum { PP_KV_BF16 = 0, PP_KV_F16 = 1, PP_KV_BF16_E4M3 = 16, PP_KV_F16_E4M3 = 17 };
 
 /*
  * pp_kv_create -- a handle of the caches of one layout; the buffers are passed
@@ -471,10 +472,12 @@ enum { PP_KV_BF16 = 0, PP_KV_F16 = 1 };
  *   blocks        blocks of a cache, 1 .. 2^30
  *   block_size    tokens per block: a power of two, 8 .. 512
  *   kv_heads      K/V heads, 1 .. 65535
- *   head_dim      a multiple of 8, 8 .. 128
- *   dtype         PP_KV_BF16 or PP_KV_F16, of the caches and of q, k, v, out
+ *   head_dim      a multiple of 8, 8 .. 128; of 16 for 8-bit caches
+ *   dtype         PP_KV_BF16 or PP_KV_F16, of the caches and of q, k, v, out;
+ *                 PP_KV_BF16_E4M3 or PP_KV_F16_E4M3: q, k, v and out of that
+ *                 type, caches of 8-bit numbers
  *   block_stride, token_stride, head_stride
- *                 elements, positive multiples of 8 of at least head_dim, of a
+ *                 elements, positive multiples of 8 (8-bit caches: 16) of at least head_dim, of a
  *                 layout in which no two rows overlap;
  *                 0, 0, 0: contiguous [blocks][block_size][kv_heads][head_dim]
  *   stream        stream of the set-up; the call synchronises it
@@ -615,6 +618,140 @@ pp_status pp_paged_attention(pp_kv *kv, int32_t requests, int32_t tokens, int32_
                              const int32_t *q_start, const int32_t *length, int32_t max_q, int32_t window,
                              float scale, void *out, int64_t out_token_stride, int64_t out_head_stride,
                              float *lse, void *stream);
+
+/*
+ * Rows at their positions: norms of query and key heads and the rotation to a
+ * token's position, in one pass, with the keys (and values) straight into the
+ * cache or the keys to rows.
+ *
+ * pp_rotary_frequencies -- host-only: frequency[i] = base^(-i / pairs) radians a
+ * token, scaled for contexts longer than those a model was trained on.  With
+ * original = 0 all are divided by `factor` (1: as they are).  Otherwise by parts:
+ * a pair that turns r = original * frequency / (2 pi) times in the original
+ * context keeps its frequency from r = fast on, has it divided by factor up to
+ * r = slow, and in between g f + (1 - g) f / factor, g = (r - slow) / (fast - slow).
+ *   pairs         0 .. 64
+ *   base, factor  > 0
+ *   frequency     host [pairs] out
+ * Errors: PP_EINVAL.
+ */
+pp_status pp_rotary_frequencies(int32_t pairs, double base, double factor, double original, double slow, double fast,
+                                double *frequency);
+
+/*
+ * pp_rotary_turns -- host-only: frequencies (radians a token, any finite ones) as
+ * 64-bit fractions of a turn, what pp_kv_rotate takes: position times turns modulo
+ * 2^64 is exact, so an angle is as good at the last position as at the first
+ * (off by 2^-53 of itself before whole turns go, and by 2^-31 rad).
+ *   frequency     host [pairs]
+ *   turns         host [pairs] out
+ * Errors: PP_EINVAL.
+ */
+pp_status pp_rotary_turns(int32_t pairs, const double *frequency, uint64_t *turns);
+
+/*
+ * pp_kv_rotate -- the step's new query and key rows, normed and rotated:
+ *   y = x                                        without a weight
+ *   y = x * weight / sqrt(mean(x^2) + eps)       with one (over a head's elements)
+ *   (y_a, y_b) -> amplitude (y_a cos t - y_b sin t, y_b cos t + y_a sin t)
+ * with t = position * frequency i for pair i < rotated / 2, (a, b) = (i, i +
+ * rotated / 2) or, interleaved, (2 i, 2 i + 1); elements from `rotated` on are y.
+ * All of it in 32 bits, rounded once; rows that are neither normed nor rotated
+ * keep their bits.  The handle gives head_dim, kv_heads and the 16-bit type; where
+ * no cache is given its own may be of either kind.
+ *   tokens        0 .. 2^30
+ *   q_heads       0 .. 2^20; with 0, q and q_out are not looked at
+ *   q, q_out      device [tokens][q_heads][head_dim]
+ *   k             device [tokens][kv_heads][head_dim]
+ *   k_out         the same, or NULL if k goes to the cache (it may go to both)
+ *   q_weight, k_weight   device [head_dim] of the rows' type, or NULL
+ *   position      device [tokens], any
+ *   rotated       even, 0 .. head_dim
+ *   turns         device [rotated / 2], from pp_rotary_turns; not read with 0
+ *   amplitude     what cos and sin are multiplied with (1: a rotation)
+ *   v, slot_map, k_cache, v_cache   as in pp_kv_write, all of them or none: k's
+ *                 results and v's rows go to their slots (negative: left out)
+ * Strides in elements, positive multiples of 8; bases and weights aligned to 16
+ * bytes.  q_out may be q and k_out k, with the same strides; else outputs lie
+ * apart from all inputs and from one another, and their rows must not overlap.
+ * A slot above the cache sets PP_EBOUNDS and is left out.
+ * Errors: PP_EINVAL, PP_ECUDA.
+ */
+pp_status pp_kv_rotate(pp_kv *kv, int32_t tokens, int32_t q_heads, const void *q, int64_t q_token_stride,
+                       int64_t q_head_stride, const void *k, int64_t k_token_stride, int64_t k_head_stride,
+                       const void *q_weight, const void *k_weight, float eps, const int32_t *position,
+                       int32_t rotated, int32_t interleaved, const uint64_t *turns, float amplitude, void *q_out,
+                       int64_t q_out_token_stride, int64_t q_out_head_stride, void *k_out,
+                       int64_t k_out_token_stride, int64_t k_out_head_stride, const void *v,
+                       int64_t v_token_stride, int64_t v_head_stride, const int64_t *slot_map, void *k_cache,
+                       void *v_cache, void *stream);
+
+/*
+ * A cache of 8-bit numbers holds twice the chunks in the same memory.  The handle
+ * is made with PP_KV_BF16_E4M3 or PP_KV_F16_E4M3; pp_block_tables works on it as
+ * on any other, pp_kv_write and pp_paged_attention refuse it.  An element is
+ * code * 2^e: an e4m3 number (4 significant bits, exponents from -6 to 8, 448 the
+ * largest, NaN and no infinity) and the exponent of its block and head, -40 .. 40.
+ * K and V have exponents of their own, device int8 [blocks][kv_heads]; numbers
+ * outside the range are read as its ends.
+ *
+ * pp_kv_write8 -- store the new tokens' K and V rows at their slots.  For each
+ * block with new rows, each head, and K and V apart,
+ *   need = the least e in [-40, 40] with |x| <= 448 * 2^e for all finite x of the new rows;
+ *   a call that writes the block's first row begins it anew: e' = need.  The
+ *   block's rows that the call does not write hold nothing then (their codes stay);
+ *   else e' = max(e, need), and where that is above e the block's other rows go to
+ *   the new scale, code' = code * 2^(e - e') to the nearest e4m3 number;
+ *   new codes are x * 2^-e' to the nearest (ties to even; beyond 448, which needs
+ *   |x| > 448 * 2^40, to that); infinities and NaN become NaN.
+ *   tokens, k, v, strides, slot_map as in pp_kv_write.  Tokens of one block stand
+ *                 next to one another, in any order, with fewer than 32 tokens that
+ *                 are left out between two of them, as pp_block_tables leaves them
+ *   k_cache, v_cache, k_exp, v_exp   device; four different buffers
+ * Every row of a request is to be written by one call a layer: a block that is
+ * shared by requests is full and no longer written.
+ * A slot above the cache sets PP_EBOUNDS and is left out.
+ * Errors: PP_EINVAL, PP_ECUDA.
+ */
+pp_status pp_kv_write8(pp_kv *kv, int32_t tokens, const void *k, int64_t k_token_stride, int64_t k_head_stride,
+                       const void *v, int64_t v_token_stride, int64_t v_head_stride, const int64_t *slot_map,
+                       void *k_cache, int8_t *k_exp, void *v_cache, int8_t *v_exp, void *stream);
+
+/*
+ * pp_kv_workspace -- host-only: bytes of workspace of a pp_paged_attention8 call
+ * with chunks.
+ *   requests, table_width   as in that call, or more
+ *   blocks        blocks that the requests' new tokens see, counted for each request
+ *                 (at most the sum of ceil(length / block_size))
+ *   bytes         host out
+ * Errors: PP_EINVAL (also a handle of 16-bit caches).
+ */
+pp_status pp_kv_workspace(const pp_kv *kv, int32_t requests, int32_t table_width, int32_t blocks, size_t *bytes);
+
+/*
+ * pp_paged_attention8 -- pp_paged_attention over a cache of 8-bit numbers, with the
+ * same formula and arguments and
+ *   k_exp, v_exp  device [blocks][kv_heads]
+ *   workspace     device, aligned to 16 bytes, pp_kv_workspace bytes or more.  Not
+ *                 looked at where max_q * (q_heads / kv_heads) <= 32
+ * Calls of few rows (that limit) read codes and exponents directly: products of codes
+ * with queries of 11 significant bits (bf16's 8 fit) and 32-bit sums, weights rounded
+ * to 11 bits for their product with V.  Calls of chunks unpack what the queries see
+ * into the workspace as rows of the 16-bit type and then are as pp_paged_attention.
+ * Unpacking is exact in bf16; in f16 beyond 65504 becomes that, and below 2^-14 it is
+ * off by 2^-25 at most.
+ * A workspace that has too few blocks for what the queries see sets PP_EBOUNDS (the
+ * missing ones read as zeros).  Calls that share a workspace must not overlap.
+ * Errors: PP_EINVAL (also a workspace that is missing or has no room for a block),
+ * PP_ECUDA.
+ */
+pp_status pp_paged_attention8(pp_kv *kv, int32_t requests, int32_t tokens, int32_t q_heads, const void *q,
+                              int64_t q_token_stride, int64_t q_head_stride, const void *k_cache,
+                              const int8_t *k_exp, const void *v_cache, const int8_t *v_exp, int32_t table_width,
+                              const int32_t *block_table, const int32_t *q_start, const int32_t *length,
+                              int32_t max_q, int32_t window, float scale, void *out, int64_t out_token_stride,
+                              int64_t out_head_stride, float *lse, void *workspace, size_t workspace_bytes,
+                              void *stream);
 
 /* Thread-local description of the last failure in this thread ("" if none). */
 const char *pp_last_error(void);

@@ -32,13 +32,14 @@ _lib = ctypes.CDLL(LIB_PATH)
 _P = ctypes.c_void_p
 _i32 = ctypes.c_int32
 _i64 = ctypes.c_int64
+_f64 = ctypes.c_double
 _st = ctypes.c_int
 
 PP_OK, PP_EINVAL, PP_ENOTTREE, PP_EOVERFLOW, PP_ENOMEM, PP_ECUDA, PP_ETIMEOUT, PP_EBOUNDS = range(8)
 STATUS_NAMES = ["PP_OK", "PP_EINVAL", "PP_ENOTTREE", "PP_EOVERFLOW", "PP_ENOMEM", "PP_ECUDA",
                 "PP_ETIMEOUT", "PP_EBOUNDS"]
 PP_TRANSFER_REQUESTER, PP_TRANSFER_SOURCE = 0, 1
-PP_KV_BF16, PP_KV_F16 = 0, 1
+PP_KV_BF16, PP_KV_F16, PP_KV_BF16_E4M3, PP_KV_F16_E4M3 = 0, 1, 16, 17
 
 
 class PPError(RuntimeError):
@@ -87,6 +88,14 @@ _SIGS = {
     "pp_kv_write": [_P, _i32, _P, _i64, _i64, _P, _i64, _i64, _P, _P, _P, _P],
     "pp_paged_attention": [_P, _i32, _i32, _i32, _P, _i64, _i64, _P, _P, _i32, _P, _P, _P, _i32, _i32,
                            ctypes.c_float, _P, _i64, _i64, _P, _P],
+    "pp_rotary_frequencies": [_i32, _f64, _f64, _f64, _f64, _f64, _P],
+    "pp_rotary_turns": [_i32, _P, _P],
+    "pp_kv_rotate": [_P, _i32, _i32, _P, _i64, _i64, _P, _i64, _i64, _P, _P, ctypes.c_float, _P, _i32, _i32, _P,
+                     ctypes.c_float, _P, _i64, _i64, _P, _i64, _i64, _P, _i64, _i64, _P, _P, _P, _P],
+    "pp_kv_write8": [_P, _i32, _P, _i64, _i64, _P, _i64, _i64, _P, _P, _P, _P, _P, _P],
+    "pp_kv_workspace": [_P, _i32, _i32, _i32, ctypes.POINTER(ctypes.c_size_t)],
+    "pp_paged_attention8": [_P, _i32, _i32, _i32, _P, _i64, _i64, _P, _P, _P, _P, _i32, _P, _P, _P, _i32, _i32,
+                            ctypes.c_float, _P, _i64, _i64, _P, _P, ctypes.c_size_t, _P],
 }
 for _name, _args in _SIGS.items():
     _f = getattr(_lib, _name)
@@ -415,11 +424,15 @@ class KVCache:
 
     _last = None                        # stream of the last attention call that may still run
 
+    _stored = None                      # element type of the caches where it is not `dtype`: float8_e4m3fn
+
     _DTYPES = {"bfloat16": PP_KV_BF16, "float16": PP_KV_F16}
 
-    def __init__(self, blocks, block_size, kv_heads, head_dim, dtype="bfloat16", strides=None, stream=None):
+    def __init__(self, blocks, block_size, kv_heads, head_dim, dtype="bfloat16", strides=None, stream=None,
+                 eight_bit=False):
         """strides: (block, token, head) in elements; None: contiguous
-        [blocks][block_size][kv_heads][head_dim]."""
+        [blocks][block_size][kv_heads][head_dim].  eight_bit: caches of float8_e4m3fn with exponents
+        (pp_kv_write8, pp_paged_attention8); dtype is that of the rows."""
         name = str(dtype).replace("torch.", "")
         if name not in self._DTYPES:
             raise ValueError("dtype must be bfloat16 or float16")
@@ -431,7 +444,10 @@ class KVCache:
         # the current stream's handle at a fiftieth of the cost of current_stream()
         self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         h = _P()
-        _check(_lib.pp_kv_create(*self.shape, self._DTYPES[name], *[int(x) for x in (strides or (0, 0, 0))],
+        if eight_bit:
+            self._stored, self._i8, self._u8 = torch.float8_e4m3fn, torch.int8, torch.uint8
+        code = self._DTYPES[name] + (PP_KV_BF16_E4M3 if eight_bit else 0)
+        _check(_lib.pp_kv_create(*self.shape, code, *[int(x) for x in (strides or (0, 0, 0))],
                                  _stream(stream), ctypes.byref(h)))
         self._h = h
         if strides is None:
@@ -439,13 +455,25 @@ class KVCache:
         self.strides = tuple(int(x) for x in strides)
 
     @classmethod
-    def like(cls, cache, stream=None):
-        """The layout of a [blocks][block_size][kv_heads][head_dim] CUDA tensor, of any strides."""
+    def like(cls, cache, stream=None, dtype=None):
+        """The layout of a [blocks][block_size][kv_heads][head_dim] CUDA tensor, of any strides.  dtype: of the
+        rows, where the cache is of float8_e4m3fn (bfloat16 by default)."""
         if cache.dim() != 4 or cache.stride(3) != 1:
             raise ValueError("expected [blocks][block_size][kv_heads][head_dim] with contiguous rows")
         # an extent of 1 may carry any stride
         strides = [s if n > 1 else cache.shape[3] for n, s in zip(cache.shape[:3], cache.stride()[:3])]
+        if str(cache.dtype) == "torch.float8_e4m3fn":
+            return cls(*cache.shape, dtype or "bfloat16", strides, stream, True)
+        if dtype is not None and str(dtype).replace("torch.", "") != str(cache.dtype).replace("torch.", ""):
+            raise ValueError(f"rows of a {cache.dtype} cache are of that type")
         return cls(*cache.shape, cache.dtype, strides, stream)
+
+    def workspace_size(self, requests, table_width, blocks):
+        """Bytes of workspace of a pp_paged_attention8 call with chunks; blocks: what the requests' new tokens see,
+        counted for each request."""
+        out = ctypes.c_size_t(0)
+        _check(_lib.pp_kv_workspace(self.handle, int(requests), int(table_width), int(blocks), ctypes.byref(out)))
+        return int(out.value)
 
     @property
     def handle(self):
@@ -510,12 +538,12 @@ class KVCache:
 
     def _cache(self, t, name):
         """Device pointer of a cache of this layout (an extent of 1 has no stride)."""
-        if t.dtype is self.dtype and t.shape == self.shape and t.get_device() == self._device:
+        if t.dtype is (self._stored or self.dtype) and t.shape == self.shape and t.get_device() == self._device:
             st = t.stride()
             if st[3] == 1 and (st[:3] == self.strides or
                                all(n == 1 or a == b for n, a, b in zip(self.shape, st, self.strides))):
                 return t.data_ptr()
-        raise ValueError(f"{name}: expected a {self.dtype} tensor on cuda:{self._device} of shape {self.shape} and "
+        raise ValueError(f"{name}: expected a {self._stored or self.dtype} tensor on cuda:{self._device} of shape {self.shape} and "
                          f"strides {self.strides + (1,)}")
 
     def _rows(self, t, name, tokens, heads):
@@ -567,4 +595,95 @@ def pp_paged_attention(kv: KVCache, q, k_cache, v_cache, block_table, q_start, l
         kv._cache(v_cache, "v_cache"), width, kv._arg(block_table, "block_table", i32, (r, width)),
         kv._arg(q_start, "q_start", i32, (r + 1,)), kv._arg(length, "length", i32, (r,)), max_q, window, scale,
         *kv._rows(out, "out", t, heads), None if lse is None else kv._arg(lse, "lse", kv._f32, (t, heads)),
+        kv._on_after_last(stream)))
+
+
+class Rotary:
+    """What pp_kv_rotate takes of a rotation: the frequencies of `rotated` / 2 pairs as fractions of a turn, on
+    the current device, the layout and the amplitude.
+
+    base, factor, original, slow, fast: pp_rotary_frequencies; frequencies (radians a token, [rotated / 2]) instead
+    of those.  amplitude: what cos and sin are multiplied with."""
+
+    def __init__(self, rotated, base=10000.0, factor=1.0, original=0, slow=1.0, fast=32.0, amplitude=1.0,
+                 interleaved=False, frequencies=None):
+        import torch
+        rotated = int(rotated)
+        if rotated < 0 or rotated % 2:
+            raise ValueError("rotated must be even and >= 0")
+        pairs = rotated // 2
+        if frequencies is None:
+            frequencies = np.zeros(max(pairs, 1))
+            _check(_lib.pp_rotary_frequencies(pairs, float(base), float(factor), float(original), float(slow), float(fast),
+                                              _host(frequencies)))
+            frequencies = frequencies[:pairs]
+        frequencies = _np(frequencies, np.float64)
+        if frequencies.shape != (pairs,):
+            raise ValueError("frequencies must be [rotated / 2]")
+        turns = np.zeros(max(pairs, 1), np.uint64)
+        _check(_lib.pp_rotary_turns(pairs, _host(frequencies), _host(turns)))
+        self.rotated, self.interleaved, self.amplitude = rotated, int(bool(interleaved)), float(amplitude)
+        self.frequencies = frequencies
+        self.turns = torch.from_numpy(turns.view(np.int64)).cuda()
+        self._device, self._ptr = self.turns.get_device(), self.turns.data_ptr()
+
+
+def pp_kv_rotate(kv: KVCache, rotary, q, k, position, q_out, k_out=None, q_weight=None, k_weight=None, eps: float = 1e-6,
+                 v=None, slot_map=None, k_cache=None, v_cache=None, stream=None):
+    """Norm (with weights [head_dim]) and rotate the rows q [T][q_heads][head_dim] and k [T][kv_heads][head_dim] to
+    position [T] int32, into q_out and k_out, or with v, slot_map [T] int64 and the caches into those.  rotary: a
+    Rotary, or None for norms alone.  q and q_out may both be None."""
+    t, h = position.shape[0], kv.shape[2]
+    none = (None, 0, 0)
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out go together")
+    if rotary is not None and rotary._device != kv._device:
+        raise ValueError(f"rotary: made on cuda:{rotary._device}, the cache is on cuda:{kv._device}")
+    if rotary is not None and rotary.rotated > kv.shape[3]:
+        raise ValueError(f"rotary: {rotary.rotated} elements of a head of {kv.shape[3]}")
+    heads, dim = 0 if q is None else q.shape[1], (kv.shape[3],)
+    _check(_lib.pp_kv_rotate(
+        kv.handle, t, heads, *(none if q is None else kv._rows(q, "q", t, heads)), *kv._rows(k, "k", t, h),
+        None if q_weight is None else kv._arg(q_weight, "q_weight", kv.dtype, dim),
+        None if k_weight is None else kv._arg(k_weight, "k_weight", kv.dtype, dim), eps,
+        kv._arg(position, "position", kv._i32, (t,)), *((0, 0, None, 1.0) if rotary is None else
+                                                        (rotary.rotated, rotary.interleaved, rotary._ptr, rotary.amplitude)),
+        *(none if q is None else kv._rows(q_out, "q_out", t, heads)),
+        *(none if k_out is None else kv._rows(k_out, "k_out", t, h)), *(none if v is None else kv._rows(v, "v", t, h)),
+        None if slot_map is None else kv._arg(slot_map, "slot_map", kv._i64, (t,)),
+        None if k_cache is None else kv._cache(k_cache, "k_cache"),
+        None if v_cache is None else kv._cache(v_cache, "v_cache"), kv._on(stream)))
+
+
+def _eight(kv: KVCache):
+    if kv._stored is None:
+        raise ValueError("the handle is of 16-bit caches: make it with eight_bit=True")
+
+
+def pp_kv_write8(kv: KVCache, k, v, slot_map, k_cache, k_exp, v_cache, v_exp, stream=None):
+    """Store rows k, v [T][kv_heads][head_dim] at slot_map [T] int64 (negative: left out) as 8-bit numbers; k_exp,
+    v_exp [blocks][kv_heads] int8: exponents of their scales."""
+    _eight(kv)
+    t, h, exps = slot_map.shape[0], kv.shape[2], (kv.shape[0], kv.shape[2])
+    _check(_lib.pp_kv_write8(kv.handle, t, *kv._rows(k, "k", t, h), *kv._rows(v, "v", t, h),
+                             kv._arg(slot_map, "slot_map", kv._i64, (t,)), kv._cache(k_cache, "k_cache"),
+                             kv._arg(k_exp, "k_exp", kv._i8, exps), kv._cache(v_cache, "v_cache"),
+                             kv._arg(v_exp, "v_exp", kv._i8, exps), kv._on(stream)))
+
+
+def pp_paged_attention8(kv: KVCache, q, k_cache, k_exp, v_cache, v_exp, block_table, q_start, length, max_q: int, out,
+                        scale: float, window: int = 0, lse=None, workspace=None, stream=None):
+    """pp_paged_attention over a cache of 8-bit numbers with exponents k_exp, v_exp [blocks][kv_heads] int8.
+    workspace: a contiguous uint8 tensor of kv.workspace_size(...) bytes, for calls with
+    max_q * (q_heads / kv_heads) > 32."""
+    _eight(kv)
+    t, heads, r, width, i32 = q.shape[0], q.shape[1], length.shape[0], block_table.shape[-1], kv._i32
+    exps = (kv.shape[0], kv.shape[2])
+    _check(_lib.pp_paged_attention8(
+        kv.handle, r, t, heads, *kv._rows(q, "q", t, heads), kv._cache(k_cache, "k_cache"),
+        kv._arg(k_exp, "k_exp", kv._i8, exps), kv._cache(v_cache, "v_cache"), kv._arg(v_exp, "v_exp", kv._i8, exps),
+        width, kv._arg(block_table, "block_table", i32, (r, width)), kv._arg(q_start, "q_start", i32, (r + 1,)),
+        kv._arg(length, "length", i32, (r,)), max_q, window, scale, *kv._rows(out, "out", t, heads),
+        None if lse is None else kv._arg(lse, "lse", kv._f32, (t, heads)),
+        *((None, 0) if workspace is None else (kv._arg(workspace, "workspace", kv._u8, workspace.shape[:1]), workspace.shape[0])),
         kv._on_after_last(stream)))

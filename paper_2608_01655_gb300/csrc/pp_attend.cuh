@@ -506,6 +506,8 @@ AttendDev attend_dev(const pp_kv *kv, const AttendArgs &c);
 pp_status prepare_attend_token();
 pp_status prepare_attend_chunk();
 pp_status launch_attend_token(pp_kv *kv, const AttendArgs &c, cudaStream_t st);
+pp_status prepare_attend_token8();
+pp_status launch_attend_token8(pp_kv *kv, const AttendArgs &c, cudaStream_t st);
 pp_status launch_attend_chunk(pp_kv *kv, const AttendArgs &c, cudaStream_t st);
 
 }  // namespace pp

@@ -4,7 +4,6 @@
 #include <climits>
 #include <cstdlib>
 #include <exception>
-#include <initializer_list>
 #include <new>
 #include <vector>
 
@@ -368,18 +367,14 @@ __global__ void __launch_bounds__(kWriteThreads) k_kv_write(WriteArgs a)
     }
 }
 
-// bytes between two rows of 16-bit elements that a 16-byte copy can start at
-static bool stride_ok(int64_t s) { return s > 0 && s % 8 == 0 && s < (int64_t)1 << 38; }
-static bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+bool stride_ok(int64_t s) { return s > 0 && s % 8 == 0 && s < (int64_t)1 << 38; }
+bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 // Whether rows of `dim` elements at sums of d * stride (0 <= d < extent) share an
 // element.  Where each stride passes all that lies within the smaller ones, as in every
 // order of dimensions with any padding, they do not.  Other layouts are searched: for
 // each difference along two dimensions the nearest ones of the third, the longest.
-struct Extent {
-    int64_t stride, count;
-};
-static bool rows_overlap(int64_t dim, std::initializer_list<Extent> all)
+bool rows_overlap(int64_t dim, std::initializer_list<Extent> all)
 {
     Extent e[3] = {{0, 1}, {0, 1}, {0, 1}};
     int n = 0;
@@ -406,7 +401,7 @@ static bool rows_overlap(int64_t dim, std::initializer_list<Extent> all)
     return false;
 }
 
-static pp_status check_device(const pp_kv *kv)
+pp_status check_device(const pp_kv *kv)
 {
     int dev = 0;
     PP_CUDA(cudaGetDevice(&dev));
@@ -414,8 +409,33 @@ static pp_status check_device(const pp_kv *kv)
     return PP_OK;
 }
 
+pp_status check_attend(const pp_kv *kv, const AttendArgs &a, bool *nothing)
+{
+    if (a.requests < 0 || a.requests > kKvMaxRequests) return fail(PP_EINVAL, "requests must be between 0 and 16384");
+    if (a.tokens < 0 || a.max_q < 0 || a.window < 0 || a.table_width < 1)
+        return fail(PP_EINVAL, "tokens, max_q and window must be >= 0, table_width >= 1");
+    if (a.q_heads < 1 || a.q_heads % kv->heads || a.q_heads > 1 << 20)
+        return fail(PP_EINVAL, "q_heads must be a positive multiple of kv_heads, at most 2^20");
+    if ((int64_t)a.tokens * a.group > 1 << 30)
+        return fail(PP_EINVAL, "tokens * q_heads / kv_heads must be at most 2^30");
+    if (!(a.scale > 0) || a.scale > 1e30f) return fail(PP_EINVAL, "scale must be positive and finite");
+    *nothing = a.requests == 0 || a.tokens == 0;
+    if (*nothing) return PP_OK;
+    if (!a.q || !a.k_cache || !a.v_cache || !a.block_table || !a.q_start || !a.length || !a.out)
+        return fail(PP_EINVAL, "null pointer");
+    if (!aligned16(a.q) || !aligned16(a.k_cache) || !aligned16(a.v_cache) || !aligned16(a.out))
+        return fail(PP_EINVAL, "q, out and the caches must be aligned to 16 bytes");
+    if (!stride_ok(a.q_token_stride) || !stride_ok(a.q_head_stride) || !stride_ok(a.out_token_stride) ||
+        !stride_ok(a.out_head_stride))
+        return fail(PP_EINVAL, "strides must be positive multiples of 8 elements below 2^38");
+    if (rows_overlap(kv->dim, {{a.out_token_stride, a.tokens}, {a.out_head_stride, a.q_heads}}))
+        return fail(PP_EINVAL, "rows of out would overlap with these strides");
+    return check_device(kv);
+}
+
 pp_status launch_attend(pp_kv *kv, const AttendArgs &a, cudaStream_t st);
 pp_status prepare_attend();            // kernel attributes on the current device
+pp_status prepare_kv8();
 
 }  // namespace pp
 
@@ -447,7 +467,9 @@ extern "C" pp_status pp_kv_create(int32_t blocks, int32_t block_size, int32_t kv
     if (kv_heads < 1 || kv_heads > 65535) return fail(PP_EINVAL, "kv_heads must be between 1 and 65535");
     if (head_dim < 8 || head_dim > kKvMaxDim || head_dim % 8)
         return fail(PP_EINVAL, "head_dim must be a multiple of 8 from 8 to 128");
-    if (dtype != PP_KV_BF16 && dtype != PP_KV_F16) return fail(PP_EINVAL, "unknown dtype");
+    const bool eight = dtype == PP_KV_BF16_E4M3 || dtype == PP_KV_F16_E4M3;
+    if (dtype != PP_KV_BF16 && dtype != PP_KV_F16 && !eight) return fail(PP_EINVAL, "unknown dtype");
+    if (eight && head_dim % 16) return fail(PP_EINVAL, "head_dim of an 8-bit cache must be a multiple of 16");
     if (block_stride == 0 && token_stride == 0 && head_stride == 0) {
         head_stride = head_dim;
         token_stride = (int64_t)kv_heads * head_dim;
@@ -455,6 +477,8 @@ extern "C" pp_status pp_kv_create(int32_t blocks, int32_t block_size, int32_t kv
     }
     if (!stride_ok(block_stride) || !stride_ok(token_stride) || !stride_ok(head_stride))
         return fail(PP_EINVAL, "strides must be positive multiples of 8 elements below 2^38");
+    if (eight && (block_stride % 16 || token_stride % 16 || head_stride % 16))
+        return fail(PP_EINVAL, "strides of an 8-bit cache must be multiples of 16 elements");
     if (token_stride < head_dim || head_stride < head_dim || block_stride < head_dim)
         return fail(PP_EINVAL, "strides must be at least head_dim: rows would overlap");
     if (rows_overlap(head_dim, {{block_stride, blocks}, {token_stride, block_size}, {head_stride, kv_heads}}))
@@ -466,7 +490,8 @@ extern "C" pp_status pp_kv_create(int32_t blocks, int32_t block_size, int32_t kv
     while ((1 << kv->block_log) < block_size) kv->block_log++;
     kv->heads = kv_heads;
     kv->dim = head_dim;
-    kv->dtype = dtype;
+    kv->dtype = eight ? dtype - PP_KV_BF16_E4M3 : dtype;
+    kv->eight = eight;
     kv->block_stride = block_stride;
     kv->token_stride = token_stride;
     kv->head_stride = head_stride;
@@ -478,6 +503,7 @@ extern "C" pp_status pp_kv_create(int32_t blocks, int32_t block_size, int32_t kv
         PP_CUDA(cudaFuncSetAttribute(k_block_tables, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                      (int)(sizeof(int32_t) * (3 * (size_t)kKvMaxRequests + 2))));
         pp_status s = prepare_attend();
+        if (s == PP_OK && kv->eight) s = prepare_kv8();
         if (s != PP_OK) return s;
         // two pieces a CTA, one CTA an SM
         const size_t slots = 2 * (size_t)kv->sm_count;
@@ -573,6 +599,7 @@ extern "C" pp_status pp_kv_write(pp_kv *kv, int32_t tokens, const void *k, int64
                                  const int64_t *slot_map, void *k_cache, void *v_cache, void *stream)
 {
     if (!kv) return fail(PP_EINVAL, "null cache handle");
+    if (kv->eight) return fail(PP_EINVAL, "the cache holds 8-bit numbers: pp_kv_write8 writes them");
     if (tokens < 0 || tokens > 1 << 30) return fail(PP_EINVAL, "tokens must be between 0 and 2^30");
     if (tokens == 0) return PP_OK;
     if (!k || !v || !slot_map || !k_cache || !v_cache) return fail(PP_EINVAL, "null pointer");
@@ -617,28 +644,11 @@ extern "C" pp_status pp_paged_attention(pp_kv *kv, int32_t requests, int32_t tok
                                         float *lse, void *stream)
 {
     if (!kv) return fail(PP_EINVAL, "null cache handle");
-    if (requests < 0 || requests > kKvMaxRequests) return fail(PP_EINVAL, "requests must be between 0 and 16384");
-    if (tokens < 0 || max_q < 0 || window < 0 || table_width < 1)
-        return fail(PP_EINVAL, "tokens, max_q and window must be >= 0, table_width >= 1");
-    if (q_heads < 1 || q_heads % kv->heads || q_heads > 1 << 20)
-        return fail(PP_EINVAL, "q_heads must be a positive multiple of kv_heads, at most 2^20");
-    if ((int64_t)tokens * (q_heads / kv->heads) > 1 << 30)
-        return fail(PP_EINVAL, "tokens * q_heads / kv_heads must be at most 2^30");
-    if (!(scale > 0) || scale > 1e30f) return fail(PP_EINVAL, "scale must be positive and finite");
-    if (requests == 0 || tokens == 0) return PP_OK;
-    if (!q || !k_cache || !v_cache || !block_table || !q_start || !length || !out)
-        return fail(PP_EINVAL, "null pointer");
-    if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out))
-        return fail(PP_EINVAL, "q, out and the caches must be aligned to 16 bytes");
-    if (!stride_ok(q_token_stride) || !stride_ok(q_head_stride) || !stride_ok(out_token_stride) ||
-        !stride_ok(out_head_stride))
-        return fail(PP_EINVAL, "strides must be positive multiples of 8 elements below 2^38");
-    if (rows_overlap(kv->dim, {{out_token_stride, tokens}, {out_head_stride, q_heads}}))
-        return fail(PP_EINVAL, "rows of out would overlap with these strides");
-    pp_status s = check_device(kv);
-    if (s != PP_OK) return s;
+    if (kv->eight) return fail(PP_EINVAL, "the cache holds 8-bit numbers: pp_paged_attention8 reads it");
     const AttendArgs a = {requests, tokens, q_heads, q_heads / kv->heads, q, q_token_stride, q_head_stride, k_cache,
                           v_cache, block_table, table_width, q_start, length, max_q, window, scale, out,
-                          out_token_stride, out_head_stride, lse};
-    return launch_attend(kv, a, (cudaStream_t)stream);
+                          out_token_stride, out_head_stride, lse, nullptr, nullptr};
+    bool nothing = false;
+    const pp_status s = check_attend(kv, a, &nothing);
+    return s != PP_OK || nothing ? s : launch_attend(kv, a, (cudaStream_t)stream);
 }

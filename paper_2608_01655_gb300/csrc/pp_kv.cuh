@@ -5,6 +5,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <initializer_list>
+
 #include "pp_internal.cuh"
 
 struct pp_kv {
@@ -15,7 +17,8 @@ struct pp_kv {
     int32_t block_log = 0;              // log2(block_size)
     int32_t heads = 0;                  // K/V heads
     int32_t dim = 0;                    // head dimension
-    int32_t dtype = 0;
+    int32_t dtype = 0;                  // PP_KV_BF16 or PP_KV_F16: of q, k, v and out, and of the caches unless `eight`
+    bool eight = false;                 // the caches hold 8-bit numbers, with an exponent a block and head
     int64_t block_stride = 0, token_stride = 0, head_stride = 0;     // elements
     int32_t *d_status = nullptr;        // device status word
     // scratch of the attention: pieces of items that several CTAs computed, their
@@ -31,6 +34,7 @@ constexpr int kKvMaxBlock = 512;
 constexpr int32_t kKvMaxRequests = 16384;
 constexpr int32_t kKvMaxBlocks = 1 << 30;
 constexpr int kPieceRows = 256;                 // rows of a piece, at most
+constexpr int kLeastExp = -40, kMostExp = 40;   // of the scales of an 8-bit cache
 
 // one call of pp_paged_attention, checked
 struct AttendArgs {
@@ -46,6 +50,7 @@ struct AttendArgs {
     void *out;
     int64_t out_token_stride, out_head_stride;
     float *lse;
+    const int8_t *k_exp, *v_exp;        // exponents of 8-bit caches, [blocks][heads]
 };
 
 // A device-side check failed; a time limit that ran out stays the status.
@@ -61,5 +66,15 @@ template <> struct KvType<__nv_bfloat16> {
 template <> struct KvType<__half> {
     static __device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
 };
+
+// Host checks that the cache's entry points share (pp_kv.cu).
+bool aligned16(const void *p);
+bool stride_ok(int64_t s);              // between rows of 16-bit elements that a 16-byte copy can start at
+struct Extent {
+    int64_t stride, count;
+};
+bool rows_overlap(int64_t dim, std::initializer_list<Extent> all);
+pp_status check_device(const pp_kv *kv);
+pp_status check_attend(const pp_kv *kv, const AttendArgs &a, bool *nothing);
 
 }  // namespace pp

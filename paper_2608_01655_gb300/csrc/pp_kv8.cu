@@ -1,0 +1,502 @@
+// A paged cache of 8-bit numbers: the write of new K and V rows, and attention over it.
+//
+// An element is code * 2^e: an e4m3 number and an exponent of its block and head.
+// Scales are powers of two, so that codes go to another scale, or to 16-bit floating
+// numbers, without a rounding but where they fall below e4m3's normal range.
+#include <algorithm>
+#include <climits>
+#include <cstring>
+#include <type_traits>
+
+#include "pp_attend.cuh"
+
+namespace pp {
+
+__device__ __forceinline__ float scale_of(int e) { return __int_as_float((e + 127) << 23); }     // 2^e
+
+// ---------------------------------------------------------------------------
+// Write.
+// ---------------------------------------------------------------------------
+struct Write8Args {
+    int32_t tokens, heads, per_head, window;            // vectors of 8 elements a head; tokens of a CTA
+    uint32_t per_head_mul;                              // x / per_head is the high half of x * this for x < 2^28
+    const uint4 *k, *v;
+    int64_t k_token, k_head, v_token, v_head;           // strides in vectors
+    const int64_t *slot;
+    uint8_t *kc, *vc;
+    int8_t *ke, *ve;
+    int64_t block_stride, token_stride, head_stride;    // bytes
+    int64_t slots;
+    int32_t block_log;
+    int32_t *status;
+};
+
+constexpr int kWrite8Warps = 8, kWrite8Threads = 32 * kWrite8Warps;
+constexpr int kWrite8Window = 32;                       // tokens of a CTA at most
+constexpr int kWrite8Held = 8;                          // vectors that a thread keeps
+
+// |x| of two 16-bit numbers; where x is infinite or NaN it becomes NaN and 0 is returned
+template <typename T> __device__ __forceinline__ uint32_t sizes(uint32_t &x)
+{
+    constexpr uint32_t e = std::is_same<T, __nv_bfloat16>::value ? 0x7f80u : 0x7c00u;
+    uint32_t m = x & 0x7fff7fffu;
+    if ((m & 0xffffu) >= e) {
+        x |= 0x7fffu;
+        m &= 0xffff0000u;
+    }
+    if (m >= e << 16) {
+        x |= 0x7fff0000u;
+        m &= 0xffffu;
+    }
+    return m;
+}
+template <typename T> __device__ __forceinline__ float low_value(uint32_t x);
+template <> __device__ __forceinline__ float low_value<__nv_bfloat16>(uint32_t x) { return __uint_as_float(x << 16); }
+template <> __device__ __forceinline__ float low_value<__half>(uint32_t x)
+{
+    return __half2float(__ushort_as_half((unsigned short)x));
+}
+// two numbers to codes, to the nearest, beyond 448 to that, NaN to NaN
+__device__ __forceinline__ uint32_t codes2(float lo, float hi)
+{
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+template <typename T> __device__ __forceinline__ uint2 codes8(const uint4 &x, float by)
+{
+    auto four = [&](uint32_t a, uint32_t b) {
+        return codes2(low_value<T>(a & 0xffffu) * by, low_value<T>(a >> 16) * by) |
+               codes2(low_value<T>(b & 0xffffu) * by, low_value<T>(b >> 16) * by) << 16;
+    };
+    return make_uint2(four(x.x, x.y), four(x.z, x.w));
+}
+// four codes times `by`
+__device__ __forceinline__ uint32_t rescale4(uint32_t x, float by)
+{
+    uint32_t h[2];
+    asm("{\n.reg .b16 lo, hi;\nmov.b32 {lo, hi}, %2;\ncvt.rn.f16x2.e4m3x2 %0, lo;\ncvt.rn.f16x2.e4m3x2 %1, hi;\n}"
+        : "=r"(h[0]), "=r"(h[1])
+        : "r"(x));
+    return codes2(low_value<__half>(h[0] & 0xffffu) * by, low_value<__half>(h[0] >> 16) * by) |
+           codes2(low_value<__half>(h[1] & 0xffffu) * by, low_value<__half>(h[1] >> 16) * by) << 16;
+}
+// the least e, kLeastExp <= e <= kMostExp, with x <= 448 * 2^e (448 = 1.75 * 2^8)
+__device__ __forceinline__ int least_exponent(float x)
+{
+    const uint32_t b = __float_as_uint(x);
+    const int e = (int)(b >> 23) - 127 - 8 + ((b & 0x7fffffu) > 0x600000u);
+    return min(max(e, kLeastExp), kMostExp);
+}
+
+// A run is the tokens of one block, which stand next to one another but for fewer than
+// 32 that are left out between two; its first token leads it.  A CTA looks for the leaders among `window`
+// tokens; a team of TEAM warps (a warp for every 16 tokens of a block) takes a run's
+// rows of one head and of K or V: their largest size, the exponent, the block's other
+// rows if that grows, the codes.  Rows up to kWrite8Held vectors a thread are read once.
+template <typename T, int TEAM>
+__global__ void __launch_bounds__(kWrite8Threads) k_kv_write8(const __grid_constant__ Write8Args a)
+{
+    __shared__ int32_t lead[kWrite8Window], past[kWrite8Window];
+    __shared__ int32_t leads;
+    __shared__ uint32_t tops[kWrite8Warps];
+    __shared__ int32_t begins[kWrite8Warps];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int32_t t0 = blockIdx.x * a.window, t1 = min(t0 + a.window, a.tokens);
+    // block of token t, -1 if it is left out
+    auto block_of = [&](int32_t t) {
+        const int64_t s = a.slot[t];
+        return s >= 0 && s < a.slots ? (int32_t)(s >> a.block_log) : -1;
+    };
+    if (warp == 0) {
+        const int32_t t = t0 + lane;
+        int32_t mine = -1, before = -1;
+        if (t < t1) {
+            if (a.slot[t] >= a.slots && blockIdx.y == 0) kv_bounds(a.status);
+            mine = block_of(t);
+            if (mine >= 0 && t > 0) before = block_of(t - 1);
+        }
+        // behind a token that is left out: the warp looks at those before it
+        for (uint32_t left = __ballot_sync(~0u, mine >= 0 && before < 0 && t > 0); left; left &= left - 1) {
+            const int src = __ffs(left) - 1;
+            const int32_t x = t0 + src - 1 - lane, b = x >= 0 ? block_of(x) : -1;
+            const uint32_t some = __ballot_sync(~0u, b >= 0);
+            const int32_t found = __shfl_sync(~0u, b, some ? __ffs(some) - 1 : 0);
+            if (lane == src && some) before = found;
+        }
+        const bool leader = mine >= 0 && before != mine;
+        const uint32_t all = __ballot_sync(~0u, leader);
+        if (leader) lead[__popc(all & ((1u << lane) - 1))] = t;
+        if (lane == 0) leads = __popc(all);
+    }
+    __syncthreads();
+    // where the runs end: at a token of another block, or with the last before 32 that are left out
+    for (int x = warp; x < leads; x += kWrite8Warps) {
+        const int32_t block = block_of(lead[x]);
+        int32_t last = lead[x];
+        for (;;) {
+            const int32_t t = last + 1 + lane, b = t < a.tokens ? block_of(t) : -1;
+            uint32_t same = __ballot_sync(~0u, b == block);
+            const uint32_t other = __ballot_sync(~0u, b >= 0 && b != block);
+            if (other) same &= (other & -other) - 1;
+            if (same) last += 32 - __clz(same);
+            if (!same || other) break;
+        }
+        if (lane == 0) past[x] = last + 1;
+    }
+    __syncthreads();
+
+    constexpr int kThreads = 32 * TEAM, kTeams = kWrite8Warps / TEAM;
+    const int team = warp / TEAM, me = tid % kThreads;
+    auto sync = [&]() {
+        if (TEAM == 1) __syncwarp();
+        else named_sync(1 + team, kThreads);
+    };
+    const int32_t units = leads * a.heads * 2;
+    for (int32_t u = blockIdx.y * kTeams + team; u < units; u += gridDim.y * kTeams) {
+        const int32_t x = u / (2 * a.heads), h = u / 2 % a.heads;
+        const bool is_v = u & 1;
+        const int32_t first = lead[x], block = block_of(first), count = (past[x] - first) * a.per_head;
+        const uint4 *src = is_v ? a.v + h * a.v_head : a.k + h * a.k_head;
+        const int64_t token = is_v ? a.v_token : a.k_token;
+        uint8_t *dst = (is_v ? a.vc : a.kc) + block * a.block_stride + h * a.head_stride;
+        int8_t *exponent = (is_v ? a.ve : a.ke) + (int64_t)block * a.heads + h;
+        const int old = min(max((int)*exponent, kLeastExp), kMostExp);
+        auto in_run = [&](int32_t l) { return (int32_t)__umulhi(l, a.per_head_mul); };
+        auto in_head = [&](int32_t l) { return l - in_run(l) * a.per_head; };
+        // vector l of the run: its token, its place in the block (-1: left out)
+        auto place = [&](int32_t l, int32_t &t) {
+            t = first + in_run(l);
+            const int64_t s = a.slot[t];
+            return s >= 0 && s < a.slots ? (int32_t)(s & ((1 << a.block_log) - 1)) : -1;
+        };
+        uint4 held[kWrite8Held];
+        int32_t row[kWrite8Held];
+        uint32_t top = 0;
+        bool begins_block = false;
+#pragma unroll
+        for (int y = 0; y < kWrite8Held; ++y) {
+            const int32_t l = me + y * kThreads;
+            int32_t t;
+            row[y] = l < count ? place(l, t) : -1;
+            if (row[y] >= 0) held[y] = src[t * token + in_head(l)];
+        }
+#pragma unroll
+        for (int y = 0; y < kWrite8Held; ++y) {
+            if (row[y] < 0) continue;
+            begins_block |= row[y] == 0;
+            top = __vmaxu2(top, __vmaxu2(__vmaxu2(sizes<T>(held[y].x), sizes<T>(held[y].y)),
+                                         __vmaxu2(sizes<T>(held[y].z), sizes<T>(held[y].w))));
+        }
+        for (int32_t l = me + kWrite8Held * kThreads; l < count; l += kThreads) {
+            int32_t t;
+            const int32_t at = place(l, t);
+            if (at < 0) continue;
+            begins_block |= at == 0;
+            uint4 y = src[t * token + in_head(l)];
+            top = __vmaxu2(top, __vmaxu2(__vmaxu2(sizes<T>(y.x), sizes<T>(y.y)), __vmaxu2(sizes<T>(y.z), sizes<T>(y.w))));
+        }
+        top = __reduce_max_sync(~0u, max(top & 0xffffu, top >> 16));
+        begins_block = __any_sync(~0u, begins_block);
+        if (TEAM > 1) {
+            if (lane == 0) {
+                tops[warp] = top;
+                begins[warp] = begins_block;
+            }
+            sync();
+#pragma unroll
+            for (int w = 0; w < TEAM; ++w) {
+                top = max(top, tops[team * TEAM + w]);
+                begins_block |= begins[team * TEAM + w] != 0;
+            }
+        }
+        const int need = least_exponent(low_value<T>(top)), e = begins_block ? need : max(old, need);
+        if (!begins_block && e > old) {
+            // the rows that the block has go to the new scale; those of this call are written over them
+            const float by = scale_of(old - e);
+            const int32_t pieces = a.per_head / 2;      // of 16 codes
+            for (int32_t l = me; l < pieces << a.block_log; l += kThreads) {
+                uint4 *p = reinterpret_cast<uint4 *>(dst + l / pieces * a.token_stride) + l % pieces;
+                const uint4 y = *p;
+                *p = make_uint4(rescale4(y.x, by), rescale4(y.y, by), rescale4(y.z, by), rescale4(y.w, by));
+            }
+        }
+        sync();                                         // all have read the exponent, and old rows are done
+        if (me == 0) *exponent = (int8_t)e;
+        const float by = scale_of(-e);
+#pragma unroll
+        for (int y = 0; y < kWrite8Held; ++y)
+            if (row[y] >= 0)
+                reinterpret_cast<uint2 *>(dst + row[y] * a.token_stride)[in_head(me + y * kThreads)] = codes8<T>(held[y], by);
+        for (int32_t l = me + kWrite8Held * kThreads; l < count; l += kThreads) {
+            int32_t t;
+            const int32_t at = place(l, t);
+            if (at < 0) continue;
+            uint4 y = src[t * token + in_head(l)];
+            sizes<T>(y.x), sizes<T>(y.y), sizes<T>(y.z), sizes<T>(y.w);
+            reinterpret_cast<uint2 *>(dst + at * a.token_stride)[in_head(l)] = codes8<T>(y, by);
+        }
+        if (TEAM > 1) sync();                           // tops and begins are free again
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Attention of chunks: the visible blocks as 16-bit rows in the caller's workspace
+// (exact in bf16), then the kernel of 16-bit caches over them.
+// ---------------------------------------------------------------------------
+struct Unpack8Args {
+    AttendDev a;
+    uint4 *k, *v;                                       // [capacity][heads][block_size][dim]
+    int32_t *table;                                     // [requests][table_width]
+    int32_t capacity;
+};
+
+constexpr int kUnpackThreads = 512;
+
+template <typename T> __device__ __forceinline__ uint32_t wide2(uint32_t codes, float by)
+{
+    uint32_t h;
+    asm("{\n.reg .b16 lo, hi;\nmov.b32 {lo, hi}, %1;\ncvt.rn.f16x2.e4m3x2 %0, lo;\n}" : "=r"(h) : "r"(codes));
+    uint32_t r = Pack<T>::two(low_value<__half>(h & 0xffffu) * by, low_value<__half>(h >> 16) * by);
+    if constexpr (std::is_same<T, __half>::value) {     // what f16 does not reach becomes its largest
+        __half2 x;
+        memcpy(&x, &r, 4);
+        const __half2 most = __half2half2(__ushort_as_half(0x7bff));
+        x = __hmax2_nan(__hmin2_nan(x, most), __hneg2(most));
+        memcpy(&r, &x, 4);
+    }
+    return r;
+}
+template <typename T> __device__ __forceinline__ void unpack16(uint4 *to, const uint4 &x, float by)
+{
+    to[0] = make_uint4(wide2<T>(x.x, by), wide2<T>(x.x >> 16, by), wide2<T>(x.y, by), wide2<T>(x.y >> 16, by));
+    to[1] = make_uint4(wide2<T>(x.z, by), wide2<T>(x.z >> 16, by), wide2<T>(x.w, by), wide2<T>(x.w >> 16, by));
+}
+
+// Blocks that a request's queries see: [lo, hi], none if hi < lo.
+__device__ __forceinline__ Keys seen_blocks(const AttendDev &a, const Req &q)
+{
+    if (q.q_len == 0 || q.length == 0) return {0, -1};
+    return {first_key(a, max(q.length - q.q_len, 0)) >> a.block_log, (q.length - 1) >> a.block_log};
+}
+
+// Every CTA sums up the requests' visible blocks (8 bytes a request, from L2 after the
+// first) and a warp takes a block and head at a time, numbered through all requests.
+// A block that several requests see is unpacked for each.  Bound by memory: a byte
+// read and two written, which the attention then reads, mostly from L2.
+template <typename T> __global__ void __launch_bounds__(kUnpackThreads) k_unpack8(const __grid_constant__ Unpack8Args u)
+{
+    extern __shared__ int32_t pre[];                    // blocks before request r
+    __shared__ int64_t warp_sum[32];
+    const AttendDev &a = u.a;
+    const int tid = threadIdx.x, lane = tid & 31;
+    const int32_t R = a.c.requests, per = (R + kUnpackThreads - 1) / kUnpackThreads;
+    const int32_t first = min(tid * per, R), past = min(first + per, R);
+    int64_t mine = 0, excl;
+    for (int32_t r = first; r < past; ++r) {
+        const Keys k = seen_blocks(a, load_req(a, r, false));
+        mine += k.hi - k.lo + 1;
+    }
+    const int64_t all = scan64(mine, &excl, warp_sum, false);
+    const int32_t total = (int32_t)min(all, (int64_t)u.capacity);
+    if (all > u.capacity && blockIdx.x == 0 && tid == 0) kv_bounds(a.status);
+    for (int32_t r = first; r < past; ++r) {
+        const Keys k = seen_blocks(a, load_req(a, r, false));
+        pre[r] = (int32_t)min(excl, (int64_t)INT_MAX);
+        excl += k.hi - k.lo + 1;
+    }
+    __syncthreads();
+
+    const int32_t warps = gridDim.x * (kUnpackThreads / 32), bs = 1 << a.block_log;
+    const int32_t pieces = a.dim / 16, count = pieces << a.block_log;   // 16 codes each, of a head's rows
+    const int64_t units = (int64_t)total * a.kv_heads;
+    for (int64_t n = blockIdx.x * (kUnpackThreads / 32) + (tid >> 5); n < units; n += warps) {
+        const int32_t x = (int32_t)quotient(n, a.kv_heads), h = (int32_t)(n - (int64_t)x * a.kv_heads);
+        int32_t r = 0;                                  // the last request that begins at x or before
+        for (int32_t len = R; len > 1;) {
+            const int32_t half = len >> 1;
+            if (pre[r + half] <= x) {
+                r += half;
+                len -= half;
+            } else {
+                len = half;
+            }
+        }
+        const int32_t j = seen_blocks(a, load_req(a, r, false)).lo + x - pre[r];
+        const int64_t entry = (int64_t)r * a.c.table_width + j;
+        const int32_t id = a.c.block_table[entry];
+        const bool ok = id >= 0 && id < a.blocks;
+        if (h == 0 && lane == 0) u.table[entry] = ok ? x : -1;
+        if (!ok) continue;
+        const int64_t from = id * a.block_stride + h * a.head_stride, at = (int64_t)id * a.kv_heads + h;
+        const uint8_t *k = static_cast<const uint8_t *>(a.c.k_cache) + from, *v = static_cast<const uint8_t *>(a.c.v_cache) + from;
+        const float kb = scale_of(min(max((int)a.c.k_exp[at], kLeastExp), kMostExp));
+        const float vb = scale_of(min(max((int)a.c.v_exp[at], kLeastExp), kMostExp));
+        const int64_t to = n * bs * (a.dim / 8);
+#pragma unroll 4
+        for (int32_t l = lane; l < count; l += 32) {
+            const int64_t in = l / pieces * a.token_stride + l % pieces * 16;
+            const uint4 y = *reinterpret_cast<const uint4 *>(k + in), z = *reinterpret_cast<const uint4 *>(v + in);
+            unpack16<T>(u.k + to + 2 * l, y, kb);
+            unpack16<T>(u.v + to + 2 * l, z, vb);
+        }
+    }
+    // blocks that have no place
+    if (all > u.capacity)
+        for (int32_t r = blockIdx.x; r < R; r += gridDim.x) {
+            const Keys k = seen_blocks(a, load_req(a, r, false));
+            for (int32_t j = k.lo + tid; j <= k.hi; j += kUnpackThreads)
+                if ((int64_t)pre[r] + j - k.lo >= total) u.table[(int64_t)r * a.c.table_width + j] = -1;
+        }
+}
+
+pp_status prepare_kv8()
+{
+    const int most = (int)sizeof(int32_t) * kKvMaxRequests;
+    PP_CUDA(cudaFuncSetAttribute(k_unpack8<__nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize, most));
+    PP_CUDA(cudaFuncSetAttribute(k_unpack8<__half>, cudaFuncAttributeMaxDynamicSharedMemorySize, most));
+    return prepare_attend_token8();
+}
+
+// A workspace: the table, then K's rows, then V's.
+static int64_t table_bytes(int32_t requests, int32_t width) { return ((int64_t)requests * width * 4 + 255) / 256 * 256; }
+static int64_t block_bytes(const pp_kv *kv) { return (int64_t)2 * kv->heads * kv->block_size * kv->dim; }
+
+// Rows (new tokens x heads of a group) of the longest request up to which a call goes
+// to the kernel of single tokens.
+constexpr int64_t kFewRows8 = 32;
+
+static pp_status launch_attend8(pp_kv *kv, AttendArgs c, void *workspace, int64_t bytes, cudaStream_t st)
+{
+    if ((int64_t)c.max_q * c.group <= kFewRows8) return launch_attend_token8(kv, c, st);
+    if (!workspace) return fail(PP_EINVAL, "chunks need a workspace of pp_kv_workspace bytes");
+    if (!aligned16(workspace)) return fail(PP_EINVAL, "workspace must be aligned to 16 bytes");
+    const int64_t head = table_bytes(c.requests, c.table_width);
+    const int64_t capacity = std::min<int64_t>((bytes - head) / (2 * block_bytes(kv)), kKvMaxBlocks);
+    if (bytes < head || capacity < 1) return fail(PP_EINVAL, "the workspace is too small: see pp_kv_workspace");
+    Unpack8Args u = {};
+    u.a = attend_dev(kv, c);
+    char *const at = static_cast<char *>(workspace);
+    u.table = reinterpret_cast<int32_t *>(at);
+    u.k = reinterpret_cast<uint4 *>(at + head);
+    u.v = reinterpret_cast<uint4 *>(at + head + capacity * block_bytes(kv));
+    u.capacity = (int32_t)capacity;
+    const size_t shared = sizeof(int32_t) * c.requests;
+    if (kv->dtype == PP_KV_BF16) k_unpack8<__nv_bfloat16><<<2 * kv->sm_count, kUnpackThreads, shared, st>>>(u);
+    else k_unpack8<__half><<<2 * kv->sm_count, kUnpackThreads, shared, st>>>(u);
+    PP_CUDA(cudaGetLastError());
+    pp_kv wide = *kv;
+    wide.eight = false;
+    wide.blocks = u.capacity;
+    wide.token_stride = kv->dim;
+    wide.head_stride = (int64_t)kv->dim * kv->block_size;
+    wide.block_stride = wide.head_stride * kv->heads;
+    c.k_cache = u.k;
+    c.v_cache = u.v;
+    c.block_table = u.table;
+    return launch_attend_chunk(&wide, c, st);
+}
+
+static pp_status check_exps(const void *k_exp, const void *v_exp)
+{
+    if (!k_exp || !v_exp) return fail(PP_EINVAL, "null exponents");
+    if (k_exp == v_exp) return fail(PP_EINVAL, "K and V have exponents of their own");
+    return PP_OK;
+}
+
+}  // namespace pp
+
+using namespace pp;
+
+extern "C" pp_status pp_kv_write8(pp_kv *kv, int32_t tokens, const void *k, int64_t k_token_stride, int64_t k_head_stride,
+                                  const void *v, int64_t v_token_stride, int64_t v_head_stride, const int64_t *slot_map,
+                                  void *k_cache, int8_t *k_exp, void *v_cache, int8_t *v_exp, void *stream)
+{
+    if (!kv) return fail(PP_EINVAL, "null cache handle");
+    if (!kv->eight) return fail(PP_EINVAL, "the cache holds 16-bit numbers: pp_kv_write writes them");
+    if (tokens < 0 || tokens > 1 << 30) return fail(PP_EINVAL, "tokens must be between 0 and 2^30");
+    if (tokens == 0) return PP_OK;
+    if (!k || !v || !slot_map || !k_cache || !v_cache) return fail(PP_EINVAL, "null pointer");
+    pp_status s = check_exps(k_exp, v_exp);
+    if (s != PP_OK) return s;
+    if (k_cache == v_cache) return fail(PP_EINVAL, "K and V need caches of their own");
+    if (!aligned16(k) || !aligned16(v) || !aligned16(k_cache) || !aligned16(v_cache))
+        return fail(PP_EINVAL, "k, v and the caches must be aligned to 16 bytes");
+    if (!stride_ok(k_token_stride) || !stride_ok(k_head_stride) || !stride_ok(v_token_stride) || !stride_ok(v_head_stride))
+        return fail(PP_EINVAL, "strides must be positive multiples of 8 elements below 2^38");
+    s = check_device(kv);
+    if (s != PP_OK) return s;
+    Write8Args a = {};
+    a.tokens = tokens;
+    a.heads = kv->heads;
+    a.per_head = kv->dim / 8;
+    a.per_head_mul = (uint32_t)((((uint64_t)1 << 32) + a.per_head - 1) / a.per_head);   // per_head <= 16: off by less than 16 / 2^32
+    a.k = static_cast<const uint4 *>(k);
+    a.v = static_cast<const uint4 *>(v);
+    a.k_token = k_token_stride / 8;
+    a.k_head = k_head_stride / 8;
+    a.v_token = v_token_stride / 8;
+    a.v_head = v_head_stride / 8;
+    a.slot = slot_map;
+    a.kc = static_cast<uint8_t *>(k_cache);
+    a.vc = static_cast<uint8_t *>(v_cache);
+    a.ke = k_exp;
+    a.ve = v_exp;
+    a.block_stride = kv->block_stride;
+    a.token_stride = kv->token_stride;
+    a.head_stride = kv->head_stride;
+    a.slots = (int64_t)kv->blocks << kv->block_log;
+    a.block_log = kv->block_log;
+    a.status = kv->d_status;
+    // two CTAs an SM; where there are fewer tokens than that, more CTAs for their heads
+    const int32_t ctas = 2 * kv->sm_count;
+    a.window = std::min(std::max((tokens + ctas - 1) / ctas, 1), kWrite8Window);
+    const int32_t windows = (tokens - 1) / a.window + 1;
+    const int team = std::min(std::max(kv->block_size / 16, 1), kWrite8Warps), teams = kWrite8Warps / team;
+    const int32_t rounds = (2 * kv->heads + teams - 1) / teams;
+    const dim3 grid(windows, std::min(std::max(ctas / windows, 1), rounds));
+    const cudaStream_t st = (cudaStream_t)stream;
+    auto launch = [&](auto *with1, auto *with2, auto *with4, auto *with8) {
+        (team == 1 ? with1 : team == 2 ? with2 : team == 4 ? with4 : with8)<<<grid, kWrite8Threads, 0, st>>>(a);
+    };
+    if (kv->dtype == PP_KV_BF16)
+        launch(k_kv_write8<__nv_bfloat16, 1>, k_kv_write8<__nv_bfloat16, 2>, k_kv_write8<__nv_bfloat16, 4>, k_kv_write8<__nv_bfloat16, 8>);
+    else
+        launch(k_kv_write8<__half, 1>, k_kv_write8<__half, 2>, k_kv_write8<__half, 4>, k_kv_write8<__half, 8>);
+    PP_CUDA(cudaGetLastError());
+    return PP_OK;
+}
+
+extern "C" pp_status pp_kv_workspace(const pp_kv *kv, int32_t requests, int32_t table_width, int32_t blocks, size_t *bytes)
+{
+    if (!kv) return fail(PP_EINVAL, "null cache handle");
+    if (!bytes) return fail(PP_EINVAL, "null pointer");
+    *bytes = 0;
+    if (!kv->eight) return fail(PP_EINVAL, "a cache of 16-bit numbers needs no workspace");
+    if (requests < 0 || requests > kKvMaxRequests) return fail(PP_EINVAL, "requests must be between 0 and 16384");
+    if (table_width < 1 || blocks < 0 || blocks > kKvMaxBlocks)
+        return fail(PP_EINVAL, "table_width must be >= 1, blocks between 0 and 2^30");
+    *bytes = (size_t)table_bytes(requests, table_width) + (size_t)std::max(blocks, 1) * 2 * (size_t)block_bytes(kv);
+    return PP_OK;
+}
+
+extern "C" pp_status pp_paged_attention8(pp_kv *kv, int32_t requests, int32_t tokens, int32_t q_heads, const void *q,
+                                         int64_t q_token_stride, int64_t q_head_stride, const void *k_cache,
+                                         const int8_t *k_exp, const void *v_cache, const int8_t *v_exp,
+                                         int32_t table_width, const int32_t *block_table, const int32_t *q_start,
+                                         const int32_t *length, int32_t max_q, int32_t window, float scale, void *out,
+                                         int64_t out_token_stride, int64_t out_head_stride, float *lse, void *workspace,
+                                         size_t workspace_bytes, void *stream)
+{
+    if (!kv) return fail(PP_EINVAL, "null cache handle");
+    if (!kv->eight) return fail(PP_EINVAL, "the cache holds 16-bit numbers: pp_paged_attention reads it");
+    const AttendArgs a = {requests, tokens, q_heads, q_heads / kv->heads, q, q_token_stride, q_head_stride, k_cache,
+                          v_cache, block_table, table_width, q_start, length, max_q, window, scale, out,
+                          out_token_stride, out_head_stride, lse, k_exp, v_exp};
+    bool nothing = false;
+    pp_status s = check_attend(kv, a, &nothing);
+    if (s != PP_OK || nothing) return s;
+    s = check_exps(k_exp, v_exp);
+    if (s != PP_OK) return s;
+    return launch_attend8(kv, a, workspace, (int64_t)std::min<size_t>(workspace_bytes, (size_t)1 << 62), (cudaStream_t)stream);
+}
