@@ -25,12 +25,18 @@
 namespace pp {
 
 namespace token {
+constexpr int kRows = 16;                           // rows of an item
+using Shape = ShapeOf<kRows, KT>;
+
 template <int HALVES> struct Layout {
     static constexpr int half = kKeys * 128;                    // bytes of 64 columns of a warp's keys
     static constexpr int rows = half * HALVES;                  // of its K or V
     static constexpr int stages = HALVES == 2 ? 3 : 6;
     static constexpr int ring = kWarps * stages * 2 * rows;
-    static constexpr int bytes = 128 + ring + Join<HALVES>::bytes;
+    static constexpr int width = 64 * HALVES;
+    static constexpr int pitch = width + 4;                     // floats of an output row in shared memory
+    static constexpr int join = kWarps / 2 * kRows * pitch * 4;
+    static constexpr int bytes = 128 + ring + join;
 };
 
 }  // namespace token
@@ -121,7 +127,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_token(const __grid_const
     constexpr int KS = 4 * HALVES;                      // 16-wide steps of the head dimension
     extern __shared__ uint8_t raw[];
     __shared__ SchedShared sched;
-    __shared__ JoinShared shared;
+    __shared__ float stat[2][kWarps][kRows];
+    __shared__ int32_t last;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t base = (smem_u32(raw) + 127) & ~127u;
     float *join = reinterpret_cast<float *>(raw + (base - smem_u32(raw)) + L::ring);
@@ -132,6 +139,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_token(const __grid_const
     // ldmatrix rows: K (keys outside, dims inside a group of four matrices), V (the other way round)
     const int krow = (lane >> 4) * 8 + (lane & 7), kpiece = (lane >> 3) & 1;
     const int vrow = ((lane >> 3) & 1) * 8 + (lane & 7), vpiece = lane >> 4;
+    const int jr = tid >> 4, jd = (tid & 15) * (4 * HALVES);          // joining: row and first column
 
     const uint32_t ring = base + warp * L::stages * 2 * L::rows;
     Feed<HALVES> feed(a, sched, ring);
@@ -292,7 +300,87 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_token(const __grid_const
             feed.ask();                                             // into the place just read
         }
 
-        finish_item<T, HALVES, false>(a, cur, o, m, l, join, shared, total, ctas);
+        // join the warps: the upper four hand theirs to the lower four, lane by lane,
+        // then a thread has one row's 4 * HALVES columns
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            l[x] += __shfl_xor_sync(~0u, l[x], 1);
+            l[x] += __shfl_xor_sync(~0u, l[x], 2);
+            if ((lane & 3) == 0) {
+                stat[0][warp][r0 + 8 * x] = m[x];
+                stat[1][warp][r0 + 8 * x] = l[x];
+            }
+        }
+        if (warp >= kWarps / 2) {
+            float4 *dst = reinterpret_cast<float4 *>(join) + (warp - kWarps / 2) * 2 * KS * 32 + lane;
+#pragma unroll
+            for (int n = 0; n < 2 * KS; ++n) dst[32 * n] = make_float4(o[n][0], o[n][1], o[n][2], o[n][3]);
+        }
+        __syncthreads();
+        if (warp < kWarps / 2) {
+            const float4 *src = reinterpret_cast<const float4 *>(join) + warp * 2 * KS * 32 + lane;
+            float f[2], g[2];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const float other = stat[0][warp + kWarps / 2][r0 + 8 * x], up = fmaxf(m[x], other);
+                const float by = up == -INFINITY ? 0.f : up;
+                f[x] = exp2_approx(m[x] - by);
+                g[x] = exp2_approx(other - by);
+                m[x] = up;
+                l[x] = f[x] * l[x] + g[x] * stat[1][warp + kWarps / 2][r0 + 8 * x];
+            }
+#pragma unroll
+            for (int n = 0; n < 2 * KS; ++n) {
+                const float4 y = src[32 * n];
+                o[n][0] = f[0] * o[n][0] + g[0] * y.x;
+                o[n][1] = f[0] * o[n][1] + g[0] * y.y;
+                o[n][2] = f[1] * o[n][2] + g[1] * y.z;
+                o[n][3] = f[1] * o[n][3] + g[1] * y.w;
+            }
+        }
+        __syncthreads();
+        if (warp < kWarps / 2) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const int row = r0 + 8 * x;
+                if ((lane & 3) == 0) {
+                    stat[0][warp][row] = m[x];
+                    stat[1][warp][row] = l[x];
+                }
+                if (row < rows) {
+                    float *dst = join + (warp * kRows + row) * L::pitch + c0;
+#pragma unroll
+                    for (int n = 0; n < 2 * KS; ++n)
+                        *reinterpret_cast<float2 *>(dst + 8 * n) = make_float2(o[n][2 * x], o[n][2 * x + 1]);
+                }
+            }
+        }
+        __syncthreads();
+        float acc[4 * HALVES], top = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (int d = 0; d < 4 * HALVES; ++d) acc[d] = 0.f;
+        if (jr < rows) {
+#pragma unroll
+            for (int w = 0; w < kWarps / 2; ++w) top = fmaxf(top, stat[0][w][jr]);
+            const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+            for (int w = 0; w < kWarps / 2; ++w) {
+                const float f = exp2_approx(stat[0][w][jr] - base);
+                sum = fmaf(f, stat[1][w][jr], sum);
+                const float4 *src = reinterpret_cast<const float4 *>(join + (w * kRows + jr) * L::pitch + jd);
+#pragma unroll
+                for (int d = 0; d < HALVES; ++d) {
+                    const float4 y = src[d];
+                    acc[4 * d] = fmaf(f, y.x, acc[4 * d]);
+                    acc[4 * d + 1] = fmaf(f, y.y, acc[4 * d + 1]);
+                    acc[4 * d + 2] = fmaf(f, y.z, acc[4 * d + 2]);
+                    acc[4 * d + 3] = fmaf(f, y.w, acc[4 * d + 3]);
+                }
+            }
+        }
+
+        leave_item<T, Shape, 4 * HALVES, kThreads>(a, cur, acc, top, sum, &last, total, ctas);
+        __syncthreads();                                // the join's memory is free again
     } while (cur.next(a));
 }
 

@@ -13,23 +13,12 @@ namespace token {
 constexpr int kWarps = 8, kThreads = 32 * kWarps;
 constexpr int kKeys = 16;                           // keys of a warp
 constexpr int KT = kKeys * kWarps;                  // keys per tile
-constexpr int kRows = 16;                           // rows of an item
 constexpr int kJoinGroup = 16;                      // pieces (8 KB) joined at a time, then their groups
 
-// Shared memory of an item's join: the rows' outputs of four warps.
-template <int HALVES> struct Join {
-    static constexpr int width = 64 * HALVES;
-    static constexpr int pitch = width + 4;                     // floats of an output row
-    static constexpr int bytes = kWarps / 2 * kRows * pitch * 4;
-};
-struct JoinShared {
-    float stat[2][kWarps][kRows];       // maxima (log2 units) and sums
-    int32_t last;
-};
-
-// Rows are (token, head of the group), token first; an item is 16 of them.
-struct Shape {
-    static constexpr int KT = token::KT;
+// Rows are (token, head of the group), token first; an item is ROWS of them, a tile KEYS keys.
+template <int ROWS, int KEYS> struct ShapeOf {
+    static constexpr int kRows = ROWS;
+    static constexpr int KT = KEYS;
     // what an item weighs beside its tiles (first rows, join): 1, 2, 3, 5 tiles take 60 requests x 4 tokens after 50 to
     // 9,000 56, 53, 48, 46 us, 300 single tokens after 50 to 3,000 85, 81, 79, 79, 256 after 100 to 8,000 -, 461, 462, 472
     static constexpr int32_t extra = 3;
@@ -92,116 +81,53 @@ __device__ __forceinline__ uint32_t lds32(uint32_t addr)
 // both 16-bit halves of a register kept or cleared
 __device__ __forceinline__ uint32_t keep(bool lo, bool hi) { return (lo ? 0xffffu : 0u) | (hi ? 0xffff0000u : 0u); }
 
+// neighbouring 32-bit columns of a piece; loads are from L2, where other CTAs left them
+template <int N> __device__ __forceinline__ void store_columns(float *to, const float (&x)[N])
+{
+    if constexpr (N == 2) {
+        *reinterpret_cast<float2 *>(to) = make_float2(x[0], x[1]);
+    } else {
+#pragma unroll
+        for (int d = 0; d < N; d += 4) *reinterpret_cast<float4 *>(to + d) = make_float4(x[d], x[d + 1], x[d + 2], x[d + 3]);
+    }
+}
+template <int N> __device__ __forceinline__ void load_columns(const float *from, float (&x)[N])
+{
+    if constexpr (N == 2) {
+        const float2 y = __ldcg(reinterpret_cast<const float2 *>(from));
+        x[0] = y.x;
+        x[1] = y.y;
+    } else {
+#pragma unroll
+        for (int d = 0; d < N; d += 4) {
+            const float4 y = __ldcg(reinterpret_cast<const float4 *>(from + d));
+            x[d] = y.x;
+            x[d + 1] = y.y;
+            x[d + 2] = y.z;
+            x[d + 3] = y.w;
+        }
+    }
+}
+
 // The place of row `row` of an item in [tokens][q_heads] rows.
-__device__ __forceinline__ int64_t item_row(const AttendDev &a, const Cursor<Shape> &cur, int32_t row, int64_t token_stride,
+template <class S>
+__device__ __forceinline__ int64_t item_row(const AttendDev &a, const Cursor<S> &cur, int32_t row, int64_t token_stride,
                                             int64_t head_stride)
 {
-    const int32_t at = cur.inner * kRows + row, tok = div_group(a, at);
+    const int32_t at = cur.inner * S::kRows + row, tok = div_group(a, at);
     return (int64_t)(cur.q.first + tok) * token_stride + (int64_t)(cur.outer * a.c.group + at - tok * a.c.group) * head_stride;
 }
 
-// The end of an item (or of a CTA's part of it): joins the warps' outputs o, maxima
-// m and sums l, leaves a piece or writes the rows.  A thread's o are of rows r0 =
-// lane / 4 and r0 + 8; o[n][2 x + y] of row r0 + 8 x is column 8 n + 2 (lane % 4) + y,
-// with EIGHT (V rows of 8-bit numbers, which come in pairs) 16 (n / 2) + 4 (lane % 4)
-// + n % 2 + 2 y.
-template <typename T, int HALVES, bool EIGHT>
-__device__ __forceinline__ void finish_item(const AttendDev &a, const Cursor<Shape> &cur, float (&o)[8 * HALVES][4],
-                                            float (&m)[2], float (&l)[2], float *join, JoinShared &sh, int64_t total,
-                                            int64_t ctas)
+// The end of an item, or of a CTA's part of it: leaves a piece or writes the rows.  A
+// thread has PER columns, from jd on, of row jr (a row is one warp's or half a warp's):
+// outputs acc not yet divided, maximum and sum.
+template <typename T, class S, int PER, int THREADS>
+__device__ __forceinline__ void leave_item(const AttendDev &a, const Cursor<S> &cur, float (&acc)[PER], float top, float sum,
+                                           int32_t *last, int64_t total, int64_t ctas)
 {
-    using J = Join<HALVES>;
-    constexpr int KS = 4 * HALVES;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r0 = lane >> 2;
-    const int jr = tid >> 4, jd = (tid & 15) * (4 * HALVES);          // joining: row and first column
-    const int32_t row0 = cur.inner * kRows, rows = min(kRows, Shape::rows(a, cur.q) - row0);
-    auto q_row = [&](int32_t row, int64_t token_stride, int64_t head_stride) { return item_row(a, cur, row, token_stride, head_stride); };
-
-    // join the warps: the upper four hand theirs to the lower four, lane by lane,
-    // then a thread has one row's 4 * HALVES columns
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-        l[x] += __shfl_xor_sync(~0u, l[x], 1);
-        l[x] += __shfl_xor_sync(~0u, l[x], 2);
-        if ((lane & 3) == 0) {
-            sh.stat[0][warp][r0 + 8 * x] = m[x];
-            sh.stat[1][warp][r0 + 8 * x] = l[x];
-        }
-    }
-    if (warp >= kWarps / 2) {
-        float4 *dst = reinterpret_cast<float4 *>(join) + (warp - kWarps / 2) * 2 * KS * 32 + lane;
-#pragma unroll
-        for (int n = 0; n < 2 * KS; ++n) dst[32 * n] = make_float4(o[n][0], o[n][1], o[n][2], o[n][3]);
-    }
-    __syncthreads();
-    if (warp < kWarps / 2) {
-        const float4 *src = reinterpret_cast<const float4 *>(join) + warp * 2 * KS * 32 + lane;
-        float f[2], g[2];
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            const float other = sh.stat[0][warp + kWarps / 2][r0 + 8 * x], up = fmaxf(m[x], other);
-            const float by = up == -INFINITY ? 0.f : up;
-            f[x] = exp2_approx(m[x] - by);
-            g[x] = exp2_approx(other - by);
-            m[x] = up;
-            l[x] = f[x] * l[x] + g[x] * sh.stat[1][warp + kWarps / 2][r0 + 8 * x];
-        }
-#pragma unroll
-        for (int n = 0; n < 2 * KS; ++n) {
-            const float4 y = src[32 * n];
-            o[n][0] = f[0] * o[n][0] + g[0] * y.x;
-            o[n][1] = f[0] * o[n][1] + g[0] * y.y;
-            o[n][2] = f[1] * o[n][2] + g[1] * y.z;
-            o[n][3] = f[1] * o[n][3] + g[1] * y.w;
-        }
-    }
-    __syncthreads();
-    if (warp < kWarps / 2) {
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            const int row = r0 + 8 * x;
-            if ((lane & 3) == 0) {
-                sh.stat[0][warp][row] = m[x];
-                sh.stat[1][warp][row] = l[x];
-            }
-            if (row < rows) {
-                float *dst = join + (warp * kRows + row) * J::pitch;
-                if constexpr (EIGHT) {
-#pragma unroll
-                    for (int n = 0; n < KS; ++n)
-                        *reinterpret_cast<float4 *>(dst + 16 * n + 4 * (lane & 3)) =
-                            make_float4(o[2 * n][2 * x], o[2 * n + 1][2 * x], o[2 * n][2 * x + 1], o[2 * n + 1][2 * x + 1]);
-                } else {
-#pragma unroll
-                    for (int n = 0; n < 2 * KS; ++n)
-                        *reinterpret_cast<float2 *>(dst + 8 * n + 2 * (lane & 3)) = make_float2(o[n][2 * x], o[n][2 * x + 1]);
-                }
-            }
-        }
-    }
-    __syncthreads();
-    float acc[4 * HALVES], top = -INFINITY, sum = 0.f;
-#pragma unroll
-    for (int d = 0; d < 4 * HALVES; ++d) acc[d] = 0.f;
-    if (jr < rows) {
-#pragma unroll
-        for (int w = 0; w < kWarps / 2; ++w) top = fmaxf(top, sh.stat[0][w][jr]);
-        const float base = top == -INFINITY ? 0.f : top;
-#pragma unroll
-        for (int w = 0; w < kWarps / 2; ++w) {
-            const float f = exp2_approx(sh.stat[0][w][jr] - base);
-            sum = fmaf(f, sh.stat[1][w][jr], sum);
-            const float4 *src = reinterpret_cast<const float4 *>(join + (w * kRows + jr) * J::pitch + jd);
-#pragma unroll
-            for (int d = 0; d < HALVES; ++d) {
-                const float4 y = src[d];
-                acc[4 * d] = fmaf(f, y.x, acc[4 * d]);
-                acc[4 * d + 1] = fmaf(f, y.y, acc[4 * d + 1]);
-                acc[4 * d + 2] = fmaf(f, y.z, acc[4 * d + 2]);
-                acc[4 * d + 3] = fmaf(f, y.w, acc[4 * d + 3]);
-            }
-        }
-    }
+    constexpr int kRows = S::kRows, kLanes = THREADS / kRows, kWidth = PER * kLanes;
+    const int tid = threadIdx.x, jr = tid / kLanes, jd = tid % kLanes * PER;
+    const int32_t row0 = cur.inner * kRows, rows = min(kRows, S::rows(a, cur.q) - row0);
 
     // an item in pieces: leave this one's, and the last to arrive joins a group's, then the groups'
     bool write = true;
@@ -211,12 +137,9 @@ __device__ __forceinline__ void finish_item(const AttendDev &a, const Cursor<Sha
         const int32_t mine = (int32_t)blockIdx.x - cta0;
         const int32_t groups = (pieces + kJoinGroup - 1) / kJoinGroup;
         auto put = [&](int32_t slot) {
-            __syncwarp();                           // a row's 16 lanes have read what one of them writes over
+            __syncwarp();                           // a row's lanes have read what one of them writes over
             if (jr < rows) {
-                float4 *dst = reinterpret_cast<float4 *>(a.piece + ((int64_t)slot * kRows + jr) * J::width + jd);
-#pragma unroll
-                for (int d = 0; d < HALVES; ++d)
-                    dst[d] = make_float4(acc[4 * d], acc[4 * d + 1], acc[4 * d + 2], acc[4 * d + 3]);
+                store_columns<PER>(a.piece + ((int64_t)slot * kRows + jr) * kWidth + jd, acc);
                 if (jd == 0) {
                     a.piece_stat[slot * 2 * kRows + jr] = top;
                     a.piece_stat[slot * 2 * kRows + kRows + jr] = sum;
@@ -228,12 +151,12 @@ __device__ __forceinline__ void finish_item(const AttendDev &a, const Cursor<Sha
             __threadfence();
             __syncthreads();
             if (tid == 0) {
-                sh.last = atomicAdd(count, 1) == of - 1;
-                if (sh.last) *count = 0;
+                *last = atomicAdd(count, 1) == of - 1;
+                if (*last) *count = 0;
             }
             __syncthreads();
             __threadfence();
-            return sh.last != 0;
+            return *last != 0;
         };
         // join pieces p0, p0 + step, ...
         auto gather = [&](int32_t p0, int32_t n, int32_t step) {
@@ -244,22 +167,16 @@ __device__ __forceinline__ void finish_item(const AttendDev &a, const Cursor<Sha
             const float base = top == -INFINITY ? 0.f : top;
             sum = 0.f;
 #pragma unroll
-            for (int d = 0; d < 4 * HALVES; ++d) acc[d] = 0.f;
+            for (int d = 0; d < PER; ++d) acc[d] = 0.f;
 #pragma unroll 4
             for (int32_t p = 0; p < n; ++p) {
                 const int32_t slot = piece_slot(cta0, p0 + p * step);
                 const float f = exp2_approx(__ldcg(a.piece_stat + slot * 2 * kRows + jr) - base);
                 sum = fmaf(f, __ldcg(a.piece_stat + slot * 2 * kRows + kRows + jr), sum);
-                const float4 *src =
-                    reinterpret_cast<const float4 *>(a.piece + ((int64_t)slot * kRows + jr) * J::width + jd);
+                float y[PER];
+                load_columns<PER>(a.piece + ((int64_t)slot * kRows + jr) * kWidth + jd, y);
 #pragma unroll
-                for (int d = 0; d < HALVES; ++d) {
-                    const float4 y = __ldcg(src + d);
-                    acc[4 * d] = fmaf(f, y.x, acc[4 * d]);
-                    acc[4 * d + 1] = fmaf(f, y.y, acc[4 * d + 1]);
-                    acc[4 * d + 2] = fmaf(f, y.z, acc[4 * d + 2]);
-                    acc[4 * d + 3] = fmaf(f, y.w, acc[4 * d + 3]);
-                }
+                for (int d = 0; d < PER; ++d) acc[d] = fmaf(f, y[d], acc[d]);
             }
         };
         put(piece_slot(cta0, mine));
@@ -275,23 +192,20 @@ __device__ __forceinline__ void finish_item(const AttendDev &a, const Cursor<Sha
         }
     }
     if (write && jr < rows) {
-        const float inv = inverse_sum(sum, Shape::pos(a, cur.q, row0 + jr) >= 0);
-        T *dst = static_cast<T *>(a.c.out) + q_row(jr, a.c.out_token_stride, a.c.out_head_stride) + jd;
-        if constexpr (HALVES == 2) {
-            if (jd < a.dim)
-                *reinterpret_cast<uint4 *>(dst) =
-                    make_uint4(Pack<T>::two(acc[0] * inv, acc[1] * inv), Pack<T>::two(acc[2] * inv, acc[3] * inv),
-                               Pack<T>::two(acc[4] * inv, acc[5] * inv), Pack<T>::two(acc[6] * inv, acc[7] * inv));
-        } else {
-            if (jd < a.dim)
-                *reinterpret_cast<uint2 *>(dst) =
-                    make_uint2(Pack<T>::two(acc[0] * inv, acc[1] * inv), Pack<T>::two(acc[2] * inv, acc[3] * inv));
+        const float inv = inverse_sum(sum, S::pos(a, cur.q, row0 + jr) >= 0);
+        T *dst = static_cast<T *>(a.c.out) + item_row(a, cur, jr, a.c.out_token_stride, a.c.out_head_stride) + jd;
+        if (jd < a.dim) {
+            uint32_t w[PER / 2];
+#pragma unroll
+            for (int d = 0; d < PER / 2; ++d) w[d] = Pack<T>::two(acc[2 * d] * inv, acc[2 * d + 1] * inv);
+            if constexpr (PER == 8) *reinterpret_cast<uint4 *>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
+            else if constexpr (PER == 4) *reinterpret_cast<uint2 *>(dst) = make_uint2(w[0], w[1]);
+            else *reinterpret_cast<uint32_t *>(dst) = w[0];
         }
         if (a.c.lse && jd == 0)
-            a.c.lse[q_row(jr, a.c.q_heads, 1)] =
+            a.c.lse[item_row(a, cur, jr, a.c.q_heads, 1)] =
                 sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
     }
-    __syncthreads();                                // the join's memory is free again
 }
 
 }  // namespace pp

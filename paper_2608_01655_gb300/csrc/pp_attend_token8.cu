@@ -12,22 +12,34 @@
 // largest value near 2^14: bf16's 8 bits fit, and what falls below 2^-24 is 2^-38 of
 // the row's largest.  Weights are rounded to 11 bits for their product.
 //
-// Items, tiles, the cut of the work and the joins are those of the 16-bit kernel; a
-// warp's 16 keys are 4 KB here.  The products' summed index may be taken in any
-// order: a lane takes 16 or 32 neighbouring codes of a K row by 16-byte loads, and Q's
-// operand is laid out to match.  V's codes come in pairs of columns from a
-// transposing load of 16-bit units; two keys' codes are put together by a permutation
-// of bytes, which leaves an output tile the even columns and the next the odd ones.
+// An item is 8 or 16 rows (new token, query head) of one K/V head.  The products are
+// transposed, keys and the head's elements outside, the rows inside: S^T = K Q^T, O^T =
+// V^T P^T.  So 8 rows fill an instruction (m16n8k16), and the codes, which have to be
+// widened, are its larger operand.  P^T's operand is S^T's accumulator with its 8 x 8
+// squares transposed, one instruction each.  The products' summed index may be taken in
+// any order: a lane takes 16 or 32 neighbouring codes of a K row by 16-byte loads, and
+// Q's operand is laid out to match.  V's codes come in pairs of columns from a
+// transposing load of 16-bit units; a permutation of bytes puts two keys' codes
+// together, and an operand's rows are the even columns, then the odd ones.
+// The cut of the work and the ring of copies are those of the 16-bit kernel; a warp's 16
+// keys are 4 KB here.
 #include "pp_attend_token.cuh"
 
 namespace pp {
 
 namespace token {
-template <int HALVES> struct Layout8 {
+// ROWS of an item, 64 * HALVES columns
+template <int ROWS, int HALVES> struct Layout8 {
+    static constexpr int warps = 8, threads = 32 * warps;
     static constexpr int rows = kKeys * 64 * HALVES;            // bytes of a warp's K or V
-    static constexpr int stages = HALVES == 2 ? 5 : 10;
-    static constexpr int ring = kWarps * stages * 2 * rows;
-    static constexpr int bytes = 128 + ring + Join<HALVES>::bytes;
+    static constexpr int stages = (ROWS == 16 ? 4 : 5) * (HALVES == 2 ? 1 : 2);
+    static constexpr int ring = warps * stages * 2 * rows;
+    static constexpr int width = 64 * HALVES;
+    static constexpr int pitch = width + 4;                     // floats of an output row in shared memory
+    static constexpr int join = warps * ROWS * pitch * 4;
+    static constexpr int bytes = 128 + ring + join;
+    static_assert(bytes < 225 * 1024, "shared memory of a CTA");
+    using Shape = ShapeOf<ROWS, kKeys * warps>;
 };
 }  // namespace token
 
@@ -56,6 +68,13 @@ __device__ __forceinline__ uint4 lds128(uint32_t addr)
     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(addr));
     return x;
 }
+// the transposed 8 x 8 square of 16-bit numbers
+__device__ __forceinline__ uint32_t transpose8(uint32_t x)
+{
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+    return r;
+}
 __device__ __forceinline__ float power_of_two(int e) { return __int_as_float((e + 127) << 23); }    // -126 <= e <= 127
 
 // 0xff in the bytes that hold NaN
@@ -65,17 +84,21 @@ __device__ __forceinline__ uint32_t nan_bytes(uint32_t x)
     return top * 0xffu;
 }
 
-// A warp's copies of its keys, as in the 16-bit kernel; beside a tile's keys go the
-// exponents of their two groups of 8 (K's and V's, a byte each).
-template <int HALVES> struct Feed8 {
-    using L = Layout8<HALVES>;
-    static constexpr int per_row = 4 * HALVES, step = 32 / per_row;     // pieces of a row, rows at a time
+// A warp's copies of its keys, tile after tile along the stretch.  Lane l keeps, of the
+// warp's keys in the l-th of the next 32 tiles, where they begin in the cache and the
+// exponents of their two groups of 8 (K's and V's, a byte each), which go beside the
+// tile's keys.
+template <class L, int HALVES> struct Feed8 {
+    using Shape = typename L::Shape;
+    static constexpr int KT = Shape::KT, per_row = 4 * HALVES, step = 32 / per_row;     // pieces of a row, rows at a time
     const AttendDev &a;
     Cursor<Shape> cur;
+    const char *from;                   // this lane's piece of slot 0's row of a step
+    int64_t v_from_k;
     uint32_t ring, slot = 0, bytes;
-    int64_t src;
     uint32_t *exps;                     // shared memory, [stages]
-    int32_t i = 0, lower, upper;
+    int32_t i = 0;
+    int64_t at0, at1;                   // keys 0 - 7 and 8 - 15, -1: not in the cache
     uint32_t scales;
     bool more;
     __device__ __forceinline__ Feed8(const AttendDev &a_, const SchedShared &sched, uint32_t ring_, uint32_t *exps_)
@@ -83,7 +106,8 @@ template <int HALVES> struct Feed8 {
     {
         const int lane = threadIdx.x & 31, sub = lane / per_row, piece = lane % per_row;
         bytes = piece * 16 < a.dim ? 16 : 0;
-        src = sub * a.token_stride + (bytes ? piece * 16 : 0);
+        from = static_cast<const char *>(a.c.k_cache) + sub * a.token_stride + (bytes ? piece * 16 : 0);
+        v_from_k = static_cast<const char *>(a.c.v_cache) - static_cast<const char *>(a.c.k_cache);
         look();
     }
     __device__ __forceinline__ int32_t first(int32_t tile) const
@@ -100,38 +124,41 @@ template <int HALVES> struct Feed8 {
     __device__ __forceinline__ void look()
     {
         const int32_t *row = a.c.block_table + (int64_t)cur.r * a.c.table_width;
-        const int32_t tile = i + (threadIdx.x & 31), j = first(tile);
-        lower = tile < cur.len ? key_block(a, row, cur.k, j, 8) : -1;
-        upper = tile >= cur.len ? -1 : a.block_log > 3 && lower >= 0 && j + 8 <= cur.k.hi ? lower : key_block(a, row, cur.k, j + 8, 8);
+        const int32_t tile = i + (threadIdx.x & 31), j = first(tile), in_block = (1 << a.block_log) - 1;
+        const int32_t lower = tile < cur.len ? key_block(a, row, cur.k, j, 8) : -1;
+        const int32_t upper =
+            tile >= cur.len ? -1 : a.block_log > 3 && lower >= 0 && j + 8 <= cur.k.hi ? lower : key_block(a, row, cur.k, j + 8, 8);
+        const int64_t head = cur.outer * a.head_stride;
+        at0 = lower < 0 ? -1 : head + lower * a.block_stride + (j & in_block) * a.token_stride;
+        at1 = upper < 0 ? -1 : head + upper * a.block_stride + ((j + 8) & in_block) * a.token_stride;
         scales = scale_of(lower);
         scales |= (upper == lower ? scales : scale_of(upper)) << 16;
     }
-    // 8 rows
-    __device__ __forceinline__ void rows8(uint32_t to, int row, const char *from, bool some) const
+    // 8 rows of K and of V
+    __device__ __forceinline__ void rows8(uint32_t to, int row, int64_t at) const
     {
         const int lane = threadIdx.x & 31, sub = lane / per_row, piece = lane % per_row;
+        const uint32_t some = at >= 0 ? bytes : 0;
+        const char *k = from + (at >= 0 ? at : 0);
 #pragma unroll
-        for (int x = 0; x < 8; x += step)
-            copy16(to + piece_at<HALVES>(row + x + sub, piece), from + src + x * a.token_stride, some ? bytes : 0);
+        for (int x = 0; x < 8; x += step) {
+            copy16(to + piece_at<HALVES>(row + x + sub, piece), k, some);
+            copy16(to + L::rows + piece_at<HALVES>(row + x + sub, piece), k + v_from_k, some);
+            k += step * a.token_stride;
+        }
     }
     // asks for the next tile, into the ring's next place
     __device__ __forceinline__ void ask()
     {
         if (more) {
-            const int32_t j0 = first(i), in_block = (1 << a.block_log) - 1;
-            const int32_t b0 = __shfl_sync(~0u, lower, i & 31), b1 = __shfl_sync(~0u, upper, i & 31);
+            const int32_t j0 = first(i);
+            const int64_t b0 = __shfl_sync(~0u, at0, i & 31), b1 = __shfl_sync(~0u, at1, i & 31);
             const uint32_t e = __shfl_sync(~0u, scales, i & 31);
             if (j0 <= cur.k.hi && j0 + kKeys - 1 >= cur.k.lo) {
                 if ((threadIdx.x & 31) == 0) exps[slot] = e;
-                const int64_t head = cur.outer * a.head_stride;
-                const int64_t at0 = head + max(b0, 0) * a.block_stride + (j0 & in_block) * a.token_stride;
-                const int64_t at1 = head + max(b1, 0) * a.block_stride + ((j0 + 8) & in_block) * a.token_stride;
-                const char *k = static_cast<const char *>(a.c.k_cache), *v = static_cast<const char *>(a.c.v_cache);
                 const uint32_t to = ring + slot * 2 * L::rows;
-                rows8(to, 0, k + at0, b0 >= 0);
-                rows8(to, 8, k + at1, b1 >= 0);
-                rows8(to + L::rows, 0, v + at0, b0 >= 0);
-                rows8(to + L::rows, 8, v + at1, b1 >= 0);
+                rows8(to, 0, b0);
+                rows8(to, 8, b1);
             }
             if (++i == cur.len) {
                 i = 0;
@@ -146,8 +173,8 @@ template <int HALVES> struct Feed8 {
     }
 };
 
-// A row's 8 * HALVES elements of a lane, as operands; `by` is what the row is to be
-// multiplied with after the product.
+// A row's 8 * HALVES pairs of elements of a lane, as operands; what the row is to be
+// multiplied with after the product is returned.
 template <int HALVES>
 __device__ __forceinline__ float query_row(const __half *, const uint4 (&x)[2 * HALVES], uint32_t (&to)[8 * HALVES])
 {
@@ -184,61 +211,75 @@ __device__ __forceinline__ float query_row(const __nv_bfloat16 *, const uint4 (&
     return power_of_two(-up);
 }
 
-template <typename T, int HALVES>
-__global__ void __launch_bounds__(kThreads, 1) k_attend_token8(const __grid_constant__ AttendDev a)
+template <typename T, int ROWS, int HALVES>
+__global__ void __launch_bounds__(Layout8<ROWS, HALVES>::threads, 1) k_attend_token8(const __grid_constant__ AttendDev a)
 {
-    using L = Layout8<HALVES>;
+    using L = Layout8<ROWS, HALVES>;
+    using Shape = typename L::Shape;
+    constexpr int NB = ROWS / 8;                        // 8 rows each
     constexpr int KS = 4 * HALVES;                      // 16-wide steps of the head dimension
+    constexpr int KT = Shape::KT;
     extern __shared__ uint8_t raw[];
     __shared__ SchedShared sched;
-    __shared__ JoinShared shared;
-    __shared__ uint32_t exps[kWarps][L::stages];
+    __shared__ float stat[2][L::warps][ROWS];
+    __shared__ uint32_t exps[L::warps][L::stages];
+    __shared__ int32_t last;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t base = (smem_u32(raw) + 127) & ~127u;
     float *join = reinterpret_cast<float *>(raw + (base - smem_u32(raw)) + L::ring);
     if (!schedule<Shape>(a, sched)) return;
     const int64_t total = sched.total, ctas = min((int64_t)gridDim.x, total);
 
-    const int r0 = lane >> 2, c0 = 2 * (lane & 3);      // this thread's rows r0, r0 + 8; its keys in an operand
-    const int dim0 = 16 * HALVES * (lane & 3);          // its elements of a K row and of Q
+    // accumulators: keys or columns g and g + 8, rows 2 c and 2 c + 1 of 8
+    const int g = lane >> 2, c = lane & 3;
+    const int dim0 = 16 * HALVES * c;                   // this lane's elements of a K row and of Q
     // ldmatrix rows of V: 8 keys and the next 8, then the same of the next piece
     const int vrow = ((lane >> 3) & 1) * 8 + (lane & 7), vpiece = lane >> 4;
 
     const uint32_t ring = base + warp * L::stages * 2 * L::rows;
-    Feed8<HALVES> feed(a, sched, ring, exps[warp]);
+    Feed8<L, HALVES> feed(a, sched, ring, exps[warp]);
 #pragma unroll 1
     for (int x = 0; x < L::stages; ++x) feed.ask();
     Cursor<Shape> cur(a, sched);
     uint32_t slot = 0;
     do {
-        const int32_t row0 = cur.inner * kRows, rows = min(kRows, Shape::rows(a, cur.q) - row0);
-        uint32_t qf[KS][4];
-        float q_by[2];
+        const int32_t row0 = cur.inner * ROWS, rows = min(ROWS, Shape::rows(a, cur.q) - row0);
+        uint32_t qf[NB][KS][2];
+        float q_by[NB][2];
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            const bool in = r0 + 8 * x < rows;
+        for (int b = 0; b < NB; ++b) {
+            const bool in = 8 * b + g < rows;
             const T *qp = static_cast<const T *>(a.c.q) +
-                          (in ? item_row(a, cur, r0 + 8 * x, a.c.q_token_stride, a.c.q_head_stride) : 0) + dim0;
+                          (in ? item_row(a, cur, 8 * b + g, a.c.q_token_stride, a.c.q_head_stride) : 0) + dim0;
             uint4 raw_q[2 * HALVES];
             uint32_t two[2 * KS];
 #pragma unroll
             for (int n = 0; n < 2 * HALVES; ++n)
                 raw_q[n] = in && dim0 + 8 * n < a.dim ? __ldg(reinterpret_cast<const uint4 *>(qp) + n) : make_uint4(0, 0, 0, 0);
-            q_by[x] = query_row<HALVES>(qp, raw_q, two);
+            const float by = query_row<HALVES>(qp, raw_q, two) * a.scale_log2;
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
-                qf[k][x] = two[2 * k];
-                qf[k][x + 2] = two[2 * k + 1];
+                qf[b][k][0] = two[2 * k];
+                qf[b][k][1] = two[2 * k + 1];
             }
+            q_by[b][0] = __shfl_sync(~0u, by, 8 * c);
+            q_by[b][1] = __shfl_sync(~0u, by, 8 * c + 4);
         }
         // keys that all rows see; the rows of one token see the same
         const int32_t pos0 = Shape::pos(a, cur.q, row0), pos1 = cur.k.hi;
         const int32_t all_lo = first_key(a, pos1), all_hi = pos0;
-        float o[2 * KS][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+        // last key and first key of row 8 b + 2 c + y (none: -1, 0)
+        auto row_pos = [&](int b, int y) { return 8 * b + 2 * c + y < rows ? Shape::pos(a, cur.q, row0 + 8 * b + 2 * c + y) : -1; };
+        float o[KS][NB][4], m[NB][2], l[NB][2];
 #pragma unroll
-        for (int n = 0; n < 2 * KS; ++n)
+        for (int b = 0; b < NB; ++b) {
+            m[b][0] = m[b][1] = -INFINITY;
+            l[b][0] = l[b][1] = 0.f;
 #pragma unroll
-            for (int x = 0; x < 4; ++x) o[n][x] = 0.f;
+            for (int n = 0; n < KS; ++n)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) o[n][b][x] = 0.f;
+        }
 
         const int32_t t0 = cur.k.lo / KT + cur.off;
 #pragma unroll 1
@@ -251,68 +292,79 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_token8(const __grid_cons
             __syncwarp();
             if (j0 <= cur.k.hi && j0 + kKeys - 1 >= cur.k.lo) {
                 const uint32_t e = *reinterpret_cast<const volatile uint32_t *>(e_at);
-                float sc[2][4];
+                float sc[NB][4];
 #pragma unroll
-                for (int n = 0; n < 2; ++n)
+                for (int b = 0; b < NB; ++b)
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) sc[n][x] = 0.f;
+                    for (int x = 0; x < 4; ++x) sc[b][x] = 0.f;
 #pragma unroll
                 for (int h = 0; h < HALVES; ++h) {
+                    const uint4 x = lds128(kt + piece_at<HALVES>(g, HALVES * c + h));
+                    const uint4 y = lds128(kt + piece_at<HALVES>(8 + g, HALVES * c + h));
+                    const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-                    for (int n = 0; n < 2; ++n) {
-                        const uint4 c = lds128(kt + piece_at<HALVES>(8 * n + r0, HALVES * (lane & 3) + h));
-                        mma16<__half>(sc[n], qf[4 * h], widen<0>(c.x), widen<1>(c.x));
-                        mma16<__half>(sc[n], qf[4 * h + 1], widen<0>(c.y), widen<1>(c.y));
-                        mma16<__half>(sc[n], qf[4 * h + 2], widen<0>(c.z), widen<1>(c.z));
-                        mma16<__half>(sc[n], qf[4 * h + 3], widen<0>(c.w), widen<1>(c.w));
+                    for (int k = 0; k < 4; ++k) {
+                        const uint32_t f[4] = {widen<0>(xs[k]), widen<0>(ys[k]), widen<1>(xs[k]), widen<1>(ys[k])};
+#pragma unroll
+                        for (int b = 0; b < NB; ++b) mma16<__half>(sc[b], f, qf[b][4 * h + k][0], qf[b][4 * h + k][1]);
                     }
                 }
                 const bool edge = j0 < all_lo || j0 + kKeys - 1 > all_hi;
                 uint32_t vk0 = ~0u, vk1 = ~0u;                      // V rows that some row sees, as the operand holds them
-                float v_up[2], v_down[2];
+                float v_down[2];
 #pragma unroll
                 for (int n = 0; n < 2; ++n) {
                     const int ke = (int8_t)(e >> 16 * n), ve = (int8_t)(e >> (16 * n + 8));
-                    const float by = a.scale_log2 * power_of_two(ke);
-                    v_up[n] = (float)ve;
+                    const float by = power_of_two(ke);
                     v_down[n] = power_of_two(-ve);
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) sc[n][x] = fmaf(sc[n][x] * by, q_by[x >> 1], v_up[n]);
+                    for (int b = 0; b < NB; ++b)
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) sc[b][2 * n + y] = fmaf(sc[b][2 * n + y] * by, q_by[b][y], (float)ve);
                 }
                 if (edge) {
+#pragma unroll
+                    for (int b = 0; b < NB; ++b)
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) {
+                            const int32_t pos = row_pos(b, y), lo = pos < 0 ? 0 : first_key(a, pos);
+#pragma unroll
+                            for (int n = 0; n < 2; ++n) {
+                                const int32_t j = j0 + g + 8 * n;
+                                if (j < lo || j > pos) sc[b][2 * n + y] = -INFINITY;
+                            }
+                        }
                     bool in[4];
 #pragma unroll
-                    for (int y = 0; y < 2; ++y) {
-                        const int32_t pos = r0 + 8 * y < rows ? Shape::pos(a, cur.q, row0 + r0 + 8 * y) : -1;
-                        const int32_t lo = pos < 0 ? 0 : first_key(a, pos);
-#pragma unroll
-                        for (int x = 0; x < 4; ++x) {
-                            const int32_t j = j0 + c0 + (x & 1) + 8 * (x >> 1);
-                            in[x] = j >= cur.k.lo && j <= cur.k.hi;
-                            if (j < lo || j > pos) sc[x >> 1][2 * y + (x & 1)] = -INFINITY;
-                        }
+                    for (int x = 0; x < 4; ++x) {
+                        const int32_t j = j0 + 2 * c + (x & 1) + 8 * (x >> 1);
+                        in[x] = j >= cur.k.lo && j <= cur.k.hi;
                     }
                     vk0 = keep(in[0], in[1]);
                     vk1 = keep(in[2], in[3]);
                 }
-                float top[2], at[2];
+                bool higher = false;
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    top[x] = fmaxf(fmaxf(sc[0][2 * x], sc[0][2 * x + 1]), fmaxf(sc[1][2 * x], sc[1][2 * x + 1]));
-                    top[x] = fmaxf(top[x], __shfl_xor_sync(~0u, top[x], 1));
-                    top[x] = fmaxf(top[x], __shfl_xor_sync(~0u, top[x], 2));
-                }
-                if (__any_sync(~0u, top[0] > m[0] || top[1] > m[1])) {
+                for (int b = 0; b < NB; ++b)
 #pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        const float up = fmaxf(m[x], top[x]);
-                        const float f = up == -INFINITY ? 1.f : exp2_approx(m[x] - up);
-                        m[x] = up;
-                        l[x] *= f;
+                    for (int y = 0; y < 2; ++y) higher |= fmaxf(sc[b][y], sc[b][2 + y]) > m[b][y];
+                if (__any_sync(~0u, higher)) {
 #pragma unroll
-                        for (int n = 0; n < 2 * KS; ++n) {
-                            o[n][2 * x] *= f;
-                            o[n][2 * x + 1] *= f;
+                    for (int b = 0; b < NB; ++b) {
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) {
+                            float up = fmaxf(sc[b][y], sc[b][2 + y]);
+                            up = fmaxf(up, __shfl_xor_sync(~0u, up, 4));
+                            up = fmaxf(up, __shfl_xor_sync(~0u, up, 8));
+                            up = fmaxf(m[b][y], fmaxf(up, __shfl_xor_sync(~0u, up, 16)));
+                            const float f = up == -INFINITY ? 1.f : exp2_approx(m[b][y] - up);
+                            m[b][y] = up;
+                            l[b][y] *= f;
+#pragma unroll
+                            for (int n = 0; n < KS; ++n) {
+                                o[n][b][y] *= f;
+                                o[n][b][2 + y] *= f;
+                            }
                         }
                     }
                 }
@@ -327,21 +379,21 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_token8(const __grid_cons
                     }
                     if (__any_sync(~0u, strange)) {
 #pragma unroll
-                        for (int y = 0; y < 2; ++y) {
-                            const int32_t pos = r0 + 8 * y < rows ? Shape::pos(a, cur.q, row0 + r0 + 8 * y) : -1;
-                            const int32_t lo = pos < 0 ? 0 : first_key(a, pos);
-#pragma unroll 1
-                            for (int32_t j = max(j0, lo); j <= min(j0 + kKeys - 1, pos); ++j) {
+                        for (int b = 0; b < NB; ++b)
 #pragma unroll
-                                for (int n = 0; n < KS; ++n) {
-                                    const uint32_t odd = nan_bytes(lds32(vt + piece_at<HALVES>(j - j0, n) + 2 * c0));
-                                    if (odd & 0xffu) o[2 * n][2 * y] = NAN;
-                                    if (odd & 0xff00u) o[2 * n + 1][2 * y] = NAN;
-                                    if (odd & 0xff0000u) o[2 * n][2 * y + 1] = NAN;
-                                    if (odd & 0xff000000u) o[2 * n + 1][2 * y + 1] = NAN;
+                            for (int y = 0; y < 2; ++y) {
+                                const int32_t pos = row_pos(b, y), lo = pos < 0 ? 0 : first_key(a, pos);
+#pragma unroll 1
+                                for (int32_t j = max(j0, lo); j <= min(j0 + kKeys - 1, pos); ++j) {
+#pragma unroll
+                                    for (int n = 0; n < KS; ++n) {
+                                        const uint32_t at = vt + piece_at<HALVES>(j - j0, n) + 2 * g;
+                                        const uint32_t odd = nan_bytes(lds32(at & ~3u)) >> 8 * (at & 2);
+                                        if (odd & 0xffu) o[n][b][y] = NAN;
+                                        if (odd & 0xff00u) o[n][b][2 + y] = NAN;
+                                    }
                                 }
                             }
-                        }
                         __syncwarp();
 #pragma unroll 1
                         for (int x = 0; x < L::rows / 512; ++x) {
@@ -351,74 +403,127 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_token8(const __grid_cons
                         __syncwarp();
                     }
                 }
-                uint32_t pf[4];
+                uint32_t pf[NB][2];
 #pragma unroll
-                for (int x = 0; x < 2; ++x) at[x] = m[x] == -INFINITY ? 0.f : m[x];
+                for (int b = 0; b < NB; ++b) {
 #pragma unroll
-                for (int n = 0; n < 2; ++n) {
+                    for (int y = 0; y < 2; ++y) {
+                        const float at = m[b][y] == -INFINITY ? 0.f : m[b][y];
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        sc[n][x] = exp2_approx(sc[n][x] - at[x >> 1]);
-                        l[x >> 1] = fmaf(sc[n][x], v_down[n], l[x >> 1]);
+                        for (int n = 0; n < 2; ++n) {
+                            sc[b][2 * n + y] = exp2_approx(sc[b][2 * n + y] - at);
+                            l[b][y] = fmaf(sc[b][2 * n + y], v_down[n], l[b][y]);
+                        }
                     }
-                    pf[2 * n] = Pack<__half>::two(sc[n][0], sc[n][1]);
-                    pf[2 * n + 1] = Pack<__half>::two(sc[n][2], sc[n][3]);
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) pf[b][n] = transpose8(Pack<__half>::two(sc[b][2 * n], sc[b][2 * n + 1]));
                 }
 #pragma unroll
                 for (int n = 0; n < KS; n += 2) {
-                    uint32_t b[4];
-                    ldsm4_trans(b, vt + piece_at<HALVES>(vrow, n + vpiece));
+                    uint32_t w[4];
+                    ldsm4_trans(w, vt + piece_at<HALVES>(vrow, n + vpiece));
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
                         // codes of columns d, d + 1 of two keys: to both keys' of d, both keys' of d + 1
-                        const uint32_t lo = __byte_perm(b[2 * x], 0, 0x3120), hi = __byte_perm(b[2 * x + 1], 0, 0x3120);
-                        uint32_t f[4] = {widen<0>(lo), widen<0>(hi), widen<1>(lo), widen<1>(hi)};
+                        const uint32_t lo = __byte_perm(w[2 * x], 0, 0x3120), hi = __byte_perm(w[2 * x + 1], 0, 0x3120);
+                        uint32_t f[4] = {widen<0>(lo), widen<1>(lo), widen<0>(hi), widen<1>(hi)};
                         if (edge) {
                             f[0] &= vk0;
-                            f[1] &= vk1;
-                            f[2] &= vk0;
+                            f[1] &= vk0;
+                            f[2] &= vk1;
                             f[3] &= vk1;
                         }
-                        mma16<__half>(o[2 * (n + x)], pf, f[0], f[1]);
-                        mma16<__half>(o[2 * (n + x) + 1], pf, f[2], f[3]);
+#pragma unroll
+                        for (int b = 0; b < NB; ++b) mma16<__half>(o[n + x][b], f, pf[b][0], pf[b][1]);
                     }
                 }
             }
             __syncwarp();
             feed.ask();                                             // into the place just read
         }
-        finish_item<T, HALVES, true>(a, cur, o, m, l, join, shared, total, ctas);
+
+        // join the warps through shared memory, where a thread then has one row's `per` columns
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                const int row = 8 * b + 2 * c + y;
+                l[b][y] += __shfl_xor_sync(~0u, l[b][y], 4);
+                l[b][y] += __shfl_xor_sync(~0u, l[b][y], 8);
+                l[b][y] += __shfl_xor_sync(~0u, l[b][y], 16);
+                if (g == 0) {
+                    stat[0][warp][row] = m[b][y];
+                    stat[1][warp][row] = l[b][y];
+                }
+                float *dst = join + (warp * ROWS + row) * L::pitch + 2 * g;
+#pragma unroll
+                for (int n = 0; n < KS; ++n) *reinterpret_cast<float2 *>(dst + 16 * n) = make_float2(o[n][b][y], o[n][b][2 + y]);
+            }
+        }
+        __syncthreads();
+        constexpr int per = L::width * ROWS / L::threads;
+        const int jr = tid / (L::threads / ROWS), jd = tid % (L::threads / ROWS) * per;
+        float acc[per], top = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (int d = 0; d < per; ++d) acc[d] = 0.f;
+#pragma unroll
+        for (int w = 0; w < L::warps; ++w) top = fmaxf(top, stat[0][w][jr]);
+        const float at = top == -INFINITY ? 0.f : top;
+#pragma unroll
+        for (int w = 0; w < L::warps; ++w) {
+            const float f = exp2_approx(stat[0][w][jr] - at);
+            sum = fmaf(f, stat[1][w][jr], sum);
+            const float *src = join + (w * ROWS + jr) * L::pitch + jd;
+#pragma unroll
+            for (int d = 0; d < per; d += 2) {
+                const float2 y = *reinterpret_cast<const float2 *>(src + d);
+                acc[d] = fmaf(f, y.x, acc[d]);
+                acc[d + 1] = fmaf(f, y.y, acc[d + 1]);
+            }
+        }
+        leave_item<T, Shape, per, L::threads>(a, cur, acc, top, sum, &last, total, ctas);
+        __syncthreads();                                // the join's memory is free again
     } while (cur.next(a));
 }
 
-template <typename T, int HALVES> static cudaError_t prepare_t()
+template <typename T, int ROWS, int HALVES> static cudaError_t prepare_t()
 {
-    return cudaFuncSetAttribute(k_attend_token8<T, HALVES>, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout8<HALVES>::bytes);
+    return cudaFuncSetAttribute(k_attend_token8<T, ROWS, HALVES>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                Layout8<ROWS, HALVES>::bytes);
+}
+template <typename T> static cudaError_t prepare_all()
+{
+    for (const cudaError_t e : {prepare_t<T, 8, 1>(), prepare_t<T, 8, 2>(), prepare_t<T, 16, 1>(), prepare_t<T, 16, 2>()})
+        if (e != cudaSuccess) return e;
+    return cudaSuccess;
 }
 
-template <typename T, int HALVES>
+template <typename T, int ROWS, int HALVES>
 static pp_status launch_t(pp_kv *kv, const AttendArgs &c, cudaStream_t st)
 {
+    using L = Layout8<ROWS, HALVES>;
     const AttendDev a = attend_dev(kv, c);
-    k_attend_token8<T, HALVES><<<kv->sm_count, kThreads, Layout8<HALVES>::bytes, st>>>(a);
+    k_attend_token8<T, ROWS, HALVES><<<kv->sm_count, L::threads, L::bytes, st>>>(a);
     PP_CUDA(cudaGetLastError());
     return PP_OK;
+}
+template <typename T> static pp_status launch_rows(pp_kv *kv, const AttendArgs &c, cudaStream_t st)
+{
+    // 8 rows an item where that is all that a request has
+    if ((int64_t)c.max_q * c.group <= 8) return kv->dim > 64 ? launch_t<T, 8, 2>(kv, c, st) : launch_t<T, 8, 1>(kv, c, st);
+    return kv->dim > 64 ? launch_t<T, 16, 2>(kv, c, st) : launch_t<T, 16, 1>(kv, c, st);
 }
 
 pp_status prepare_attend_token8()
 {
-    PP_CUDA((prepare_t<__nv_bfloat16, 1>()));
-    PP_CUDA((prepare_t<__nv_bfloat16, 2>()));
-    PP_CUDA((prepare_t<__half, 1>()));
-    PP_CUDA((prepare_t<__half, 2>()));
+    PP_CUDA(prepare_all<__nv_bfloat16>());
+    PP_CUDA(prepare_all<__half>());
     return PP_OK;
 }
 
 pp_status launch_attend_token8(pp_kv *kv, const AttendArgs &c, cudaStream_t st)
 {
-    if (kv->dtype == PP_KV_BF16)
-        return kv->dim > 64 ? launch_t<__nv_bfloat16, 2>(kv, c, st) : launch_t<__nv_bfloat16, 1>(kv, c, st);
-    return kv->dim > 64 ? launch_t<__half, 2>(kv, c, st) : launch_t<__half, 1>(kv, c, st);
+    return kv->dtype == PP_KV_BF16 ? launch_rows<__nv_bfloat16>(kv, c, st) : launch_rows<__half>(kv, c, st);
 }
 
 }  // namespace pp
