@@ -119,14 +119,14 @@ __device__ __forceinline__ int64_t item_row(const AttendDev &a, const Cursor<S> 
 }
 
 // The end of an item, or of a CTA's part of it: leaves a piece or writes the rows.  A
-// thread has PER columns, from jd on, of row jr (a row is one warp's or half a warp's):
-// outputs acc not yet divided, maximum and sum.
-template <typename T, class S, int PER, int THREADS>
-__device__ __forceinline__ void leave_item(const AttendDev &a, const Cursor<S> &cur, float (&acc)[PER], float top, float sum,
-                                           int32_t *last, int64_t total, int64_t ctas)
+// thread (tid of THREADS, which sync() is for) has PER columns, from jd on, of row jr (a
+// row is within a warp): outputs acc not yet divided, maximum and sum.
+template <typename T, class S, int PER, int THREADS, class SYNC>
+__device__ __forceinline__ void leave_item(const AttendDev &a, const Cursor<S> &cur, int tid, float (&acc)[PER], float top,
+                                           float sum, int32_t *last, int64_t total, int64_t ctas, SYNC sync)
 {
     constexpr int kRows = S::kRows, kLanes = THREADS / kRows, kWidth = PER * kLanes;
-    const int tid = threadIdx.x, jr = tid / kLanes, jd = tid % kLanes * PER;
+    const int jr = tid / kLanes, jd = tid % kLanes * PER;
     const int32_t row0 = cur.inner * kRows, rows = min(kRows, S::rows(a, cur.q) - row0);
 
     // an item in pieces: leave this one's, and the last to arrive joins a group's, then the groups'
@@ -149,12 +149,12 @@ __device__ __forceinline__ void leave_item(const AttendDev &a, const Cursor<S> &
         // true in the CTA that arrives last of `of`
         auto arrive = [&](int32_t *count, int32_t of) {
             __threadfence();
-            __syncthreads();
+            sync();
             if (tid == 0) {
                 *last = atomicAdd(count, 1) == of - 1;
                 if (*last) *count = 0;
             }
-            __syncthreads();
+            sync();
             __threadfence();
             return *last != 0;
         };
@@ -198,7 +198,10 @@ __device__ __forceinline__ void leave_item(const AttendDev &a, const Cursor<S> &
             uint32_t w[PER / 2];
 #pragma unroll
             for (int d = 0; d < PER / 2; ++d) w[d] = Pack<T>::two(acc[2 * d] * inv, acc[2 * d + 1] * inv);
-            if constexpr (PER == 8) *reinterpret_cast<uint4 *>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
+            if constexpr (PER == 16) {
+                reinterpret_cast<uint4 *>(dst)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+                reinterpret_cast<uint4 *>(dst)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+            } else if constexpr (PER == 8) *reinterpret_cast<uint4 *>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
             else if constexpr (PER == 4) *reinterpret_cast<uint2 *>(dst) = make_uint2(w[0], w[1]);
             else *reinterpret_cast<uint32_t *>(dst) = w[0];
         }

@@ -30,15 +30,19 @@ namespace pp {
 namespace token {
 // ROWS of an item, 64 * HALVES columns
 template <int ROWS, int HALVES> struct Layout8 {
-    static constexpr int warps = 8, threads = 32 * warps;
+    static constexpr int warps = ROWS == 8 ? 12 : 8;            // at the products; four more at the outputs
+    static constexpr int threads = 32 * (warps + 4);
     static constexpr int rows = kKeys * 64 * HALVES;            // bytes of a warp's K or V
-    static constexpr int stages = (ROWS == 16 ? 4 : 5) * (HALVES == 2 ? 1 : 2);
+    static constexpr int stages = (ROWS == 8 ? 3 : 4) * (HALVES == 2 ? 1 : 2);
     static constexpr int ring = warps * stages * 2 * rows;
     static constexpr int width = 64 * HALVES;
     static constexpr int pitch = width + 4;                     // floats of an output row in shared memory
     static constexpr int join = warps * ROWS * pitch * 4;
     static constexpr int bytes = 128 + ring + join;
     static_assert(bytes < 225 * 1024, "shared memory of a CTA");
+    // of a thread: the launch's 128 (168 for 12 warps), shared out
+    static constexpr int output_registers = ROWS == 8 ? 80 : 88, registers = ROWS == 8 ? 144 : 208;
+    static_assert(128 * output_registers + 32 * warps * registers <= threads * (ROWS == 8 ? 128 : 168), "registers of a CTA");
     using Shape = ShapeOf<ROWS, kKeys * warps>;
 };
 }  // namespace token
@@ -93,26 +97,36 @@ template <class L, int HALVES> struct Feed8 {
     static constexpr int KT = Shape::KT, per_row = 4 * HALVES, step = 32 / per_row;     // pieces of a row, rows at a time
     const AttendDev &a;
     Cursor<Shape> cur;
-    const char *from;                   // this lane's piece of slot 0's row of a step
-    int64_t v_from_k;
-    uint32_t ring, slot = 0, bytes;
+    const char *from;                   // this lane's piece of a step's rows, where the cache's first key is
+    int64_t v_from_k, stride;           // bytes; of `step` rows
+    uint32_t ring, slot = 0, dst, bytes;
     uint32_t *exps;                     // shared memory, [stages]
-    int32_t i = 0;
+    int32_t i = 0, j0;                  // tile of the part, its first key of this warp
     int64_t at0, at1;                   // keys 0 - 7 and 8 - 15, -1: not in the cache
     uint32_t scales;
-    bool more;
+    bool more, wide;                    // wide: rows have all their pieces
     __device__ __forceinline__ Feed8(const AttendDev &a_, const SchedShared &sched, uint32_t ring_, uint32_t *exps_)
-        : a(a_), cur(a_, sched), ring(ring_), exps(exps_), more(true)
+        : a(a_), cur(a_, sched), stride(step * a_.token_stride), ring(ring_), exps(exps_), more(true), wide(a_.dim == 64 * HALVES)
     {
         const int lane = threadIdx.x & 31, sub = lane / per_row, piece = lane % per_row;
+        dst = piece_at<HALVES>(sub, piece);
         bytes = piece * 16 < a.dim ? 16 : 0;
         from = static_cast<const char *>(a.c.k_cache) + sub * a.token_stride + (bytes ? piece * 16 : 0);
         v_from_k = static_cast<const char *>(a.c.v_cache) - static_cast<const char *>(a.c.k_cache);
-        look();
+        enter();
     }
-    __device__ __forceinline__ int32_t first(int32_t tile) const
+    // a part's first tile
+    __device__ __forceinline__ void enter()
     {
-        return (cur.k.lo / KT + cur.off + tile) * KT + (int32_t)(threadIdx.x >> 5) * kKeys;
+        i = 0;
+        j0 = (cur.k.lo / KT + cur.off) * KT + (int32_t)(threadIdx.x >> 5) * kKeys;
+        if (threadIdx.x < 32) {         // the item's queries, which are read when this tile's turn comes
+            const int32_t row = threadIdx.x % Shape::kRows, rows = Shape::rows(a, cur.q) - cur.inner * Shape::kRows;
+            const char *q = static_cast<const char *>(a.c.q) + 2 * item_row(a, cur, min(row, rows - 1), a.c.q_token_stride, a.c.q_head_stride);
+            const int32_t at = threadIdx.x / Shape::kRows * 128;
+            if (row < rows && at < 2 * a.dim) asm volatile("prefetch.global.L2 [%0];" ::"l"(q + at));
+        }
+        look();
     }
     __device__ __forceinline__ uint32_t scale_of(int32_t block) const
     {
@@ -124,46 +138,57 @@ template <class L, int HALVES> struct Feed8 {
     __device__ __forceinline__ void look()
     {
         const int32_t *row = a.c.block_table + (int64_t)cur.r * a.c.table_width;
-        const int32_t tile = i + (threadIdx.x & 31), j = first(tile), in_block = (1 << a.block_log) - 1;
-        const int32_t lower = tile < cur.len ? key_block(a, row, cur.k, j, 8) : -1;
+        const int32_t ahead = threadIdx.x & 31, j = j0 + ahead * KT, in_block = (1 << a.block_log) - 1;
+        const bool in = i + ahead < cur.len;
+        const int32_t lower = in ? key_block(a, row, cur.k, j, 8) : -1;
         const int32_t upper =
-            tile >= cur.len ? -1 : a.block_log > 3 && lower >= 0 && j + 8 <= cur.k.hi ? lower : key_block(a, row, cur.k, j + 8, 8);
+            !in ? -1 : a.block_log > 3 && lower >= 0 && j + 8 <= cur.k.hi ? lower : key_block(a, row, cur.k, j + 8, 8);
         const int64_t head = cur.outer * a.head_stride;
         at0 = lower < 0 ? -1 : head + lower * a.block_stride + (j & in_block) * a.token_stride;
         at1 = upper < 0 ? -1 : head + upper * a.block_stride + ((j + 8) & in_block) * a.token_stride;
         scales = scale_of(lower);
         scales |= (upper == lower ? scales : scale_of(upper)) << 16;
     }
-    // 8 rows of K and of V
-    __device__ __forceinline__ void rows8(uint32_t to, int row, int64_t at) const
+    // 8 rows of K and of V, from row `row` of the tile on
+    template <bool ALL> __device__ __forceinline__ void rows8(uint32_t to, int row, int64_t at) const
     {
-        const int lane = threadIdx.x & 31, sub = lane / per_row, piece = lane % per_row;
-        const uint32_t some = at >= 0 ? bytes : 0;
-        const char *k = from + (at >= 0 ? at : 0);
+        const uint32_t some = ALL || at >= 0 ? bytes : 0;
+        const char *k = from + (ALL || at >= 0 ? at : 0);
 #pragma unroll
         for (int x = 0; x < 8; x += step) {
-            copy16(to + piece_at<HALVES>(row + x + sub, piece), k, some);
-            copy16(to + L::rows + piece_at<HALVES>(row + x + sub, piece), k + v_from_k, some);
-            k += step * a.token_stride;
+            // row & 7 = x + sub, x = 0 or 4, so the swizzle of a line of 128 bytes changes by 4 pieces
+            const uint32_t d = to + (row + x) * 64 * HALVES + (dst ^ (x << 4));
+            if constexpr (ALL) {
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d), "l"(k) : "memory");
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d + L::rows), "l"(k + v_from_k) : "memory");
+            } else {
+                copy16(d, k, some);
+                copy16(d + L::rows, k + v_from_k, some);
+            }
+            k += stride;
         }
     }
     // asks for the next tile, into the ring's next place
     __device__ __forceinline__ void ask()
     {
         if (more) {
-            const int32_t j0 = first(i);
             const int64_t b0 = __shfl_sync(~0u, at0, i & 31), b1 = __shfl_sync(~0u, at1, i & 31);
             const uint32_t e = __shfl_sync(~0u, scales, i & 31);
             if (j0 <= cur.k.hi && j0 + kKeys - 1 >= cur.k.lo) {
                 if ((threadIdx.x & 31) == 0) exps[slot] = e;
                 const uint32_t to = ring + slot * 2 * L::rows;
-                rows8(to, 0, b0);
-                rows8(to, 8, b1);
+                if (wide && b0 >= 0 && b1 >= 0) {
+                    rows8<true>(to, 0, b0);
+                    rows8<true>(to, 8, b1);
+                } else {
+                    rows8<false>(to, 0, b0);
+                    rows8<false>(to, 8, b1);
+                }
             }
+            j0 += KT;
             if (++i == cur.len) {
-                i = 0;
                 more = cur.next(a);
-                if (more) look();
+                if (more) enter();
             } else if ((i & 31) == 0) {
                 look();
             }
@@ -211,25 +236,26 @@ __device__ __forceinline__ float query_row(const __nv_bfloat16 *, const uint4 (&
     return power_of_two(-up);
 }
 
+// A warp's part of a row's statistics; the join's place is handed over by barriers.
+template <int ROWS, int HALVES> struct Shared8 {
+    using L = Layout8<ROWS, HALVES>;
+    SchedShared sched;
+    float stat[2][L::warps][ROWS];
+    uint32_t exps[L::warps][L::stages];
+    int32_t last;
+};
+constexpr int kJoinFull = 1, kJoinFree = 2, kOutput = 3;        // named barriers
+
+// The products of a warp's keys, item after item.
 template <typename T, int ROWS, int HALVES>
-__global__ void __launch_bounds__(Layout8<ROWS, HALVES>::threads, 1) k_attend_token8(const __grid_constant__ AttendDev a)
+__device__ __forceinline__ void product_role(const AttendDev &a, Shared8<ROWS, HALVES> &sh, uint8_t *raw, uint32_t base, float *join)
 {
     using L = Layout8<ROWS, HALVES>;
     using Shape = typename L::Shape;
     constexpr int NB = ROWS / 8;                        // 8 rows each
     constexpr int KS = 4 * HALVES;                      // 16-wide steps of the head dimension
     constexpr int KT = Shape::KT;
-    extern __shared__ uint8_t raw[];
-    __shared__ SchedShared sched;
-    __shared__ float stat[2][L::warps][ROWS];
-    __shared__ uint32_t exps[L::warps][L::stages];
-    __shared__ int32_t last;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const uint32_t base = (smem_u32(raw) + 127) & ~127u;
-    float *join = reinterpret_cast<float *>(raw + (base - smem_u32(raw)) + L::ring);
-    if (!schedule<Shape>(a, sched)) return;
-    const int64_t total = sched.total, ctas = min((int64_t)gridDim.x, total);
-
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     // accumulators: keys or columns g and g + 8, rows 2 c and 2 c + 1 of 8
     const int g = lane >> 2, c = lane & 3;
     const int dim0 = 16 * HALVES * c;                   // this lane's elements of a K row and of Q
@@ -237,11 +263,12 @@ __global__ void __launch_bounds__(Layout8<ROWS, HALVES>::threads, 1) k_attend_to
     const int vrow = ((lane >> 3) & 1) * 8 + (lane & 7), vpiece = lane >> 4;
 
     const uint32_t ring = base + warp * L::stages * 2 * L::rows;
-    Feed8<L, HALVES> feed(a, sched, ring, exps[warp]);
+    Feed8<L, HALVES> feed(a, sh.sched, ring, sh.exps[warp]);
 #pragma unroll 1
     for (int x = 0; x < L::stages; ++x) feed.ask();
-    Cursor<Shape> cur(a, sched);
+    Cursor<Shape> cur(a, sh.sched);
     uint32_t slot = 0;
+    bool again = false;
     do {
         const int32_t row0 = cur.inner * ROWS, rows = min(ROWS, Shape::rows(a, cur.q) - row0);
         uint32_t qf[NB][KS][2];
@@ -285,7 +312,7 @@ __global__ void __launch_bounds__(Layout8<ROWS, HALVES>::threads, 1) k_attend_to
 #pragma unroll 1
         for (int32_t i = 0; i < cur.len; ++i) {
             const uint32_t kt = ring + slot * 2 * L::rows, vt = kt + L::rows;
-            const uint32_t *const e_at = &exps[warp][slot];
+            const uint32_t *const e_at = &sh.exps[warp][slot];
             if (++slot == L::stages) slot = 0;
             const int32_t j0 = (t0 + i) * KT + warp * kKeys;        // this warp's first key
             asm volatile("cp.async.wait_group %0;" ::"n"(L::stages - 1) : "memory");
@@ -442,7 +469,9 @@ __global__ void __launch_bounds__(Layout8<ROWS, HALVES>::threads, 1) k_attend_to
             feed.ask();                                             // into the place just read
         }
 
-        // join the warps through shared memory, where a thread then has one row's `per` columns
+        // hand over, once the last item's place has been read
+        if (again) named_sync(kJoinFree, L::threads);
+        again = true;
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
 #pragma unroll
@@ -452,38 +481,73 @@ __global__ void __launch_bounds__(Layout8<ROWS, HALVES>::threads, 1) k_attend_to
                 l[b][y] += __shfl_xor_sync(~0u, l[b][y], 8);
                 l[b][y] += __shfl_xor_sync(~0u, l[b][y], 16);
                 if (g == 0) {
-                    stat[0][warp][row] = m[b][y];
-                    stat[1][warp][row] = l[b][y];
+                    sh.stat[0][warp][row] = m[b][y];
+                    sh.stat[1][warp][row] = l[b][y];
                 }
                 float *dst = join + (warp * ROWS + row) * L::pitch + 2 * g;
 #pragma unroll
                 for (int n = 0; n < KS; ++n) *reinterpret_cast<float2 *>(dst + 16 * n) = make_float2(o[n][b][y], o[n][b][2 + y]);
             }
         }
-        __syncthreads();
-        constexpr int per = L::width * ROWS / L::threads;
-        const int jr = tid / (L::threads / ROWS), jd = tid % (L::threads / ROWS) * per;
+        named_arrive(kJoinFull, L::threads);
+    } while (cur.next(a));
+    named_sync(kJoinFree, L::threads);
+}
+
+// Joins the warps' parts of the items, and the pieces of items that other CTAs have
+// parts of, while the other warps are at the next item.
+template <typename T, int ROWS, int HALVES>
+__device__ __forceinline__ void output_role(const AttendDev &a, Shared8<ROWS, HALVES> &sh, const float *join)
+{
+    using L = Layout8<ROWS, HALVES>;
+    using Shape = typename L::Shape;
+    constexpr int per = L::width * ROWS / 128;
+    const int t = threadIdx.x & 127, jr = t / (128 / ROWS), jd = t % (128 / ROWS) * per;
+    const int64_t total = sh.sched.total, ctas = min((int64_t)gridDim.x, total);
+    Cursor<Shape> cur(a, sh.sched);
+    do {
         float acc[per], top = -INFINITY, sum = 0.f;
 #pragma unroll
         for (int d = 0; d < per; ++d) acc[d] = 0.f;
+        named_sync(kJoinFull, L::threads);
 #pragma unroll
-        for (int w = 0; w < L::warps; ++w) top = fmaxf(top, stat[0][w][jr]);
+        for (int w = 0; w < L::warps; ++w) top = fmaxf(top, sh.stat[0][w][jr]);
         const float at = top == -INFINITY ? 0.f : top;
-#pragma unroll
+#pragma unroll 4
         for (int w = 0; w < L::warps; ++w) {
-            const float f = exp2_approx(stat[0][w][jr] - at);
-            sum = fmaf(f, stat[1][w][jr], sum);
-            const float *src = join + (w * ROWS + jr) * L::pitch + jd;
+            const float f = exp2_approx(sh.stat[0][w][jr] - at);
+            sum = fmaf(f, sh.stat[1][w][jr], sum);
+            const float4 *src = reinterpret_cast<const float4 *>(join + (w * ROWS + jr) * L::pitch + jd);
 #pragma unroll
-            for (int d = 0; d < per; d += 2) {
-                const float2 y = *reinterpret_cast<const float2 *>(src + d);
+            for (int d = 0; d < per; d += 4) {
+                const float4 y = src[d / 4];
                 acc[d] = fmaf(f, y.x, acc[d]);
                 acc[d + 1] = fmaf(f, y.y, acc[d + 1]);
+                acc[d + 2] = fmaf(f, y.z, acc[d + 2]);
+                acc[d + 3] = fmaf(f, y.w, acc[d + 3]);
             }
         }
-        leave_item<T, Shape, per, L::threads>(a, cur, acc, top, sum, &last, total, ctas);
-        __syncthreads();                                // the join's memory is free again
+        named_arrive(kJoinFree, L::threads);
+        leave_item<T, Shape, per, 128>(a, cur, t, acc, top, sum, &sh.last, total, ctas, [] { named_sync(kOutput, 128); });
     } while (cur.next(a));
+}
+
+template <typename T, int ROWS, int HALVES>
+__global__ void __launch_bounds__(Layout8<ROWS, HALVES>::threads, 1) k_attend_token8(const __grid_constant__ AttendDev a)
+{
+    using L = Layout8<ROWS, HALVES>;
+    extern __shared__ uint8_t raw[];
+    __shared__ Shared8<ROWS, HALVES> shared;
+    const uint32_t base = (smem_u32(raw) + 127) & ~127u;
+    float *join = reinterpret_cast<float *>(raw + (base - smem_u32(raw)) + L::ring);
+    if (!schedule<typename L::Shape>(a, shared.sched)) return;
+    if (threadIdx.x < 32 * L::warps) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(L::registers));
+        product_role<T, ROWS, HALVES>(a, shared, raw, base, join);
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::output_registers));
+        output_role<T, ROWS, HALVES>(a, shared, join);
+    }
 }
 
 template <typename T, int ROWS, int HALVES> static cudaError_t prepare_t()
