@@ -379,7 +379,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_token(const __grid_const
             }
         }
 
-        leave_item<T, Shape, 4 * HALVES, kThreads>(a, cur, tid, acc, top, sum, &last, total, ctas, [] { __syncthreads(); });
+        leave_item<T, Shape, 4 * HALVES, kThreads, kJoinGroup>(a, cur, tid, acc, top, sum, &last, total, ctas, [] { __syncthreads(); });
         __syncthreads();                                // the join's memory is free again
     } while (cur.next(a));
 }

@@ -121,13 +121,17 @@ __device__ __forceinline__ int64_t item_row(const AttendDev &a, const Cursor<S> 
 // The end of an item, or of a CTA's part of it: leaves a piece or writes the rows.  A
 // thread (tid of THREADS, which sync() is for) has PER columns, from jd on, of row jr (a
 // row is within a warp): outputs acc not yet divided, maximum and sum.
-template <typename T, class S, int PER, int THREADS, class SYNC>
+// GROUP: pieces that are joined at a time, then their groups; 0: 8, or the square root of
+// the pieces if they are more.
+template <typename T, class S, int PER, int THREADS, int GROUP, class SYNC>
 __device__ __forceinline__ void leave_item(const AttendDev &a, const Cursor<S> &cur, int tid, float (&acc)[PER], float top,
                                            float sum, int32_t *last, int64_t total, int64_t ctas, SYNC sync)
 {
     constexpr int kRows = S::kRows, kLanes = THREADS / kRows, kWidth = PER * kLanes;
     const int jr = tid / kLanes, jd = tid % kLanes * PER;
     const int32_t row0 = cur.inner * kRows, rows = min(kRows, S::rows(a, cur.q) - row0);
+    const int lane_of_row = tid % kLanes;
+    const uint32_t row_lanes = (uint32_t)(((uint64_t)1 << kLanes) - 1) << ((tid & 31) - lane_of_row);
 
     // an item in pieces: leave this one's, and the last to arrive joins a group's, then the groups'
     bool write = true;
@@ -135,7 +139,10 @@ __device__ __forceinline__ void leave_item(const AttendDev &a, const Cursor<S> &
         const int64_t g0 = cur.g - cur.off;
         const int32_t cta0 = owner(g0, total, ctas), pieces = owner(g0 + cur.tiles - 1, total, ctas) - cta0 + 1;
         const int32_t mine = (int32_t)blockIdx.x - cta0;
-        const int32_t groups = (pieces + kJoinGroup - 1) / kJoinGroup;
+        int32_t group = GROUP ? GROUP : 8;
+        if (!GROUP && pieces > group)
+            while (group * group < pieces) ++group;
+        const int32_t groups = (pieces + group - 1) / group;
         auto put = [&](int32_t slot) {
             __syncwarp();                           // a row's lanes have read what one of them writes over
             if (jr < rows) {
@@ -161,9 +168,24 @@ __device__ __forceinline__ void leave_item(const AttendDev &a, const Cursor<S> &
         // join pieces p0, p0 + step, ...
         auto gather = [&](int32_t p0, int32_t n, int32_t step) {
             if (jr >= rows) return;
-            top = -INFINITY;
-            for (int32_t p = 0; p < n; ++p)
-                top = fmaxf(top, __ldcg(a.piece_stat + piece_slot(cta0, p0 + p * step) * 2 * kRows + jr));
+            if constexpr (GROUP != 0) {
+                top = -INFINITY;
+                for (int32_t p = 0; p < n; ++p)
+                    top = fmaxf(top, __ldcg(a.piece_stat + piece_slot(cta0, p0 + p * step) * 2 * kRows + jr));
+            }
+            auto stat = [&](int32_t p) { return a.piece_stat + piece_slot(cta0, p0 + p * step) * 2 * kRows + jr; };
+            constexpr int kOwn = GROUP ? 1 : (20 + kLanes - 1) / kLanes;    // a lane's pieces (20 * 20 are more than CTAs)
+            float own[kOwn];
+            if constexpr (GROUP == 0) {
+                // the statistics, a piece a lane, on their way together
+#pragma unroll
+                for (int x = 0; x < kOwn; ++x) own[x] = lane_of_row + x * kLanes < n ? __ldcg(stat(lane_of_row + x * kLanes)) : -INFINITY;
+                top = own[0];
+#pragma unroll
+                for (int x = 1; x < kOwn; ++x) top = fmaxf(top, own[x]);
+#pragma unroll
+                for (int o = kLanes / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(row_lanes, top, o));
+            }
             const float base = top == -INFINITY ? 0.f : top;
             sum = 0.f;
 #pragma unroll
@@ -171,8 +193,8 @@ __device__ __forceinline__ void leave_item(const AttendDev &a, const Cursor<S> &
 #pragma unroll 4
             for (int32_t p = 0; p < n; ++p) {
                 const int32_t slot = piece_slot(cta0, p0 + p * step);
-                const float f = exp2_approx(__ldcg(a.piece_stat + slot * 2 * kRows + jr) - base);
-                sum = fmaf(f, __ldcg(a.piece_stat + slot * 2 * kRows + kRows + jr), sum);
+                const float f = exp2_approx(__ldcg(stat(p)) - base);
+                sum = fmaf(f, __ldcg(stat(p) + kRows), sum);
                 float y[PER];
                 load_columns<PER>(a.piece + ((int64_t)slot * kRows + jr) * kWidth + jd, y);
 #pragma unroll
@@ -180,14 +202,14 @@ __device__ __forceinline__ void leave_item(const AttendDev &a, const Cursor<S> &
             }
         };
         put(piece_slot(cta0, mine));
-        const int32_t grp = mine / kJoinGroup, p0 = grp * kJoinGroup, n = min(kJoinGroup, pieces - p0);
+        const int32_t grp = mine / group, p0 = grp * group, n = min(group, pieces - p0);
         write = arrive(a.count + piece_slot(cta0, p0), n);
         if (write) {
             gather(p0, n, 1);
             if (groups > 1) {
                 put(piece_slot(cta0, p0));
                 write = arrive(a.count + 2 * gridDim.x + piece_slot(cta0, 0), groups);
-                if (write) gather(0, groups, kJoinGroup);
+                if (write) gather(0, groups, group);
             }
         }
     }

@@ -173,9 +173,7 @@ template <class L, int HALVES> struct Feed8 {
     {
         if (more) {
             const int64_t b0 = __shfl_sync(~0u, at0, i & 31), b1 = __shfl_sync(~0u, at1, i & 31);
-            const uint32_t e = __shfl_sync(~0u, scales, i & 31);
             if (j0 <= cur.k.hi && j0 + kKeys - 1 >= cur.k.lo) {
-                if ((threadIdx.x & 31) == 0) exps[slot] = e;
                 const uint32_t to = ring + slot * 2 * L::rows;
                 if (wide && b0 >= 0 && b1 >= 0) {
                     rows8<true>(to, 0, b0);
@@ -184,6 +182,9 @@ template <class L, int HALVES> struct Feed8 {
                     rows8<false>(to, 0, b0);
                     rows8<false>(to, 8, b1);
                 }
+                // after the copies, which need not wait for them
+                const uint32_t e = __shfl_sync(~0u, scales, i & 31);
+                if ((threadIdx.x & 31) == 0) exps[slot] = e;
             }
             j0 += KT;
             if (++i == cur.len) {
@@ -528,7 +529,7 @@ __device__ __forceinline__ void output_role(const AttendDev &a, Shared8<ROWS, HA
             }
         }
         named_arrive(kJoinFree, L::threads);
-        leave_item<T, Shape, per, 128>(a, cur, t, acc, top, sum, &sh.last, total, ctas, [] { named_sync(kOutput, 128); });
+        leave_item<T, Shape, per, 128, 0>(a, cur, t, acc, top, sum, &sh.last, total, ctas, [] { named_sync(kOutput, 128); });
     } while (cur.next(a));
 }
 
