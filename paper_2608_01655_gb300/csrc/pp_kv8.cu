@@ -19,7 +19,6 @@ __device__ __forceinline__ float scale_of(int e) { return __int_as_float((e + 12
 // ---------------------------------------------------------------------------
 struct Write8Args {
     int32_t tokens, heads, per_head, window;            // vectors of 8 elements a head; tokens of a CTA
-    uint32_t per_head_mul;                              // x / per_head is the high half of x * this for x < 2^28
     const uint4 *k, *v;
     int64_t k_token, k_head, v_token, v_head;           // strides in vectors
     const int64_t *slot;
@@ -31,14 +30,29 @@ struct Write8Args {
     int32_t *status;
 };
 
+#ifndef CT8
+#define CT8 3
+#endif
+#ifndef WB8
+#define WB8 3
+#endif
 constexpr int kWrite8Warps = 8, kWrite8Threads = 32 * kWrite8Warps;
-constexpr int kWrite8Window = 32;                       // tokens of a CTA at most
+constexpr int kWrite8Window = 32;                       // tokens of a CTA at most: a lane each
 constexpr int kWrite8Held = 8;                          // vectors that a thread keeps
+constexpr int kWrite8Long = 48;                         // tokens of a run from which the CTA takes it
 
+// bits of a 16-bit infinity
+template <typename T> constexpr uint32_t kInfinity = std::is_same<T, __nv_bfloat16>::value ? 0x7f80u : 0x7c00u;
+
+// the larger of `top` and |x| of 8 numbers, even and odd ones apart; infinities and NaN as they are
+__device__ __forceinline__ uint32_t largest(uint32_t top, const uint4 &x)
+{
+    return __vimax3_u16x2(__vimax3_u16x2(top, x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), x.z & 0x7fff7fffu, x.w & 0x7fff7fffu);
+}
 // |x| of two 16-bit numbers; where x is infinite or NaN it becomes NaN and 0 is returned
 template <typename T> __device__ __forceinline__ uint32_t sizes(uint32_t &x)
 {
-    constexpr uint32_t e = std::is_same<T, __nv_bfloat16>::value ? 0x7f80u : 0x7c00u;
+    constexpr uint32_t e = kInfinity<T>;
     uint32_t m = x & 0x7fff7fffu;
     if ((m & 0xffffu) >= e) {
         x |= 0x7fffu;
@@ -50,12 +64,20 @@ template <typename T> __device__ __forceinline__ uint32_t sizes(uint32_t &x)
     }
     return m;
 }
+template <typename T> __device__ __forceinline__ uint32_t sizes8(uint4 &x)
+{
+    const uint32_t a = sizes<T>(x.x), b = sizes<T>(x.y), c = sizes<T>(x.z), d = sizes<T>(x.w);
+    return __vmaxu2(__vmaxu2(a, b), __vmaxu2(c, d));
+}
 template <typename T> __device__ __forceinline__ float low_value(uint32_t x);
 template <> __device__ __forceinline__ float low_value<__nv_bfloat16>(uint32_t x) { return __uint_as_float(x << 16); }
 template <> __device__ __forceinline__ float low_value<__half>(uint32_t x)
 {
-    return __half2float(__ushort_as_half((unsigned short)x));
+    return __half2float(__ushort_as_half((unsigned short)(x & 0xffffu)));
 }
+template <typename T> __device__ __forceinline__ float high_value(uint32_t x);
+template <> __device__ __forceinline__ float high_value<__nv_bfloat16>(uint32_t x) { return __uint_as_float(x & 0xffff0000u); }
+template <> __device__ __forceinline__ float high_value<__half>(uint32_t x) { return low_value<__half>(x >> 16); }
 // two numbers to codes, to the nearest, beyond 448 to that, NaN to NaN
 __device__ __forceinline__ uint32_t codes2(float lo, float hi)
 {
@@ -66,8 +88,7 @@ __device__ __forceinline__ uint32_t codes2(float lo, float hi)
 template <typename T> __device__ __forceinline__ uint2 codes8(const uint4 &x, float by)
 {
     auto four = [&](uint32_t a, uint32_t b) {
-        return codes2(low_value<T>(a & 0xffffu) * by, low_value<T>(a >> 16) * by) |
-               codes2(low_value<T>(b & 0xffffu) * by, low_value<T>(b >> 16) * by) << 16;
+        return codes2(low_value<T>(a) * by, high_value<T>(a) * by) | codes2(low_value<T>(b) * by, high_value<T>(b) * by) << 16;
     };
     return make_uint2(four(x.x, x.y), four(x.z, x.w));
 }
@@ -89,154 +110,216 @@ __device__ __forceinline__ int least_exponent(float x)
     return min(max(e, kLeastExp), kMostExp);
 }
 
-// A run is the tokens of one block, which stand next to one another but for fewer than
-// 32 that are left out between two; its first token leads it.  A CTA looks for the leaders among `window`
-// tokens; a team of TEAM warps (a warp for every 16 tokens of a block) takes a run's
-// rows of one head and of K or V: their largest size, the exponent, the block's other
-// rows if that grows, the codes.  Rows up to kWrite8Held vectors a thread are read once.
-template <typename T, int TEAM>
-__global__ void __launch_bounds__(kWrite8Threads) k_kv_write8(const __grid_constant__ Write8Args a)
-{
-    __shared__ int32_t lead[kWrite8Window], past[kWrite8Window];
-    __shared__ int32_t leads;
-    __shared__ uint32_t tops[kWrite8Warps];
-    __shared__ int32_t begins[kWrite8Warps];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int32_t t0 = blockIdx.x * a.window, t1 = min(t0 + a.window, a.tokens);
-    // block of token t, -1 if it is left out
-    auto block_of = [&](int32_t t) {
-        const int64_t s = a.slot[t];
-        return s >= 0 && s < a.slots ? (int32_t)(s >> a.block_log) : -1;
-    };
-    if (warp == 0) {
-        const int32_t t = t0 + lane;
-        int32_t mine = -1, before = -1;
-        if (t < t1) {
-            if (a.slot[t] >= a.slots && blockIdx.y == 0) kv_bounds(a.status);
-            mine = block_of(t);
-            if (mine >= 0 && t > 0) before = block_of(t - 1);
-        }
-        // behind a token that is left out: the warp looks at those before it
-        for (uint32_t left = __ballot_sync(~0u, mine >= 0 && before < 0 && t > 0); left; left &= left - 1) {
-            const int src = __ffs(left) - 1;
-            const int32_t x = t0 + src - 1 - lane, b = x >= 0 ? block_of(x) : -1;
-            const uint32_t some = __ballot_sync(~0u, b >= 0);
-            const int32_t found = __shfl_sync(~0u, b, some ? __ffs(some) - 1 : 0);
-            if (lane == src && some) before = found;
-        }
-        const bool leader = mine >= 0 && before != mine;
-        const uint32_t all = __ballot_sync(~0u, leader);
-        if (leader) lead[__popc(all & ((1u << lane) - 1))] = t;
-        if (lane == 0) leads = __popc(all);
-    }
-    __syncthreads();
-    // where the runs end: at a token of another block, or with the last before 32 that are left out
-    for (int x = warp; x < leads; x += kWrite8Warps) {
-        const int32_t block = block_of(lead[x]);
-        int32_t last = lead[x];
-        for (;;) {
-            const int32_t t = last + 1 + lane, b = t < a.tokens ? block_of(t) : -1;
-            uint32_t same = __ballot_sync(~0u, b == block);
-            const uint32_t other = __ballot_sync(~0u, b >= 0 && b != block);
-            if (other) same &= (other & -other) - 1;
-            if (same) last += 32 - __clz(same);
-            if (!same || other) break;
-        }
-        if (lane == 0) past[x] = last + 1;
-    }
-    __syncthreads();
+// A run, and what a warp knows of it: lanes' places in the block of the 64 tokens from t0
+// on (-1: left out).
+struct Run8 {
+    int32_t first, count, block;                        // first token, tokens to the last one, block
+    int32_t lead, here, after;                          // first - t0; of tokens t0 + lane, t0 + 32 + lane
+};
+template <int TEAM> struct Team8 {                      // shared memory of a team
+    uint32_t top[TEAM];
+    int32_t begins[TEAM];
+};
 
-    constexpr int kThreads = 32 * TEAM, kTeams = kWrite8Warps / TEAM;
-    const int team = warp / TEAM, me = tid % kThreads;
+// A head of K or V (unit = 2 h + is_v) of a run by a team of TEAM warps: the largest size,
+// the exponent, the block's other rows if that grows, the codes.  kWrite8Held vectors a
+// thread are read once.
+template <typename T, int TEAM>
+__device__ __forceinline__ void write_unit(const Write8Args &a, const Run8 &run, int32_t unit, Team8<TEAM> *sh)
+{
+    constexpr int kThreads = 32 * TEAM;
+    const int me = threadIdx.x % kThreads, lane = me & 31, warp = me >> 5;
     auto sync = [&]() {
         if (TEAM == 1) __syncwarp();
-        else named_sync(1 + team, kThreads);
+        else __syncthreads();
     };
-    const int32_t units = leads * a.heads * 2;
-    for (int32_t u = blockIdx.y * kTeams + team; u < units; u += gridDim.y * kTeams) {
-        const int32_t x = u / (2 * a.heads), h = u / 2 % a.heads;
-        const bool is_v = u & 1;
-        const int32_t first = lead[x], block = block_of(first), count = (past[x] - first) * a.per_head;
-        const uint4 *src = is_v ? a.v + h * a.v_head : a.k + h * a.k_head;
-        const int64_t token = is_v ? a.v_token : a.k_token;
-        uint8_t *dst = (is_v ? a.vc : a.kc) + block * a.block_stride + h * a.head_stride;
-        int8_t *exponent = (is_v ? a.ve : a.ke) + (int64_t)block * a.heads + h;
-        const int old = min(max((int)*exponent, kLeastExp), kMostExp);
-        auto in_run = [&](int32_t l) { return (int32_t)__umulhi(l, a.per_head_mul); };
-        auto in_head = [&](int32_t l) { return l - in_run(l) * a.per_head; };
-        // vector l of the run: its token, its place in the block (-1: left out)
-        auto place = [&](int32_t l, int32_t &t) {
-            t = first + in_run(l);
-            const int64_t s = a.slot[t];
-            return s >= 0 && s < a.slots ? (int32_t)(s & ((1 << a.block_log) - 1)) : -1;
-        };
-        uint4 held[kWrite8Held];
-        int32_t row[kWrite8Held];
-        uint32_t top = 0;
-        bool begins_block = false;
+    const bool is_v = unit & 1;
+    const int32_t h = unit >> 1;
+    // a lane has vector `col` of a row of every step's `some` rows a warp
+    const int some = 32 / a.per_head, sub = lane / a.per_head, col = lane - sub * a.per_head;
+    const int32_t step = TEAM * some, ahead = warp * some + sub, past = sub < some ? run.count : 0;     // past: no row from here on
+    const int64_t token = is_v ? a.v_token : a.k_token;
+    const uint4 *src = (is_v ? a.v + h * a.v_head : a.k + h * a.k_head) + run.first * token + col;
+    uint8_t *dst = (is_v ? a.vc : a.kc) + run.block * a.block_stride + h * a.head_stride;
+    int8_t *exponent = (is_v ? a.ve : a.ke) + (int64_t)run.block * a.heads + h;
+    // place in the block of token n of the run (-1: left out)
+    auto load_place = [&](int32_t n) {
+        const int64_t s = a.slot[run.first + n];
+        return s >= 0 && s < a.slots ? (int32_t)(s & ((1 << a.block_log) - 1)) : -1;
+    };
+    auto place = [&](int32_t n) {                       // the warp's lanes together
+        if (TEAM > 1) return n < past ? load_place(n) : -1;
+        const int32_t at = run.lead + n, x = __shfl_sync(~0u, run.here, at & 31), y = __shfl_sync(~0u, run.after, at & 31);
+        return n >= past ? -1 : at < 32 ? x : at < 64 ? y : load_place(n);
+    };
+    // rows that are left out are loaded and not used, so that no load waits for a slot
+    uint4 held[kWrite8Held];
+    int32_t row[kWrite8Held];
+    const int old = min(max((int)*exponent, kLeastExp), kMostExp);
 #pragma unroll
-        for (int y = 0; y < kWrite8Held; ++y) {
-            const int32_t l = me + y * kThreads;
-            int32_t t;
-            row[y] = l < count ? place(l, t) : -1;
-            if (row[y] >= 0) held[y] = src[t * token + in_head(l)];
+    for (int y = 0; y < kWrite8Held; ++y) {
+        row[y] = -1;
+        if (y * step < run.count) {                     // not only this lane's rows
+            const int32_t n = ahead + y * step;
+            held[y] = n < past ? __ldg(src + n * token) : make_uint4(0, 0, 0, 0);
+            row[y] = place(n);
         }
+    }
+    const int32_t rest = ahead + kWrite8Held * step;    // rows that are read again
+    uint32_t top = 0;
+    bool begins = false;
 #pragma unroll
-        for (int y = 0; y < kWrite8Held; ++y) {
-            if (row[y] < 0) continue;
-            begins_block |= row[y] == 0;
-            top = __vmaxu2(top, __vmaxu2(__vmaxu2(sizes<T>(held[y].x), sizes<T>(held[y].y)),
-                                         __vmaxu2(sizes<T>(held[y].z), sizes<T>(held[y].w))));
+    for (int y = 0; y < kWrite8Held; ++y)
+        if (y * step < run.count) {
+            begins |= row[y] == 0;
+            if (row[y] >= 0) top = largest(top, held[y]);
         }
-        for (int32_t l = me + kWrite8Held * kThreads; l < count; l += kThreads) {
-            int32_t t;
-            const int32_t at = place(l, t);
-            if (at < 0) continue;
-            begins_block |= at == 0;
-            uint4 y = src[t * token + in_head(l)];
-            top = __vmaxu2(top, __vmaxu2(__vmaxu2(sizes<T>(y.x), sizes<T>(y.y)), __vmaxu2(sizes<T>(y.z), sizes<T>(y.w))));
-        }
-        top = __reduce_max_sync(~0u, max(top & 0xffffu, top >> 16));
-        begins_block = __any_sync(~0u, begins_block);
+    for (int32_t n = rest; n < past; n += step) {
+        const int32_t at = load_place(n);
+        begins |= at == 0;
+        if (at >= 0) top = largest(top, __ldg(src + n * token));
+    }
+    begins = __any_sync(~0u, begins);
+    if (TEAM > 1 && lane == 0) sh->begins[warp] = begins;
+    // the largest of the team's
+    auto all_of = [&](uint32_t mine) {
+        mine = __reduce_max_sync(~0u, max(mine & 0xffffu, mine >> 16));
         if (TEAM > 1) {
-            if (lane == 0) {
-                tops[warp] = top;
-                begins[warp] = begins_block;
-            }
+            if (lane == 0) sh->top[warp] = mine;
             sync();
 #pragma unroll
-            for (int w = 0; w < TEAM; ++w) {
-                top = max(top, tops[team * TEAM + w]);
-                begins_block |= begins[team * TEAM + w] != 0;
-            }
+            for (int w = 0; w < TEAM; ++w) mine = max(mine, sh->top[w]);
         }
-        const int need = least_exponent(low_value<T>(top)), e = begins_block ? need : max(old, need);
-        if (!begins_block && e > old) {
-            // the rows that the block has go to the new scale; those of this call are written over them
-            const float by = scale_of(old - e);
-            const int32_t pieces = a.per_head / 2;      // of 16 codes
-            for (int32_t l = me; l < pieces << a.block_log; l += kThreads) {
-                uint4 *p = reinterpret_cast<uint4 *>(dst + l / pieces * a.token_stride) + l % pieces;
-                const uint4 y = *p;
-                *p = make_uint4(rescale4(y.x, by), rescale4(y.y, by), rescale4(y.z, by), rescale4(y.w, by));
-            }
-        }
-        sync();                                         // all have read the exponent, and old rows are done
-        if (me == 0) *exponent = (int8_t)e;
-        const float by = scale_of(-e);
+        return mine;
+    };
+    top = all_of(top);
+    if (TEAM > 1)
+#pragma unroll
+        for (int w = 0; w < TEAM; ++w) begins |= sh->begins[w] != 0;
+    const bool strange = top >= kInfinity<T>;           // the same in all the team
+    if (strange) {                                      // the largest finite one; the others become NaN
+        sync();                                         // all have read the first ones
+        top = 0;
 #pragma unroll
         for (int y = 0; y < kWrite8Held; ++y)
-            if (row[y] >= 0)
-                reinterpret_cast<uint2 *>(dst + row[y] * a.token_stride)[in_head(me + y * kThreads)] = codes8<T>(held[y], by);
-        for (int32_t l = me + kWrite8Held * kThreads; l < count; l += kThreads) {
-            int32_t t;
-            const int32_t at = place(l, t);
-            if (at < 0) continue;
-            uint4 y = src[t * token + in_head(l)];
-            sizes<T>(y.x), sizes<T>(y.y), sizes<T>(y.z), sizes<T>(y.w);
-            reinterpret_cast<uint2 *>(dst + at * a.token_stride)[in_head(l)] = codes8<T>(y, by);
+            if (row[y] >= 0) top = __vmaxu2(top, sizes8<T>(held[y]));
+        for (int32_t n = rest; n < past; n += step) {
+            uint4 x = __ldg(src + n * token);
+            if (load_place(n) >= 0) top = __vmaxu2(top, sizes8<T>(x));
         }
-        if (TEAM > 1) sync();                           // tops and begins are free again
+        top = all_of(top);
+    }
+    const int need = least_exponent(low_value<T>(top)), e = begins ? need : max(old, need);
+    if (!begins && e > old) {
+        // the rows that the block has go to the new scale; those of this call are written over them
+        const float by = scale_of(old - e);
+        const int32_t pieces = a.per_head / 2;          // of 16 codes
+        for (int32_t l = me; l < pieces << a.block_log; l += kThreads) {
+            uint4 *p = reinterpret_cast<uint4 *>(dst + l / pieces * a.token_stride) + l % pieces;
+            const uint4 x = *p;
+            *p = make_uint4(rescale4(x.x, by), rescale4(x.y, by), rescale4(x.z, by), rescale4(x.w, by));
+        }
+    }
+    sync();                                             // all have read the exponent, and old rows are done
+    if (me == 0) *exponent = (int8_t)e;
+    const float by = scale_of(-e);
+    dst += 8 * col;
+#pragma unroll
+    for (int y = 0; y < kWrite8Held; ++y)
+        if (y * step < run.count && row[y] >= 0) *reinterpret_cast<uint2 *>(dst + row[y] * a.token_stride) = codes8<T>(held[y], by);
+    for (int32_t n = rest; n < past; n += step) {
+        const int32_t at = load_place(n);
+        if (at < 0) continue;
+        uint4 x = __ldg(src + n * token);
+        if (strange) sizes8<T>(x);
+        *reinterpret_cast<uint2 *>(dst + at * a.token_stride) = codes8<T>(x, by);
+    }
+    if (TEAM > 1) sync();                               // the team's shared memory is free again
+}
+
+// A run is the tokens of one block, which stand next to one another but for fewer than
+// 32 that are left out between two; its first token leads it.  Every warp of a CTA finds
+// the leaders among `window` tokens by itself, from their slots and those of 32 tokens to
+// either side.  A warp takes a run's rows of one head and of K or V; of long runs (blocks
+// that have them: LONG) the CTA does.
+template <typename T, bool LONG>
+__global__ void __launch_bounds__(kWrite8Threads, WB8) k_kv_write8(const __grid_constant__ Write8Args a)
+{
+    __shared__ Team8<kWrite8Warps> team;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int32_t t0 = blockIdx.x * a.window, t1 = min(t0 + a.window, a.tokens);
+    // block of token t, -1 if it is left out or no token
+    auto block_of = [&](int32_t t) {
+        const int64_t s = t >= 0 && t < a.tokens ? a.slot[t] : -1;
+        return s >= 0 && s < a.slots ? (int32_t)(s >> a.block_log) : -1;
+    };
+    auto place_of = [&](int32_t t, int32_t block) { return block < 0 ? -1 : (int32_t)(a.slot[t] & ((1 << a.block_log) - 1)); };
+    const int32_t before = block_of(t0 - 32 + lane), here = block_of(t0 + lane), after = block_of(t0 + 32 + lane);
+    const int32_t place_here = place_of(t0 + lane, here), place_after = place_of(t0 + 32 + lane, after);
+    if (warp == 0 && blockIdx.y == 0 && t0 + lane < t1 && a.slot[t0 + lane] >= a.slots) kv_bounds(a.status);
+    // tokens that are not left out: 64 from t0 - 32 on, and 64 from t0 on
+    const uint32_t known_before = __ballot_sync(~0u, before >= 0), known = __ballot_sync(~0u, here >= 0);
+    const uint32_t known_after = __ballot_sync(~0u, after >= 0);
+    // the nearest of the 32 before this lane's token, and its block
+    const uint64_t back = (((uint64_t)known << 32 | known_before) >> lane) & 0xffffffffu;     // bit 31: the one before
+    const int nearest = 31 - __clz((uint32_t)back) + lane;                                  // counted from t0 - 32
+    const int32_t block_before = __shfl_sync(~0u, before, nearest & 31), block_here = __shfl_sync(~0u, here, nearest & 31);
+    const bool leads = here >= 0 && ((uint32_t)back == 0 || (nearest < 32 ? block_before : block_here) != here);
+    const uint32_t leaders = __ballot_sync(~0u, leads), later = leaders & ~1u << lane;
+    // a run that another one follows here ends with the last token before that
+    const int32_t counted = later ? 31 - __clz(known & (later & -later) - 1) - lane + 1 : 0;
+
+    // the tokens of the run that lane f's token leads, counted from that: all before one of another block, or before 32 left out
+    auto run_of = [&](int f, int32_t block) {
+        const uint64_t same = (uint64_t)__ballot_sync(~0u, after == block) << 32 | __ballot_sync(~0u, here == block);
+        const uint64_t valid = (uint64_t)known_after << 32 | known, from = ~0ull << f;
+        uint64_t none = ~valid & from;                  // then: bits that begin 32 left out
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) none &= none >> o;
+        const uint64_t ends = (valid & ~same & from) | none;
+        const uint64_t mine = same & from & (ends ? (ends & -ends) - 1 : ~0ull);
+        int32_t last = 63 - __clzll(mine);
+        if (!ends && t0 + 64 < a.tokens) {              // it may go on: 128 tokens at a time
+            last += t0;
+            for (bool more = true; more;) {
+                int32_t b[4];
+                const int32_t at = last + 1;
+#pragma unroll
+                for (int y = 0; y < 4; ++y) b[y] = block_of(at + 32 * y + lane);
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    if (!more) continue;
+                    uint32_t good = __ballot_sync(~0u, b[y] == block);
+                    const uint32_t other = __ballot_sync(~0u, b[y] >= 0 && b[y] != block);
+                    if (other) good &= (other & -other) - 1;
+                    if (good) last = at + 32 * y + 31 - __clz(good);
+                    // 32 left out, or more to come than this can tell: the next look is from `last` on
+                    if (other || !good) more = false;
+                    else if (good != ~0u) break;
+                }
+            }
+            last -= t0;
+        }
+        return last - f + 1;
+    };
+
+    // the warps of this CTA, and of those of the same tokens, share the units of all runs out
+    const int32_t all = 2 * a.heads, workers = gridDim.y * kWrite8Warps;
+    int32_t next = blockIdx.y * kWrite8Warps + warp;    // this warp's next unit, counted from the run's first
+    for (uint32_t left = leaders & (uint32_t)((1ull << (t1 - t0)) - 1); left; left &= left - 1) {
+        const int lead = __ffs(left) - 1;
+        const int32_t block = __shfl_sync(~0u, here, lead), count = __shfl_sync(~0u, counted, lead);
+        if (!LONG && next >= all) {                     // none of this run
+            next -= all;
+            continue;
+        }
+        const Run8 run = {t0 + lead, count ? count : run_of(lead, block), block, lead, place_here, place_after};
+        if (LONG && run.count > kWrite8Long) {
+            for (int32_t u = blockIdx.y; u < all; u += gridDim.y) write_unit<T, kWrite8Warps>(a, run, u, &team);
+            continue;
+        }
+        for (; next < all; next += workers) write_unit<T, 1>(a, run, next, nullptr);
+        next -= all;
     }
 }
 
@@ -430,7 +513,6 @@ extern "C" pp_status pp_kv_write8(pp_kv *kv, int32_t tokens, const void *k, int6
     a.tokens = tokens;
     a.heads = kv->heads;
     a.per_head = kv->dim / 8;
-    a.per_head_mul = (uint32_t)((((uint64_t)1 << 32) + a.per_head - 1) / a.per_head);   // per_head <= 16: off by less than 16 / 2^32
     a.k = static_cast<const uint4 *>(k);
     a.v = static_cast<const uint4 *>(v);
     a.k_token = k_token_stride / 8;
@@ -448,21 +530,17 @@ extern "C" pp_status pp_kv_write8(pp_kv *kv, int32_t tokens, const void *k, int6
     a.slots = (int64_t)kv->blocks << kv->block_log;
     a.block_log = kv->block_log;
     a.status = kv->d_status;
-    // two CTAs an SM; where there are fewer tokens than that, more CTAs for their heads
-    const int32_t ctas = 2 * kv->sm_count;
+    // With few tokens a CTA has fewer of them, and more CTAs share their heads out.
+    const int32_t ctas = CT8 * kv->sm_count, block = kv->block_size;
     a.window = std::min(std::max((tokens + ctas - 1) / ctas, 1), kWrite8Window);
     const int32_t windows = (tokens - 1) / a.window + 1;
-    const int team = std::min(std::max(kv->block_size / 16, 1), kWrite8Warps), teams = kWrite8Warps / team;
-    const int32_t rounds = (2 * kv->heads + teams - 1) / teams;
-    const dim3 grid(windows, std::min(std::max(ctas / windows, 1), rounds));
+    const bool has_long = block > kWrite8Long;
+    const int32_t useful = has_long ? 2 * kv->heads : (2 * kv->heads + kWrite8Warps - 1) / kWrite8Warps;
+    const dim3 grid(windows, std::min(std::max((has_long ? 4 : 1) * ctas / windows, 1), useful));
     const cudaStream_t st = (cudaStream_t)stream;
-    auto launch = [&](auto *with1, auto *with2, auto *with4, auto *with8) {
-        (team == 1 ? with1 : team == 2 ? with2 : team == 4 ? with4 : with8)<<<grid, kWrite8Threads, 0, st>>>(a);
-    };
-    if (kv->dtype == PP_KV_BF16)
-        launch(k_kv_write8<__nv_bfloat16, 1>, k_kv_write8<__nv_bfloat16, 2>, k_kv_write8<__nv_bfloat16, 4>, k_kv_write8<__nv_bfloat16, 8>);
-    else
-        launch(k_kv_write8<__half, 1>, k_kv_write8<__half, 2>, k_kv_write8<__half, 4>, k_kv_write8<__half, 8>);
+    auto launch = [&](auto *shorts, auto *longs) { (has_long ? longs : shorts)<<<grid, kWrite8Threads, 0, st>>>(a); };
+    if (kv->dtype == PP_KV_BF16) launch(k_kv_write8<__nv_bfloat16, false>, k_kv_write8<__nv_bfloat16, true>);
+    else launch(k_kv_write8<__half, false>, k_kv_write8<__half, true>);
     PP_CUDA(cudaGetLastError());
     return PP_OK;
 }

@@ -39,8 +39,13 @@ struct RotateArgs {
 
 enum { kHalf = 0, kInterleaved = 1, kHalfOdd = 2 };     // kHalf: R / 2 is a multiple of 8
 
-constexpr int kRotateThreads = 256;
-constexpr int kRotateRows = 2;                          // rows of a group on their way
+#ifndef RT
+#define RT 128
+#define RD 6
+#define RB 5
+#endif
+constexpr int kRotateThreads = RT;
+constexpr int kRotateAhead = RD;                        // rows of a group on their way
 
 template <typename T> __device__ __forceinline__ float2 floats(uint32_t x);
 template <> __device__ __forceinline__ float2 floats<__nv_bfloat16>(uint32_t x)
@@ -79,33 +84,79 @@ __device__ __forceinline__ void angle(int32_t position, uint64_t turns, float am
 
 // A group of LANES lanes takes a token, or with `split` a share of its rows; a lane two
 // vectors of 8 elements of each row, in half layout those of 8 pairs, so that a pair is
-// one lane's and a lane's angles serve all its rows.  Bound by memory: 4 bytes an
-// element.
-template <typename T, int LAYOUT, int LANES>
-__global__ void __launch_bounds__(kRotateThreads) k_kv_rotate(const __grid_constant__ RotateArgs a)
+// one lane's and a lane's angles serve all its rows.  The norm's weights are multiplied
+// into them once a token, and a row by its norm in the end:
+//   y_a' = n (x_a (w_a cos) - x_b (w_b sin)),  y_b' = n (x_b (w_b cos) + x_a (w_a sin)).
+// Bound by memory, 4 bytes an element: each lane copies its vectors of the next rows to
+// places of its own in shared memory, so that many are on their way without registers.
+template <typename T, int LAYOUT, int LANES, bool NORM>
+__global__ void __launch_bounds__(kRotateThreads, RB) k_kv_rotate(const __grid_constant__ RotateArgs a)
 {
+    __shared__ uint4 ahead[kRotateAhead][2][kRotateThreads];
     const int lane = threadIdx.x % LANES;
     const int64_t group = (int64_t)blockIdx.x * (kRotateThreads / LANES) + threadIdx.x / LANES;
     const int32_t t = (int32_t)min(group / a.split, (int64_t)a.tokens - 1), share = (int32_t)(group % a.split);
     const bool in = group < (int64_t)a.tokens * a.split;
 
-    // this lane's vectors, per_head: none
+    // this lane's vectors, from per_head on: none
     const int32_t turned = LAYOUT == kHalf ? a.rotated / 16 : 0;        // lanes with vectors of pairs
+    const bool first_half = LAYOUT == kHalf && lane < turned;
     int32_t at[2];
-    if (LAYOUT == kHalf && lane < turned) {
-        at[0] = lane;
-        at[1] = lane + turned;
-    } else if (LAYOUT == kHalf) {
-        at[0] = 2 * turned + 2 * (lane - turned);
-        at[1] = at[0] + 1;
+    if (LAYOUT == kHalf) {
+        at[0] = first_half ? lane : 2 * lane;
+        at[1] = first_half ? lane + turned : 2 * lane + 1;
     } else {
         at[0] = lane;
         at[1] = lane + LANES;
     }
     const bool has[2] = {at[0] < a.per_head, at[1] < a.per_head};
 
-    // the angles: of pair i in half layout, of vector x's pair i - 4 x interleaved, of
-    // element i otherwise
+    int64_t cache = -1;                                 // the token's place in the caches
+    if (a.slot && in) {
+        const int64_t s = a.slot[t];
+        if (s >= a.slots) {
+            if (share == 0 && lane == 0) kv_bounds(a.status);
+        } else if (s >= 0) {
+            cache = (s >> a.block_log) * a.block_stride + (s & ((1 << a.block_log) - 1)) * a.token_stride;
+        }
+    }
+
+    // The rows: share, share + split, ... of q (kind 0), of k (1), of v (2).  Every group of a warp takes the same
+    // number of steps of each kind, with rows or without.
+    const int32_t kinds = a.slot ? 3 : 2;
+    int32_t ask_kind = 0, ask_head = share;
+    int ask_place = 0;
+    auto ask = [&]() {
+        while (ask_kind < kinds && ask_head - share >= a.heads[min(ask_kind, 1)]) {
+            ++ask_kind;
+            ask_head = share;
+        }
+        if (ask_kind < kinds) {
+            const bool is_v = ask_kind == 2;
+            const RotateRows &r = a.rows[min(ask_kind, 1)];
+            const uint4 *src = is_v ? a.v + t * a.v_token + ask_head * a.v_head : r.in + t * r.in_token + ask_head * r.in_head;
+            if (in && ask_head < a.heads[min(ask_kind, 1)] && !(is_v && cache < 0)) {
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+                    if (has[x])
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(&ahead[ask_place][x][threadIdx.x])),
+                                     "l"(src + at[x])
+                                     : "memory");
+            }
+            ask_head += a.split;
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        if (++ask_place == kRotateAhead) ask_place = 0;
+    };
+#pragma unroll
+    for (int x = 0; x < 2; ++x)                         // vectors that a row does not have count as zeros
+        if (!has[x])
+#pragma unroll
+            for (int y = 0; y < kRotateAhead; ++y) ahead[y][x][threadIdx.x] = make_uint4(0, 0, 0, 0);
+#pragma unroll 1
+    for (int x = 0; x < kRotateAhead; ++x) ask();
+
+    // cos and sin: of pair i in half layout, of vector i / 4's pair i % 4 interleaved, of element i otherwise
     constexpr int kAngles = LAYOUT == kHalfOdd ? 16 : 8;
     float cos[kAngles], sin[kAngles];
     const int32_t position = a.position[t], pairs = a.rotated / 2;
@@ -113,7 +164,7 @@ __global__ void __launch_bounds__(kRotateThreads) k_kv_rotate(const __grid_const
     for (int i = 0; i < kAngles; ++i) {
         int32_t pair;
         if (LAYOUT == kHalf) {
-            pair = lane < turned ? 8 * lane + i : pairs;
+            pair = first_half ? 8 * lane + i : pairs;
         } else if (LAYOUT == kInterleaved) {
             pair = 4 * at[i / 4] + i % 4;
         } else {
@@ -125,113 +176,108 @@ __global__ void __launch_bounds__(kRotateThreads) k_kv_rotate(const __grid_const
         if (pair < pairs) angle(position, a.turns[pair], a.amplitude, cos[i], sin[i]);
     }
 
-    const int32_t nq = a.heads[0], nk = a.heads[1], all = nq + nk + (a.slot ? nk : 0);
-    int64_t cache = -1;                                 // the token's place in the caches
-    if (a.slot && in) {
-        const int64_t s = a.slot[t];
-        if (s >= a.slots) {
-            if (share == 0 && lane == 0) kv_bounds(a.status);
-        } else if (s >= 0) {
-            cache = (s >> a.block_log) * a.block_stride + (s & ((1 << a.block_log) - 1)) * a.token_stride;
-        }
-    }
-    uint4 weight[2][2];
-#pragma unroll
-    for (int n = 0; n < 2; ++n)
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-            weight[n][x] = a.rows[n].weight && has[x] ? __ldg(a.rows[n].weight + at[x]) : make_uint4(0, 0, 0, 0);
-
-    // every group of a warp takes the same number of steps, with rows or without
-    const int32_t steps = (all + a.split - 1) / a.split;
+    int place = 0;
 #pragma unroll 1
-    for (int32_t step = 0; step < steps; step += kRotateRows) {
-        uint4 raw[kRotateRows][2];
-        bool live[kRotateRows];
+    for (int kind = 0; kind < kinds; ++kind) {
+        const bool is_v = kind == 2;
+        const RotateRows &r = a.rows[min(kind, 1)];
+        const int32_t heads = a.heads[min(kind, 1)];
+        const bool norm = NORM && !is_v && r.weight;
+        // Of a lane's 8 pairs: what x_a and x_b count for in y_a', and in y_b'.  Where a pair does not turn cos is 1.
+        float aa[8], ab[8], bb[8], ba[8], w[16];
 #pragma unroll
-        for (int y = 0; y < kRotateRows; ++y) {
-            const int32_t row = (step + y) * a.split + share;
-            live[y] = in && step + y < steps && row < all;
-            const bool is_v = row >= nq + nk, is_k = row >= nq;
-            const RotateRows &r = a.rows[is_k];
-            const int32_t h = row - (is_v ? nq + nk : is_k ? nq : 0);
-            const uint4 *src = is_v ? a.v + t * a.v_token + h * a.v_head : r.in + t * r.in_token + h * r.in_head;
+        for (int x = 0; x < 2; ++x) {
+            if (NORM && norm && has[x]) floats8<T>(__ldg(r.weight + at[x]), w + 8 * x);
+            else
 #pragma unroll
-            for (int x = 0; x < 2; ++x) raw[y][x] = live[y] && has[x] && !(is_v && cache < 0) ? src[at[x]] : make_uint4(0, 0, 0, 0);
+                for (int i = 0; i < 8; ++i) w[8 * x + i] = 1.f;
         }
+        if (LAYOUT != kHalfOdd) {
 #pragma unroll
-        for (int y = 0; y < kRotateRows; ++y) {
-            const int32_t row = (step + y) * a.split + share;
-            const bool is_v = row >= nq + nk, is_k = row >= nq;
-            const RotateRows &r = a.rows[is_k];
-            const int32_t h = row - (is_v ? nq + nk : is_k ? nq : 0);
-            float e[16];
-            floats8<T>(raw[y][0], e);
-            floats8<T>(raw[y][1], e + 8);
-            float other[16];                            // kHalfOdd: the pairs' other elements
-            float w_other[16];
-            if (LAYOUT == kHalfOdd && live[y] && !is_v) {
-                const T *base = reinterpret_cast<const T *>(r.in + t * r.in_token + h * r.in_head);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int32_t d = 8 * at[i / 8] + i % 8, p = d < pairs ? d + pairs : d - pairs;
-                    const bool some = has[i / 8] && d < a.rotated;
-                    other[i] = some ? KvType<T>::to_float(base[p]) : 0.f;
-                    w_other[i] = some && r.weight ? KvType<T>::to_float(reinterpret_cast<const T *>(r.weight)[p]) : 1.f;
-                }
+            for (int i = 0; i < 8; ++i) {
+                const int lo = LAYOUT == kHalf ? i : 2 * i, hi = LAYOUT == kHalf ? i + 8 : 2 * i + 1;
+                aa[i] = NORM ? w[lo] * cos[i] : cos[i];
+                ab[i] = NORM ? w[hi] * sin[i] : sin[i];
+                bb[i] = NORM ? w[hi] * cos[i] : cos[i];
+                ba[i] = NORM ? w[lo] * sin[i] : sin[i];
             }
-            if (a.rows[0].weight || a.rows[1].weight) { // the lanes of a warp may have rows of both
-                float sum = 0.f;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) sum = fmaf(e[i], e[i], sum);
-#pragma unroll
-                for (int o = LANES / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
-                const float by = rsqrtf(fmaf(sum, a.inverse_dim, a.eps));
-                if (!is_v && r.weight) {
-                    float w[16];
-                    floats8<T>(weight[is_k][0], w);
-                    floats8<T>(weight[is_k][1], w + 8);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        e[i] = e[i] * by * w[i];
-                        if (LAYOUT == kHalfOdd) other[i] = other[i] * by * w_other[i];
-                    }
-                }
-            }
+        }
+#pragma unroll 1
+        for (int32_t h = share; h - share < heads; h += a.split) {
+            const bool live = in && h < heads;
+            asm volatile("cp.async.wait_group %0;" ::"n"(kRotateAhead - 1) : "memory");
+            if (LAYOUT == kHalfOdd) __syncwarp();       // the others' vectors are read too
+            const uint4 raw[2] = {ahead[place][0][threadIdx.x], ahead[place][1][threadIdx.x]};
+            uint4 packed[2] = {raw[0], raw[1]};
             if (!is_v) {
+                float e[16];
+                floats8<T>(raw[0], e);
+                floats8<T>(raw[1], e + 8);
+                float by = 1.f;
+                if (NORM) {                             // lanes of a warp differ in their rows, not in the kind
+                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) sum[i & 3] = fmaf(e[i], e[i], sum[i & 3]);
+                    float all = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+#pragma unroll
+                    for (int o = LANES / 2; o > 0; o >>= 1) all += __shfl_xor_sync(~0u, all, o);
+                    if (norm) by = rsqrtf(fmaf(all, a.inverse_dim, a.eps));
+                }
+                bool changed = true;                    // else the row's bits stay
                 if (LAYOUT == kHalf) {
-                    if (lane < turned) {
+                    if (first_half) {
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
                             const float lo = e[i], hi = e[8 + i];
-                            e[i] = lo * cos[i] - hi * sin[i];
-                            e[8 + i] = hi * cos[i] + lo * sin[i];
+                            e[i] = by * (lo * aa[i] - hi * ab[i]);
+                            e[8 + i] = by * (hi * bb[i] + lo * ba[i]);
                         }
+                    } else if (norm) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            e[i] = by * (e[i] * aa[i]);
+                            e[8 + i] = by * (e[8 + i] * bb[i]);
+                        }
+                    } else {
+                        changed = false;
                     }
                 } else if (LAYOUT == kInterleaved) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        if (4 * at[i / 4] + i % 4 >= pairs) continue;
                         const float lo = e[2 * i], hi = e[2 * i + 1];
-                        e[2 * i] = lo * cos[i] - hi * sin[i];
-                        e[2 * i + 1] = hi * cos[i] + lo * sin[i];
+                        const bool turns = 4 * at[i / 4] + i % 4 < pairs;
+                        e[2 * i] = by * (turns ? lo * aa[i] - hi * ab[i] : lo * aa[i]);
+                        e[2 * i + 1] = by * (turns ? hi * bb[i] + lo * ba[i] : hi * bb[i]);
                     }
                 } else {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        const int32_t d = 8 * at[i / 8] + i % 8;
-                        if (d < a.rotated) e[i] = e[i] * cos[i] + (d < pairs ? -other[i] : other[i]) * sin[i];
+                        const int32_t d = 8 * at[i / 8] + i % 8, p = d < pairs ? d + pairs : d - pairs;
+                        const float own = norm ? by * (e[i] * w[i]) : e[i];
+                        e[i] = own;
+                        if (has[i / 8] && d < a.rotated) {
+                            const int v = p / 8;        // the vector, at lane v % LANES
+                            const T *from = reinterpret_cast<const T *>(&ahead[place][v / LANES][threadIdx.x - lane + v % LANES]);
+                            float other = KvType<T>::to_float(from[p % 8]);
+                            if (norm) other = by * (other * KvType<T>::to_float(reinterpret_cast<const T *>(r.weight)[p]));
+                            e[i] = own * cos[i] + (d < pairs ? -other : other) * sin[i];
+                        }
                     }
                 }
+                if (changed) {
+                    packed[0] = pack8<T>(e);
+                    packed[1] = pack8<T>(e + 8);
+                }
             }
-            __syncwarp();                               // all have read a row that may be written in place
-            if (!live[y]) continue;
+            if (LAYOUT == kHalfOdd) __syncwarp();       // all have read what the next copies overwrite
+            if (++place == kRotateAhead) place = 0;
+            ask();
+            if (!live) continue;
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 if (!has[x]) continue;
-                const uint4 packed = is_v ? raw[y][x] : pack8<T>(e + 8 * x);
-                if (!is_v && r.out) r.out[t * r.out_token + h * r.out_head + at[x]] = packed;
-                if (is_k && cache >= 0) (is_v ? a.vc : a.kc)[cache + h * a.head_stride + at[x]] = packed;
+                if (!is_v && r.out) r.out[t * r.out_token + h * r.out_head + at[x]] = packed[x];
+                if (kind >= 1 && cache >= 0) (is_v ? a.vc : a.kc)[cache + h * a.head_stride + at[x]] = packed[x];
             }
         }
     }
@@ -349,27 +395,44 @@ extern "C" pp_status pp_kv_rotate(pp_kv *kv, int32_t tokens, int32_t q_heads, co
     const int layout = interleaved ? kInterleaved : rotated % 16 == 0 ? kHalf : kHalfOdd;
     const int lanes = kv->dim > 64 ? 8 : kv->dim > 32 ? 4 : kv->dim > 16 ? 2 : 1;
     const int32_t rows = q_heads + kv->heads * (caches ? 2 : 1);
-    // with few tokens several groups share a token's rows, so that there is a warp for every scheduler or so
-    const int64_t want = (int64_t)kv->sm_count * 8 * (32 / lanes);
-    a.split = (int32_t)std::min<int64_t>(std::max<int64_t>(want / tokens, 1), rows);
+    // How many groups share a token's rows: all groups take rounds of as many as the SMs hold, of rows and of the
+    // token's angles, which take as long as some kAngleRows rows.  30,011 tokens of 36 rows: 2.5 rounds of whole
+    // tokens, which are 3, or 4.9 of halves.
+    constexpr int kAngleRows = 3;
+    const int64_t held = (int64_t)kv->sm_count * RB * (kRotateThreads / lanes);
+    int64_t least = INT64_MAX;
+    for (int32_t split = 1; split <= std::min(rows, 64); ++split) {
+        auto share = [&](int64_t n) { return (n + split - 1) / split; };
+        const int64_t rounds = ((int64_t)tokens * split + held - 1) / held;
+        const int64_t cost = rounds * (share(q_heads) + share(kv->heads) * (caches ? 2 : 1) + kAngleRows);
+        if (cost < least) {
+            least = cost;
+            a.split = split;
+        }
+    }
     const int64_t groups = (int64_t)tokens * a.split, per_cta = kRotateThreads / lanes;
     const int64_t grid = (groups + per_cta - 1) / per_cta;
     if (grid > INT_MAX) return fail(PP_EINVAL, "too many tokens");
     const cudaStream_t st = (cudaStream_t)stream;
     auto launch = [&](auto type) {
         using T = decltype(type);
-        auto of = [&](auto l) {
+        auto of = [&](auto l, auto n) {
             constexpr int LAYOUT = decltype(l)::value;
+            constexpr bool NORM = decltype(n)::value;
             switch (lanes) {
-            case 1: k_kv_rotate<T, LAYOUT, 1><<<(int)grid, kRotateThreads, 0, st>>>(a); break;
-            case 2: k_kv_rotate<T, LAYOUT, 2><<<(int)grid, kRotateThreads, 0, st>>>(a); break;
-            case 4: k_kv_rotate<T, LAYOUT, 4><<<(int)grid, kRotateThreads, 0, st>>>(a); break;
-            default: k_kv_rotate<T, LAYOUT, 8><<<(int)grid, kRotateThreads, 0, st>>>(a);
+            case 1: k_kv_rotate<T, LAYOUT, 1, NORM><<<(int)grid, kRotateThreads, 0, st>>>(a); break;
+            case 2: k_kv_rotate<T, LAYOUT, 2, NORM><<<(int)grid, kRotateThreads, 0, st>>>(a); break;
+            case 4: k_kv_rotate<T, LAYOUT, 4, NORM><<<(int)grid, kRotateThreads, 0, st>>>(a); break;
+            default: k_kv_rotate<T, LAYOUT, 8, NORM><<<(int)grid, kRotateThreads, 0, st>>>(a);
             }
         };
-        if (layout == kHalf) of(std::integral_constant<int, kHalf>());
-        else if (layout == kInterleaved) of(std::integral_constant<int, kInterleaved>());
-        else of(std::integral_constant<int, kHalfOdd>());
+        auto with = [&](auto l) {
+            if (q_weight || k_weight) of(l, std::true_type());
+            else of(l, std::false_type());
+        };
+        if (layout == kHalf) with(std::integral_constant<int, kHalf>());
+        else if (layout == kInterleaved) with(std::integral_constant<int, kInterleaved>());
+        else with(std::integral_constant<int, kHalfOdd>());
     };
     if (kv->dtype == PP_KV_BF16) launch(__nv_bfloat16());
     else launch(__half());
