@@ -110,11 +110,8 @@ __device__ __forceinline__ int least_exponent(float x)
     return min(max(e, kLeastExp), kMostExp);
 }
 
-// A run, and what a warp knows of it: lanes' places in the block of the 64 tokens from t0
-// on (-1: left out).
 struct Run8 {
     int32_t first, count, block;                        // first token, tokens to the last one, block
-    int32_t lead, here, after;                          // first - t0; of tokens t0 + lane, t0 + 32 + lane
 };
 template <int TEAM> struct Team8 {                      // shared memory of a team
     uint32_t top[TEAM];
@@ -122,9 +119,9 @@ template <int TEAM> struct Team8 {                      // shared memory of a te
 };
 
 // A head of K or V (unit = 2 h + is_v) of a run by a team of TEAM warps: the largest size,
-// the exponent, the block's other rows if that grows, the codes.  kWrite8Held vectors a
-// thread are read once.
-template <typename T, int TEAM>
+// the exponent, the block's other rows if that grows, the codes.  STEPS vectors a thread
+// are read once.
+template <typename T, int TEAM, int STEPS>
 __device__ __forceinline__ void write_unit(const Write8Args &a, const Run8 &run, int32_t unit, Team8<TEAM> *sh)
 {
     constexpr int kThreads = 32 * TEAM;
@@ -143,39 +140,30 @@ __device__ __forceinline__ void write_unit(const Write8Args &a, const Run8 &run,
     uint8_t *dst = (is_v ? a.vc : a.kc) + run.block * a.block_stride + h * a.head_stride;
     int8_t *exponent = (is_v ? a.ve : a.ke) + (int64_t)run.block * a.heads + h;
     // place in the block of token n of the run (-1: left out)
-    auto load_place = [&](int32_t n) {
+    auto place = [&](int32_t n) {
         const int64_t s = a.slot[run.first + n];
         return s >= 0 && s < a.slots ? (int32_t)(s & ((1 << a.block_log) - 1)) : -1;
     };
-    auto place = [&](int32_t n) {                       // the warp's lanes together
-        if (TEAM > 1) return n < past ? load_place(n) : -1;
-        const int32_t at = run.lead + n, x = __shfl_sync(~0u, run.here, at & 31), y = __shfl_sync(~0u, run.after, at & 31);
-        return n >= past ? -1 : at < 32 ? x : at < 64 ? y : load_place(n);
-    };
     // rows that are left out are loaded and not used, so that no load waits for a slot
-    uint4 held[kWrite8Held];
-    int32_t row[kWrite8Held];
+    uint4 held[STEPS];
+    int32_t row[STEPS];
     const int old = min(max((int)*exponent, kLeastExp), kMostExp);
 #pragma unroll
-    for (int y = 0; y < kWrite8Held; ++y) {
-        row[y] = -1;
-        if (y * step < run.count) {                     // not only this lane's rows
-            const int32_t n = ahead + y * step;
-            held[y] = n < past ? __ldg(src + n * token) : make_uint4(0, 0, 0, 0);
-            row[y] = place(n);
-        }
+    for (int y = 0; y < STEPS; ++y) {
+        const int32_t n = ahead + y * step;
+        held[y] = n < past ? __ldg(src + n * token) : make_uint4(0, 0, 0, 0);
+        row[y] = n < past ? place(n) : -1;
     }
-    const int32_t rest = ahead + kWrite8Held * step;    // rows that are read again
+    const int32_t rest = ahead + STEPS * step;    // rows that are read again
     uint32_t top = 0;
     bool begins = false;
 #pragma unroll
-    for (int y = 0; y < kWrite8Held; ++y)
-        if (y * step < run.count) {
-            begins |= row[y] == 0;
-            if (row[y] >= 0) top = largest(top, held[y]);
-        }
+    for (int y = 0; y < STEPS; ++y) {
+        begins |= row[y] == 0;
+        if (row[y] >= 0) top = largest(top, held[y]);
+    }
     for (int32_t n = rest; n < past; n += step) {
-        const int32_t at = load_place(n);
+        const int32_t at = place(n);
         begins |= at == 0;
         if (at >= 0) top = largest(top, __ldg(src + n * token));
     }
@@ -201,11 +189,11 @@ __device__ __forceinline__ void write_unit(const Write8Args &a, const Run8 &run,
         sync();                                         // all have read the first ones
         top = 0;
 #pragma unroll
-        for (int y = 0; y < kWrite8Held; ++y)
+        for (int y = 0; y < STEPS; ++y)
             if (row[y] >= 0) top = __vmaxu2(top, sizes8<T>(held[y]));
         for (int32_t n = rest; n < past; n += step) {
             uint4 x = __ldg(src + n * token);
-            if (load_place(n) >= 0) top = __vmaxu2(top, sizes8<T>(x));
+            if (place(n) >= 0) top = __vmaxu2(top, sizes8<T>(x));
         }
         top = all_of(top);
     }
@@ -225,10 +213,10 @@ __device__ __forceinline__ void write_unit(const Write8Args &a, const Run8 &run,
     const float by = scale_of(-e);
     dst += 8 * col;
 #pragma unroll
-    for (int y = 0; y < kWrite8Held; ++y)
-        if (y * step < run.count && row[y] >= 0) *reinterpret_cast<uint2 *>(dst + row[y] * a.token_stride) = codes8<T>(held[y], by);
+    for (int y = 0; y < STEPS; ++y)
+        if (row[y] >= 0) *reinterpret_cast<uint2 *>(dst + row[y] * a.token_stride) = codes8<T>(held[y], by);
     for (int32_t n = rest; n < past; n += step) {
-        const int32_t at = load_place(n);
+        const int32_t at = place(n);
         if (at < 0) continue;
         uint4 x = __ldg(src + n * token);
         if (strange) sizes8<T>(x);
@@ -253,9 +241,7 @@ __global__ void __launch_bounds__(kWrite8Threads, WB8) k_kv_write8(const __grid_
         const int64_t s = t >= 0 && t < a.tokens ? a.slot[t] : -1;
         return s >= 0 && s < a.slots ? (int32_t)(s >> a.block_log) : -1;
     };
-    auto place_of = [&](int32_t t, int32_t block) { return block < 0 ? -1 : (int32_t)(a.slot[t] & ((1 << a.block_log) - 1)); };
     const int32_t before = block_of(t0 - 32 + lane), here = block_of(t0 + lane), after = block_of(t0 + 32 + lane);
-    const int32_t place_here = place_of(t0 + lane, here), place_after = place_of(t0 + 32 + lane, after);
     if (warp == 0 && blockIdx.y == 0 && t0 + lane < t1 && a.slot[t0 + lane] >= a.slots) kv_bounds(a.status);
     // tokens that are not left out: 64 from t0 - 32 on, and 64 from t0 on
     const uint32_t known_before = __ballot_sync(~0u, before >= 0), known = __ballot_sync(~0u, here >= 0);
@@ -313,12 +299,16 @@ __global__ void __launch_bounds__(kWrite8Threads, WB8) k_kv_write8(const __grid_
             next -= all;
             continue;
         }
-        const Run8 run = {t0 + lead, count ? count : run_of(lead, block), block, lead, place_here, place_after};
+        const Run8 run = {t0 + lead, count ? count : run_of(lead, block), block};
         if (LONG && run.count > kWrite8Long) {
-            for (int32_t u = blockIdx.y; u < all; u += gridDim.y) write_unit<T, kWrite8Warps>(a, run, u, &team);
+            for (int32_t u = blockIdx.y; u < all; u += gridDim.y) write_unit<T, kWrite8Warps, kWrite8Held>(a, run, u, &team);
             continue;
         }
-        for (; next < all; next += workers) write_unit<T, 1>(a, run, next, nullptr);
+        const bool few = run.count <= 2 * (32 / a.per_head);       // two steps' rows
+        for (; next < all; next += workers) {
+            if (few) write_unit<T, 1, 2>(a, run, next, nullptr);
+            else write_unit<T, 1, kWrite8Held>(a, run, next, nullptr);
+        }
         next -= all;
     }
 }

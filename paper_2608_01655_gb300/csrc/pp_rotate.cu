@@ -41,7 +41,7 @@ enum { kHalf = 0, kInterleaved = 1, kHalfOdd = 2 };     // kHalf: R / 2 is a mul
 
 #ifndef RT
 #define RT 128
-#define RD 6
+#define RD 4
 #define RB 5
 #endif
 constexpr int kRotateThreads = RT;
@@ -67,9 +67,55 @@ template <typename T> __device__ __forceinline__ void floats8(const uint4 &x, fl
         to[2 * i + 1] = y.y;
     }
 }
-template <typename T> __device__ __forceinline__ uint4 pack8(const float *x)
+// two 32-bit numbers in a register pair
+__device__ __forceinline__ uint64_t pack2(float lo, float hi)
 {
-    return make_uint4(Pack<T>::two(x[0], x[1]), Pack<T>::two(x[2], x[3]), Pack<T>::two(x[4], x[5]), Pack<T>::two(x[6], x[7]));
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float2 unpack2(uint64_t x)
+{
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+template <typename T> __device__ __forceinline__ void twos(const uint4 &x, uint64_t (&to)[4])
+{
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 y = floats<T>(w[i]);
+        to[i] = pack2(y.x, y.y);
+    }
+}
+template <typename T> __device__ __forceinline__ uint4 pack8(const uint64_t (&x)[4])
+{
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 y = unpack2(x[i]);
+        w[i] = Pack<T>::two(y.x, y.y);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // cos and sin of position * frequency.  `turns` is the frequency as a 64-bit fraction of
@@ -124,27 +170,33 @@ __global__ void __launch_bounds__(kRotateThreads, RB) k_kv_rotate(const __grid_c
     // The rows: share, share + split, ... of q (kind 0), of k (1), of v (2).  Every group of a warp takes the same
     // number of steps of each kind, with rows or without.
     const int32_t kinds = a.slot ? 3 : 2;
-    int32_t ask_kind = 0, ask_head = share;
+    const uint4 *ask_at = nullptr;                      // the next row, and from one to the next
+    int64_t ask_step = 0;
+    int32_t ask_kind = -1, ask_steps = 0, ask_rows = 0; // steps to come of this kind, those with a row of this group
     int ask_place = 0;
     auto ask = [&]() {
-        while (ask_kind < kinds && ask_head - share >= a.heads[min(ask_kind, 1)]) {
+        while (ask_steps == 0 && ask_kind < kinds - 1) {
             ++ask_kind;
-            ask_head = share;
-        }
-        if (ask_kind < kinds) {
+            const int32_t heads = a.heads[min(ask_kind, 1)];
             const bool is_v = ask_kind == 2;
             const RotateRows &r = a.rows[min(ask_kind, 1)];
-            const uint4 *src = is_v ? a.v + t * a.v_token + ask_head * a.v_head : r.in + t * r.in_token + ask_head * r.in_head;
-            if (in && ask_head < a.heads[min(ask_kind, 1)] && !(is_v && cache < 0)) {
-#pragma unroll
-                for (int x = 0; x < 2; ++x)
-                    if (has[x])
-                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(&ahead[ask_place][x][threadIdx.x])),
-                                     "l"(src + at[x])
-                                     : "memory");
-            }
-            ask_head += a.split;
+            const int64_t head = is_v ? a.v_head : r.in_head;
+            ask_at = (is_v ? a.v + t * a.v_token : r.in + t * r.in_token) + share * head;
+            ask_step = a.split * head;
+            ask_steps = (heads + a.split - 1) / a.split;
+            ask_rows = !in || (is_v && cache < 0) || heads <= share ? 0 : (heads - share + a.split - 1) / a.split;
         }
+        if (ask_rows > 0) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+                if (has[x])
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(&ahead[ask_place][x][threadIdx.x])),
+                                 "l"(ask_at + at[x])
+                                 : "memory");
+        }
+        ask_at += ask_step;
+        --ask_rows;
+        if (ask_steps > 0) --ask_steps;
         asm volatile("cp.async.commit_group;" ::: "memory");
         if (++ask_place == kRotateAhead) ask_place = 0;
     };
@@ -183,8 +235,13 @@ __global__ void __launch_bounds__(kRotateThreads, RB) k_kv_rotate(const __grid_c
         const RotateRows &r = a.rows[min(kind, 1)];
         const int32_t heads = a.heads[min(kind, 1)];
         const bool norm = NORM && !is_v && r.weight;
+        // where the next row goes, and from one to the next
+        uint4 *out = is_v || !r.out ? nullptr : r.out + t * r.out_token + share * r.out_head;
+        uint4 *stored = kind == 0 || cache < 0 ? nullptr : (is_v ? a.vc : a.kc) + cache + share * a.head_stride;
+        const int64_t out_step = a.split * r.out_head, stored_step = a.split * a.head_stride;
         // Of a lane's 8 pairs: what x_a and x_b count for in y_a', and in y_b'.  Where a pair does not turn cos is 1.
-        float aa[8], ab[8], bb[8], ba[8], w[16];
+        float w[16];
+        uint64_t aa[4], ab[4], bb[4], ba[4];            // two each
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
             if (NORM && norm && has[x]) floats8<T>(__ldg(r.weight + at[x]), w + 8 * x);
@@ -193,50 +250,68 @@ __global__ void __launch_bounds__(kRotateThreads, RB) k_kv_rotate(const __grid_c
                 for (int i = 0; i < 8; ++i) w[8 * x + i] = 1.f;
         }
         if (LAYOUT != kHalfOdd) {
+            float f[4][8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int lo = LAYOUT == kHalf ? i : 2 * i, hi = LAYOUT == kHalf ? i + 8 : 2 * i + 1;
-                aa[i] = NORM ? w[lo] * cos[i] : cos[i];
-                ab[i] = NORM ? w[hi] * sin[i] : sin[i];
-                bb[i] = NORM ? w[hi] * cos[i] : cos[i];
-                ba[i] = NORM ? w[lo] * sin[i] : sin[i];
+                f[0][i] = NORM ? w[lo] * cos[i] : cos[i];
+                f[1][i] = NORM ? w[hi] * -sin[i] : -sin[i];
+                f[2][i] = NORM ? w[hi] * cos[i] : cos[i];
+                f[3][i] = NORM ? w[lo] * sin[i] : sin[i];
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                // half layout: pairs 2 i and 2 i + 1; interleaved: of pairs 2 i, 2 i + 1 what both of a pair's are multiplied with
+                aa[i] = pack2(f[0][2 * i], f[0][2 * i + 1]);
+                ab[i] = pack2(f[1][2 * i], f[1][2 * i + 1]);
+                bb[i] = pack2(f[2][2 * i], f[2][2 * i + 1]);
+                ba[i] = pack2(f[3][2 * i], f[3][2 * i + 1]);
             }
         }
 #pragma unroll 1
-        for (int32_t h = share; h - share < heads; h += a.split) {
+        for (int32_t h = share, steps = (heads + a.split - 1) / a.split; steps > 0; --steps, h += a.split) {
             const bool live = in && h < heads;
             asm volatile("cp.async.wait_group %0;" ::"n"(kRotateAhead - 1) : "memory");
             if (LAYOUT == kHalfOdd) __syncwarp();       // the others' vectors are read too
             const uint4 raw[2] = {ahead[place][0][threadIdx.x], ahead[place][1][threadIdx.x]};
             uint4 packed[2] = {raw[0], raw[1]};
             if (!is_v) {
-                float e[16];
-                floats8<T>(raw[0], e);
-                floats8<T>(raw[1], e + 8);
+                uint64_t e[2][4];                       // two elements each
+                twos<T>(raw[0], e[0]);
+                twos<T>(raw[1], e[1]);
                 float by = 1.f;
                 if (NORM) {                             // lanes of a warp differ in their rows, not in the kind
-                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                    uint64_t sum[2] = {0, 0};
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) sum[i & 3] = fmaf(e[i], e[i], sum[i & 3]);
-                    float all = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                    for (int i = 0; i < 4; ++i) {
+                        sum[0] = fma2(e[0][i], e[0][i], sum[0]);
+                        sum[1] = fma2(e[1][i], e[1][i], sum[1]);
+                    }
+                    const float2 two = unpack2(add2(sum[0], sum[1]));
+                    float all = two.x + two.y;
 #pragma unroll
                     for (int o = LANES / 2; o > 0; o >>= 1) all += __shfl_xor_sync(~0u, all, o);
                     if (norm) by = rsqrtf(fmaf(all, a.inverse_dim, a.eps));
                 }
+                const uint64_t by2 = pack2(by, by);
                 bool changed = true;                    // else the row's bits stay
                 if (LAYOUT == kHalf) {
                     if (first_half) {
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const float lo = e[i], hi = e[8 + i];
-                            e[i] = by * (lo * aa[i] - hi * ab[i]);
-                            e[8 + i] = by * (hi * bb[i] + lo * ba[i]);
+                        for (int i = 0; i < 4; ++i) {
+                            const uint64_t lo = e[0][i], hi = e[1][i];
+                            e[0][i] = fma2(lo, aa[i], mul2(hi, ab[i]));
+                            e[1][i] = fma2(hi, bb[i], mul2(lo, ba[i]));
+                            if (NORM) {
+                                e[0][i] = mul2(e[0][i], by2);
+                                e[1][i] = mul2(e[1][i], by2);
+                            }
                         }
                     } else if (norm) {
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            e[i] = by * (e[i] * aa[i]);
-                            e[8 + i] = by * (e[8 + i] * bb[i]);
+                        for (int i = 0; i < 4; ++i) {
+                            e[0][i] = mul2(mul2(e[0][i], aa[i]), by2);
+                            e[1][i] = mul2(mul2(e[1][i], bb[i]), by2);
                         }
                     } else {
                         changed = false;
@@ -244,41 +319,49 @@ __global__ void __launch_bounds__(kRotateThreads, RB) k_kv_rotate(const __grid_c
                 } else if (LAYOUT == kInterleaved) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const float lo = e[2 * i], hi = e[2 * i + 1];
+                        const float2 x = unpack2(e[i / 4][i % 4]), fa = unpack2(aa[i / 2]), fb = unpack2(ab[i / 2]);
+                        const float2 ga = unpack2(bb[i / 2]), gb = unpack2(ba[i / 2]);
+                        const float a0 = i % 2 ? fa.y : fa.x, b0 = i % 2 ? fb.y : fb.x, a1 = i % 2 ? ga.y : ga.x, b1 = i % 2 ? gb.y : gb.x;
                         const bool turns = 4 * at[i / 4] + i % 4 < pairs;
-                        e[2 * i] = by * (turns ? lo * aa[i] - hi * ab[i] : lo * aa[i]);
-                        e[2 * i + 1] = by * (turns ? hi * bb[i] + lo * ba[i] : hi * bb[i]);
+                        const float lo = turns ? x.x * a0 + x.y * b0 : x.x * a0, hi = turns ? x.y * a1 + x.x * b1 : x.y * a1;
+                        e[i / 4][i % 4] = NORM ? mul2(pack2(lo, hi), by2) : pack2(lo, hi);
                     }
                 } else {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int32_t d = 8 * at[i / 8] + i % 8, p = d < pairs ? d + pairs : d - pairs;
-                        const float own = norm ? by * (e[i] * w[i]) : e[i];
-                        e[i] = own;
-                        if (has[i / 8] && d < a.rotated) {
-                            const int v = p / 8;        // the vector, at lane v % LANES
-                            const T *from = reinterpret_cast<const T *>(&ahead[place][v / LANES][threadIdx.x - lane + v % LANES]);
-                            float other = KvType<T>::to_float(from[p % 8]);
-                            if (norm) other = by * (other * KvType<T>::to_float(reinterpret_cast<const T *>(r.weight)[p]));
-                            e[i] = own * cos[i] + (d < pairs ? -other : other) * sin[i];
+                    for (int i = 0; i < 16; i += 2) {
+                        const float2 x = unpack2(e[i / 8][i % 8 / 2]);
+                        float y[2] = {x.x, x.y};
+#pragma unroll
+                        for (int z = 0; z < 2; ++z) {
+                            const int32_t d = 8 * at[i / 8] + i % 8 + z, p = d < pairs ? d + pairs : d - pairs;
+                            if (norm) y[z] = by * (y[z] * w[i + z]);
+                            if (has[i / 8] && d < a.rotated) {
+                                const int v = p / 8;    // the vector, at lane v % LANES
+                                const T *from = reinterpret_cast<const T *>(&ahead[place][v / LANES][threadIdx.x - lane + v % LANES]);
+                                float other = KvType<T>::to_float(from[p % 8]);
+                                if (norm) other = by * (other * KvType<T>::to_float(reinterpret_cast<const T *>(r.weight)[p]));
+                                y[z] = y[z] * cos[i + z] + (d < pairs ? -other : other) * sin[i + z];
+                            }
                         }
+                        e[i / 8][i % 8 / 2] = pack2(y[0], y[1]);
                     }
                 }
                 if (changed) {
-                    packed[0] = pack8<T>(e);
-                    packed[1] = pack8<T>(e + 8);
+                    packed[0] = pack8<T>(e[0]);
+                    packed[1] = pack8<T>(e[1]);
                 }
             }
             if (LAYOUT == kHalfOdd) __syncwarp();       // all have read what the next copies overwrite
             if (++place == kRotateAhead) place = 0;
             ask();
-            if (!live) continue;
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-                if (!has[x]) continue;
-                if (!is_v && r.out) r.out[t * r.out_token + h * r.out_head + at[x]] = packed[x];
-                if (kind >= 1 && cache >= 0) (is_v ? a.vc : a.kc)[cache + h * a.head_stride + at[x]] = packed[x];
+                if (!live || !has[x]) continue;
+                if (out) out[at[x]] = packed[x];
+                if (stored) stored[at[x]] = packed[x];
             }
+            if (out) out += out_step;
+            if (stored) stored += stored_step;
         }
     }
 }
