@@ -30,13 +30,8 @@ struct Write8Args {
     int32_t *status;
 };
 
-#ifndef CT8
-#define CT8 3
-#endif
-#ifndef WB8
-#define WB8 3
-#endif
 constexpr int kWrite8Warps = 8, kWrite8Threads = 32 * kWrite8Warps;
+constexpr int kWrite8Ctas = 3;                          // of an SM
 constexpr int kWrite8Window = 32;                       // tokens of a CTA at most: a lane each
 constexpr int kWrite8Held = 8;                          // vectors that a thread keeps
 constexpr int kWrite8Long = 48;                         // tokens of a run from which the CTA takes it
@@ -231,7 +226,7 @@ __device__ __forceinline__ void write_unit(const Write8Args &a, const Run8 &run,
 // either side.  A warp takes a run's rows of one head and of K or V; of long runs (blocks
 // that have them: LONG) the CTA does.
 template <typename T, bool LONG>
-__global__ void __launch_bounds__(kWrite8Threads, WB8) k_kv_write8(const __grid_constant__ Write8Args a)
+__global__ void __launch_bounds__(kWrite8Threads, kWrite8Ctas) k_kv_write8(const __grid_constant__ Write8Args a)
 {
     __shared__ Team8<kWrite8Warps> team;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -521,7 +516,7 @@ extern "C" pp_status pp_kv_write8(pp_kv *kv, int32_t tokens, const void *k, int6
     a.block_log = kv->block_log;
     a.status = kv->d_status;
     // With few tokens a CTA has fewer of them, and more CTAs share their heads out.
-    const int32_t ctas = CT8 * kv->sm_count, block = kv->block_size;
+    const int32_t ctas = kWrite8Ctas * kv->sm_count, block = kv->block_size;
     a.window = std::min(std::max((tokens + ctas - 1) / ctas, 1), kWrite8Window);
     const int32_t windows = (tokens - 1) / a.window + 1;
     const bool has_long = block > kWrite8Long;

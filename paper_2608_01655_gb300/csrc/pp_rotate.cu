@@ -39,13 +39,9 @@ struct RotateArgs {
 
 enum { kHalf = 0, kInterleaved = 1, kHalfOdd = 2 };     // kHalf: R / 2 is a multiple of 8
 
-#ifndef RT
-#define RT 128
-#define RD 4
-#define RB 5
-#endif
-constexpr int kRotateThreads = RT;
-constexpr int kRotateAhead = RD;                        // rows of a group on their way
+constexpr int kRotateThreads = 128;
+constexpr int kRotateAhead = 4;                         // rows of a group on their way
+constexpr int kRotateCtas = 4;                          // of an SM
 
 template <typename T> __device__ __forceinline__ float2 floats(uint32_t x);
 template <> __device__ __forceinline__ float2 floats<__nv_bfloat16>(uint32_t x)
@@ -136,21 +132,23 @@ __device__ __forceinline__ void angle(int32_t position, uint64_t turns, float am
 // Bound by memory, 4 bytes an element: each lane copies its vectors of the next rows to
 // places of its own in shared memory, so that many are on their way without registers.
 template <typename T, int LAYOUT, int LANES, bool NORM>
-__global__ void __launch_bounds__(kRotateThreads, RB) k_kv_rotate(const __grid_constant__ RotateArgs a)
+__global__ void __launch_bounds__(kRotateThreads, kRotateCtas) k_kv_rotate(const __grid_constant__ RotateArgs a)
 {
     __shared__ uint4 ahead[kRotateAhead][2][kRotateThreads];
-    const int lane = threadIdx.x % LANES;
-    const int64_t group = (int64_t)blockIdx.x * (kRotateThreads / LANES) + threadIdx.x / LANES;
+    constexpr int kGroups = 32 / LANES;                 // of a warp
+    const int lane = threadIdx.x % 32 % LANES, of_warp = threadIdx.x % 32 / LANES;
+    const int64_t group = ((int64_t)blockIdx.x * (kRotateThreads / 32) + threadIdx.x / 32) * kGroups + of_warp;
     const int32_t t = (int32_t)min(group / a.split, (int64_t)a.tokens - 1), share = (int32_t)(group % a.split);
-    const bool in = group < (int64_t)a.tokens * a.split;
+    const bool in = of_warp < kGroups && group < (int64_t)a.tokens * a.split;
 
     // this lane's vectors, from per_head on: none
     const int32_t turned = LAYOUT == kHalf ? a.rotated / 16 : 0;        // lanes with vectors of pairs
     const bool first_half = LAYOUT == kHalf && lane < turned;
     int32_t at[2];
-    if (LAYOUT == kHalf) {
-        at[0] = first_half ? lane : 2 * lane;
-        at[1] = first_half ? lane + turned : 2 * lane + 1;
+    if (LAYOUT == kHalf) {                              // the other lanes' in two stretches
+        const int32_t others = (a.per_head - 2 * turned + 1) / 2;
+        at[0] = lane < turned + others ? lane + (first_half ? 0 : turned) : a.per_head;
+        at[1] = lane < turned + others ? at[0] + (first_half ? turned : others) : a.per_head;
     } else {
         at[0] = lane;
         at[1] = lane + LANES;
@@ -167,36 +165,36 @@ __global__ void __launch_bounds__(kRotateThreads, RB) k_kv_rotate(const __grid_c
         }
     }
 
-    // The rows: share, share + split, ... of q (kind 0), of k (1), of v (2).  Every group of a warp takes the same
-    // number of steps of each kind, with rows or without.
-    const int32_t kinds = a.slot ? 3 : 2;
+    // The rows: share, share + split, ... of those of q (kind 0), then of k (1), then of v (2).  Every group of a warp
+    // takes the same number of steps.
+    const int32_t nq = a.heads[0], nk = a.heads[1], all = nq + nk * (a.slot ? 2 : 1);
+    auto first_of = [&](int kind) { return kind == 0 ? 0 : kind == 1 ? nq : nq + nk; };
+    auto past = [&](int kind) { return kind == 0 ? nq : kind == 1 ? nq + nk : all; };
     const uint4 *ask_at = nullptr;                      // the next row, and from one to the next
     int64_t ask_step = 0;
-    int32_t ask_kind = -1, ask_steps = 0, ask_rows = 0; // steps to come of this kind, those with a row of this group
+    int32_t ask_row = share, ask_past = 0;              // its number, and where that of the next kind begins
     int ask_place = 0;
     auto ask = [&]() {
-        while (ask_steps == 0 && ask_kind < kinds - 1) {
-            ++ask_kind;
-            const int32_t heads = a.heads[min(ask_kind, 1)];
-            const bool is_v = ask_kind == 2;
-            const RotateRows &r = a.rows[min(ask_kind, 1)];
-            const int64_t head = is_v ? a.v_head : r.in_head;
-            ask_at = (is_v ? a.v + t * a.v_token : r.in + t * r.in_token) + share * head;
-            ask_step = a.split * head;
-            ask_steps = (heads + a.split - 1) / a.split;
-            ask_rows = !in || (is_v && cache < 0) || heads <= share ? 0 : (heads - share + a.split - 1) / a.split;
-        }
-        if (ask_rows > 0) {
+        if (in && ask_row < all) {
+            if (ask_row >= ask_past) {
+                const int kind = ask_row < nq ? 0 : ask_row < nq + nk ? 1 : 2;
+                const RotateRows &r = a.rows[min(kind, 1)];
+                const int64_t head = kind == 2 ? a.v_head : r.in_head;
+                ask_at = (kind == 2 ? a.v + t * a.v_token : r.in + t * r.in_token) + (ask_row - first_of(kind)) * head;
+                ask_step = a.split * head;
+                ask_past = past(kind);
+                if (kind == 2 && cache < 0) ask_row = all;
+            }
+            if (ask_row < all)
 #pragma unroll
-            for (int x = 0; x < 2; ++x)
-                if (has[x])
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(&ahead[ask_place][x][threadIdx.x])),
-                                 "l"(ask_at + at[x])
-                                 : "memory");
+                for (int x = 0; x < 2; ++x)
+                    if (has[x])
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(&ahead[ask_place][x][threadIdx.x])),
+                                     "l"(ask_at + at[x])
+                                     : "memory");
+            ask_at += ask_step;
+            ask_row += a.split;
         }
-        ask_at += ask_step;
-        --ask_rows;
-        if (ask_steps > 0) --ask_steps;
         asm volatile("cp.async.commit_group;" ::: "memory");
         if (++ask_place == kRotateAhead) ask_place = 0;
     };
@@ -228,141 +226,162 @@ __global__ void __launch_bounds__(kRotateThreads, RB) k_kv_rotate(const __grid_c
         if (pair < pairs) angle(position, a.turns[pair], a.amplitude, cos[i], sin[i]);
     }
 
-    int place = 0;
-#pragma unroll 1
-    for (int kind = 0; kind < kinds; ++kind) {
-        const bool is_v = kind == 2;
+    // Of a lane's 8 pairs: what x_a and x_b count for in y_a', and in y_b', two pairs each.  Where a pair does not turn
+    // cos is 1.
+    uint64_t aa[4], ab[4], bb[4], ba[4];
+    float w[LAYOUT == kHalfOdd ? 16 : 1];
+    const uint4 *weight = nullptr;                      // of the rows at hand
+    uint4 *out = nullptr, *stored = nullptr;            // where the next one goes
+    int64_t out_step = 0, stored_step = 0;
+    int32_t row = share, row_past = 0;
+    bool is_v = false;
+    auto enter = [&]() {                                // rows of another kind
+        const int kind = row < nq ? 0 : row < nq + nk ? 1 : 2;
         const RotateRows &r = a.rows[min(kind, 1)];
-        const int32_t heads = a.heads[min(kind, 1)];
-        const bool norm = NORM && !is_v && r.weight;
-        // where the next row goes, and from one to the next
-        uint4 *out = is_v || !r.out ? nullptr : r.out + t * r.out_token + share * r.out_head;
-        uint4 *stored = kind == 0 || cache < 0 ? nullptr : (is_v ? a.vc : a.kc) + cache + share * a.head_stride;
-        const int64_t out_step = a.split * r.out_head, stored_step = a.split * a.head_stride;
-        // Of a lane's 8 pairs: what x_a and x_b count for in y_a', and in y_b'.  Where a pair does not turn cos is 1.
-        float w[16];
-        uint64_t aa[4], ab[4], bb[4], ba[4];            // two each
+        const int32_t h = row - first_of(kind);
+        row_past = past(kind);
+        is_v = kind == 2;
+        out = is_v || !r.out ? nullptr : r.out + t * r.out_token + h * r.out_head;
+        stored = kind == 0 || cache < 0 ? nullptr : (is_v ? a.vc : a.kc) + cache + h * a.head_stride;
+        out_step = a.split * r.out_head;
+        stored_step = a.split * a.head_stride;
+        if (is_v) return;
+        weight = NORM ? r.weight : nullptr;
+        float u[16];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-            if (NORM && norm && has[x]) floats8<T>(__ldg(r.weight + at[x]), w + 8 * x);
+            if (NORM && weight && has[x]) floats8<T>(__ldg(weight + at[x]), u + 8 * x);
             else
 #pragma unroll
-                for (int i = 0; i < 8; ++i) w[8 * x + i] = 1.f;
+                for (int i = 0; i < 8; ++i) u[8 * x + i] = 1.f;
         }
-        if (LAYOUT != kHalfOdd) {
+        if constexpr (LAYOUT == kHalfOdd) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) w[i] = u[i];
+        } else {
             float f[4][8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int lo = LAYOUT == kHalf ? i : 2 * i, hi = LAYOUT == kHalf ? i + 8 : 2 * i + 1;
-                f[0][i] = NORM ? w[lo] * cos[i] : cos[i];
-                f[1][i] = NORM ? w[hi] * -sin[i] : -sin[i];
-                f[2][i] = NORM ? w[hi] * cos[i] : cos[i];
-                f[3][i] = NORM ? w[lo] * sin[i] : sin[i];
+                f[0][i] = NORM ? u[lo] * cos[i] : cos[i];
+                f[1][i] = NORM ? u[hi] * -sin[i] : -sin[i];
+                f[2][i] = NORM ? u[hi] * cos[i] : cos[i];
+                f[3][i] = NORM ? u[lo] * sin[i] : sin[i];
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                // half layout: pairs 2 i and 2 i + 1; interleaved: of pairs 2 i, 2 i + 1 what both of a pair's are multiplied with
                 aa[i] = pack2(f[0][2 * i], f[0][2 * i + 1]);
                 ab[i] = pack2(f[1][2 * i], f[1][2 * i + 1]);
                 bb[i] = pack2(f[2][2 * i], f[2][2 * i + 1]);
                 ba[i] = pack2(f[3][2 * i], f[3][2 * i + 1]);
             }
         }
+    };
+    int place = 0;
 #pragma unroll 1
-        for (int32_t h = share, steps = (heads + a.split - 1) / a.split; steps > 0; --steps, h += a.split) {
-            const bool live = in && h < heads;
-            asm volatile("cp.async.wait_group %0;" ::"n"(kRotateAhead - 1) : "memory");
-            if (LAYOUT == kHalfOdd) __syncwarp();       // the others' vectors are read too
-            const uint4 raw[2] = {ahead[place][0][threadIdx.x], ahead[place][1][threadIdx.x]};
-            uint4 packed[2] = {raw[0], raw[1]};
-            if (!is_v) {
-                uint64_t e[2][4];                       // two elements each
-                twos<T>(raw[0], e[0]);
-                twos<T>(raw[1], e[1]);
-                float by = 1.f;
-                if (NORM) {                             // lanes of a warp differ in their rows, not in the kind
-                    uint64_t sum[2] = {0, 0};
+    for (int32_t steps = (all + a.split - 1) / a.split; steps > 0; --steps, row += a.split) {
+        const bool live = in && row < all;
+        if (live && row >= row_past) enter();
+        asm volatile("cp.async.wait_group %0;" ::"n"(kRotateAhead - 1) : "memory");
+        if (LAYOUT == kHalfOdd) __syncwarp();           // the others' vectors are read too
+        const uint4 raw[2] = {ahead[place][0][threadIdx.x], ahead[place][1][threadIdx.x]};
+        uint4 packed[2] = {raw[0], raw[1]};
+        uint64_t e[2][4];                               // two elements each
+        twos<T>(raw[0], e[0]);
+        twos<T>(raw[1], e[1]);
+        const bool norm = NORM && weight;
+        float by = 1.f;
+        if (NORM) {
+            uint64_t sum[2] = {0, 0};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                sum[0] = fma2(e[0][i], e[0][i], sum[0]);
+                sum[1] = fma2(e[1][i], e[1][i], sum[1]);
+            }
+            const float2 two = unpack2(add2(sum[0], sum[1]));
+            const float mine = two.x + two.y;
+            float total = mine;
+            if constexpr ((LANES & (LANES - 1)) == 0) {
+#pragma unroll
+                for (int o = LANES / 2; o > 0; o >>= 1) total += __shfl_xor_sync(~0u, total, o);
+            } else {
+                // in the same order for all lanes
+                total = 0.f;
+#pragma unroll
+                for (int o = 0; o < LANES; ++o) total += __shfl_sync(~0u, mine, min(of_warp * LANES + o, 31));
+            }
+            if (norm) by = rsqrtf(fmaf(total, a.inverse_dim, a.eps));
+        }
+        const uint64_t by2 = pack2(by, by);
+        if (!is_v) {
+            bool changed = true;                        // else the row's bits stay
+            if (LAYOUT == kHalf) {
+                if (first_half) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        sum[0] = fma2(e[0][i], e[0][i], sum[0]);
-                        sum[1] = fma2(e[1][i], e[1][i], sum[1]);
-                    }
-                    const float2 two = unpack2(add2(sum[0], sum[1]));
-                    float all = two.x + two.y;
-#pragma unroll
-                    for (int o = LANES / 2; o > 0; o >>= 1) all += __shfl_xor_sync(~0u, all, o);
-                    if (norm) by = rsqrtf(fmaf(all, a.inverse_dim, a.eps));
-                }
-                const uint64_t by2 = pack2(by, by);
-                bool changed = true;                    // else the row's bits stay
-                if (LAYOUT == kHalf) {
-                    if (first_half) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const uint64_t lo = e[0][i], hi = e[1][i];
-                            e[0][i] = fma2(lo, aa[i], mul2(hi, ab[i]));
-                            e[1][i] = fma2(hi, bb[i], mul2(lo, ba[i]));
-                            if (NORM) {
-                                e[0][i] = mul2(e[0][i], by2);
-                                e[1][i] = mul2(e[1][i], by2);
-                            }
+                        const uint64_t lo = e[0][i], hi = e[1][i];
+                        e[0][i] = fma2(lo, aa[i], mul2(hi, ab[i]));
+                        e[1][i] = fma2(hi, bb[i], mul2(lo, ba[i]));
+                        if (NORM) {
+                            e[0][i] = mul2(e[0][i], by2);
+                            e[1][i] = mul2(e[1][i], by2);
                         }
-                    } else if (norm) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            e[0][i] = mul2(mul2(e[0][i], aa[i]), by2);
-                            e[1][i] = mul2(mul2(e[1][i], bb[i]), by2);
-                        }
-                    } else {
-                        changed = false;
                     }
-                } else if (LAYOUT == kInterleaved) {
+                } else if (norm) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float2 x = unpack2(e[i / 4][i % 4]), fa = unpack2(aa[i / 2]), fb = unpack2(ab[i / 2]);
-                        const float2 ga = unpack2(bb[i / 2]), gb = unpack2(ba[i / 2]);
-                        const float a0 = i % 2 ? fa.y : fa.x, b0 = i % 2 ? fb.y : fb.x, a1 = i % 2 ? ga.y : ga.x, b1 = i % 2 ? gb.y : gb.x;
-                        const bool turns = 4 * at[i / 4] + i % 4 < pairs;
-                        const float lo = turns ? x.x * a0 + x.y * b0 : x.x * a0, hi = turns ? x.y * a1 + x.x * b1 : x.y * a1;
-                        e[i / 4][i % 4] = NORM ? mul2(pack2(lo, hi), by2) : pack2(lo, hi);
+                    for (int i = 0; i < 4; ++i) {
+                        e[0][i] = mul2(mul2(e[0][i], aa[i]), by2);
+                        e[1][i] = mul2(mul2(e[1][i], bb[i]), by2);
                     }
                 } else {
+                    changed = false;
+                }
+            } else if (LAYOUT == kInterleaved) {
 #pragma unroll
-                    for (int i = 0; i < 16; i += 2) {
-                        const float2 x = unpack2(e[i / 8][i % 8 / 2]);
-                        float y[2] = {x.x, x.y};
+                for (int i = 0; i < 8; ++i) {
+                    const float2 x = unpack2(e[i / 4][i % 4]), fa = unpack2(aa[i / 2]), fb = unpack2(ab[i / 2]);
+                    const float2 ga = unpack2(bb[i / 2]), gb = unpack2(ba[i / 2]);
+                    const float a0 = i % 2 ? fa.y : fa.x, b0 = i % 2 ? fb.y : fb.x, a1 = i % 2 ? ga.y : ga.x, b1 = i % 2 ? gb.y : gb.x;
+                    const bool turns = 4 * at[i / 4] + i % 4 < pairs;
+                    const float lo = turns ? x.x * a0 + x.y * b0 : x.x * a0, hi = turns ? x.y * a1 + x.x * b1 : x.y * a1;
+                    e[i / 4][i % 4] = NORM ? mul2(pack2(lo, hi), by2) : pack2(lo, hi);
+                }
+            } else if constexpr (LAYOUT == kHalfOdd) {
 #pragma unroll
-                        for (int z = 0; z < 2; ++z) {
-                            const int32_t d = 8 * at[i / 8] + i % 8 + z, p = d < pairs ? d + pairs : d - pairs;
-                            if (norm) y[z] = by * (y[z] * w[i + z]);
-                            if (has[i / 8] && d < a.rotated) {
-                                const int v = p / 8;    // the vector, at lane v % LANES
-                                const T *from = reinterpret_cast<const T *>(&ahead[place][v / LANES][threadIdx.x - lane + v % LANES]);
-                                float other = KvType<T>::to_float(from[p % 8]);
-                                if (norm) other = by * (other * KvType<T>::to_float(reinterpret_cast<const T *>(r.weight)[p]));
-                                y[z] = y[z] * cos[i + z] + (d < pairs ? -other : other) * sin[i + z];
-                            }
+                for (int i = 0; i < 16; i += 2) {
+                    const float2 x = unpack2(e[i / 8][i % 8 / 2]);
+                    float y[2] = {x.x, x.y};
+#pragma unroll
+                    for (int z = 0; z < 2; ++z) {
+                        const int32_t d = 8 * at[i / 8] + i % 8 + z, p = d < pairs ? d + pairs : d - pairs;
+                        if (norm) y[z] = by * (y[z] * w[i + z]);
+                        if (has[i / 8] && d < a.rotated) {
+                            const int v = p / 8;        // the vector, at lane v % LANES
+                            const T *from = reinterpret_cast<const T *>(&ahead[place][v / LANES][threadIdx.x - lane + v % LANES]);
+                            float other = KvType<T>::to_float(from[p % 8]);
+                            if (norm) other = by * (other * KvType<T>::to_float(reinterpret_cast<const T *>(weight)[p]));
+                            y[z] = y[z] * cos[i + z] + (d < pairs ? -other : other) * sin[i + z];
                         }
-                        e[i / 8][i % 8 / 2] = pack2(y[0], y[1]);
                     }
-                }
-                if (changed) {
-                    packed[0] = pack8<T>(e[0]);
-                    packed[1] = pack8<T>(e[1]);
+                    e[i / 8][i % 8 / 2] = pack2(y[0], y[1]);
                 }
             }
-            if (LAYOUT == kHalfOdd) __syncwarp();       // all have read what the next copies overwrite
-            if (++place == kRotateAhead) place = 0;
-            ask();
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                if (!live || !has[x]) continue;
-                if (out) out[at[x]] = packed[x];
-                if (stored) stored[at[x]] = packed[x];
+            if (changed) {
+                packed[0] = pack8<T>(e[0]);
+                packed[1] = pack8<T>(e[1]);
             }
-            if (out) out += out_step;
-            if (stored) stored += stored_step;
         }
+        if (LAYOUT == kHalfOdd) __syncwarp();           // all have read what the next copies overwrite
+        if (++place == kRotateAhead) place = 0;
+        ask();
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            if (!live || !has[x]) continue;
+            if (out) out[at[x]] = packed[x];
+            if (stored) stored[at[x]] = packed[x];
+        }
+        if (out) out += out_step;
+        if (stored) stored += stored_step;
     }
 }
 
@@ -476,25 +495,23 @@ extern "C" pp_status pp_kv_rotate(pp_kv *kv, int32_t tokens, int32_t q_heads, co
     }
     a.status = kv->d_status;
     const int layout = interleaved ? kInterleaved : rotated % 16 == 0 ? kHalf : kHalfOdd;
-    const int lanes = kv->dim > 64 ? 8 : kv->dim > 32 ? 4 : kv->dim > 16 ? 2 : 1;
+    const int lanes = kv->dim > 96 ? 8 : kv->dim > 80 ? 6 : kv->dim > 64 ? 5 : kv->dim > 32 ? 4 : kv->dim > 16 ? 2 : 1;
     const int32_t rows = q_heads + kv->heads * (caches ? 2 : 1);
     // How many groups share a token's rows: all groups take rounds of as many as the SMs hold, of rows and of the
-    // token's angles, which take as long as some kAngleRows rows.  30,011 tokens of 36 rows: 2.5 rounds of whole
-    // tokens, which are 3, or 4.9 of halves.
+    // token's angles, which take as long as some kAngleRows rows.  30,011 tokens of 36 rows: 3.1 rounds of whole
+    // tokens, which are 4 of 39 rows, or 6.2 of halves, 7 of 21.
     constexpr int kAngleRows = 3;
-    const int64_t held = (int64_t)kv->sm_count * RB * (kRotateThreads / lanes);
+    const int64_t per_cta = kRotateThreads / 32 * (32 / lanes), held = (int64_t)kv->sm_count * kRotateCtas * per_cta;
     int64_t least = INT64_MAX;
     for (int32_t split = 1; split <= std::min(rows, 64); ++split) {
-        auto share = [&](int64_t n) { return (n + split - 1) / split; };
         const int64_t rounds = ((int64_t)tokens * split + held - 1) / held;
-        const int64_t cost = rounds * (share(q_heads) + share(kv->heads) * (caches ? 2 : 1) + kAngleRows);
+        const int64_t cost = rounds * ((rows + split - 1) / split + kAngleRows);
         if (cost < least) {
             least = cost;
             a.split = split;
         }
     }
-    const int64_t groups = (int64_t)tokens * a.split, per_cta = kRotateThreads / lanes;
-    const int64_t grid = (groups + per_cta - 1) / per_cta;
+    const int64_t grid = ((int64_t)tokens * a.split + per_cta - 1) / per_cta;
     if (grid > INT_MAX) return fail(PP_EINVAL, "too many tokens");
     const cudaStream_t st = (cudaStream_t)stream;
     auto launch = [&](auto type) {
@@ -506,6 +523,8 @@ extern "C" pp_status pp_kv_rotate(pp_kv *kv, int32_t tokens, int32_t q_heads, co
             case 1: k_kv_rotate<T, LAYOUT, 1, NORM><<<(int)grid, kRotateThreads, 0, st>>>(a); break;
             case 2: k_kv_rotate<T, LAYOUT, 2, NORM><<<(int)grid, kRotateThreads, 0, st>>>(a); break;
             case 4: k_kv_rotate<T, LAYOUT, 4, NORM><<<(int)grid, kRotateThreads, 0, st>>>(a); break;
+            case 5: k_kv_rotate<T, LAYOUT, 5, NORM><<<(int)grid, kRotateThreads, 0, st>>>(a); break;
+            case 6: k_kv_rotate<T, LAYOUT, 6, NORM><<<(int)grid, kRotateThreads, 0, st>>>(a); break;
             default: k_kv_rotate<T, LAYOUT, 8, NORM><<<(int)grid, kRotateThreads, 0, st>>>(a);
             }
         };
