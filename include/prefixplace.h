@@ -732,7 +732,7 @@ pp_status pp_kv_workspace(const pp_kv *kv, int32_t requests, int32_t table_width
  * pp_paged_attention8 -- pp_paged_attention over a cache of 8-bit numbers, with the
  * same formula and arguments and
  *   k_exp, v_exp  device [blocks][kv_heads]
- *   workspace     device, aligned to 16 bytes, pp_kv_workspace bytes or more.  Not
+ *   workspace     device, aligned to 32 bytes, pp_kv_workspace bytes or more.  Not
  *                 looked at where max_q * (q_heads / kv_heads) <= 32
  * Calls of few rows (that limit) read codes and exponents directly: products of codes
  * with queries of 11 significant bits (bf16's 8 fit) and 32-bit sums, weights rounded

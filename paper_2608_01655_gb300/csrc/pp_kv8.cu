@@ -321,11 +321,12 @@ struct Unpack8Args {
 
 constexpr int kUnpackThreads = 512;
 
+// two codes (the low half) times `by`, as two 16-bit numbers
 template <typename T> __device__ __forceinline__ uint32_t wide2(uint32_t codes, float by)
 {
-    uint32_t h;
+    uint32_t h, r;
     asm("{\n.reg .b16 lo, hi;\nmov.b32 {lo, hi}, %1;\ncvt.rn.f16x2.e4m3x2 %0, lo;\n}" : "=r"(h) : "r"(codes));
-    uint32_t r = Pack<T>::two(low_value<__half>(h & 0xffffu) * by, low_value<__half>(h >> 16) * by);
+    r = Pack<T>::two(low_value<__half>(h) * by, high_value<__half>(h) * by);
     if constexpr (std::is_same<T, __half>::value) {     // what f16 does not reach becomes its largest
         __half2 x;
         memcpy(&x, &r, 4);
@@ -337,8 +338,11 @@ template <typename T> __device__ __forceinline__ uint32_t wide2(uint32_t codes, 
 }
 template <typename T> __device__ __forceinline__ void unpack16(uint4 *to, const uint4 &x, float by)
 {
-    to[0] = make_uint4(wide2<T>(x.x, by), wide2<T>(x.x >> 16, by), wide2<T>(x.y, by), wide2<T>(x.y >> 16, by));
-    to[1] = make_uint4(wide2<T>(x.z, by), wide2<T>(x.z >> 16, by), wide2<T>(x.w, by), wide2<T>(x.w >> 16, by));
+    // a whole sector
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(wide2<T>(x.x, by)),
+                 "r"(wide2<T>(x.x >> 16, by)), "r"(wide2<T>(x.y, by)), "r"(wide2<T>(x.y >> 16, by)), "r"(wide2<T>(x.z, by)),
+                 "r"(wide2<T>(x.z >> 16, by)), "r"(wide2<T>(x.w, by)), "r"(wide2<T>(x.w >> 16, by))
+                 : "memory");
 }
 
 // Blocks that a request's queries see: [lo, hi], none if hi < lo.
@@ -349,15 +353,17 @@ __device__ __forceinline__ Keys seen_blocks(const AttendDev &a, const Req &q)
 }
 
 // Every CTA sums up the requests' visible blocks (8 bytes a request, from L2 after the
-// first) and a warp takes a block and head at a time, numbered through all requests.
-// A block that several requests see is unpacked for each.  Bound by memory: a byte
-// read and two written, which the attention then reads, mostly from L2.
-template <typename T> __global__ void __launch_bounds__(kUnpackThreads) k_unpack8(const __grid_constant__ Unpack8Args u)
+// first) and a warp takes up to 16 rows of a block and head at a time, numbered through
+// all requests; a lane has one piece of 16 codes of every few rows.  A block that several
+// requests see is unpacked for each.  Bound by memory: a byte read and two written, which
+// the attention then reads, mostly from L2.
+template <typename T> __global__ void __launch_bounds__(kUnpackThreads, 2) k_unpack8(const __grid_constant__ Unpack8Args u)
 {
-    extern __shared__ int32_t pre[];                    // blocks before request r
+    extern __shared__ int32_t pre[];                    // blocks before request r, then its first
     __shared__ int64_t warp_sum[32];
     const AttendDev &a = u.a;
     const int tid = threadIdx.x, lane = tid & 31;
+    int32_t *const low = pre + a.c.requests;
     const int32_t R = a.c.requests, per = (R + kUnpackThreads - 1) / kUnpackThreads;
     const int32_t first = min(tid * per, R), past = min(first + per, R);
     int64_t mine = 0, excl;
@@ -371,15 +377,20 @@ template <typename T> __global__ void __launch_bounds__(kUnpackThreads) k_unpack
     for (int32_t r = first; r < past; ++r) {
         const Keys k = seen_blocks(a, load_req(a, r, false));
         pre[r] = (int32_t)min(excl, (int64_t)INT_MAX);
+        low[r] = k.lo;
         excl += k.hi - k.lo + 1;
     }
     __syncthreads();
 
-    const int32_t warps = gridDim.x * (kUnpackThreads / 32), bs = 1 << a.block_log;
-    const int32_t pieces = a.dim / 16, count = pieces << a.block_log;   // 16 codes each, of a head's rows
-    const int64_t units = (int64_t)total * a.kv_heads;
+    const int32_t warps = gridDim.x * (kUnpackThreads / 32), rows_log = min(a.block_log, 4);
+    const int32_t parts_log = a.block_log - rows_log;   // of a block
+    const int32_t pieces = a.dim / 16, some = 32 / pieces;              // a row's, rows at a time
+    const int32_t sub = lane / pieces, piece = lane - sub * pieces;
+    const int64_t units = (int64_t)total * a.kv_heads << parts_log;
     for (int64_t n = blockIdx.x * (kUnpackThreads / 32) + (tid >> 5); n < units; n += warps) {
-        const int32_t x = (int32_t)quotient(n, a.kv_heads), h = (int32_t)(n - (int64_t)x * a.kv_heads);
+        const int64_t of_block = n >> parts_log;
+        const int32_t x = (int32_t)quotient(of_block, a.kv_heads), h = (int32_t)(of_block - (int64_t)x * a.kv_heads);
+        const int32_t row0 = (int32_t)(n & ((1 << parts_log) - 1)) << rows_log;
         int32_t r = 0;                                  // the last request that begins at x or before
         for (int32_t len = R; len > 1;) {
             const int32_t half = len >> 1;
@@ -390,23 +401,33 @@ template <typename T> __global__ void __launch_bounds__(kUnpackThreads) k_unpack
                 len = half;
             }
         }
-        const int32_t j = seen_blocks(a, load_req(a, r, false)).lo + x - pre[r];
+        const int32_t j = low[r] + x - pre[r];
         const int64_t entry = (int64_t)r * a.c.table_width + j;
         const int32_t id = a.c.block_table[entry];
         const bool ok = id >= 0 && id < a.blocks;
-        if (h == 0 && lane == 0) u.table[entry] = ok ? x : -1;
+        if (h == 0 && row0 == 0 && lane == 0) u.table[entry] = ok ? x : -1;
         if (!ok) continue;
-        const int64_t from = id * a.block_stride + h * a.head_stride, at = (int64_t)id * a.kv_heads + h;
+        const int64_t from = id * a.block_stride + h * a.head_stride + piece * 16, at = (int64_t)id * a.kv_heads + h;
         const uint8_t *k = static_cast<const uint8_t *>(a.c.k_cache) + from, *v = static_cast<const uint8_t *>(a.c.v_cache) + from;
         const float kb = scale_of(min(max((int)a.c.k_exp[at], kLeastExp), kMostExp));
         const float vb = scale_of(min(max((int)a.c.v_exp[at], kLeastExp), kMostExp));
-        const int64_t to = n * bs * (a.dim / 8);
-#pragma unroll 4
-        for (int32_t l = lane; l < count; l += 32) {
-            const int64_t in = l / pieces * a.token_stride + l % pieces * 16;
-            const uint4 y = *reinterpret_cast<const uint4 *>(k + in), z = *reinterpret_cast<const uint4 *>(v + in);
-            unpack16<T>(u.k + to + 2 * l, y, kb);
-            unpack16<T>(u.v + to + 2 * l, z, vb);
+        const int64_t to = (of_block << a.block_log) * (2 * pieces) + 2 * piece;
+        uint4 y[4], z[4];                               // 16 rows of 8 pieces are four steps
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int32_t row = i * some + sub;
+            if (sub < some && row < 1 << rows_log) {
+                y[i] = *reinterpret_cast<const uint4 *>(k + (row0 + row) * a.token_stride);
+                z[i] = *reinterpret_cast<const uint4 *>(v + (row0 + row) * a.token_stride);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int32_t row = i * some + sub;
+            if (sub < some && row < 1 << rows_log) {
+                unpack16<T>(u.k + to + (row0 + row) * (2 * pieces), y[i], kb);
+                unpack16<T>(u.v + to + (row0 + row) * (2 * pieces), z[i], vb);
+            }
         }
     }
     // blocks that have no place
@@ -420,7 +441,7 @@ template <typename T> __global__ void __launch_bounds__(kUnpackThreads) k_unpack
 
 pp_status prepare_kv8()
 {
-    const int most = (int)sizeof(int32_t) * kKvMaxRequests;
+    const int most = 2 * (int)sizeof(int32_t) * kKvMaxRequests;
     PP_CUDA(cudaFuncSetAttribute(k_unpack8<__nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize, most));
     PP_CUDA(cudaFuncSetAttribute(k_unpack8<__half>, cudaFuncAttributeMaxDynamicSharedMemorySize, most));
     return prepare_attend_token8();
@@ -438,7 +459,7 @@ static pp_status launch_attend8(pp_kv *kv, AttendArgs c, void *workspace, int64_
 {
     if ((int64_t)c.max_q * c.group <= kFewRows8) return launch_attend_token8(kv, c, st);
     if (!workspace) return fail(PP_EINVAL, "chunks need a workspace of pp_kv_workspace bytes");
-    if (!aligned16(workspace)) return fail(PP_EINVAL, "workspace must be aligned to 16 bytes");
+    if (reinterpret_cast<uintptr_t>(workspace) & 31) return fail(PP_EINVAL, "workspace must be aligned to 32 bytes");
     const int64_t head = table_bytes(c.requests, c.table_width);
     const int64_t capacity = std::min<int64_t>((bytes - head) / (2 * block_bytes(kv)), kKvMaxBlocks);
     if (bytes < head || capacity < 1) return fail(PP_EINVAL, "the workspace is too small: see pp_kv_workspace");
@@ -449,7 +470,7 @@ static pp_status launch_attend8(pp_kv *kv, AttendArgs c, void *workspace, int64_
     u.k = reinterpret_cast<uint4 *>(at + head);
     u.v = reinterpret_cast<uint4 *>(at + head + capacity * block_bytes(kv));
     u.capacity = (int32_t)capacity;
-    const size_t shared = sizeof(int32_t) * c.requests;
+    const size_t shared = 2 * sizeof(int32_t) * c.requests;
     if (kv->dtype == PP_KV_BF16) k_unpack8<__nv_bfloat16><<<2 * kv->sm_count, kUnpackThreads, shared, st>>>(u);
     else k_unpack8<__half><<<2 * kv->sm_count, kUnpackThreads, shared, st>>>(u);
     PP_CUDA(cudaGetLastError());
