@@ -733,7 +733,7 @@ pp_status pp_kv_workspace(const pp_kv *kv, int32_t requests, int32_t table_width
  * same formula and arguments and
  *   k_exp, v_exp  device [blocks][kv_heads]
  *   workspace     device, aligned to 32 bytes, pp_kv_workspace bytes or more.  Not
- *                 looked at where max_q * (q_heads / kv_heads) <= 32
+ *                 looked at where max_q * (q_heads / kv_heads) <= 48
  * Calls of few rows (that limit) read codes and exponents directly: products of codes
  * with queries of 11 significant bits (bf16's 8 fit) and 32-bit sums, weights rounded
  * to 11 bits for their product with V.  Calls of chunks unpack what the queries see

@@ -675,7 +675,7 @@ def pp_paged_attention8(kv: KVCache, q, k_cache, k_exp, v_cache, v_exp, block_ta
                         scale: float, window: int = 0, lse=None, workspace=None, stream=None):
     """pp_paged_attention over a cache of 8-bit numbers with exponents k_exp, v_exp [blocks][kv_heads] int8.
     workspace: a contiguous uint8 tensor of kv.workspace_size(...) bytes, for calls with
-    max_q * (q_heads / kv_heads) > 32."""
+    max_q * (q_heads / kv_heads) > 48."""
     _eight(kv)
     t, heads, r, width, i32 = q.shape[0], q.shape[1], length.shape[0], block_table.shape[-1], kv._i32
     exps = (kv.shape[0], kv.shape[2])

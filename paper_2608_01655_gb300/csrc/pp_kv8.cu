@@ -452,8 +452,14 @@ static int64_t table_bytes(int32_t requests, int32_t width) { return ((int64_t)r
 static int64_t block_bytes(const pp_kv *kv) { return (int64_t)2 * kv->heads * kv->block_size * kv->dim; }
 
 // Rows (new tokens x heads of a group) of the longest request up to which a call goes
-// to the kernel of single tokens.
-constexpr int64_t kFewRows8 = 32;
+// to the kernel of single tokens.  That one reads codes once for every 16 rows; chunks'
+// are unpacked, which costs 15 us and more, and take 256 rows whatever there are.  In us,
+// 2 K/V heads of 128, single passes after a flush of L2, 32 requests after 5,000 tokens /
+// 4 after 2,000 / 1 after 50,000 (64 rows here by items of 16):
+//   32 rows   68 : 104 / 25 : 43 / 35 : 74
+//   64       123 : 104 / 23 : 43 / 47 : 74
+// In between the batch's times meet at some 52.
+constexpr int64_t kFewRows8 = 48;
 
 static pp_status launch_attend8(pp_kv *kv, AttendArgs c, void *workspace, int64_t bytes, cudaStream_t st)
 {

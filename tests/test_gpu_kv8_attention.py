@@ -71,7 +71,7 @@ def _case(pp, fresh, cached, heads, kv_heads, dim, dtype=BF, block=16, window=0,
     scale = dim ** -0.5 if scale is None else scale
     table_t = _i32(table)
     max_q = max(fresh + [0]) if max_q is None else max_q
-    direct = max_q * (heads // kv_heads) <= 32
+    direct = max_q * (heads // kv_heads) <= 48
     with pp.KVCache.like(code[0], dtype=dtype) as kv:
         size = kv.workspace_size(len(fresh), table.shape[1], sum(need) + room)
         workspace = None if direct else torch.full((size,), 0x7f, dtype=torch.uint8, device="cuda")
@@ -179,7 +179,7 @@ def test_sharp_and_flat_weights(pp, fresh):
     _case(pp, fresh, [900, 500], 8, 2, 64, scale=1e-6)
 
 
-@pytest.mark.parametrize("max_q", [1, 40])
+@pytest.mark.parametrize("max_q", [1, 100])
 @pytest.mark.parametrize("dim", [64, 128])
 def test_scales_far_apart(pp, max_q, dim):
     """Blocks' values of sizes from 2^-40 to 2^40, with the weight on the small ones, on the large ones and on all."""
@@ -196,7 +196,7 @@ def test_scales_far_apart(pp, max_q, dim):
         _case(pp, [1, 1, 1], [1000, 77, 350], 4, 1, dim, BF, max_q=max_q, scale=scale, edit=edit, block=8)
 
 
-@pytest.mark.parametrize("max_q", [1, 40])
+@pytest.mark.parametrize("max_q", [1, 100])
 def test_keys_scales_far_apart(pp, max_q):
     def edit(q, code, exp, table):
         exp[0][:] = (torch.arange(exp[0].numel(), device="cuda") % 9 - 30).view(exp[0].shape).to(torch.int8)
@@ -207,7 +207,7 @@ def test_exponents_outside_the_range_are_read_as_its_ends(pp):
     def edit(q, code, exp, table):
         exp[1][::3] = 100
         exp[1][1::3] = -100
-    for max_q in (1, 40):
+    for max_q in (1, 100):
         _case(pp, [1, 1], [500, 77], 4, 2, 64, BF, max_q=max_q, edit=edit)
 
 
@@ -242,7 +242,7 @@ def test_nan_in_seen_rows(pp, fresh):
 
 def test_infinite_queries(pp):
     """All visible scores -infinity: 0 / 0, as the formula has it."""
-    for max_q in (1, 40):
+    for max_q in (1, 100):
         for dtype in (BF, HF):
             q = torch.zeros((1, 1, 64), dtype=dtype, device="cuda")
             q[0, 0, 0] = -math.inf
@@ -268,12 +268,12 @@ def test_f16_of_large_and_small_values(pp):
     out = torch.empty_like(q)
     with pp.KVCache.like(code[0], dtype=HF) as kv:
         w = torch.empty(kv.workspace_size(1, 1, 1), dtype=torch.uint8, device="cuda")
-        pp.pp_paged_attention8(kv, q, code[0], ke, code[1], ve, _i32([[0]]), _i32([0, 1]), _i32([1]), 40, out, 1.0, workspace=w)
+        pp.pp_paged_attention8(kv, q, code[0], ke, code[1], ve, _i32([[0]]), _i32([0, 1]), _i32([1]), 100, out, 1.0, workspace=w)
         kv.sync()
     assert out[0, 0, :3].tolist() == [65504.0, -65504.0, 256.0] and out[0, 0, 3].isnan() and (out[0, 0, 4:] == 0).all()
 
 
-@pytest.mark.parametrize("max_q", [1, 40])
+@pytest.mark.parametrize("max_q", [1, 100])
 def test_bounds(pp, max_q):
     """Blocks out of range read as zeros, lengths and offsets are cut; all reported, none of it fatal."""
     kc, ke = ref.to8(torch.randn((4, 16, 2, 64), device="cuda"))
@@ -310,7 +310,7 @@ def test_a_workspace_that_is_too_small(pp):
         def run(bytes_):
             out = torch.zeros_like(q)
             w = None if bytes_ is None else torch.empty(bytes_, dtype=torch.uint8, device="cuda")
-            pp.pp_paged_attention8(kv, q, kc, ke, vc, ve, table, q_start, length, 40, out, 0.1, workspace=w)
+            pp.pp_paged_attention8(kv, q, kc, ke, vc, ve, table, q_start, length, 100, out, 0.1, workspace=w)
             return out
         for bytes_ in (None, 0, 16, kv.workspace_size(2, 4, 1) - 1):
             with pytest.raises(pp.PPError, match="workspace"):
@@ -324,7 +324,7 @@ def test_a_workspace_that_is_too_small(pp):
             assert got.isfinite().all() and torch.equal(got[:40], want[:40]) == (blocks >= 4)
         with pytest.raises(pp.PPError, match="aligned"):
             w = torch.empty(kv.workspace_size(2, 4, 8) + 8, dtype=torch.uint8, device="cuda")[8:]
-            pp.pp_paged_attention8(kv, q, kc, ke, vc, ve, table, q_start, length, 40, torch.zeros_like(q), 0.1, workspace=w)
+            pp.pp_paged_attention8(kv, q, kc, ke, vc, ve, table, q_start, length, 100, torch.zeros_like(q), 0.1, workspace=w)
 
 
 def test_refusals(pp):
