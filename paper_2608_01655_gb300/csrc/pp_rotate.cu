@@ -503,13 +503,14 @@ extern "C" pp_status pp_kv_rotate(pp_kv *kv, int32_t tokens, int32_t q_heads, co
     constexpr int kAngleRows = 3;
     const int64_t per_cta = kRotateThreads / 32 * (32 / lanes), held = (int64_t)kv->sm_count * kRotateCtas * per_cta;
     int64_t least = INT64_MAX;
-    for (int32_t split = 1; split <= std::min(rows, 64); ++split) {
-        const int64_t rounds = ((int64_t)tokens * split + held - 1) / held;
-        const int64_t cost = rounds * ((rows + split - 1) / split + kAngleRows);
+    for (int32_t split = 1, share; split <= 64; split = (rows + share - 2) / (share - 1)) {    // the least for each share
+        share = (rows + split - 1) / split;
+        const int64_t rounds = ((int64_t)tokens * split + held - 1) / held, cost = rounds * (share + kAngleRows);
         if (cost < least) {
             least = cost;
             a.split = split;
         }
+        if (share == 1) break;
     }
     const int64_t grid = ((int64_t)tokens * a.split + per_cta - 1) / per_cta;
     if (grid > INT_MAX) return fail(PP_EINVAL, "too many tokens");
