@@ -32,9 +32,7 @@ struct Write8Args {
 
 constexpr int kWrite8Warps = 8, kWrite8Threads = 32 * kWrite8Warps;
 constexpr int kWrite8Ctas = 3;                          // of an SM
-constexpr int kWrite8Window = 32;                       // tokens of a CTA at most: a lane each
-constexpr int kWrite8Held = 8;                          // vectors that a thread keeps
-constexpr int kWrite8Long = 48;                         // tokens of a run from which the CTA takes it
+constexpr int kWrite8Held = 8;                          // vectors that a lane has on their way
 
 // bits of a 16-bit infinity
 template <typename T> constexpr uint32_t kInfinity = std::is_same<T, __nv_bfloat16>::value ? 0x7f80u : 0x7c00u;
@@ -108,28 +106,48 @@ __device__ __forceinline__ int least_exponent(float x)
 struct Run8 {
     int32_t first, count, block;                        // first token, tokens to the last one, block
 };
-template <int TEAM> struct Team8 {                      // shared memory of a team
-    uint32_t top[TEAM];
-    int32_t begins[TEAM];
+// Shared memory of a CTA: a place for every vector that a lane has on its way, and what the
+// warps of a team tell each other.
+struct Write8Shared {
+    uint4 held[kWrite8Warps][kWrite8Held][32];
+    uint32_t top[kWrite8Warps];
+    int32_t begins[kWrite8Warps];
+    uint8_t list[kWrite8Warps][32];                     // tokens that are runs
 };
 
+// What becomes of the exponents, from the size of the largest finite new element.
+__device__ __forceinline__ int next_exponent(float top, bool begins, int old)
+{
+    const int need = least_exponent(top);
+    return begins ? need : max(old, need);
+}
+// Some lanes' (of `lanes`, me among them) share of a block's rows of one head to a new scale.
+__device__ __forceinline__ void rescale_rows(const Write8Args &a, uint8_t *rows, float by, int me, int lanes)
+{
+    const int32_t pieces = a.per_head / 2;              // of 16 codes
+    for (int32_t l = me; l < pieces << a.block_log; l += lanes) {
+        uint4 *p = reinterpret_cast<uint4 *>(rows + l / pieces * a.token_stride) + l % pieces;
+        const uint4 x = *p;
+        *p = make_uint4(rescale4(x.x, by), rescale4(x.y, by), rescale4(x.z, by), rescale4(x.w, by));
+    }
+}
+
 // A head of K or V (unit = 2 h + is_v) of a run by a team of TEAM warps: the largest size,
-// the exponent, the block's other rows if that grows, the codes.  STEPS vectors a thread
-// are read once.
-template <typename T, int TEAM, int STEPS>
-__device__ __forceinline__ void write_unit(const Write8Args &a, const Run8 &run, int32_t unit, Team8<TEAM> *sh)
+// the exponent, the block's other rows if that grows, the codes.  A lane has vector `col`
+// of a row of every step's `some` rows a warp; those of kWrite8Held steps are read once.
+template <typename T, int TEAM>
+__device__ __forceinline__ void write_unit(const Write8Args &a, const Run8 &run, int32_t unit, Write8Shared &sh)
 {
     constexpr int kThreads = 32 * TEAM;
-    const int me = threadIdx.x % kThreads, lane = me & 31, warp = me >> 5;
-    auto sync = [&]() {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, of_team = warp % TEAM, me = 32 * of_team + lane;
+    auto sync = [&]() {                                 // a barrier of its own for every team of every size
         if (TEAM == 1) __syncwarp();
-        else __syncthreads();
+        else named_sync((TEAM == 2 ? 1 : TEAM == 4 ? 5 : 7) + warp / TEAM, kThreads);
     };
     const bool is_v = unit & 1;
     const int32_t h = unit >> 1;
-    // a lane has vector `col` of a row of every step's `some` rows a warp
     const int some = 32 / a.per_head, sub = lane / a.per_head, col = lane - sub * a.per_head;
-    const int32_t step = TEAM * some, ahead = warp * some + sub, past = sub < some ? run.count : 0;     // past: no row from here on
+    const int32_t step = TEAM * some, ahead = of_team * some + sub, past = sub < some ? run.count : 0;  // past: no row from here on
     const int64_t token = is_v ? a.v_token : a.k_token;
     const uint4 *src = (is_v ? a.v + h * a.v_head : a.k + h * a.k_head) + run.first * token + col;
     uint8_t *dst = (is_v ? a.vc : a.kc) + run.block * a.block_stride + h * a.head_stride;
@@ -140,171 +158,225 @@ __device__ __forceinline__ void write_unit(const Write8Args &a, const Run8 &run,
         return s >= 0 && s < a.slots ? (int32_t)(s & ((1 << a.block_log) - 1)) : -1;
     };
     // rows that are left out are loaded and not used, so that no load waits for a slot
-    uint4 held[STEPS];
-    int32_t row[STEPS];
-    const int old = min(max((int)*exponent, kLeastExp), kMostExp);
+    uint4(*held)[32] = sh.held[warp];
+    int32_t row[kWrite8Held];
 #pragma unroll
-    for (int y = 0; y < STEPS; ++y) {
+    for (int y = 0; y < kWrite8Held; ++y) {
         const int32_t n = ahead + y * step;
-        held[y] = n < past ? __ldg(src + n * token) : make_uint4(0, 0, 0, 0);
+        if (n < past) copy16(smem_u32(&held[y][lane]), reinterpret_cast<const char *>(src + n * token), 16);
         row[y] = n < past ? place(n) : -1;
     }
-    const int32_t rest = ahead + STEPS * step;    // rows that are read again
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    const int old = min(max((int)*exponent, kLeastExp), kMostExp);
+    const int32_t rest = ahead + kWrite8Held * step;    // rows that are read again
     uint32_t top = 0;
     bool begins = false;
-#pragma unroll
-    for (int y = 0; y < STEPS; ++y) {
-        begins |= row[y] == 0;
-        if (row[y] >= 0) top = largest(top, held[y]);
-    }
+#pragma unroll 4
     for (int32_t n = rest; n < past; n += step) {
         const int32_t at = place(n);
         begins |= at == 0;
-        if (at >= 0) top = largest(top, __ldg(src + n * token));
+        const uint4 x = __ldg(src + n * token);
+        if (at >= 0) top = largest(top, x);
+    }
+    copies_wait();                                      // a lane reads what it copied itself
+#pragma unroll
+    for (int y = 0; y < kWrite8Held; ++y) {
+        begins |= row[y] == 0;
+        if (row[y] >= 0) top = largest(top, held[y][lane]);
     }
     begins = __any_sync(~0u, begins);
-    if (TEAM > 1 && lane == 0) sh->begins[warp] = begins;
+    if (TEAM > 1 && lane == 0) sh.begins[warp] = begins;
     // the largest of the team's
     auto all_of = [&](uint32_t mine) {
         mine = __reduce_max_sync(~0u, max(mine & 0xffffu, mine >> 16));
         if (TEAM > 1) {
-            if (lane == 0) sh->top[warp] = mine;
+            if (lane == 0) sh.top[warp] = mine;
             sync();
 #pragma unroll
-            for (int w = 0; w < TEAM; ++w) mine = max(mine, sh->top[w]);
+            for (int w = 0; w < TEAM; ++w) mine = max(mine, sh.top[warp - of_team + w]);
         }
         return mine;
     };
     top = all_of(top);
     if (TEAM > 1)
 #pragma unroll
-        for (int w = 0; w < TEAM; ++w) begins |= sh->begins[w] != 0;
+        for (int w = 0; w < TEAM; ++w) begins |= sh.begins[warp - of_team + w] != 0;
     const bool strange = top >= kInfinity<T>;           // the same in all the team
     if (strange) {                                      // the largest finite one; the others become NaN
         sync();                                         // all have read the first ones
         top = 0;
-#pragma unroll
-        for (int y = 0; y < STEPS; ++y)
-            if (row[y] >= 0) top = __vmaxu2(top, sizes8<T>(held[y]));
-        for (int32_t n = rest; n < past; n += step) {
+        for (int32_t n = ahead; n < past; n += step) {
             uint4 x = __ldg(src + n * token);
             if (place(n) >= 0) top = __vmaxu2(top, sizes8<T>(x));
         }
         top = all_of(top);
     }
-    const int need = least_exponent(low_value<T>(top)), e = begins ? need : max(old, need);
-    if (!begins && e > old) {
-        // the rows that the block has go to the new scale; those of this call are written over them
-        const float by = scale_of(old - e);
-        const int32_t pieces = a.per_head / 2;          // of 16 codes
-        for (int32_t l = me; l < pieces << a.block_log; l += kThreads) {
-            uint4 *p = reinterpret_cast<uint4 *>(dst + l / pieces * a.token_stride) + l % pieces;
-            const uint4 x = *p;
-            *p = make_uint4(rescale4(x.x, by), rescale4(x.y, by), rescale4(x.z, by), rescale4(x.w, by));
-        }
-    }
+    const int e = next_exponent(low_value<T>(top), begins, old);
+    // the rows that the block has go to the new scale; those of this call are written over them
+    if (!begins && e > old) rescale_rows(a, dst, scale_of(old - e), me, kThreads);
     sync();                                             // all have read the exponent, and old rows are done
     if (me == 0) *exponent = (int8_t)e;
     const float by = scale_of(-e);
     dst += 8 * col;
-#pragma unroll
-    for (int y = 0; y < STEPS; ++y)
-        if (row[y] >= 0) *reinterpret_cast<uint2 *>(dst + row[y] * a.token_stride) = codes8<T>(held[y], by);
-    for (int32_t n = rest; n < past; n += step) {
-        const int32_t at = place(n);
-        if (at < 0) continue;
-        uint4 x = __ldg(src + n * token);
+    auto put = [&](int32_t at, uint4 x) {
         if (strange) sizes8<T>(x);
         *reinterpret_cast<uint2 *>(dst + at * a.token_stride) = codes8<T>(x, by);
+    };
+#pragma unroll
+    for (int y = 0; y < kWrite8Held; ++y)
+        if (row[y] >= 0) put(row[y], held[y][lane]);
+#pragma unroll 4
+    for (int32_t n = rest; n < past; n += step) {
+        const int32_t at = place(n);
+        const uint4 x = __ldg(src + n * token);
+        if (at >= 0) put(at, x);
     }
     if (TEAM > 1) sync();                               // the team's shared memory is free again
 }
 
+// Runs of one token among the 32 from t0 on, whose lanes `list` names: units first .. past
+// - 1 of theirs, counted run after run, side by side.  block: of each lane's token.  (Two or
+// four times as many together cost a step of 64 tokens 0.4 and 1.1 us more, in code, and
+// save 30,011 tokens nothing.)
+template <typename T>
+__device__ __forceinline__ void write_singles(const Write8Args &a, int32_t t0, int32_t block, const uint8_t *list, int32_t first, int32_t past)
+{
+    const int lane = threadIdx.x & 31, some = 32 / a.per_head, sub = lane / a.per_head, col = lane - sub * a.per_head, all = 2 * a.heads;
+    const int32_t n = first + sub, r = n / all, u = n - r * all, h = u >> 1;
+    const bool live = sub < some && n < past;
+    const int from = live ? list[r] : 0;
+    const int32_t b = __shfl_sync(~0u, block, from), t = t0 + from;
+    uint8_t *const rows = (u & 1 ? a.vc : a.kc) + b * a.block_stride + h * a.head_stride;       // the block's, of the head
+    int8_t *const exponent = (u & 1 ? a.ve : a.ke) + (int64_t)b * a.heads + h;
+    uint4 x = make_uint4(0, 0, 0, 0);
+    int32_t at = 0;
+    int old = 0;
+    if (live) {
+        x = __ldg(u & 1 ? a.v + t * a.v_token + h * a.v_head + col : a.k + t * a.k_token + h * a.k_head + col);
+        at = (int32_t)(a.slot[t] & ((1 << a.block_log) - 1));
+        old = min(max((int)*exponent, kLeastExp), kMostExp);
+    }
+    uint32_t top = largest(0, x), mine = 0;
+    if (__any_sync(~0u, (top & 0xffffu) >= kInfinity<T> || top >> 16 >= kInfinity<T>)) top = sizes8<T>(x);
+    top = max(top & 0xffffu, top >> 16);
+    for (int s = 0; s < some; ++s) {
+        const uint32_t of_unit = __reduce_max_sync(~0u, sub == s ? top : 0);
+        if (sub == s) mine = of_unit;
+    }
+    const int e = next_exponent(low_value<T>(mine), at == 0, old);
+    // units whose scale grows, one after another
+    for (uint32_t grow = __ballot_sync(~0u, live && col == 0 && at != 0 && e > old); grow; grow &= grow - 1) {
+        const int src = __ffs(grow) - 1;
+        const uint64_t where = __shfl_sync(~0u, (uint64_t)rows, src);
+        rescale_rows(a, reinterpret_cast<uint8_t *>(where), scale_of(__shfl_sync(~0u, old - e, src)), lane, 32);
+    }
+    __syncwarp();                                       // all have read the exponents, and old rows are done
+    if (!live) return;
+    if (col == 0) *exponent = (int8_t)e;
+    *reinterpret_cast<uint2 *>(rows + at * a.token_stride + 8 * col) = codes8<T>(x, scale_of(-e));
+}
+
 // A run is the tokens of one block, which stand next to one another but for fewer than
 // 32 that are left out between two; its first token leads it.  Every warp of a CTA finds
-// the leaders among `window` tokens by itself, from their slots and those of 32 tokens to
-// either side.  A warp takes a run's rows of one head and of K or V; of long runs (blocks
-// that have them: LONG) the CTA does.
-template <typename T, bool LONG>
+// the leaders among `window` tokens by itself, 32 at a time, from their slots and those of
+// 32 tokens to either side.  A run's rows of one head and of K or V are a team's, a warp
+// for every kWrite8Held steps of them, TEAMS warps at most; those of runs of one token go
+// several to a warp.
+template <typename T, int TEAMS>
 __global__ void __launch_bounds__(kWrite8Threads, kWrite8Ctas) k_kv_write8(const __grid_constant__ Write8Args a)
 {
-    __shared__ Team8<kWrite8Warps> team;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int32_t t0 = blockIdx.x * a.window, t1 = min(t0 + a.window, a.tokens);
+    __shared__ Write8Shared sh;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     // block of token t, -1 if it is left out or no token
     auto block_of = [&](int32_t t) {
         const int64_t s = t >= 0 && t < a.tokens ? a.slot[t] : -1;
         return s >= 0 && s < a.slots ? (int32_t)(s >> a.block_log) : -1;
     };
-    const int32_t before = block_of(t0 - 32 + lane), here = block_of(t0 + lane), after = block_of(t0 + 32 + lane);
-    if (warp == 0 && blockIdx.y == 0 && t0 + lane < t1 && a.slot[t0 + lane] >= a.slots) kv_bounds(a.status);
-    // tokens that are not left out: 64 from t0 - 32 on, and 64 from t0 on
-    const uint32_t known_before = __ballot_sync(~0u, before >= 0), known = __ballot_sync(~0u, here >= 0);
-    const uint32_t known_after = __ballot_sync(~0u, after >= 0);
-    // the nearest of the 32 before this lane's token, and its block
-    const uint64_t back = (((uint64_t)known << 32 | known_before) >> lane) & 0xffffffffu;     // bit 31: the one before
-    const int nearest = 31 - __clz((uint32_t)back) + lane;                                  // counted from t0 - 32
-    const int32_t block_before = __shfl_sync(~0u, before, nearest & 31), block_here = __shfl_sync(~0u, here, nearest & 31);
-    const bool leads = here >= 0 && ((uint32_t)back == 0 || (nearest < 32 ? block_before : block_here) != here);
-    const uint32_t leaders = __ballot_sync(~0u, leads), later = leaders & ~1u << lane;
-    // a run that another one follows here ends with the last token before that
-    const int32_t counted = later ? 31 - __clz(known & (later & -later) - 1) - lane + 1 : 0;
-
-    // the tokens of the run that lane f's token leads, counted from that: all before one of another block, or before 32 left out
-    auto run_of = [&](int f, int32_t block) {
-        const uint64_t same = (uint64_t)__ballot_sync(~0u, after == block) << 32 | __ballot_sync(~0u, here == block);
-        const uint64_t valid = (uint64_t)known_after << 32 | known, from = ~0ull << f;
-        uint64_t none = ~valid & from;                  // then: bits that begin 32 left out
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) none &= none >> o;
-        const uint64_t ends = (valid & ~same & from) | none;
-        const uint64_t mine = same & from & (ends ? (ends & -ends) - 1 : ~0ull);
-        int32_t last = 63 - __clzll(mine);
-        if (!ends && t0 + 64 < a.tokens) {              // it may go on: 128 tokens at a time
-            last += t0;
-            for (bool more = true; more;) {
-                int32_t b[4];
-                const int32_t at = last + 1;
-#pragma unroll
-                for (int y = 0; y < 4; ++y) b[y] = block_of(at + 32 * y + lane);
-#pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                    if (!more) continue;
-                    uint32_t good = __ballot_sync(~0u, b[y] == block);
-                    const uint32_t other = __ballot_sync(~0u, b[y] >= 0 && b[y] != block);
-                    if (other) good &= (other & -other) - 1;
-                    if (good) last = at + 32 * y + 31 - __clz(good);
-                    // 32 left out, or more to come than this can tell: the next look is from `last` on
-                    if (other || !good) more = false;
-                    else if (good != ~0u) break;
-                }
-            }
-            last -= t0;
-        }
-        return last - f + 1;
-    };
-
     // the warps of this CTA, and of those of the same tokens, share the units of all runs out
-    const int32_t all = 2 * a.heads, workers = gridDim.y * kWrite8Warps;
-    int32_t next = blockIdx.y * kWrite8Warps + warp;    // this warp's next unit, counted from the run's first
-    for (uint32_t left = leaders & (uint32_t)((1ull << (t1 - t0)) - 1); left; left &= left - 1) {
-        const int lead = __ffs(left) - 1;
-        const int32_t block = __shfl_sync(~0u, here, lead), count = __shfl_sync(~0u, counted, lead);
-        if (!LONG && next >= all) {                     // none of this run
-            next -= all;
-            continue;
+    const int32_t all = 2 * a.heads, workers = gridDim.y * kWrite8Warps, some = 32 / a.per_head;
+    int32_t next = blockIdx.y * kWrite8Warps + warp;    // this warp's next task, counted from the run's first
+    const int32_t begin = blockIdx.x * a.window, end = min(begin + a.window, a.tokens);
+    int32_t before = block_of(begin - 32 + lane), here = block_of(begin + lane), after = block_of(begin + 32 + lane);
+    for (int32_t t0 = begin; t0 < end; t0 += 32) {
+        const int32_t t1 = min(t0 + 32, end), later_on = t1 < end ? block_of(t0 + 64 + lane) : -1;
+        if (warp == 0 && blockIdx.y == 0 && t0 + lane < t1 && a.slot[t0 + lane] >= a.slots) kv_bounds(a.status);
+        // tokens that are not left out: 64 from t0 - 32 on, and 64 from t0 on
+        const uint32_t known_before = __ballot_sync(~0u, before >= 0), known = __ballot_sync(~0u, here >= 0);
+        const uint32_t known_after = __ballot_sync(~0u, after >= 0);
+        // the nearest of the 32 before this lane's token, and its block
+        const uint64_t back = (((uint64_t)known << 32 | known_before) >> lane) & 0xffffffffu;     // bit 31: the one before
+        const int nearest = 31 - __clz((uint32_t)back) + lane;                                  // counted from t0 - 32
+        const int32_t block_before = __shfl_sync(~0u, before, nearest & 31), block_here = __shfl_sync(~0u, here, nearest & 31);
+        const bool leads = here >= 0 && ((uint32_t)back == 0 || (nearest < 32 ? block_before : block_here) != here);
+        const uint32_t leaders = __ballot_sync(~0u, leads), later = leaders & ~1u << lane;
+        // a run that another one follows here ends with the last token before that
+        const int32_t counted = later ? 31 - __clz(known & (later & -later) - 1) - lane + 1 : 0;
+
+        // the tokens of the run that lane f's token leads, counted from that: all before one of another block, or before 32 left out
+        auto run_of = [&](int f, int32_t block) {
+            const uint64_t same = (uint64_t)__ballot_sync(~0u, after == block) << 32 | __ballot_sync(~0u, here == block);
+            const uint64_t valid = (uint64_t)known_after << 32 | known, from = ~0ull << f;
+            uint64_t none = ~valid & from;                  // then: bits that begin 32 left out
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) none &= none >> o;
+            const uint64_t ends = (valid & ~same & from) | none;
+            const uint64_t mine = same & from & (ends ? (ends & -ends) - 1 : ~0ull);
+            int32_t last = 63 - __clzll(mine);
+            if (!ends && t0 + 64 < a.tokens) {              // it may go on: 128 tokens at a time
+                last += t0;
+                for (bool more = true; more;) {
+                    int32_t b[4];
+                    const int32_t at = last + 1;
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) b[y] = block_of(at + 32 * y + lane);
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) {
+                        if (!more) continue;
+                        uint32_t good = __ballot_sync(~0u, b[y] == block);
+                        const uint32_t other = __ballot_sync(~0u, b[y] >= 0 && b[y] != block);
+                        if (other) good &= (other & -other) - 1;
+                        if (good) last = at + 32 * y + 31 - __clz(good);
+                        // 32 left out, or more to come than this can tell: the next look is from `last` on
+                        if (other || !good) more = false;
+                        else if (good != ~0u) break;
+                    }
+                }
+                last -= t0;
+            }
+            return last - f + 1;
+        };
+        uint32_t left = leaders & (uint32_t)((1ull << (t1 - t0)) - 1);
+        const uint32_t singles = __ballot_sync(~0u, counted == 1) & left;
+        if (singles) {
+            if (singles >> lane & 1) sh.list[warp][__popc(singles & ((1u << lane) - 1))] = (uint8_t)lane;
+            __syncwarp();
+            const int32_t units = __popc(singles) * all, tasks = (units + some - 1) / some;
+            for (; next < tasks; next += workers) write_singles<T>(a, t0, here, sh.list[warp], next * some, units);
+            next -= tasks;
+            __syncwarp();                               // the list is free again
         }
-        const Run8 run = {t0 + lead, count ? count : run_of(lead, block), block};
-        if (LONG && run.count > kWrite8Long) {
-            for (int32_t u = blockIdx.y; u < all; u += gridDim.y) write_unit<T, kWrite8Warps, kWrite8Held>(a, run, u, &team);
-            continue;
+        for (left &= ~singles; left; left &= left - 1) {
+            const int lead = __ffs(left) - 1;
+            const int32_t block = __shfl_sync(~0u, here, lead), count = __shfl_sync(~0u, counted, lead);
+            const Run8 run = {t0 + lead, count ? count : run_of(lead, block), block};
+            const int32_t warps = (run.count + kWrite8Held * some - 1) / (kWrite8Held * some);     // with rows
+            if (TEAMS == 1 || warps == 1) {
+                for (; next < all; next += workers) write_unit<T, 1>(a, run, next, sh);
+                next -= all;
+                continue;
+            }
+            auto by_teams = [&](auto size) {
+                constexpr int TEAM = decltype(size)::value;
+                constexpr int kTeams = kWrite8Warps / TEAM;
+                for (int32_t u = blockIdx.y * kTeams + warp / TEAM; u < all; u += gridDim.y * kTeams) write_unit<T, TEAM>(a, run, u, sh);
+            };
+            if (TEAMS == 2 || warps == 2) by_teams(std::integral_constant<int, 2>());
+            else if (TEAMS == 4 || warps <= 4) by_teams(std::integral_constant<int, TEAMS < 4 ? TEAMS : 4>());
+            else by_teams(std::integral_constant<int, TEAMS>());
         }
-        const bool few = run.count <= 2 * (32 / a.per_head);       // two steps' rows
-        for (; next < all; next += workers) {
-            if (few) write_unit<T, 1, 2>(a, run, next, nullptr);
-            else write_unit<T, 1, kWrite8Held>(a, run, next, nullptr);
-        }
-        next -= all;
+        before = here;
+        here = after;
+        after = later_on;
     }
 }
 
@@ -542,17 +614,24 @@ extern "C" pp_status pp_kv_write8(pp_kv *kv, int32_t tokens, const void *k, int6
     a.slots = (int64_t)kv->blocks << kv->block_log;
     a.block_log = kv->block_log;
     a.status = kv->d_status;
-    // With few tokens a CTA has fewer of them, and more CTAs share their heads out.
-    const int32_t ctas = kWrite8Ctas * kv->sm_count, block = kv->block_size;
-    a.window = std::min(std::max((tokens + ctas - 1) / ctas, 1), kWrite8Window);
+    // CTAs for one round of the SMs, or fewer where blocks are larger than that and a CTA would have no run's first
+    // token; more CTAs share its heads out, as far as its warps would not take them in one go.
+    const int32_t ctas = kWrite8Ctas * kv->sm_count, held = kWrite8Held * (32 / a.per_head);
+    const int32_t warps = std::min((kv->block_size + held - 1) / held, kWrite8Warps);      // of a whole block's rows
+    const int32_t teams = warps <= 1 ? 1 : warps <= 2 ? 2 : warps <= 4 ? 4 : 8;
+    const int32_t even = (tokens - 1) / ctas + 1;
+    a.window = kv->block_size > 32 ? std::max(even, std::min(kv->block_size, 4 * even)) : even;
     const int32_t windows = (tokens - 1) / a.window + 1;
-    const bool has_long = block > kWrite8Long;
-    const int32_t useful = has_long ? 2 * kv->heads : (2 * kv->heads + kWrite8Warps - 1) / kWrite8Warps;
-    const dim3 grid(windows, std::min(std::max((has_long ? 4 : 1) * ctas / windows, 1), useful));
+    const int32_t rounds = (2 * kv->heads * teams + kWrite8Warps - 1) / kWrite8Warps;
+    const dim3 grid(windows, std::min(std::max(2 * ctas / windows, 1), rounds));
     const cudaStream_t st = (cudaStream_t)stream;
-    auto launch = [&](auto *shorts, auto *longs) { (has_long ? longs : shorts)<<<grid, kWrite8Threads, 0, st>>>(a); };
-    if (kv->dtype == PP_KV_BF16) launch(k_kv_write8<__nv_bfloat16, false>, k_kv_write8<__nv_bfloat16, true>);
-    else launch(k_kv_write8<__half, false>, k_kv_write8<__half, true>);
+    auto launch = [&](auto *of1, auto *of2, auto *of4, auto *of8) {
+        (teams == 1 ? of1 : teams == 2 ? of2 : teams == 4 ? of4 : of8)<<<grid, kWrite8Threads, 0, st>>>(a);
+    };
+    if (kv->dtype == PP_KV_BF16)
+        launch(k_kv_write8<__nv_bfloat16, 1>, k_kv_write8<__nv_bfloat16, 2>, k_kv_write8<__nv_bfloat16, 4>, k_kv_write8<__nv_bfloat16, 8>);
+    else
+        launch(k_kv_write8<__half, 1>, k_kv_write8<__half, 2>, k_kv_write8<__half, 4>, k_kv_write8<__half, 8>);
     PP_CUDA(cudaGetLastError());
     return PP_OK;
 }

@@ -104,6 +104,28 @@ def test_single_rows(pp, tokens, heads):
     c.check()
 
 
+@pytest.mark.parametrize("block,tokens,dim", [(8, 9000, 64), (16, 40_000, 128), (32, 20_000, 16), (64, 20_000, 128),
+                                              (128, 15_000, 80), (256, 15_000, 32), (512, 40_000, 128)])
+def test_many_tokens(pp, block, tokens, dim):
+    """More tokens than a CTA looks at together; runs of one, few and many rows next to one another."""
+    torch.manual_seed(block)
+    rng = np.random.default_rng(block)
+    slot, at = [], 0
+    while len(slot) < tokens:
+        first = 0 if rng.random() < 0.3 else int(rng.integers(0, block))
+        n = int(rng.choice([1, 1, 1, 2, 3, 17, 40, 3 * block]))
+        place = first + np.arange(n)
+        slot += ((at + place // block) * block + place % block).tolist()
+        at += (first + n - 1) // block + 1
+    slot = np.array(slot[:tokens])
+    slot[rng.random(tokens) < 0.02] = -1
+    c = _Cache(at, block, 1, dim, BF, seed=block)
+    with pp.KVCache.like(c.code[0]) as kv:
+        c.write(pp, kv, _rows(tokens, 1, dim, BF, 2.0), _rows(tokens, 1, dim, BF, 2.0), slot)
+        kv.sync()
+    c.check()
+
+
 def test_a_block_that_grows_token_by_token(pp):
     """The scale only grows, until the block is begun anew."""
     c = _Cache(2, 16, 2, 32, HF, seed=5)
