@@ -26,7 +26,9 @@ namespace pp {
 
 namespace token {
 constexpr int kRows = 16;                           // rows of an item
-using Shape = ShapeOf<kRows, KT>;
+// an item's weight of 1, 2, 3, 5 tiles: 60 requests x 4 tokens after 50 to 9,000 56, 53, 48, 46 us, 300 single tokens
+// after 50 to 3,000 85, 81, 79, 79, 256 after 100 to 8,000 -, 461, 462, 472
+using Shape = ShapeOf<kRows, KT, 3>;
 
 template <int HALVES> struct Layout {
     static constexpr int half = kKeys * 128;                    // bytes of 64 columns of a warp's keys
@@ -139,7 +141,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_token(const __grid_const
     // ldmatrix rows: K (keys outside, dims inside a group of four matrices), V (the other way round)
     const int krow = (lane >> 4) * 8 + (lane & 7), kpiece = (lane >> 3) & 1;
     const int vrow = ((lane >> 3) & 1) * 8 + (lane & 7), vpiece = lane >> 4;
-    const int jr = tid >> 4, jd = (tid & 15) * (4 * HALVES);          // joining: row and first column
+    const int jr = tid >> 4, jd = (tid & 15) * 4;       // joining: row and first columns, 64 apart
 
     const uint32_t ring = base + warp * L::stages * 2 * L::rows;
     Feed<HALVES> feed(a, sched, ring);
@@ -370,7 +372,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_token(const __grid_const
                 const float4 *src = reinterpret_cast<const float4 *>(join + (w * kRows + jr) * L::pitch + jd);
 #pragma unroll
                 for (int d = 0; d < HALVES; ++d) {
-                    const float4 y = src[d];
+                    const float4 y = src[16 * d];
                     acc[4 * d] = fmaf(f, y.x, acc[4 * d]);
                     acc[4 * d + 1] = fmaf(f, y.y, acc[4 * d + 1]);
                     acc[4 * d + 2] = fmaf(f, y.z, acc[4 * d + 2]);

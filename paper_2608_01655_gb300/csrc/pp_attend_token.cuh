@@ -16,12 +16,11 @@ constexpr int KT = kKeys * kWarps;                  // keys per tile
 constexpr int kJoinGroup = 16;                      // pieces (8 KB) joined at a time, then their groups
 
 // Rows are (token, head of the group), token first; an item is ROWS of them, a tile KEYS keys.
-template <int ROWS, int KEYS> struct ShapeOf {
+// EXTRA: what an item weighs beside its tiles (first rows, join).
+template <int ROWS, int KEYS, int EXTRA> struct ShapeOf {
     static constexpr int kRows = ROWS;
     static constexpr int KT = KEYS;
-    // what an item weighs beside its tiles (first rows, join): 1, 2, 3, 5 tiles take 60 requests x 4 tokens after 50 to
-    // 9,000 56, 53, 48, 46 us, 300 single tokens after 50 to 3,000 85, 81, 79, 79, 256 after 100 to 8,000 -, 461, 462, 472
-    static constexpr int32_t extra = 3;
+    static constexpr int32_t extra = EXTRA;
     static constexpr bool many = false;
     static __device__ __forceinline__ int32_t outer(const AttendDev &a) { return a.kv_heads; }
     static __device__ __forceinline__ int32_t rows(const AttendDev &a, const Req &q) { return q.q_len * a.c.group; }
@@ -81,26 +80,30 @@ __device__ __forceinline__ uint32_t lds32(uint32_t addr)
 // both 16-bit halves of a register kept or cleared
 __device__ __forceinline__ uint32_t keep(bool lo, bool hi) { return (lo ? 0xffffu : 0u) | (hi ? 0xffff0000u : 0u); }
 
-// neighbouring 32-bit columns of a piece; loads are from L2, where other CTAs left them
-template <int N> __device__ __forceinline__ void store_columns(float *to, const float (&x)[N])
+// A thread's N columns of a row of which it has those from 4 `lane` on, four of every STEP
+// (N up to 4: the N from N `lane` on): neighbouring threads' loads are neighbours.
+template <int N> constexpr int kChunk = N < 4 ? N : 4;
+template <int N, int STEP> __device__ __forceinline__ void store_columns(float *row, int lane, const float (&x)[N])
 {
     if constexpr (N == 2) {
-        *reinterpret_cast<float2 *>(to) = make_float2(x[0], x[1]);
+        *reinterpret_cast<float2 *>(row + 2 * lane) = make_float2(x[0], x[1]);
     } else {
 #pragma unroll
-        for (int d = 0; d < N; d += 4) *reinterpret_cast<float4 *>(to + d) = make_float4(x[d], x[d + 1], x[d + 2], x[d + 3]);
+        for (int d = 0; d < N; d += 4)
+            *reinterpret_cast<float4 *>(row + 4 * lane + d / 4 * STEP) = make_float4(x[d], x[d + 1], x[d + 2], x[d + 3]);
     }
 }
-template <int N> __device__ __forceinline__ void load_columns(const float *from, float (&x)[N])
+// from L2, where other CTAs left them
+template <int N, int STEP> __device__ __forceinline__ void load_columns(const float *row, int lane, float (&x)[N])
 {
     if constexpr (N == 2) {
-        const float2 y = __ldcg(reinterpret_cast<const float2 *>(from));
+        const float2 y = __ldcg(reinterpret_cast<const float2 *>(row + 2 * lane));
         x[0] = y.x;
         x[1] = y.y;
     } else {
 #pragma unroll
         for (int d = 0; d < N; d += 4) {
-            const float4 y = __ldcg(reinterpret_cast<const float4 *>(from + d));
+            const float4 y = __ldcg(reinterpret_cast<const float4 *>(row + 4 * lane + d / 4 * STEP));
             x[d] = y.x;
             x[d + 1] = y.y;
             x[d + 2] = y.z;
@@ -119,8 +122,8 @@ __device__ __forceinline__ int64_t item_row(const AttendDev &a, const Cursor<S> 
 }
 
 // The end of an item, or of a CTA's part of it: leaves a piece or writes the rows.  A
-// thread (tid of THREADS, which sync() is for) has PER columns, from jd on, of row jr (a
-// row is within a warp): outputs acc not yet divided, maximum and sum.
+// thread (tid of THREADS, which sync() is for) has PER columns of row jr (a row is within a
+// warp), as in store_columns: outputs acc not yet divided, maximum and sum.
 // GROUP: pieces that are joined at a time, then their groups; 0: 8, or the square root of
 // the pieces if they are more.
 template <typename T, class S, int PER, int THREADS, int GROUP, class SYNC>
@@ -128,10 +131,10 @@ __device__ __forceinline__ void leave_item(const AttendDev &a, const Cursor<S> &
                                            float sum, int32_t *last, int64_t total, int64_t ctas, SYNC sync)
 {
     constexpr int kRows = S::kRows, kLanes = THREADS / kRows, kWidth = PER * kLanes;
-    const int jr = tid / kLanes, jd = tid % kLanes * PER;
+    constexpr int kStep = kChunk<PER> * kLanes;
+    const int jr = tid / kLanes, lane = tid % kLanes;
     const int32_t row0 = cur.inner * kRows, rows = min(kRows, S::rows(a, cur.q) - row0);
-    const int lane_of_row = tid % kLanes;
-    const uint32_t row_lanes = (uint32_t)(((uint64_t)1 << kLanes) - 1) << ((tid & 31) - lane_of_row);
+    const uint32_t row_lanes = (uint32_t)(((uint64_t)1 << kLanes) - 1) << ((tid & 31) - lane);
 
     // an item in pieces: leave this one's, and the last to arrive joins a group's, then the groups'
     bool write = true;
@@ -146,8 +149,8 @@ __device__ __forceinline__ void leave_item(const AttendDev &a, const Cursor<S> &
         auto put = [&](int32_t slot) {
             __syncwarp();                           // a row's lanes have read what one of them writes over
             if (jr < rows) {
-                store_columns<PER>(a.piece + ((int64_t)slot * kRows + jr) * kWidth + jd, acc);
-                if (jd == 0) {
+                store_columns<PER, kStep>(a.piece + ((int64_t)slot * kRows + jr) * kWidth, lane, acc);
+                if (lane == 0) {
                     a.piece_stat[slot * 2 * kRows + jr] = top;
                     a.piece_stat[slot * 2 * kRows + kRows + jr] = sum;
                 }
@@ -179,7 +182,7 @@ __device__ __forceinline__ void leave_item(const AttendDev &a, const Cursor<S> &
             if constexpr (GROUP == 0) {
                 // the statistics, a piece a lane, on their way together
 #pragma unroll
-                for (int x = 0; x < kOwn; ++x) own[x] = lane_of_row + x * kLanes < n ? __ldcg(stat(lane_of_row + x * kLanes)) : -INFINITY;
+                for (int x = 0; x < kOwn; ++x) own[x] = lane + x * kLanes < n ? __ldcg(stat(lane + x * kLanes)) : -INFINITY;
                 top = own[0];
 #pragma unroll
                 for (int x = 1; x < kOwn; ++x) top = fmaxf(top, own[x]);
@@ -196,7 +199,7 @@ __device__ __forceinline__ void leave_item(const AttendDev &a, const Cursor<S> &
                 const float f = exp2_approx(__ldcg(stat(p)) - base);
                 sum = fmaf(f, __ldcg(stat(p) + kRows), sum);
                 float y[PER];
-                load_columns<PER>(a.piece + ((int64_t)slot * kRows + jr) * kWidth + jd, y);
+                load_columns<PER, kStep>(a.piece + ((int64_t)slot * kRows + jr) * kWidth, lane, y);
 #pragma unroll
                 for (int d = 0; d < PER; ++d) acc[d] = fmaf(f, y[d], acc[d]);
             }
@@ -215,19 +218,15 @@ __device__ __forceinline__ void leave_item(const AttendDev &a, const Cursor<S> &
     }
     if (write && jr < rows) {
         const float inv = inverse_sum(sum, S::pos(a, cur.q, row0 + jr) >= 0);
-        T *dst = static_cast<T *>(a.c.out) + item_row(a, cur, jr, a.c.out_token_stride, a.c.out_head_stride) + jd;
-        if (jd < a.dim) {
-            uint32_t w[PER / 2];
+        T *dst = static_cast<T *>(a.c.out) + item_row(a, cur, jr, a.c.out_token_stride, a.c.out_head_stride) + kChunk<PER> * lane;
 #pragma unroll
-            for (int d = 0; d < PER / 2; ++d) w[d] = Pack<T>::two(acc[2 * d] * inv, acc[2 * d + 1] * inv);
-            if constexpr (PER == 16) {
-                reinterpret_cast<uint4 *>(dst)[0] = make_uint4(w[0], w[1], w[2], w[3]);
-                reinterpret_cast<uint4 *>(dst)[1] = make_uint4(w[4], w[5], w[6], w[7]);
-            } else if constexpr (PER == 8) *reinterpret_cast<uint4 *>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
-            else if constexpr (PER == 4) *reinterpret_cast<uint2 *>(dst) = make_uint2(w[0], w[1]);
-            else *reinterpret_cast<uint32_t *>(dst) = w[0];
+        for (int d = 0; d < PER; d += kChunk<PER>) {
+            if (kChunk<PER> * lane + d / kChunk<PER> * kStep >= a.dim) continue;
+            const uint32_t two = Pack<T>::two(acc[d] * inv, acc[d + 1] * inv);
+            if constexpr (kChunk<PER> == 2) *reinterpret_cast<uint32_t *>(dst) = two;
+            else *reinterpret_cast<uint2 *>(dst + d / 4 * kStep) = make_uint2(two, Pack<T>::two(acc[d + 2] * inv, acc[d + 3] * inv));
         }
-        if (a.c.lse && jd == 0)
+        if (a.c.lse && lane == 0)
             a.c.lse[item_row(a, cur, jr, a.c.q_heads, 1)] =
                 sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
     }

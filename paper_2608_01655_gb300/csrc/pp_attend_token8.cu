@@ -43,7 +43,9 @@ template <int ROWS, int HALVES> struct Layout8 {
     // of a thread: the launch's 128 (168 for 12 warps), shared out
     static constexpr int output_registers = ROWS == 8 ? 80 : 88, registers = ROWS == 8 ? 144 : 208;
     static_assert(128 * output_registers + 32 * warps * registers <= threads * (ROWS == 8 ? 128 : 168), "registers of a CTA");
-    using Shape = ShapeOf<ROWS, kKeys * warps>;
+    // an item's weight: 8 rows 2, 3, 5 tiles: 128 tokens after 200 to 16,000 133, 128, 132 us, 300 after 50 to 3,000 48, 47,
+    // 50; 16 rows 3, 6, 9: 60 requests x 4 after 50 to 9,000 84, 68, 68, 20 x 3 after 100 to 5,000 26, 27, 45
+    using Shape = ShapeOf<ROWS, kKeys * warps, ROWS == 8 ? 3 : 6>;
 };
 }  // namespace token
 
@@ -503,7 +505,7 @@ __device__ __forceinline__ void output_role(const AttendDev &a, Shared8<ROWS, HA
     using L = Layout8<ROWS, HALVES>;
     using Shape = typename L::Shape;
     constexpr int per = L::width * ROWS / 128;
-    const int t = threadIdx.x & 127, jr = t / (128 / ROWS), jd = t % (128 / ROWS) * per;
+    const int t = threadIdx.x & 127, jr = t / (128 / ROWS), lane = t % (128 / ROWS);
     const int64_t total = sh.sched.total, ctas = min((int64_t)gridDim.x, total);
     Cursor<Shape> cur(a, sh.sched);
     do {
@@ -518,10 +520,10 @@ __device__ __forceinline__ void output_role(const AttendDev &a, Shared8<ROWS, HA
         for (int w = 0; w < L::warps; ++w) {
             const float f = exp2_approx(sh.stat[0][w][jr] - at);
             sum = fmaf(f, sh.stat[1][w][jr], sum);
-            const float4 *src = reinterpret_cast<const float4 *>(join + (w * ROWS + jr) * L::pitch + jd);
+            const float4 *src = reinterpret_cast<const float4 *>(join + (w * ROWS + jr) * L::pitch) + lane;
 #pragma unroll
             for (int d = 0; d < per; d += 4) {
-                const float4 y = src[d / 4];
+                const float4 y = src[d / 4 * (128 / ROWS)];
                 acc[d] = fmaf(f, y.x, acc[d]);
                 acc[d + 1] = fmaf(f, y.y, acc[d + 1]);
                 acc[d + 2] = fmaf(f, y.z, acc[d + 2]);
