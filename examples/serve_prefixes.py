@@ -1,6 +1,6 @@
 """Serve from a planned target: from pp_plan_run to attention over the worker's cache.
 
-    python examples/serve_prefixes.py [requests [decode steps]]
+    python examples/serve_prefixes.py [requests [decode steps [8]]]
 
 Plans the tiny workload, lays worker 0's resident chunks out as blocks of a paged
 K/V cache (pp_chunk_map) and stores their rows.  Then requests arrive whose
@@ -42,6 +42,21 @@ class Layer:
         return qkv.split((HEADS, KV_HEADS, KV_HEADS), dim=1)
 
 
+class RotatedLayer(Layer):
+    """Queries and keys normed and rotated to their positions, in place."""
+
+    def __init__(self, kv):
+        super().__init__()
+        self.kv, self.rotary = kv, pp.Rotary(DIM)
+        self.norm = torch.full((DIM,), 1.5, dtype=torch.bfloat16, device="cuda")
+
+    def __call__(self, token, position):
+        qkv = (self.embedding[token] @ self.weight).to(torch.bfloat16).unflatten(1, (-1, DIM))
+        q, k, v = qkv.split((HEADS, KV_HEADS, KV_HEADS), dim=1)
+        pp.pp_kv_rotate(self.kv, self.rotary, q, k, position.int(), q, k_out=k, q_weight=self.norm, k_weight=self.norm)
+        return q, k, v
+
+
 def chunk_tokens(chunk, count):
     return (chunk * 40_503 + np.arange(count) * 977) % VOCABULARY
 
@@ -54,7 +69,7 @@ def path_of(parent, chunk):
     return path[::-1]
 
 
-def run(requests=24, steps=4, seed=0):
+def run(requests=24, steps=4, seed=0, eight_bit=False):
     torch.cuda.set_device(0)
     rng = np.random.default_rng(seed)
     inst = wl.make(0)
@@ -79,11 +94,29 @@ def run(requests=24, steps=4, seed=0):
         sequence[r, len(ids):] = rng.integers(0, VOCABULARY, size=width * BLOCK - len(ids))     # what it will generate
     sequence = torch.tensor(sequence, device="cuda")
 
-    layer = Layer()
     blocks = used + requests * width
-    k_cache, v_cache = (torch.empty((blocks, BLOCK, KV_HEADS, DIM), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    k_cache, v_cache = (torch.empty((blocks, BLOCK, KV_HEADS, DIM), device="cuda",
+                                    dtype=torch.float8_e4m3fn if eight_bit else torch.bfloat16) for _ in range(2))
+    k_exp, v_exp = (torch.empty((blocks, KV_HEADS), dtype=torch.int8, device="cuda") for _ in range(2))
     i32 = lambda a: torch.tensor(np.asarray(a, np.int32), device="cuda")
     with pp.KVCache.like(k_cache) as kv:
+        layer = RotatedLayer(kv) if eight_bit else Layer()
+        workspace = torch.empty(kv.workspace_size(requests, width, int(-(-length // BLOCK).sum())) if eight_bit else 0,
+                                dtype=torch.uint8, device="cuda")
+
+        def write(k, v, slot):
+            if eight_bit:
+                pp.pp_kv_write8(kv, k, v, slot, k_cache, k_exp, v_cache, v_exp)
+            else:
+                pp.pp_kv_write(kv, k, v, slot, k_cache, v_cache)
+
+        def attend(q, table, q_start, now, max_q, out):
+            if eight_bit:
+                pp.pp_paged_attention8(kv, q, k_cache, k_exp, v_cache, v_exp, table, q_start, now, max_q, out, DIM ** -0.5,
+                                       workspace=workspace)
+            else:
+                pp.pp_paged_attention(kv, q, k_cache, v_cache, table, q_start, now, max_q, out, DIM ** -0.5)
+
         # the resident chunks' rows, as their materialisation would leave them
         for b in np.flatnonzero(resident):
             count = SLOT_TOKENS * int(inst.weight[b])
@@ -91,7 +124,7 @@ def run(requests=24, steps=4, seed=0):
             first = end * BLOCK - count
             position = torch.arange(first, first + count, device="cuda")
             _, k, v = layer(torch.tensor(chunk_tokens(b, count), device="cuda"), position)
-            pp.pp_kv_write(kv, k, v, position + (base - begin) * BLOCK, k_cache, v_cache)
+            write(k, v, position + (base - begin) * BLOCK)
 
         table = torch.full((requests, width), -1, dtype=torch.int32, device="cuda")
         free = torch.arange(used, blocks, dtype=torch.int32, device="cuda")
@@ -116,10 +149,9 @@ def run(requests=24, steps=4, seed=0):
                                               (q_start[1:] - q_start[:-1]).long())
             place = position[:fresh].long()
             q, k, v = layer(sequence[request, place], place)
-            pp.pp_kv_write(kv, k, v, slot[:fresh], k_cache, v_cache)
+            write(k, v, slot[:fresh])
             out = torch.empty((fresh, HEADS, DIM), dtype=torch.bfloat16, device="cuda")
-            pp.pp_paged_attention(kv, q, k_cache, v_cache, table, q_start, now_dev, int(np.diff(starts).max()), out,
-                                  DIM ** -0.5)
+            attend(q, table, q_start, now_dev, int(np.diff(starts).max()), out)
             kv.sync()
             if step == 0:
                 cached_tokens = int(now.sum()) - fresh
@@ -147,7 +179,7 @@ def check(layer, sequence, length, starts, out, some):
 
 
 if __name__ == "__main__":
-    result = run(*(int(x) for x in sys.argv[1:3]))
+    result = run(*(int(x) for x in sys.argv[1:3]), eight_bit=sys.argv[3:4] == ["8"])
     print(f"{result['resident_chunks']} chunks resident; of {result['prompt_tokens']} prompt tokens of "
           f"{result['requests']} requests {result['cached_tokens']} came from the cache; largest difference from "
           f"attention over whole prompts {result['worst_error']:.1e}")
