@@ -92,7 +92,7 @@ constexpr int64_t kFewRows = 32;
 
 pp_status launch_attend(pp_kv *kv, const AttendArgs &c, cudaStream_t st)
 {
-    return (int64_t)c.max_q * c.group <= kFewRows ? launch_attend_token(kv, c, st) : launch_attend_chunk(kv, c, st);
+    return (int64_t)c.max_q * c.group <= kFewRows ? launch_attend_token(kv, c, st) : launch_attend_chunk(kv, c, false, st);
 }
 
 }  // namespace pp

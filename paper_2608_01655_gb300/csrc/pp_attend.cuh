@@ -513,6 +513,6 @@ pp_status prepare_attend_chunk();
 pp_status launch_attend_token(pp_kv *kv, const AttendArgs &c, cudaStream_t st);
 pp_status prepare_attend_token8();
 pp_status launch_attend_token8(pp_kv *kv, const AttendArgs &c, cudaStream_t st);
-pp_status launch_attend_chunk(pp_kv *kv, const AttendArgs &c, cudaStream_t st);
+pp_status launch_attend_chunk(pp_kv *kv, const AttendArgs &c, bool beside, cudaStream_t st);
 
 }  // namespace pp

@@ -1006,7 +1006,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (tid < kBad) sh.bad[tid] = 0;
-    if (!schedule<Shape>(a, sh.sched)) return;
+    // What comes from the kernel before, where this one was launched beside its end (pp_kv8.cu): table and rows.  All
+    // CTAs wait for it, so that this kernel's end is its end too.
+    auto wait_for_rows = [] { asm volatile("griddepcontrol.wait;" ::: "memory"); };
+    if (!schedule<Shape>(a, sh.sched)) {
+        wait_for_rows();
+        return;
+    }
     if (warp == 12) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&sh.tmem)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
@@ -1015,6 +1021,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
     __syncthreads();
     tc_after();
     const uint32_t tmem = sh.tmem;
+
+    wait_for_rows();
 
     // 512 threads x 128 registers = 128 x (2 for softmax + for output + for the others)
     constexpr int kSoftmax = HALVES == 2 ? 144 : 128, kOutput = HALVES == 2 ? 144 : 160, kOthers = 512 - 2 * kSoftmax - kOutput;
@@ -1051,7 +1059,7 @@ template <typename T, int HALVES> static cudaError_t prepare_t()
 }
 
 template <typename T, int HALVES>
-static pp_status launch_t(pp_kv *kv, const AttendArgs &c, cudaStream_t st)
+static pp_status launch_t(pp_kv *kv, const AttendArgs &c, bool beside, cudaStream_t st)
 {
     const AttendDev a = attend_dev(kv, c);
     CUtensorMap km, vm;
@@ -1059,8 +1067,22 @@ static pp_status launch_t(pp_kv *kv, const AttendArgs &c, cudaStream_t st)
     pp_status s = cache_map(kv, c.k_cache, rows, &km);
     if (s == PP_OK) s = cache_map(kv, c.v_cache, rows, &vm);
     if (s != PP_OK) return s;
-    k_attend_chunk<T, HALVES><<<kv->sm_count, kThreads, shared_bytes<HALVES>(), st>>>(a, km, vm);
-    PP_CUDA(cudaGetLastError());
+    if (!beside) {
+        k_attend_chunk<T, HALVES><<<kv->sm_count, kThreads, shared_bytes<HALVES>(), st>>>(a, km, vm);
+        PP_CUDA(cudaGetLastError());
+        return PP_OK;
+    }
+    cudaLaunchAttribute early = {};
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t config = {};
+    config.gridDim = dim3(kv->sm_count);
+    config.blockDim = dim3(kThreads);
+    config.dynamicSmemBytes = shared_bytes<HALVES>();
+    config.stream = st;
+    config.attrs = &early;
+    config.numAttrs = 1;
+    PP_CUDA(cudaLaunchKernelEx(&config, k_attend_chunk<T, HALVES>, a, km, vm));
     return PP_OK;
 }
 
@@ -1073,11 +1095,12 @@ pp_status prepare_attend_chunk()
     return PP_OK;
 }
 
-pp_status launch_attend_chunk(pp_kv *kv, const AttendArgs &c, cudaStream_t st)
+// beside: the kernel before lets this one start while it ends; only its last CTAs' results are waited for.
+pp_status launch_attend_chunk(pp_kv *kv, const AttendArgs &c, bool beside, cudaStream_t st)
 {
     if (kv->dtype == PP_KV_BF16)
-        return kv->dim > 64 ? launch_t<__nv_bfloat16, 2>(kv, c, st) : launch_t<__nv_bfloat16, 1>(kv, c, st);
-    return kv->dim > 64 ? launch_t<__half, 2>(kv, c, st) : launch_t<__half, 1>(kv, c, st);
+        return kv->dim > 64 ? launch_t<__nv_bfloat16, 2>(kv, c, beside, st) : launch_t<__nv_bfloat16, 1>(kv, c, beside, st);
+    return kv->dim > 64 ? launch_t<__half, 2>(kv, c, beside, st) : launch_t<__half, 1>(kv, c, beside, st);
 }
 
 }  // namespace pp

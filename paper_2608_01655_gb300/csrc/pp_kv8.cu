@@ -436,6 +436,8 @@ template <typename T> __global__ void __launch_bounds__(kUnpackThreads, 2) k_unp
     const AttendDev &a = u.a;
     const int tid = threadIdx.x, lane = tid & 31;
     int32_t *const low = pre + a.c.requests;
+    // the attention's launch and its cut of the work, which need nothing from here, go beside this kernel's end
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int32_t R = a.c.requests, per = (R + kUnpackThreads - 1) / kUnpackThreads;
     const int32_t first = min(tid * per, R), past = min(first + per, R);
     int64_t mine = 0, excl;
@@ -561,7 +563,7 @@ static pp_status launch_attend8(pp_kv *kv, AttendArgs c, void *workspace, int64_
     c.k_cache = u.k;
     c.v_cache = u.v;
     c.block_table = u.table;
-    return launch_attend_chunk(&wide, c, st);
+    return launch_attend_chunk(&wide, c, true, st);
 }
 
 static pp_status check_exps(const void *k_exp, const void *v_exp)
