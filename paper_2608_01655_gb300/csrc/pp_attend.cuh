@@ -33,10 +33,16 @@ struct AttendDev {
     float *piece;                       // pieces' outputs, [slot][...]
     float *piece_stat;                  // their maxima (log2 units) and sums
     int32_t *count;                     // [2][slots] state of the joins, left at 0 by every launch
+    int32_t few_pieces;                 // stretches are long enough that a join takes no longer than they do
     int64_t wait_limit;                 // cycles after which one wait gives up
     uint32_t lost;                      // bytes of a K tile that are waited for and never come (tests)
 };
 
+// With few_pieces: what a piece costs its item's join, in tiles.  Of an item of T tiles in stretches of s the
+// last ends after s + kPieceTiles T / s tiles, least with s = sqrt(kPieceTiles T).  Stretches of less than two tiles
+// are left alone.  2 requests of 85 tokens after 9,300 and 11,200 (2 heads on 1), one tile a stretch 60 us and more, with
+// 0.15, 0.42, 1.2 32, 40, 44; 34 after 20,000 (8 on 2) 52, 40, 41, 49; 100 after 50,000 (16 on 2) 68, 67, 67, 69.
+constexpr float kPieceTiles = 0.15f;
 constexpr int64_t kAttendLimitCycles = 4000ll * 1000 * 1000;  // about 2 s
 constexpr int64_t kAttendTestCycles = 4ll * 1000 * 1000;      // about 2 ms, while pp_test_inject has copies lost
 
@@ -87,7 +93,7 @@ struct Place {
 };
 struct SchedShared {
     int64_t warp_sum[32];
-    int64_t total, begin;
+    int64_t total, begin, ctas;
     int32_t count, extra;
     Place first, end;                   // where the stretch begins; the tile after it
 };
@@ -196,9 +202,14 @@ template <class S> __device__ __forceinline__ bool schedule(const AttendDev &a, 
     if (tiles == 0) return false;
     // with few tiles a CTA, every tile to a CTA of its own counts more than an even load; every stretch has a tile
     const int32_t extra = tiles >= (S::extra < 4 ? 4 : S::extra + 1) * (int64_t)gridDim.x ? S::extra : 0;
-    const int64_t total = tiles + (extra ? scan64(items, &excl_items, sm.warp_sum, few) * outer * extra : 0);
+    const int64_t all_items = extra || a.few_pieces ? scan64(items, &excl_items, sm.warp_sum, few) * outer : 0;
+    const int64_t total = tiles + all_items * extra;
     excl += excl_items * extra;
-    const int64_t ctas = min((int64_t)gridDim.x, total);
+    int64_t ctas = min((int64_t)gridDim.x, total);
+    if (a.few_pieces) {
+        const float least = sqrtf(kPieceTiles * (float)tiles / (float)all_items);
+        if (least >= 2.f) ctas = min(ctas, max((int64_t)((float)total / least), (int64_t)1));
+    }
     if (blockIdx.x >= ctas) return false;
     const int64_t begin = quotient(total * blockIdx.x, ctas), end = quotient(total * (blockIdx.x + 1), ctas);
     for (int32_t base = 0; base < R; base += T) {
@@ -254,6 +265,7 @@ template <class S> __device__ __forceinline__ bool schedule(const AttendDev &a, 
         sm.extra = extra;
         sm.begin = begin;
         sm.total = total;
+        sm.ctas = ctas;
     }
     __syncthreads();
     return true;

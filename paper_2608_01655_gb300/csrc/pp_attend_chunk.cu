@@ -874,7 +874,7 @@ __device__ __forceinline__ void output_role(const AttendDev &a, const SchedShare
 {
     using L = Layout<HALVES>;
     const int t = threadIdx.x & 127;
-    const int64_t line = sched.total, ctas = min((int64_t)gridDim.x, line);
+    const int64_t line = sched.total, ctas = sched.ctas;
     Cursor<Shape> cur(a, sched);
     uint32_t turn[2] = {0, 0};
     int32_t item = 0;
@@ -1061,7 +1061,8 @@ template <typename T, int HALVES> static cudaError_t prepare_t()
 template <typename T, int HALVES>
 static pp_status launch_t(pp_kv *kv, const AttendArgs &c, bool beside, cudaStream_t st)
 {
-    const AttendDev a = attend_dev(kv, c);
+    AttendDev a = attend_dev(kv, c);
+    a.few_pieces = beside;
     CUtensorMap km, vm;
     const int32_t rows = std::min(kv->block_size, KT);
     pp_status s = cache_map(kv, c.k_cache, rows, &km);
