@@ -101,6 +101,17 @@ for _name, _args in _SIGS.items():
     _f = getattr(_lib, _name)
     _f.argtypes = _args
     _f.restype = _st
+# The cache's calls and tensor checks, made many times a serving step, through an extension module instead of
+# ctypes; where Python's headers were missing at the build, they stay here.
+try:
+    from . import _pp_call as _fast
+except ImportError:
+    _fast = None
+if _fast is not None:
+    _KINDS = {_P: "p", _i32: "i", _i64: "l", ctypes.c_float: "f", ctypes.c_size_t: "z"}
+    for _name in ("pp_block_tables", "pp_kv_write", "pp_paged_attention", "pp_kv_rotate", "pp_kv_write8", "pp_paged_attention8"):
+        _fast.bind(_name, "".join(_KINDS[t] for t in _SIGS[_name]), ctypes.cast(getattr(_lib, _name), _P).value)
+        setattr(_lib, _name, getattr(_fast, _name))
 _lib.pp_dp_bits_size.argtypes = [_P, _i32, _i32]
 _lib.pp_dp_bits_size.restype = ctypes.c_size_t
 _lib.pp_last_error.argtypes = []
@@ -531,14 +542,22 @@ class KVCache:
 
     def _arg(self, t, name, dtype, shape):
         """Device pointer of a contiguous tensor of this type and shape on the handle's device."""
-        if t.dtype is dtype and t.shape == shape and t.get_device() == self._device and t.is_contiguous():
+        if _fast is not None:
+            pointer = _fast.contiguous(t, dtype, shape, self._device)
+            if pointer is not None:
+                return pointer
+        elif t.dtype is dtype and t.shape == shape and t.get_device() == self._device and t.is_contiguous():
             return t.data_ptr()
         raise ValueError(f"{name}: expected a contiguous tensor {list(shape)} of {dtype} on cuda:{self._device}, got "
                          f"{list(t.shape)} of {t.dtype} on {t.device}, strides {list(t.stride())}")
 
     def _cache(self, t, name):
         """Device pointer of a cache of this layout (an extent of 1 has no stride)."""
-        if t.dtype is (self._stored or self.dtype) and t.shape == self.shape and t.get_device() == self._device:
+        if _fast is not None:
+            pointer = _fast.cache(t, self._stored or self.dtype, self.shape, self.strides, self._device)
+            if pointer is not None:
+                return pointer
+        elif t.dtype is (self._stored or self.dtype) and t.shape == self.shape and t.get_device() == self._device:
             st = t.stride()
             if st[3] == 1 and (st[:3] == self.strides or
                                all(n == 1 or a == b for n, a, b in zip(self.shape, st, self.strides))):
@@ -548,7 +567,11 @@ class KVCache:
 
     def _rows(self, t, name, tokens, heads):
         """Pointer, token stride and head stride of [tokens][heads][head_dim] rows."""
-        if t.dtype is self.dtype and t.shape == (tokens, heads, self.shape[3]) and t.get_device() == self._device:
+        if _fast is not None:
+            found = _fast.rows(t, self.dtype, tokens, heads, self.shape[3], self._device)
+            if found is not None:
+                return found
+        elif t.dtype is self.dtype and t.shape == (tokens, heads, self.shape[3]) and t.get_device() == self._device:
             st = t.stride()
             if st[2] == 1 or not tokens:
                 # an extent of 1 may carry any stride

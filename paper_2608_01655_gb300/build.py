@@ -2,8 +2,9 @@
 
 Each .cu file under csrc/ is compiled in parallel, then linked into one
 shared library next to this file; the benchmark's bandwidth probe
-(probe/pp_probe.cu) becomes a library of its own, libpp_probe.so.  The CUDA
-runtime is linked statically, so the libraries need only the driver at run
+(probe/pp_probe.cu) becomes a library of its own, libpp_probe.so.  csrc/pp_call.c
+is a Python extension with the cache's calls, _pp_call, where Python's headers
+are installed.  The CUDA runtime is linked statically, so the libraries need only the driver at run
 time and no torch symbols.
 """
 from __future__ import annotations
@@ -12,6 +13,7 @@ import concurrent.futures as cf
 import os
 import shutil
 import subprocess
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -20,6 +22,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libprefixplace.so")
 PROBE_SRC = os.path.join(HERE, "probe", "pp_probe.cu")
 PROBE_LIB = os.path.join(HERE, "libpp_probe.so")   # the benchmark's bandwidth probe, not the planner
+CALL_SRC = os.path.join(CSRC, "pp_call.c")
+CALL_LIB = os.path.join(HERE, "_pp_call" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-I" + INCLUDE, "-I" + CSRC]
 
@@ -41,8 +45,17 @@ def _deps():
     return files
 
 
+def _python_include():
+    """Where Python.h is, None if it is not installed."""
+    path = sysconfig.get_paths()["include"]
+    return path if os.path.exists(os.path.join(path, "Python.h")) else None
+
+
 def up_to_date() -> bool:
     if not os.path.exists(LIB) or not os.path.exists(PROBE_LIB):
+        return False
+    if _python_include() and (not os.path.exists(CALL_LIB) or any(
+            os.path.getmtime(f) > os.path.getmtime(CALL_LIB) for f in (CALL_SRC, os.path.join(INCLUDE, "prefixplace.h")))):
         return False
     t = os.path.getmtime(LIB)
     tp = os.path.getmtime(PROBE_LIB)
@@ -75,10 +88,21 @@ def build(force: bool = False, verbose: bool = False, extra=()) -> str:
             raise RuntimeError(f"nvcc failed for {PROBE_SRC}:\n{r.stdout}\n{r.stderr}")
         os.replace(tmp, PROBE_LIB)
 
+    def build_call():
+        if not _python_include():
+            return
+        tmp = CALL_LIB + f".tmp{os.getpid()}"
+        cmd = [shutil.which("gcc") or "cc", "-O2", "-Wall", "-shared", "-fPIC", "-I" + _python_include(), "-I" + INCLUDE, CALL_SRC, "-o", tmp]
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        if r.returncode != 0:
+            raise RuntimeError(f"gcc failed for {CALL_SRC}:\n{r.stdout}\n{r.stderr}")
+        os.replace(tmp, CALL_LIB)
+
     with cf.ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as ex:
-        probe = ex.submit(build_probe)
+        probe, call = ex.submit(build_probe), ex.submit(build_call)
         objs = list(ex.map(compile_one, sources()))
         probe.result()
+        call.result()
     tmp = LIB + f".tmp{os.getpid()}"
     cmd = [nvcc, *ARCH, "-shared", "-o", tmp, *objs]
     r = subprocess.run(cmd, capture_output=True, text=True)

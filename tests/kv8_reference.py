@@ -126,8 +126,7 @@ def attention8(q, kc, ke, vc, ve, table, q_start, length, scale, window, direct)
         j = torch.arange(n, device=dev)
         pages, inv = torch.unique(table[r].long()[j // block], return_inverse=True)
         size = torch.exp2(ve[pages].double().clamp(LEAST, MOST))                          # [pages][h]
-        k = scaled(kc[pages] if kc.is_contiguous() else kc.view(torch.uint8)[pages].view(torch.float8_e4m3fn), ke[pages])
-        v = scaled(vc[pages] if vc.is_contiguous() else vc.view(torch.uint8)[pages].view(torch.float8_e4m3fn), ve[pages])
+        k, v = (scaled(c.view(torch.uint8)[pages].view(torch.float8_e4m3fn), e[pages]) for c, e in ((kc, ke), (vc, ve)))
         k = k[inv, j % block].permute(1, 2, 0)                                            # [h][d][n]
         v = v[inv, j % block].transpose(0, 1)                                             # [h][n][d]
         size = size[inv].transpose(0, 1)                                                  # [h][n]

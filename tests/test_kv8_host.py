@@ -125,8 +125,11 @@ def test_rotary_arguments(lib):
 CALLS = ("pp_kv_rotate", "pp_kv_write8", "pp_paged_attention8")
 
 
-@pytest.fixture
-def pp(lib, monkeypatch):
+@pytest.fixture(params=["extension", "Python"])
+def pp(lib, monkeypatch, request):
+    """The binding's checks, of the extension module and of the binding itself."""
+    if request.param == "Python":
+        monkeypatch.setattr(lib, "_fast", None)
     calls = []
     entry = lambda name: lambda *args: calls.append((name, args)) or 0
     monkeypatch.setattr(lib, "_lib", types.SimpleNamespace(**{n: entry(n) for n in CALLS + ("pp_kv_write", "pp_kv_destroy")}))
