@@ -656,8 +656,8 @@ pp_status pp_rotary_turns(int32_t pairs, const double *frequency, uint64_t *turn
  *   (y_a, y_b) -> amplitude (y_a cos t - y_b sin t, y_b cos t + y_a sin t)
  * with t = position * frequency i for pair i < rotated / 2, (a, b) = (i, i +
  * rotated / 2) or, interleaved, (2 i, 2 i + 1); elements from `rotated` on are y.
- * All of it in 32 bits, rounded once; rows that are neither normed nor rotated
- * keep their bits.  The handle gives head_dim, kv_heads and the 16-bit type; where
+ * All of it in 32 bits, rounded once; elements that are neither normed nor rotated
+ * keep their bits (a NaN stays a NaN).  The handle gives head_dim, kv_heads and the 16-bit type; where
  * no cache is given its own may be of either kind.
  *   tokens        0 .. 2^30
  *   q_heads       0 .. 2^20; with 0, q and q_out are not looked at

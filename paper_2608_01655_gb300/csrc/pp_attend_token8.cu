@@ -23,6 +23,16 @@
 // together, and an operand's rows are the even columns, then the odd ones.
 // The cut of the work and the ring of copies are those of the 16-bit kernel; a warp's 16
 // keys are 4 KB here.
+//
+// Bound by memory, half the 16-bit kernel's bytes, with little room for instructions: a
+// code is widened, two to an instruction, on the pipe that the softmax uses too (57% of
+// its cycles; all 55% of the issue slots, matrix instructions 16%).  12 warps at the
+// products and four that join and store beside them: 128 tokens after 200 to 16,000, 28
+// heads on 4 of 128, take 130 us (763 MB, 5.8 TB/s; 112 at the rate of a copy), where
+// rows as the larger operand, 16 of them, took 172, and transposed products without
+// warps for the outputs 150.  2 after 131,000 and 200,000: 41 us a call in a graph (26 at
+// the rate of a copy; 5.5 before the first products, 26 of tiles, 8 to 10 of joins), 4
+// after 36 to 900: 11.
 #include "pp_attend_token.cuh"
 
 namespace pp {

@@ -282,6 +282,12 @@ __device__ __forceinline__ void write_singles(const Write8Args &a, int32_t t0, i
 // 32 tokens to either side.  A run's rows of one head and of K or V are a team's, a warp
 // for every kWrite8Held steps of them, TEAMS warps at most; those of runs of one token go
 // several to a warp.
+// Three bytes an element, all read and written once where a run fits kWrite8Held steps; a
+// run's chain of slots, rows, largest size and codes is what takes the time: 30,011 tokens
+// of 4 heads of 128 take 23 us from cold caches (14 at the rate of a copy, 60% of the issue
+// slots), with blocks of 32 28, of 64 29, of 512 52; as 30,011 runs of one token (2 heads)
+// 35.  64 single tokens of 2 heads: 2.7 us a call in a graph.  K and V of a head by one
+// warp together: 25 us for 30,011 tokens, 3.7 for 64.
 template <typename T, int TEAMS>
 __global__ void __launch_bounds__(kWrite8Threads, kWrite8Ctas) k_kv_write8(const __grid_constant__ Write8Args a)
 {
@@ -427,8 +433,11 @@ __device__ __forceinline__ Keys seen_blocks(const AttendDev &a, const Req &q)
 // Every CTA sums up the requests' visible blocks (8 bytes a request, from L2 after the
 // first) and a warp takes up to 16 rows of a block and head at a time, numbered through
 // all requests; a lane has one piece of 16 codes of every few rows.  A block that several
-// requests see is unpacked for each.  Bound by memory: a byte read and two written, which
-// the attention then reads, mostly from L2.
+// requests see is unpacked for each.  A byte read and two written, which the attention
+// then reads, mostly from L2: 20 us for 32,768 tokens of 4 heads of 128 (100 MB, 5 TB/s),
+// 13 for 8 requests of up to 8,900 tokens and 2 heads, 43 for 24 of up to 8,000 with 16
+// heads of 64.  The short ones wait for the requests' sums and for three loads in a row
+// (table, exponents, codes); the attention's launch and its cut of the work go beside them.
 template <typename T> __global__ void __launch_bounds__(kUnpackThreads, 2) k_unpack8(const __grid_constant__ Unpack8Args u)
 {
     extern __shared__ int32_t pre[];                    // blocks before request r, then its first
@@ -530,8 +539,8 @@ static int64_t block_bytes(const pp_kv *kv) { return (int64_t)2 * kv->heads * kv
 // are unpacked, which costs 15 us and more, and take 256 rows whatever there are.  In us,
 // 2 K/V heads of 128, single passes after a flush of L2, 32 requests after 5,000 tokens /
 // 4 after 2,000 / 1 after 50,000 (64 rows here by items of 16):
-//   32 rows   68 : 104 / 25 : 43 / 35 : 74
-//   64       123 : 104 / 23 : 43 / 47 : 74
+//   32 rows   68 : 104 / 25 : 37 / 35 : 70
+//   64       123 : 104 / 23 : 37 / 47 : 70
 // In between the batch's times meet at some 52.
 constexpr int64_t kFewRows8 = 48;
 

@@ -131,6 +131,11 @@ __device__ __forceinline__ void angle(int32_t position, uint64_t turns, float am
 //   y_a' = n (x_a (w_a cos) - x_b (w_b sin)),  y_b' = n (x_b (w_b cos) + x_a (w_a sin)).
 // Bound by memory, 4 bytes an element: each lane copies its vectors of the next rows to
 // places of its own in shared memory, so that many are on their way without registers.
+// 30,011 tokens of 28 + 4 heads of 128 with norms, into the cache: 100 us from cold
+// caches, 5.5 TB/s (82 us at the rate of a copy); without norms 85.  The norms' sums and
+// products are a third of the instructions, which take 60% of the issue slots.  3 or 6
+// rows ahead and 5 or 6 CTAs an SM were no faster than 4 and 4.  64 tokens of 16 + 2
+// heads: 3.7 us a call in a graph.
 template <typename T, int LAYOUT, int LANES, bool NORM>
 __global__ void __launch_bounds__(kRotateThreads, kRotateCtas) k_kv_rotate(const __grid_constant__ RotateArgs a)
 {
