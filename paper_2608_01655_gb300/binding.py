@@ -3,10 +3,10 @@
 Argument marshalling only: every step of the planner runs in the library's
 CUDA kernels.  Calls go by ctypes; those of the paged cache, which a step makes
 for every layer, and the checks of their tensors go by a small extension module
-(csrc/pp_call.c) where it has been built, which takes 2 us less a call.  Device buffers are torch CUDA tensors (PyTorch provides device
-memory and streams, nothing else); host buffers are numpy arrays.  If the
-library has not been built, importing this module raises ImportError: there is
-no CPU fallback.
+(csrc/pp_call.c) where it has been built, which takes 2 us less a call.  Device
+buffers are torch CUDA tensors (PyTorch provides device memory and streams,
+nothing else); host buffers are numpy arrays.  If the library has not been
+built, importing this module raises ImportError: there is no CPU fallback.
 """
 from __future__ import annotations
 
