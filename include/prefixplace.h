@@ -735,8 +735,9 @@ pp_status pp_kv_workspace(const pp_kv *kv, int32_t requests, int32_t table_width
  *   workspace     device, aligned to 32 bytes, pp_kv_workspace bytes or more.  Not
  *                 looked at where max_q * (q_heads / kv_heads) <= 48
  * Calls of few rows (that limit) read codes and exponents directly: products of codes
- * with queries of 11 significant bits (bf16's 8 fit) and 32-bit sums, weights rounded
- * to 11 bits for their product with V.  Calls of chunks unpack what the queries see
+ * with queries of 11 significant bits (bf16's 8 fit) and 32-bit sums; for their product
+ * with V weights times their blocks' V scales are rounded to 11 bits down to 2^-29 of a
+ * row's largest, and are off by 2^-40 of that below.  Calls of chunks unpack what the queries see
  * into the workspace as rows of the 16-bit type and then are as pp_paged_attention.
  * Unpacking is exact in bf16; in f16 beyond 65504 becomes that, and below 2^-14 it is
  * off by 2^-25 at most.

@@ -5,12 +5,16 @@
 //   o = sum_j exp(s_j) 2^ve c_j / sum_j exp(s_j).
 // Codes become 16-bit floating numbers exactly, and stay without their scales: K's
 // multiplies the score, V's is added to it in log2 units.  So a weight is
-//   w_j = exp2(s_j log2(e) + ve - m),  m = max over j of s_j log2(e) + ve,
-// at most 1 whatever the blocks' sizes are, and the sum below is of w_j 2^-ve.  (ve is
-// from -40 to 40: a weight that is lost below 2^-126 is less than 2^-46 of that sum.)
+//   w_j = exp2(s_j log2(e) + ve - m),  m = max over j of s_j log2(e) + ve - 15,
+// at most 2^15 whatever the blocks' sizes are, and the sum below is of w_j 2^-ve.  (ve is
+// from -40 to 40: a weight that is lost below 2^-126 is less than 2^-61 of that sum.)
 // Queries become 16-bit numbers of 11 bits with a power of two for each row, its
 // largest value near 2^14: bf16's 8 bits fit, and what falls below 2^-24 is 2^-38 of
-// the row's largest.  Weights are rounded to 11 bits for their product.
+// the row's largest.  Weights are rounded to 16-bit numbers for their product, the sum is
+// of unrounded ones: 11 bits down to 2^-29 of the largest, below that off by 2^-40 of it.
+// So 2^20 keys lose 2^-11 of the scale of the largest one's block at most (448 of them
+// 2^-40 each), about e4m3's own last step at that scale, 2^-10.  With weights up to 1
+// instead of 2^15, many small ones beside a large one were part of the sum alone.
 //
 // An item is 8 or 16 rows (new token, query head) of one K/V head.  The products are
 // transposed, keys and the head's elements outside, the rows inside: S^T = K Q^T, O^T =
@@ -258,6 +262,7 @@ template <int ROWS, int HALVES> struct Shared8 {
     int32_t last;
 };
 constexpr int kJoinFull = 1, kJoinFree = 2, kOutput = 3;        // named barriers
+constexpr float kTopWeight = 15.f;                              // log2 of the largest weight: f16 ends at 2^16
 
 // The products of a warp's keys, item after item.
 template <typename T, int ROWS, int HALVES>
@@ -448,7 +453,7 @@ __device__ __forceinline__ void product_role(const AttendDev &a, Shared8<ROWS, H
                 for (int b = 0; b < NB; ++b) {
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
-                        const float at = m[b][y] == -INFINITY ? 0.f : m[b][y];
+                        const float at = m[b][y] == -INFINITY ? 0.f : m[b][y] - kTopWeight;
 #pragma unroll
                         for (int n = 0; n < 2; ++n) {
                             sc[b][2 * n + y] = exp2_approx(sc[b][2 * n + y] - at);
@@ -494,7 +499,7 @@ __device__ __forceinline__ void product_role(const AttendDev &a, Shared8<ROWS, H
                 l[b][y] += __shfl_xor_sync(~0u, l[b][y], 8);
                 l[b][y] += __shfl_xor_sync(~0u, l[b][y], 16);
                 if (g == 0) {
-                    sh.stat[0][warp][row] = m[b][y];
+                    sh.stat[0][warp][row] = m[b][y] - kTopWeight;
                     sh.stat[1][warp][row] = l[b][y];
                 }
                 float *dst = join + (warp * ROWS + row) * L::pitch + 2 * g;

@@ -95,9 +95,10 @@ def scaled(code, exponent):
 # ---------------------------------------------------------------------------
 # Attention
 # ---------------------------------------------------------------------------
-def attention8(q, kc, ke, vc, ve, table, q_start, length, scale, window, direct):
+def attention8(q, kc, ke, vc, ve, table, q_start, length, scale, window, direct, lost=2.0 ** -25):
     """out and lse in 64 bits, and bounds of their errors.  direct: the kernel that reads codes; else that of
-    rows unpacked to q's type.
+    rows unpacked to q's type.  lost: the largest error of a weight below its 16-bit type's normal range, of the
+    largest w_j 2^ve_j (direct).
 
     With u the unit roundoff of the type, D the head dimension, w_j the weights
     relative to the largest and l = sum w_j >= 1:
@@ -107,7 +108,7 @@ def attention8(q, kc, ke, vc, ve, table, q_start, length, scale, window, direct)
                the exponential; unpacked f16: 2^-25 of each k;
                a weight's relative error is 2 c at most;
       weights  direct: 2^-11 w |v| each, and below f16's normal range, whose unit is the
-               largest w_j 2^ve_j, 2^-25 of that times the code;
+               largest w_j 2^ve_j, `lost` of that times the code;
                unpacked: u w |v|, in f16 below its normal range 2^-25 |v|;
       V        unpacked f16: 2^-25;
       output   u |o|, in f16 at least 2^-25."""
@@ -154,7 +155,7 @@ def attention8(q, kc, ke, vc, ve, table, q_start, length, scale, window, direct)
             lse_tol[x] = c.reshape(heads) + 2.0 ** -20 * (1 + lse[x].abs())
             if direct:
                 unit = (w * sz).amax(-1, keepdim=True)                                    # what a weight of 1 stands for
-                low = 2.0 ** -25 * unit * (vv.abs() / sz.transpose(1, 2)).sum(1)[:, None] / l
+                low = lost * unit * (vv.abs() / sz.transpose(1, 2)).sum(1)[:, None] / l
                 weights = 2.0 ** -11 * mass + low
             else:
                 weights = u * mass + tiny * (vv.abs().sum(1)[:, None] / l + 1)
