@@ -641,8 +641,10 @@ pp_status pp_rotary_frequencies(int32_t pairs, double base, double factor, doubl
 /*
  * pp_rotary_turns -- host-only: frequencies (radians a token, any finite ones) as
  * 64-bit fractions of a turn, what pp_kv_rotate takes: position times turns modulo
- * 2^64 is exact, so an angle is as good at the last position as at the first
- * (off by 2^-53 of itself before whole turns go, and by 2^-31 rad).
+ * 2^64 is exact, so whole turns go without a rounding at the last position as at the
+ * first.  A stored fraction is off by 2^-52 of the frequency and 2^-65 of a turn, an angle
+ * by `position` times that and, where pp_kv_rotate makes a 32-bit number of it, by 2^-23
+ * rad more (its top 32 bits, then 24 of them).
  *   frequency     host [pairs]
  *   turns         host [pairs] out
  * Errors: PP_EINVAL.

@@ -115,7 +115,8 @@ template <typename T> __device__ __forceinline__ uint4 pack8(const uint64_t (&x)
 }
 
 // cos and sin of position * frequency.  `turns` is the frequency as a 64-bit fraction of
-// a turn: the product modulo 2^64 is exact, and its high half a signed fraction.
+// a turn: the product modulo 2^64 is exact, and its high half a signed fraction (cut to
+// 2^-29.3 rad, then rounded to 24 bits: 2^-23.3 rad).
 __device__ __forceinline__ void angle(int32_t position, uint64_t turns, float amplitude, float &cos, float &sin)
 {
     const int32_t part = (int32_t)((uint64_t)(int64_t)position * turns >> 32);
@@ -419,8 +420,10 @@ extern "C" pp_status pp_rotary_turns(int32_t pairs, const double *frequency, uin
     for (int32_t i = 0; i < pairs; ++i)
         if (!std::isfinite(frequency[i])) return fail(PP_EINVAL, "frequencies must be finite");
     for (int32_t i = 0; i < pairs; ++i) {
-        const double t = frequency[i] / 6.283185307179586, part = t - std::floor(t);
-        turns[i] = part < 1.0 ? (uint64_t)std::ldexp(part, 64) : 0;     // a tiny negative frequency rounds to a whole turn
+        // of the size, so that what is below a whole turn keeps its bits whatever the sign is
+        const double t = std::fabs(frequency[i]) / 6.283185307179586;
+        const uint64_t part = (uint64_t)std::rint(std::ldexp(t - std::floor(t), 64));
+        turns[i] = frequency[i] < 0 ? 0 - part : part;
     }
     return PP_OK;
 }
