@@ -11,6 +11,7 @@
 #include <type_traits>
 
 #include "pp_attend.cuh"
+#include "pp_rotate_lanes.h"
 
 namespace pp {
 
@@ -142,23 +143,14 @@ __global__ void __launch_bounds__(kRotateThreads, kRotateCtas) k_kv_rotate(const
 {
     __shared__ uint4 ahead[kRotateAhead][2][kRotateThreads];
     constexpr int kGroups = 32 / LANES;                 // of a warp
-    const int lane = threadIdx.x % 32 % LANES, of_warp = threadIdx.x % 32 / LANES;
+    const int32_t turned = LAYOUT == kHalf ? a.rotated / 16 : -1;       // lanes with vectors of pairs
+    const RotateLane vectors = rotate_lane(threadIdx.x, LANES, a.per_head, turned);
+    const int lane = vectors.lane, of_warp = vectors.of_warp;
     const int64_t group = ((int64_t)blockIdx.x * (kRotateThreads / 32) + threadIdx.x / 32) * kGroups + of_warp;
     const int32_t t = (int32_t)min(group / a.split, (int64_t)a.tokens - 1), share = (int32_t)(group % a.split);
     const bool in = of_warp < kGroups && group < (int64_t)a.tokens * a.split;
-
-    // this lane's vectors, from per_head on: none
-    const int32_t turned = LAYOUT == kHalf ? a.rotated / 16 : 0;        // lanes with vectors of pairs
-    const bool first_half = LAYOUT == kHalf && lane < turned;
-    int32_t at[2];
-    if (LAYOUT == kHalf) {                              // the other lanes' in two stretches
-        const int32_t others = (a.per_head - 2 * turned + 1) / 2;
-        at[0] = lane < turned + others ? lane + (first_half ? 0 : turned) : a.per_head;
-        at[1] = lane < turned + others ? at[0] + (first_half ? turned : others) : a.per_head;
-    } else {
-        at[0] = lane;
-        at[1] = lane + LANES;
-    }
+    const bool first_half = LAYOUT == kHalf && vectors.at[0] < turned;
+    const int32_t at[2] = {vectors.at[0], vectors.at[1]};     // this lane's vectors, from per_head on: none
     const bool has[2] = {at[0] < a.per_head, at[1] < a.per_head};
 
     int64_t cache = -1;                                 // the token's place in the caches
@@ -362,8 +354,8 @@ __global__ void __launch_bounds__(kRotateThreads, kRotateCtas) k_kv_rotate(const
                         const int32_t d = 8 * at[i / 8] + i % 8 + z, p = d < pairs ? d + pairs : d - pairs;
                         if (norm) y[z] = by * (y[z] * w[i + z]);
                         if (has[i / 8] && d < a.rotated) {
-                            const int v = p / 8;        // the vector, at lane v % LANES
-                            const T *from = reinterpret_cast<const T *>(&ahead[place][v / LANES][threadIdx.x - lane + v % LANES]);
+                            const T *from = reinterpret_cast<const T *>(
+                                &ahead[place][rotate_which(LANES, p / 8)][rotate_holder(threadIdx.x, LANES, p / 8)]);
                             float other = KvType<T>::to_float(from[p % 8]);
                             if (norm) other = by * (other * KvType<T>::to_float(reinterpret_cast<const T *>(weight)[p]));
                             y[z] = y[z] * cos[i + z] + (d < pairs ? -other : other) * sin[i + z];
@@ -503,7 +495,7 @@ extern "C" pp_status pp_kv_rotate(pp_kv *kv, int32_t tokens, int32_t q_heads, co
     }
     a.status = kv->d_status;
     const int layout = interleaved ? kInterleaved : rotated % 16 == 0 ? kHalf : kHalfOdd;
-    const int lanes = kv->dim > 96 ? 8 : kv->dim > 80 ? 6 : kv->dim > 64 ? 5 : kv->dim > 32 ? 4 : kv->dim > 16 ? 2 : 1;
+    const int lanes = rotate_lanes(kv->dim);
     const int32_t rows = q_heads + kv->heads * (caches ? 2 : 1);
     // How many groups share a token's rows: all groups take rounds of as many as the SMs hold, of rows and of the
     // token's angles, which take as long as some kAngleRows rows.  30,011 tokens of 36 rows: 3.1 rounds of whole
