@@ -483,7 +483,7 @@ enum { PP_KV_BF16 = 0, PP_KV_F16 = 1, PP_KV_BF16_E4M3 = 16, PP_KV_F16_E4M3 = 17 
  *   stream        stream of the set-up; the call synchronises it
  *   out           receives the handle (NULL on failure)
  * The handle owns a device status word and 40 MB of scratch of the attention
- * (on 152 SMs).  Its device (the current one) must be current in later calls.  pp_kv_sync reads
+ * (on 152 SMs), for 8-bit caches 4 bytes a block more.  Its device (the current one) must be current in later calls.  pp_kv_sync reads
  * the status.  pp_paged_attention calls on one handle use its scratch and must
  * not overlap on the GPU; on one stream they never do.  No call after this one
  * allocates or synchronises, so all can be captured in a CUDA graph.
@@ -499,7 +499,8 @@ pp_status pp_kv_destroy(pp_kv *kv);
  * pp_kv_sync -- synchronise `stream`, then read and clear the handle's device
  * status word.  Returns PP_OK, PP_EBOUNDS (a length, block, slot, chunk or
  * token count given in device memory was out of range; what it would have
- * reached was left out), PP_ETIMEOUT or PP_ECUDA.
+ * reached was left out; or a map of pp_kv_write8 with a block's tokens apart),
+ * PP_ETIMEOUT or PP_ECUDA.
  */
 pp_status pp_kv_sync(pp_kv *kv, void *stream);
 

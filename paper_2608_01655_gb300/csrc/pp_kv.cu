@@ -512,6 +512,10 @@ extern "C" pp_status pp_kv_create(int32_t blocks, int32_t block_size, int32_t kv
         const size_t count_bytes = 4 * slots * sizeof(int32_t);
         PP_CUDA(cudaMalloc(&kv->d_count, count_bytes));
         PP_CUDA(cudaMemsetAsync(kv->d_count, 0, count_bytes, (cudaStream_t)stream));
+        if (kv->eight) {
+            PP_CUDA(cudaMalloc(&kv->d_claim, (size_t)kv->blocks * sizeof(int32_t)));
+            PP_CUDA(cudaMemsetAsync(kv->d_claim, 0xff, (size_t)kv->blocks * sizeof(int32_t), (cudaStream_t)stream));
+        }
         PP_CUDA(cudaStreamSynchronize((cudaStream_t)stream));
         return PP_OK;
     };
@@ -535,6 +539,7 @@ extern "C" pp_status pp_kv_destroy(pp_kv *kv)
         cudaFree(kv->d_piece);
         cudaFree(kv->d_piece_stat);
         cudaFree(kv->d_count);
+        cudaFree(kv->d_claim);
         cudaSetDevice(cur);
     }
     delete kv;
@@ -556,7 +561,7 @@ extern "C" pp_status pp_kv_sync(pp_kv *kv, void *stream)
     PP_CUDA(cudaStreamSynchronize(st));
     if (v == PP_ETIMEOUT) return fail(PP_ETIMEOUT, "a bounded device wait ran out");
     if (v == PP_EBOUNDS)
-        return fail(PP_EBOUNDS, "device bounds check failed (a length, block, slot, chunk or token count)");
+        return fail(PP_EBOUNDS, "device bounds check failed (a length, block, slot, chunk or token count, or a block's tokens apart)");
     return fail(PP_ECUDA, "unknown device status " + std::to_string(v));
 }
 

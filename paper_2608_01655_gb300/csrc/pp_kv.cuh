@@ -25,6 +25,7 @@ struct pp_kv {
     // maxima and sums, and arrival counts (0 between launches)
     float *d_piece = nullptr, *d_piece_stat = nullptr;
     int32_t *d_count = nullptr;
+    int32_t *d_claim = nullptr;         // 8-bit caches: a token a block, by which a write finds blocks whose tokens lie apart
 };
 
 namespace pp {
