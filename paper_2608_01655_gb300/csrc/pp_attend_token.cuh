@@ -80,35 +80,24 @@ __device__ __forceinline__ uint32_t lds32(uint32_t addr)
 // both 16-bit halves of a register kept or cleared
 __device__ __forceinline__ uint32_t keep(bool lo, bool hi) { return (lo ? 0xffffu : 0u) | (hi ? 0xffff0000u : 0u); }
 
-// A thread's N columns of a row of which it has those from 4 `lane` on, four of every STEP
-// (N up to 4: the N from N `lane` on): neighbouring threads' loads are neighbours.
-template <int N> constexpr int kChunk = N < 4 ? N : 4;
+// A thread's N columns of a row: those from 4 `lane` on, four of every STEP, so that
+// neighbouring threads' loads are neighbours.
 template <int N, int STEP> __device__ __forceinline__ void store_columns(float *row, int lane, const float (&x)[N])
 {
-    if constexpr (N == 2) {
-        *reinterpret_cast<float2 *>(row + 2 * lane) = make_float2(x[0], x[1]);
-    } else {
 #pragma unroll
-        for (int d = 0; d < N; d += 4)
-            *reinterpret_cast<float4 *>(row + 4 * lane + d / 4 * STEP) = make_float4(x[d], x[d + 1], x[d + 2], x[d + 3]);
-    }
+    for (int d = 0; d < N; d += 4)
+        *reinterpret_cast<float4 *>(row + 4 * lane + d / 4 * STEP) = make_float4(x[d], x[d + 1], x[d + 2], x[d + 3]);
 }
 // from L2, where other CTAs left them
 template <int N, int STEP> __device__ __forceinline__ void load_columns(const float *row, int lane, float (&x)[N])
 {
-    if constexpr (N == 2) {
-        const float2 y = __ldcg(reinterpret_cast<const float2 *>(row + 2 * lane));
-        x[0] = y.x;
-        x[1] = y.y;
-    } else {
 #pragma unroll
-        for (int d = 0; d < N; d += 4) {
-            const float4 y = __ldcg(reinterpret_cast<const float4 *>(row + 4 * lane + d / 4 * STEP));
-            x[d] = y.x;
-            x[d + 1] = y.y;
-            x[d + 2] = y.z;
-            x[d + 3] = y.w;
-        }
+    for (int d = 0; d < N; d += 4) {
+        const float4 y = __ldcg(reinterpret_cast<const float4 *>(row + 4 * lane + d / 4 * STEP));
+        x[d] = y.x;
+        x[d + 1] = y.y;
+        x[d + 2] = y.z;
+        x[d + 3] = y.w;
     }
 }
 
@@ -131,7 +120,8 @@ __device__ __forceinline__ void leave_item(const AttendDev &a, const Cursor<S> &
                                            float sum, int32_t *last, int64_t total, int64_t ctas, SYNC sync)
 {
     constexpr int kRows = S::kRows, kLanes = THREADS / kRows, kWidth = PER * kLanes;
-    constexpr int kStep = kChunk<PER> * kLanes;
+    constexpr int kStep = 4 * kLanes;
+    static_assert(PER % 4 == 0, "columns go four at a time");
     const int jr = tid / kLanes, lane = tid % kLanes;
     const int32_t row0 = cur.inner * kRows, rows = min(kRows, S::rows(a, cur.q) - row0);
     const uint32_t row_lanes = (uint32_t)(((uint64_t)1 << kLanes) - 1) << ((tid & 31) - lane);
@@ -218,13 +208,12 @@ __device__ __forceinline__ void leave_item(const AttendDev &a, const Cursor<S> &
     }
     if (write && jr < rows) {
         const float inv = inverse_sum(sum, S::pos(a, cur.q, row0 + jr) >= 0);
-        T *dst = static_cast<T *>(a.c.out) + item_row(a, cur, jr, a.c.out_token_stride, a.c.out_head_stride) + kChunk<PER> * lane;
+        T *dst = static_cast<T *>(a.c.out) + item_row(a, cur, jr, a.c.out_token_stride, a.c.out_head_stride) + 4 * lane;
 #pragma unroll
-        for (int d = 0; d < PER; d += kChunk<PER>) {
-            if (kChunk<PER> * lane + d / kChunk<PER> * kStep >= a.dim) continue;
-            const uint32_t two = Pack<T>::two(acc[d] * inv, acc[d + 1] * inv);
-            if constexpr (kChunk<PER> == 2) *reinterpret_cast<uint32_t *>(dst) = two;
-            else *reinterpret_cast<uint2 *>(dst + d / 4 * kStep) = make_uint2(two, Pack<T>::two(acc[d + 2] * inv, acc[d + 3] * inv));
+        for (int d = 0; d < PER; d += 4) {
+            if (4 * lane + d / 4 * kStep >= a.dim) continue;
+            *reinterpret_cast<uint2 *>(dst + d / 4 * kStep) =
+                make_uint2(Pack<T>::two(acc[d] * inv, acc[d + 1] * inv), Pack<T>::two(acc[d + 2] * inv, acc[d + 3] * inv));
         }
         if (a.c.lse && lane == 0)
             a.c.lse[item_row(a, cur, jr, a.c.q_heads, 1)] =
