@@ -625,7 +625,10 @@ extern "C" pp_status pp_kv_write8(pp_kv *kv, int32_t tokens, const void *k, int6
     if (!k || !v || !slot_map || !k_cache || !v_cache) return fail(PP_EINVAL, "null pointer");
     pp_status s = check_exps(k_exp, v_exp);
     if (s != PP_OK) return s;
-    if (k_cache == v_cache) return fail(PP_EINVAL, "K and V need caches of their own");
+    const void *const buffers[4] = {k_cache, v_cache, k_exp, v_exp};
+    for (int i = 1; i < 4; ++i)
+        for (int j = 0; j < i; ++j)
+            if (buffers[i] == buffers[j]) return fail(PP_EINVAL, "caches and exponents must be four different buffers");
     if (!aligned16(k) || !aligned16(v) || !aligned16(k_cache) || !aligned16(v_cache))
         return fail(PP_EINVAL, "k, v and the caches must be aligned to 16 bytes");
     if (!stride_ok(k_token_stride) || !stride_ok(k_head_stride) || !stride_ok(v_token_stride) || !stride_ok(v_head_stride))

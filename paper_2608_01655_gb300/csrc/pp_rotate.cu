@@ -457,6 +457,16 @@ extern "C" pp_status pp_kv_rotate(pp_kv *kv, int32_t tokens, int32_t q_heads, co
         return fail(PP_EINVAL, "rows of q_out would overlap with these strides");
     if (k_out && rows_overlap(kv->dim, {{k_out_token_stride, tokens}, {k_out_head_stride, kv->heads}}))
         return fail(PP_EINVAL, "rows of k_out would overlap with these strides");
+    // buffers that begin at one place share a row, which two groups would write, or one while another reads it
+    const void *const outs[4] = {q_heads > 0 ? q_out : nullptr, k_out, k_cache, v_cache};
+    const void *const ins[3] = {q_heads > 0 ? q : nullptr, k, v};
+    for (int i = 0; i < 4; ++i) {
+        for (int j = 0; outs[i] && j < 4; ++j)
+            if (j != i && outs[j] == outs[i]) return fail(PP_EINVAL, "q_out, k_out and the caches must be different buffers");
+        for (int j = 0; outs[i] && j < 3; ++j)
+            if ((j != i || j == 2) && ins[j] == outs[i])
+                return fail(PP_EINVAL, "an output over another one's input: only q_out may be q and k_out k");
+    }
     // in place a row is read before it is written; other rows over it would be a race
     if ((q_heads > 0 && q_out == q && tokens * (int64_t)q_heads > 1 &&
          ((tokens > 1 && q_out_token_stride != q_token_stride) || (q_heads > 1 && q_out_head_stride != q_head_stride))) ||
