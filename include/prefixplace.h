@@ -633,8 +633,9 @@ pp_status pp_paged_attention(pp_kv *kv, int32_t requests, int32_t tokens, int32_
  * r = slow, and in between g f + (1 - g) f / factor, g = (r - slow) / (fast - slow).
  *   pairs         0 .. 64
  *   base, factor  > 0
+ *   slow, fast    finite, slow below fast; not looked at with original = 0
  *   frequency     host [pairs] out
- * Errors: PP_EINVAL.
+ * Errors: PP_EINVAL (also a frequency that would not be finite).
  */
 pp_status pp_rotary_frequencies(int32_t pairs, double base, double factor, double original, double slow, double fast,
                                 double *frequency);

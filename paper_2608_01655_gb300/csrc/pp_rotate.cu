@@ -395,13 +395,17 @@ extern "C" pp_status pp_rotary_frequencies(int32_t pairs, double base, double fa
     if (!(base > 0) || !std::isfinite(base)) return fail(PP_EINVAL, "base must be positive and finite");
     if (!(factor > 0) || !std::isfinite(factor)) return fail(PP_EINVAL, "factor must be positive and finite");
     if (!(original >= 0) || !std::isfinite(original)) return fail(PP_EINVAL, "original must be >= 0 and finite");
-    if (original > 0 && !(slow < fast)) return fail(PP_EINVAL, "slow must be below fast");
+    if (original > 0 && (!(slow < fast) || !std::isfinite(slow) || !std::isfinite(fast)))
+        return fail(PP_EINVAL, "slow must be below fast, and both finite");
     const double turn = 6.283185307179586;
+    double out[kKvMaxDim / 2];
     for (int32_t i = 0; i < pairs; ++i) {
         const double f = std::pow(base, -(double)i / pairs);
         const double keep = original > 0 ? std::min(std::max((original * f / turn - slow) / (fast - slow), 0.0), 1.0) : 0.0;
-        frequency[i] = f * (keep + (1.0 - keep) / factor);
+        out[i] = f * (keep + (1.0 - keep) / factor);
+        if (!std::isfinite(out[i])) return fail(PP_EINVAL, "base and factor give a frequency that is not finite");
     }
+    std::copy_n(out, pairs, frequency);
     return PP_OK;
 }
 

@@ -52,3 +52,24 @@ def test_angles_of_small_negative_frequencies_at_far_positions(lib):
     part = position * got % (1 << 64)
     angle = Fraction(part - (1 << 64 if part >> 63 else 0), 1 << 64) * TWO_PI
     assert abs(angle + Fraction(1e-9) * position) <= 2.2 * 2.0 ** -52 + 2 * math.pi * 2.0 ** (31 - 65)
+
+
+@pytest.mark.parametrize("args", [(4, 1e4, 1, 9, -math.inf, 2), (4, 1e4, 1, 9, 1, math.inf), (4, 1e4, 1, 9, -math.inf, math.inf),
+                                  (64, 1e-320, 1, 0, 1, 2), (4, 1e-300, 1e-200, 0, 1, 2), (4, 1e4, 5e-324, 0, 1, 2)])
+def test_frequencies_that_are_no_numbers_are_refused(lib, args):
+    """Ramps without an end, and powers and quotients beyond the largest number."""
+    out = np.full(64, 7.0)
+    assert lib._lib.pp_rotary_frequencies(*args, out.ctypes.data_as(ctypes.c_void_p)) == lib.PP_EINVAL
+    assert (out == 7).all() and lib.last_error()
+
+
+def test_a_ramp_is_not_looked_at_without_an_original_context(lib):
+    out = np.zeros(4)
+    assert lib._lib.pp_rotary_frequencies(4, 16.0, 2.0, 0.0, -math.inf, math.nan, out.ctypes.data_as(ctypes.c_void_p)) == lib.PP_OK
+    assert np.allclose(out, [0.5, 0.25, 0.125, 0.0625], rtol=1e-15, atol=0)
+
+
+def test_pairs_that_keep_their_frequency_do_so_whatever_the_factor(lib):
+    out = np.zeros(2)
+    assert lib._lib.pp_rotary_frequencies(2, 4.0, 5e-324, 1e6, 1.0, 2.0, out.ctypes.data_as(ctypes.c_void_p)) == lib.PP_OK
+    assert out.tolist() == [1.0, 0.5]
