@@ -691,7 +691,11 @@ pp_status pp_kv_rotate(pp_kv *kv, int32_t tokens, int32_t q_heads, const void *q
                        void *v_cache, void *stream);
 
 /*
- * A cache of 8-bit numbers holds twice the chunks in the same memory.  The handle
+ * A cache of 8-bit numbers holds twice the chunks in the same memory.  Calls of few
+ * rows need nothing beside it; those of chunks need a workspace of two bytes an element
+ * for every block that their requests see, shared ones once for each request: a call
+ * whose requests see all of a cache without sharing holds three bytes an element, where
+ * a 16-bit cache holds two.  Prefills cut into calls of few requests need the least.  The handle
  * is made with PP_KV_BF16_E4M3 or PP_KV_F16_E4M3; pp_block_tables works on it as
  * on any other, pp_kv_write and pp_paged_attention refuse it.  An element is
  * code * 2^e: an e4m3 number (4 significant bits, exponents from -6 to 8, 448 the
@@ -723,7 +727,7 @@ pp_status pp_kv_write8(pp_kv *kv, int32_t tokens, const void *k, int64_t k_token
 
 /*
  * pp_kv_workspace -- host-only: bytes of workspace of a pp_paged_attention8 call
- * with chunks.
+ * with chunks: a table, and 4 * block_size * kv_heads * head_dim a block.
  *   requests, table_width   as in that call, or more
  *   blocks        blocks that the requests' new tokens see, counted for each request
  *                 (at most the sum of ceil(length / block_size))

@@ -483,7 +483,7 @@ class KVCache:
 
     def workspace_size(self, requests, table_width, blocks):
         """Bytes of workspace of a pp_paged_attention8 call with chunks; blocks: what the requests' new tokens see,
-        counted for each request."""
+        counted for each request.  A block takes twice its size in the cache."""
         out = ctypes.c_size_t(0)
         _check(_lib.pp_kv_workspace(self.handle, int(requests), int(table_width), int(blocks), ctypes.byref(out)))
         return int(out.value)
@@ -687,7 +687,7 @@ def _eight(kv: KVCache):
 
 def pp_kv_write8(kv: KVCache, k, v, slot_map, k_cache, k_exp, v_cache, v_exp, stream=None):
     """Store rows k, v [T][kv_heads][head_dim] at slot_map [T] int64 (negative: left out) as 8-bit numbers; k_exp,
-    v_exp [blocks][kv_heads] int8: exponents of their scales."""
+    v_exp [blocks][kv_heads] int8: exponents of their scales.  A block's tokens stand next to one another."""
     _eight(kv)
     t, h, exps = slot_map.shape[0], kv.shape[2], (kv.shape[0], kv.shape[2])
     _check(_lib.pp_kv_write8(kv.handle, t, *kv._rows(k, "k", t, h), *kv._rows(v, "v", t, h),
