@@ -608,6 +608,8 @@ pp_status pp_kv_write(pp_kv *kv, int32_t tokens, const void *k, int64_t k_token_
  * output's sum are 32-bit; the weights are rounded to the cache's type for
  * their product with V.  Results do not depend on the run, but the last bits
  * may depend on which other requests are in the call.
+ * A weight is off by |scale q.k| 2^-23 of itself, as 32-bit scores are; scores above
+ * 2^26 in size may make a row NaN.
  * A block out of range that a query would see (its rows read as zeros), or
  * lengths and offsets out of range (cut to the range), set PP_EBOUNDS.
  * Errors: PP_EINVAL (also q_heads above 2^20, tokens * q_heads / kv_heads above
@@ -745,7 +747,8 @@ pp_status pp_kv_workspace(const pp_kv *kv, int32_t requests, int32_t table_width
  * Calls of few rows (that limit) read codes and exponents directly: products of codes
  * with queries of 11 significant bits (bf16's 8 fit) and 32-bit sums; for their product
  * with V weights times their blocks' V scales are rounded to 11 bits down to 2^-29 of a
- * row's largest, and are off by 2^-40 of that below.  Calls of chunks unpack what the queries see
+ * row's largest, and are off by 2^-40 of that below; scores may be of any finite size.
+ * Calls of chunks unpack what the queries see
  * into the workspace as rows of the 16-bit type and then are as pp_paged_attention.
  * Unpacking is exact in bf16; in f16 beyond 65504 becomes that, and below 2^-14 it is
  * off by 2^-25 at most.

@@ -262,7 +262,9 @@ template <int ROWS, int HALVES> struct Shared8 {
     int32_t last;
 };
 constexpr int kJoinFull = 1, kJoinFree = 2, kOutput = 3;        // named barriers
-constexpr float kTopWeight = 15.f;                              // log2 of the largest weight: f16 ends at 2^16
+// What is subtracted from a row's scores, from their maximum: the largest weight is 2^15 (f16 ends at 2^16).  Rounded
+// up, so that it is not more where scores are so large that 15 is not a number of their steps.
+__device__ __forceinline__ float below(float top) { return __fsub_ru(top, 15.f); }
 
 // The products of a warp's keys, item after item.
 template <typename T, int ROWS, int HALVES>
@@ -402,7 +404,7 @@ __device__ __forceinline__ void product_role(const AttendDev &a, Shared8<ROWS, H
                             up = fmaxf(up, __shfl_xor_sync(~0u, up, 4));
                             up = fmaxf(up, __shfl_xor_sync(~0u, up, 8));
                             up = fmaxf(m[b][y], fmaxf(up, __shfl_xor_sync(~0u, up, 16)));
-                            const float f = up == -INFINITY ? 1.f : exp2_approx(m[b][y] - up);
+                            const float f = up == -INFINITY ? 1.f : exp2_approx(below(m[b][y]) - below(up));
                             m[b][y] = up;
                             l[b][y] *= f;
 #pragma unroll
@@ -453,7 +455,7 @@ __device__ __forceinline__ void product_role(const AttendDev &a, Shared8<ROWS, H
                 for (int b = 0; b < NB; ++b) {
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
-                        const float at = m[b][y] == -INFINITY ? 0.f : m[b][y] - kTopWeight;
+                        const float at = m[b][y] == -INFINITY ? 0.f : below(m[b][y]);
 #pragma unroll
                         for (int n = 0; n < 2; ++n) {
                             sc[b][2 * n + y] = exp2_approx(sc[b][2 * n + y] - at);
@@ -499,7 +501,7 @@ __device__ __forceinline__ void product_role(const AttendDev &a, Shared8<ROWS, H
                 l[b][y] += __shfl_xor_sync(~0u, l[b][y], 8);
                 l[b][y] += __shfl_xor_sync(~0u, l[b][y], 16);
                 if (g == 0) {
-                    sh.stat[0][warp][row] = m[b][y] - kTopWeight;
+                    sh.stat[0][warp][row] = below(m[b][y]);
                     sh.stat[1][warp][row] = l[b][y];
                 }
                 float *dst = join + (warp * ROWS + row) * L::pitch + 2 * g;

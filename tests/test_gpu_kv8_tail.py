@@ -88,3 +88,34 @@ def test_a_long_tail_in_pieces(pp, tail, gap):
 def test_scales_that_push_weights_to_the_ends(pp, gap):
     """The strong keys' values 2^30 below and above the others': weights of either kind fall off the other's."""
     _run(pp, 200, 701, 8, 2, 64, BF, 10, gap, 30)
+
+
+@pytest.mark.parametrize("size", [10, 20, 22, 23, 24, 25, 26, 27, 28, 30, 34, 50])
+@pytest.mark.parametrize("heads", [1, 9])
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_scores_of_any_size(pp, size, heads, dtype):
+    """One key far above the others, at 2^size and more: its V row is the output however coarse the scores' steps are.
+    Keys come in an order in which the maximum moves many times, by small and large steps."""
+    gen = torch.Generator(device="cuda").manual_seed(size)
+    blocks, dim = 90, 64
+    kc, vc = (torch.rand((blocks, 16, 1, dim), generator=gen, device="cuda") for _ in range(2))
+    kc[..., 0] = torch.linspace(0.25, 0.5, blocks * 16, device="cuda").view(blocks, 16, 1)
+    kc[77, 5, 0, 0] = 1.0
+    (kc, ke), (vc, ve) = ref.to8(kc), ref.to8(vc)
+    assert (ke == -8).all()
+    ke += torch.tensor(size - 20 + 8, dtype=torch.int8, device="cuda").clamp(max=48)
+    rest = 2.0 ** (size - int(ke[0, 0]) - 8)                # what the exponents leave to the scale
+    q = torch.zeros((2, heads, dim), dtype=dtype, device="cuda")
+    q[..., 0] = torch.arange(1, heads + 1, device="cuda")
+    out, lse = torch.empty_like(q), torch.empty((2, heads), device="cuda")
+    table, length = [list(range(blocks))] * 2, [blocks * 16, blocks * 16 - 77]
+    with pp.KVCache.like(kc, dtype=dtype) as kv:
+        pp.pp_paged_attention8(kv, q, kc, ke, vc, ve, _i32(table), _i32([0, 1, 2]), _i32(length), 1, out, rest, lse=lse)
+        kv.sync()
+    v = ref.scaled(vc, ve)[77, 5, 0]
+    u = ref.UNIT[dtype]
+    # the next key is 2^(size - 2) behind; weights and sums of one key cancel but for roundings of 2^-11 and 2^-20
+    assert ((out.double() - v).abs() <= 1.01 * (u + 2.0 ** -11 + 2.0 ** -20) * v.abs() + ref.TINY[dtype]).all()
+    score = q[..., 0].double() * ref.scaled(kc, ke)[77, 5, 0, 0] * rest
+    assert float(score.min()) >= 2.0 ** size * 0.99
+    assert ((lse.double() - score).abs() <= score * 2.0 ** -20).all()
