@@ -697,9 +697,10 @@ pp_status pp_kv_rotate(pp_kv *kv, int32_t tokens, int32_t q_heads, const void *q
  * rows need nothing beside it; those of chunks need a workspace of two bytes an element
  * for every block that their requests see, shared ones once for each request: a call
  * whose requests see all of a cache without sharing holds three bytes an element, where
- * a 16-bit cache holds two.  Prefills cut into calls of few requests need the least.  The handle
- * is made with PP_KV_BF16_E4M3 or PP_KV_F16_E4M3; pp_block_tables works on it as
- * on any other, pp_kv_write and pp_paged_attention refuse it.  An element is
+ * a 16-bit cache holds two.  Prefills cut into calls of few requests need the least.
+ *
+ * The handle is made with PP_KV_BF16_E4M3 or PP_KV_F16_E4M3; pp_block_tables works on
+ * it as on any other, pp_kv_write and pp_paged_attention refuse it.  An element is
  * code * 2^e: an e4m3 number (4 significant bits, exponents from -6 to 8, 448 the
  * largest, NaN and no infinity) and the exponent of its block and head, -40 .. 40.
  * K and V have exponents of their own, device int8 [blocks][kv_heads]; numbers
@@ -748,10 +749,9 @@ pp_status pp_kv_workspace(const pp_kv *kv, int32_t requests, int32_t table_width
  * with queries of 11 significant bits (bf16's 8 fit) and 32-bit sums; for their product
  * with V weights times their blocks' V scales are rounded to 11 bits down to 2^-29 of a
  * row's largest, and are off by 2^-40 of that below; scores may be of any finite size.
- * Calls of chunks unpack what the queries see
- * into the workspace as rows of the 16-bit type and then are as pp_paged_attention.
- * Unpacking is exact in bf16; in f16 beyond 65504 becomes that, and below 2^-14 it is
- * off by 2^-25 at most.
+ * Calls of chunks unpack what the queries see into the workspace as rows of the 16-bit
+ * type and then are as pp_paged_attention.  Unpacking is exact in bf16; in f16 beyond
+ * 65504 becomes that, and below 2^-14 it is off by 2^-25 at most.
  * A workspace that has too few blocks for what the queries see sets PP_EBOUNDS (the
  * missing ones read as zeros).  Calls that share a workspace must not overlap.
  * Errors: PP_EINVAL (also a workspace that is missing or has no room for a block),

@@ -147,3 +147,28 @@ def test_a_captured_call_reports_what_its_map_holds_when_it_is_replayed(pp):
             slot.copy_(torch.tensor(m))
             graph.replay()
             assert c.reported() == (m is bad)
+
+
+def test_layers_on_two_streams_at_once(pp):
+    """One handle, two layers' caches, the same maps and others with the same blocks: none is reported, all are right."""
+    rng = np.random.default_rng(3)
+    block, blocks, h, dim = 16, 200, 2, 64
+    maps = [np.concatenate([b * block + np.arange(block) for b in rng.permutation(blocks)]) for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    layers = []
+    for i in range(2):
+        code = [torch.zeros((blocks, block, h, dim), dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn) for _ in range(2)]
+        exp = [torch.zeros((blocks, h), dtype=torch.int8, device="cuda") for _ in range(2)]
+        rows = [torch.randn((blocks * block, h, dim), device="cuda").to(torch.bfloat16) for _ in range(2)]
+        layers.append((rows, torch.tensor(maps[i], device="cuda"), code, exp))
+    torch.cuda.synchronize()
+    with pp.KVCache.like(layers[0][2][0]) as kv:
+        for _ in range(50):
+            for stream, (rows, slot, code, exp) in zip(streams, layers):
+                pp.pp_kv_write8(kv, *rows, slot, code[0], exp[0], code[1], exp[1], stream=stream)
+        for stream in streams:
+            kv.sync(stream)
+        for (rows, _, code, exp), slot in zip(layers, maps):
+            for x, c, e in zip(rows, code, exp):
+                want, we = ref.write8(x.double().cpu().numpy(), slot, np.zeros((blocks, block, h, dim)), np.zeros((blocks, h)), block)
+                assert np.array_equal(we, e.cpu().numpy()) and np.array_equal(want, ref.values(c))
